@@ -154,11 +154,56 @@ bf_status bf_op_embedding_bwd(int dtype, int S_mb, int S_seq, int S_voc, int S_h
  * [n_rows]); loss_out[0] = sum of row_loss in a fixed order.  A label outside 0..S_voc-1 zeroes its row. */
 bf_status bf_op_ce_loss(int dtype, int n_rows, int S_voc, void* z, const int32_t* labels, float scale, float* row_loss,
                         float* loss_out, void* stream);
+/* The output projection and its softmax cross-entropy in one, in pieces of the vocabulary: the logits z = y w_out^T of
+ * n_rows rows (w_out [S_voc, S_hidden], y [n_rows, S_hidden], both `dtype`) are never kept.
+ *   _fwd  lse[t] = logsumexp(z[t]);  row_loss[t] = (lse[t] - z[t, label]) * scale;  loss_out[0] = sum of row_loss, added in
+ *         a fixed order (in fp64).  All device fp32.
+ *   _bwd  from that lse: with dz = (softmax(z) - onehot(label)) * scale,
+ *         dy[n_rows, S_hidden] (`dtype`) = dz w_out;  dw[S_voc, S_hidden] (fp32) = (accumulate ? dw : 0) + dz^T y
+ * labels: device int32 [n_rows].  A row whose label is outside 0..S_voc-1 has row_loss 0, dy 0 and no part in dw, whatever
+ * its y holds.  Sums have a fixed order: no atomics.  bf16 tensors of 16-byte aligned rows (S_hidden % 8 == 0) run on the
+ * bf16 matrix cores with logits and statistics in fp32, dw to fp32 precision; fp32 tensors and other rows as fp32 products.
+ * S_piece: columns of a piece (0: the library's choice, 256 MiB of dz); work: device scratch, 256-byte aligned, of
+ * bf_op_vocab_loss_work_bytes(..., backward = 0 or 1) bytes (0 for bad sizes), owned by the caller; calls that overlap need
+ * their own.  Sizes are 1 to 2^21. */
+size_t bf_op_vocab_loss_work_bytes(int dtype, int n_rows, int S_hidden, int S_voc, int S_piece, int backward);
+bf_status bf_op_vocab_loss_fwd(int dtype, int n_rows, int S_hidden, int S_voc, int S_piece, const void* y, const void* w_out,
+                               const int32_t* labels, float scale, float* lse, float* row_loss, float* loss_out, void* work,
+                               size_t work_bytes, void* stream);
+bf_status bf_op_vocab_loss_bwd(int dtype, int n_rows, int S_hidden, int S_voc, int S_piece, const void* y, const void* w_out,
+                               const int32_t* labels, const float* lse, float scale, void* dy, float* dw, int accumulate,
+                               void* work, size_t work_bytes, void* stream);
 
 /* Fused Adam over n contiguous fp32 parameters (bias-corrected, decoupled weight decay), step t >= 1;
  * w_lp: bf16 copy of w to refresh, or NULL. */
 bf_status bf_op_adam(size_t n, float* w, float* m, float* v, const float* g, void* w_lp, int t,
                      float lr, float beta1, float beta2, float adam_eps, float weight_decay, void* stream);
+
+/* Global gradient norm and clipping, over a list of tensors of one type (`dtype`: fp32 main-grads or bf16 gradients).  The
+ * lists (g, dst, n, tensors) are host arrays, read during the call; the tensors they name are device memory, aligned to their
+ * elements and no more.  A tensor of no elements is skipped, its pointers may be NULL.
+ *
+ *   out[0] = norm = sqrt(sum over all tensors and elements of g^2), squares and sums in fp64 and in a fixed order
+ *   out[1] = coefficient = norm > max_norm ? max_norm / norm : 1;  NaN where a gradient is infinite or NaN
+ *
+ * out: device fp32 [2].  max_norm > 0 (infinity: the norm alone).  work: device scratch of bf_op_grad_norm_work_bytes(...)
+ * bytes, 8-byte aligned, owned by the caller; calls that overlap need their own.  Nothing waits on the host. */
+size_t bf_op_grad_norm_work_bytes(int n_tensors, const size_t* n);
+bf_status bf_op_grad_norm(int dtype, int n_tensors, const void* const* g, const size_t* n, float max_norm, float* out,
+                          void* work, size_t work_bytes, void* stream);
+/* dst_i = g_i * coef[0], rounded once; dst_i may be g_i, but no tensor may overlap another.  coef: device fp32. */
+bf_status bf_op_grad_scale(int dtype, int n_tensors, const void* const* g, void* const* dst, const size_t* n,
+                           const float* coef, void* stream);
+/* bf_op_adam on g_i * coef[0] for a list of tensors in one go (the gradients themselves stay as they are).  A coefficient
+ * that is not finite leaves the step out: w, m, v and w_lp stay as they were. */
+typedef struct {
+  float *w, *m, *v;
+  const float* g;
+  void* w_lp; /* bf16 copy of w to refresh, or NULL */
+  size_t n;
+} bf_adam_tensor;
+bf_status bf_op_adam_clipped(int n_tensors, const bf_adam_tensor* tensors, const float* coef, int t, float lr, float beta1,
+                             float beta2, float adam_eps, float weight_decay, void* stream);
 
 #ifdef __cplusplus
 }

@@ -62,6 +62,10 @@ class bf_sched_stats(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("makespan", "busy", "bubble_num", "bubble_den", "peak_live")]
 
 
+class bf_adam_tensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("w", "m", "v", "g", "w_lp")] + [("n", C.c_size_t)]
+
+
 _P = C.c_void_p
 _FP = C.POINTER(C.c_float)
 _SIGNATURES = {
@@ -112,6 +116,13 @@ _SIGNATURES = {
     "bf_op_embedding_fwd": (C.c_int, [C.c_int] * 5 + [_P, _P, _P, _P, _P]),
     "bf_op_embedding_bwd": (C.c_int, [C.c_int] * 5 + [_P, _P, _P, _P, C.c_int, _P]),
     "bf_op_ce_loss": (C.c_int, [C.c_int] * 3 + [_P, _P, C.c_float, _P, _P, _P]),
+    "bf_op_vocab_loss_work_bytes": (C.c_size_t, [C.c_int] * 6),
+    "bf_op_vocab_loss_fwd": (C.c_int, [C.c_int] * 5 + [_P, _P, _P, C.c_float, _P, _P, _P, _P, C.c_size_t, _P]),
+    "bf_op_vocab_loss_bwd": (C.c_int, [C.c_int] * 5 + [_P, _P, _P, _P, C.c_float, _P, _P, C.c_int, _P, C.c_size_t, _P]),
+    "bf_op_grad_norm_work_bytes": (C.c_size_t, [C.c_int, _P]),
+    "bf_op_grad_norm": (C.c_int, [C.c_int, C.c_int, _P, _P, C.c_float, _P, _P, C.c_size_t, _P]),
+    "bf_op_grad_scale": (C.c_int, [C.c_int, C.c_int, _P, _P, _P, _P, _P]),
+    "bf_op_adam_clipped": (C.c_int, [C.c_int, _P, _P, C.c_int] + [C.c_float] * 5 + [_P]),
     "bf_op_adam": (C.c_int, [C.c_size_t, _P, _P, _P, _P, _P, C.c_int] + [C.c_float] * 5 + [_P]),
 }
 
@@ -420,3 +431,109 @@ def bf_op_ce_loss(dtype, n_rows, S_voc, z, labels, scale, row_loss, loss_out):
 def bf_op_adam(n, w, m, v, g, w_lp, t, lr, beta1, beta2, adam_eps, weight_decay):
     check(load().bf_op_adam(n, _ptr(w), _ptr(m), _ptr(v), _ptr(g), _ptr(w_lp), t, lr, beta1, beta2, adam_eps,
                             weight_decay, _stream()))
+
+
+def _tensors(who, tensors, dtype):
+    """Checks tensors that a kernel is to work on: dense, of `dtype` (torch), on the current device."""
+    import torch
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t.dtype is not dtype or not t.is_contiguous() or t.device.type != "cuda" or t.device.index != dev:
+            raise ValueError("%s: needs contiguous %s tensors on cuda:%d, got %s on %s, strides %s" % (who, dtype, dev, t.dtype, t.device, t.stride()))
+
+
+def _torch_dtype(dtype):
+    import torch
+    return torch.bfloat16 if dtype == BF_BF16 else torch.float32
+
+
+def _work(who, work, n):
+    """The caller's scratch, or n bytes from torch's allocator (in the current stream's order)."""
+    import torch
+    if work is None:
+        return torch.empty(max(n, 1), dtype=torch.uint8, device="cuda")
+    _tensors(who, (work,), work.dtype)
+    return work
+
+
+def _list(tensors):
+    return (C.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors]), (C.c_size_t * len(tensors))(*[t.numel() for t in tensors])
+
+
+def _elems(who, tensor, n):
+    if tensor.numel() < n:
+        raise ValueError("%s: a tensor of %d elements where %d are used" % (who, tensor.numel(), n))
+
+
+def bf_op_vocab_loss_work_bytes(dtype, n_rows, S_hidden, S_voc, S_piece=0, backward=0):
+    return load().bf_op_vocab_loss_work_bytes(dtype, n_rows, S_hidden, S_voc, S_piece, backward)
+
+
+def _vocab_loss(who, dtype, n_rows, S_hidden, S_voc, S_piece, backward, y, w_out, labels, fp32, small, work):
+    import torch
+    _tensors(who, (y, w_out), _torch_dtype(dtype))
+    _tensors(who, (labels,), torch.int32)
+    _tensors(who, fp32, torch.float32)
+    _elems(who, y, n_rows * S_hidden)
+    _elems(who, w_out, S_voc * S_hidden)
+    for t in (labels,) + small:
+        _elems(who, t, n_rows)
+    return _work(who, work, bf_op_vocab_loss_work_bytes(dtype, n_rows, S_hidden, S_voc, S_piece, backward))
+
+
+def bf_op_vocab_loss_fwd(dtype, n_rows, S_hidden, S_voc, y, w_out, labels, scale, lse, row_loss, loss_out, S_piece=0, work=None):
+    who = "bf_op_vocab_loss_fwd"
+    work = _vocab_loss(who, dtype, n_rows, S_hidden, S_voc, S_piece, 0, y, w_out, labels, (lse, row_loss, loss_out), (lse, row_loss), work)
+    _elems(who, loss_out, 1)
+    check(load().bf_op_vocab_loss_fwd(dtype, n_rows, S_hidden, S_voc, S_piece, y.data_ptr(), w_out.data_ptr(), labels.data_ptr(), scale, lse.data_ptr(),
+                                      row_loss.data_ptr(), loss_out.data_ptr(), work.data_ptr(), work.numel() * work.element_size(), _stream()))
+
+
+def bf_op_vocab_loss_bwd(dtype, n_rows, S_hidden, S_voc, y, w_out, labels, lse, scale, dy, dw, accumulate=0, S_piece=0, work=None):
+    who = "bf_op_vocab_loss_bwd"
+    work = _vocab_loss(who, dtype, n_rows, S_hidden, S_voc, S_piece, 1, y, w_out, labels, (lse, dw), (lse,), work)
+    _tensors(who, (dy,), _torch_dtype(dtype))
+    _elems(who, dy, n_rows * S_hidden)
+    _elems(who, dw, S_voc * S_hidden)
+    check(load().bf_op_vocab_loss_bwd(dtype, n_rows, S_hidden, S_voc, S_piece, y.data_ptr(), w_out.data_ptr(), labels.data_ptr(), lse.data_ptr(), scale,
+                                      dy.data_ptr(), dw.data_ptr(), accumulate, work.data_ptr(), work.numel() * work.element_size(), _stream()))
+
+
+def bf_op_grad_norm_work_bytes(tensors):
+    return load().bf_op_grad_norm_work_bytes(len(tensors), _list(tensors)[1])
+
+
+def bf_op_grad_norm(dtype, tensors, max_norm, out, work=None):
+    """out (fp32, 2 elements) = norm over a list of gradients, coefficient that clips it to max_norm."""
+    import torch
+    _tensors("bf_op_grad_norm", tensors, _torch_dtype(dtype))
+    _tensors("bf_op_grad_norm", (out,), torch.float32)
+    if out.numel() < 2:
+        raise ValueError("bf_op_grad_norm: out needs 2 elements")
+    lib, (g, n) = load(), _list(tensors)
+    work = _work("bf_op_grad_norm", work, lib.bf_op_grad_norm_work_bytes(len(tensors), n))
+    check(lib.bf_op_grad_norm(dtype, len(tensors), g, n, max_norm, out.data_ptr(), work.data_ptr(), work.numel() * work.element_size(), _stream()))
+
+
+def bf_op_grad_scale(dtype, tensors, dst, coef):
+    """dst[i] = tensors[i] * coef (device fp32); dst may be the tensors themselves."""
+    import torch
+    _tensors("bf_op_grad_scale", tensors, _torch_dtype(dtype))
+    _tensors("bf_op_grad_scale", dst, _torch_dtype(dtype))
+    _tensors("bf_op_grad_scale", (coef,), torch.float32)
+    (g, n), (d, m) = _list(tensors), _list(dst)
+    if list(n) != list(m) or not coef.numel():
+        raise ValueError("bf_op_grad_scale: the lists differ in their sizes, or coef is empty")
+    check(load().bf_op_grad_scale(dtype, len(tensors), g, d, n, coef.data_ptr(), _stream()))
+
+
+def bf_op_adam_clipped(tensors, coef, t, lr, beta1, beta2, adam_eps, weight_decay):
+    """The Adam step number t on gradients times coef (device fp32).  tensors: (w, m, v, g, w_lp) each, w_lp bf16 or None."""
+    import torch
+    _tensors("bf_op_adam_clipped", [x for q in tensors for x in q[:4]] + [coef], torch.float32)
+    _tensors("bf_op_adam_clipped", [q[4] for q in tensors if q[4] is not None], torch.bfloat16)
+    if not coef.numel() or any(x is not None and x.numel() != q[0].numel() for q in tensors for x in q[1:]):
+        raise ValueError("bf_op_adam_clipped: tensors of different sizes in one entry, or an empty coef")
+    a = (bf_adam_tensor * len(tensors))(*[(w.data_ptr(), m.data_ptr(), v.data_ptr(), g.data_ptr(), None if lp is None else lp.data_ptr(), w.numel())
+                                          for w, m, v, g, lp in tensors])
+    check(load().bf_op_adam_clipped(len(tensors), a, coef.data_ptr(), t, lr, beta1, beta2, adam_eps, weight_decay, _stream()))

@@ -23,7 +23,24 @@ enum Epilogue {
   E_BIAS_RES = 2,   // C = acc + bias[n] + R[m,n]
   E_BIAS_GELU = 3,  // C = acc + bias[n];  C2 = gelu(C)
   E_GELU_BWD = 4,   // C = acc * gelu'(R[m,n])      (R holds the pre-activation)
-  E_ACCUM = 5       // fp32 C = (accumulate ? C : 0) + acc
+  E_ACCUM = 5,      // fp32 C = (accumulate ? C : 0) + acc
+  // The vocabulary loss (acc[m,n] = logit of row m and column n; matrix-core kernel only, see gemm_mfma_logits_*)
+  E_LSE = 6,        // per row and tile: maximum and sum of exponentials; the label's logit.  No C
+  E_DLOGITS = 7     // C = bf16 parts of (exp(acc - lse[m]) - [n is m's label]) * scale
+};
+
+// What the vocabulary loss needs beside the product.
+struct LogitArgs {
+  const int32_t* label = nullptr;  // [M]
+  const float* lse = nullptr;      // [M], E_DLOGITS
+  float* part = nullptr;           // [tiles_n][M][2] E_LSE
+  float* at_label = nullptr;       // [M] E_LSE: logit of the label's column
+  float scale = 0.f;
+  int col0 = 0;                    // the vocabulary's column that the product's column 0 is
+  int S_voc = 0;
+  int parts = 0;                   // E_DLOGITS: bf16 parts, plane elements apart
+  size_t plane = 0;
+  int ldc = 0;                     // row length of a plane, a multiple of 8 (columns past N are written as zeros)
 };
 
 struct GemmArgs {
@@ -58,6 +75,9 @@ struct GemmArgs {
   // whose tiles would leave half of the chip idle (see gemm_splitk_slices) and finishes it with a second kernel.
   float* splitk_ws = nullptr;
   size_t splitk_ws_elems = 0;
+  // Matrix-core kernel: row length of A where it is not K (forward / dgrad layouts) or M (weight gradient)
+  int lda = 0;
+  LogitArgs logit;  // E_LSE, E_DLOGITS
   // Matrix-core kernel: only the first m_part rows / n_part columns of C (0: all of them; whole tiles)
   int m_part = 0, n_part = 0;
   // The product shares the chip with another stream's kernels (two chains of micro-batches): compute units that
@@ -111,6 +131,21 @@ bool gemm_mfma_in_rounds(int layout, int epi, const GemmArgs& a);
 // E_NONE, E_BIAS, E_BIAS_RES.
 bf_status gemm_splitk_finish(int epi, int M, int N, int slices, const float* part, const float* bias, const void* R,
                              void* C, hipStream_t st);
+// Products of the vocabulary loss on the bf16 matrix cores; 16-byte aligned operands, S_hidden % 8 == 0, any number of rows and
+// columns (gemm_mfma_logits_supported).  rows x cols logits = y[rows, h] w[cols, h]^T:
+//   _lse      leaves E_LSE's partial statistics in a.logit.part, *tiles rows of them (at most gemm_mfma_logits_tiles)
+//   _grad     leaves E_DLOGITS' planes
+//   _dy       planes[slices][rows][h] (fp32) = (accumulate ? planes : 0) + dz[rows, cols] w[cols, h], slice y of the columns in plane y
+//   _dw       dw[cols, h] (fp32) = (accumulate ? dw : 0) + the sum over parts of dz_part^T y
+bool gemm_mfma_logits_supported(int rows, int cols, int h);
+int gemm_mfma_logits_tiles(int rows, int cols);
+bf_status gemm_mfma_logits_lse(int rows, int cols, int h, const void* y, const void* w, const LogitArgs& l, int* tiles, hipStream_t st);
+bf_status gemm_mfma_logits_grad(int rows, int cols, int h, const void* y, const void* w, const LogitArgs& l, void* dz, hipStream_t st);
+int gemm_mfma_logits_dy_slices(int rows, int cols, int h);
+bf_status gemm_mfma_logits_dy(int rows, int cols, int h, const void* dz, int ldz, int parts, size_t plane, const void* w, float* planes, int slices,
+                              int accumulate, hipStream_t st);
+bf_status gemm_mfma_logits_dw(int rows, int cols, int h, const void* dz, int ldz, int parts, size_t plane, const void* y, float* dw, int accumulate,
+                              hipStream_t st);
 bf_status gemm(int dtype, int kernels, int layout, int epi, const GemmArgs& a, hipStream_t st);
 
 bf_status layernorm_fwd(int dtype, int T, int h, const void* x, const float* g, const float* b, float eps,
@@ -192,10 +227,22 @@ bf_status embedding_bwd(int dtype, int S_mb, int S_seq, int S_voc, int h, const 
 bf_status ce_loss(int dtype, int n_rows, int S_voc, void* z, const int32_t* labels, float scale, float* row_loss,
                   float* loss_out, hipStream_t st);
 
+// The same loss from the projection's input, in pieces of the vocabulary, without the logits (see bf_ops.h).
+size_t vocab_loss_work_bytes(int dtype, int rows, int h, int V, int piece, int backward);
+bf_status vocab_loss_fwd(int dtype, int rows, int h, int V, int piece, const void* y, const void* w, const int32_t* label, float scale, float* lse,
+                         float* row_loss, float* loss, void* work, size_t work_bytes, hipStream_t st);
+bf_status vocab_loss_bwd(int dtype, int rows, int h, int V, int piece, const void* y, const void* w, const int32_t* label, const float* lse, float scale,
+                         void* dy, float* dw, int accumulate, void* work, size_t work_bytes, hipStream_t st);
+
 // Fused Adam over n contiguous parameters; w_lp (bf16 copy) may be null.
 // t_dev: device step counter read by the kernel (then t is ignored), or null for the host value t
 bf_status adam_step(size_t n, float* w, float* m, float* v, const float* g, bf16_t* w_lp, int t, const int* t_dev, float lr,
                     float beta1, float beta2, float eps, float wd, hipStream_t st);
+// Gradient norm over a list of tensors, clipping, Adam on clipped gradients (host lists of device pointers; see bf_ops.h).
+size_t grad_norm_work_bytes(int n_tensors, const size_t* n);
+bf_status grad_norm(int dtype, int n_tensors, const void* const* g, const size_t* n, float max_norm, float* out, void* work, size_t work_bytes,
+                    hipStream_t st);
+bf_status grad_scale(int dtype, int n_tensors, const void* const* g, void* const* dst, const size_t* n, const float* coef, hipStream_t st);
 bf_status bump_step(int* t_dev, hipStream_t st);
 bf_status cast_f32_to_bf16(size_t n, const float* src, bf16_t* dst, hipStream_t st);
 bf_status fill_f32(size_t n, float* dst, float value, hipStream_t st);

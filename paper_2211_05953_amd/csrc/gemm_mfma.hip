@@ -16,6 +16,8 @@
 // row (l / 16) * 4 + r, column l % 16.  The 16 x 16 x 32 form is used because the step runs at the
 // socket power limit: in a register-only loop on random operands it sustains 2.00 PFLOP/s where
 // the 32 x 32 x 16 form sustains 1.81 (both reach 2.48 on zeros).
+#include <float.h>
+
 #include <atomic>
 #include <type_traits>
 
@@ -209,6 +211,64 @@ __device__ __forceinline__ bf16x8 load_frag(const bf16_t* lds, int r16, int kk, 
   }
 }
 
+// The vocabulary loss's arguments, for the epilogues that have them; other kernels carry nothing.
+struct NoLogitArgs {};
+template <int EPI> struct LogitArgsOf { typedef NoLogitArgs type; };
+template <> struct LogitArgsOf<E_LSE> { typedef LogitArgs type; };
+template <> struct LogitArgsOf<E_DLOGITS> { typedef LogitArgs type; };
+
+// Eight adjacent logits of a row; the BN / 8 lanes that hold the rest of the tile's row are neighbours.
+// E_LSE: the row's maximum and sum of exponentials over the tile.  The maximum is held to finite values, so that a row
+// of -inf sums to 0 (not NaN) and one with an infinity to infinity.
+template <int EPI, int BN>
+__device__ __forceinline__ void logit_epilogue(const float (&v)[8], size_t row, int col, int N, int M, int bn, void* C, const LogitArgs& lg) {
+  constexpr float LOG2E = 1.4426950408889634f;
+  const int label = lg.label[row], at = label - lg.col0 - col;  // the label's place among the eight
+  if constexpr (EPI == E_LSE) {
+    float m = -FLT_MAX, s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = col + e < N ? fmaxf(m, v[e]) : m;
+#pragma unroll
+    for (int o = 1; o < BN / 8; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    m = fminf(m, FLT_MAX);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += col + e < N ? __builtin_amdgcn_exp2f((v[e] - m) * LOG2E) : 0.f;
+#pragma unroll
+    for (int o = 1; o < BN / 8; o <<= 1) s += __shfl_xor(s, o, 64);
+    if (col % BN == 0) {
+      float* p = lg.part + ((size_t)bn * M + row) * 2;
+      p[0] = m;
+      p[1] = s;
+    }
+    if (at >= 0 && at < 8 && col + at < N) {
+      float z = v[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) z = at == e ? v[e] : z;
+      lg.at_label[row] = z;
+    }
+  } else {
+    if (col >= lg.ldc) return;
+    const bool known = label >= 0 && label < lg.S_voc;
+    const float lse = lg.lse[row];
+    float d[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float p = __builtin_amdgcn_exp2f((v[e] - lse) * LOG2E) - (at == e ? 1.f : 0.f);
+      d[e] = known && col + e < N ? p * lg.scale : 0.f;
+    }
+    bf16_t* out = reinterpret_cast<bf16_t*>(C) + row * (size_t)lg.ldc + col;
+    for (int k = 0; k < lg.parts; ++k, out += lg.plane) {
+      bf16x8 o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        o[e] = (__bf16)d[e];
+        d[e] -= (float)o[e];
+      }
+      *reinterpret_cast<bf16x8*>(out) = o;
+    }
+  }
+}
+
 // AK: A is K-contiguous in memory (forward, dgrad); BKC: B is K-contiguous (dgrad)
 // SEG_POW2: the k-tiles per segment are a power of two (weight gradient only; true for every
 // sequence length that is one): the segment of a k-tile is then a shift, not a division, which
@@ -221,7 +281,7 @@ __global__ __launch_bounds__(TL::NT * TL::KG) void gemm_mfma_kernel(int M, int N
                                                            const float* __restrict__ bias, const TO* __restrict__ R,
                                                            TO* __restrict__ C2, int accumulate, int tiles_m, int remap,
                                                            int n_seg, size_t seg_a, size_t seg_b, float* __restrict__ colpart,
-                                                           int ldk) {
+                                                           int ldk, int k_whole, typename LogitArgsOf<EPI>::type lg) {
   constexpr int BM = TL::BM, BN = TL::BN, NT = TL::NT, MI = TL::MI, NI = TL::NI, KG = TL::KG;
   constexpr int A_ST = stage_elems<AK, BM>(), B_ST = stage_elems<BKC, BN>();
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
@@ -253,8 +313,8 @@ __global__ __launch_bounds__(TL::NT * TL::KG) void gemm_mfma_kernel(int M, int N
   }
   const int m0 = bm * BM, n0 = bn * BN;
   // ldk: row length of the operands that are stored K-contiguous; equal to K except in a split-K launch, where K is
-  // the length of the slice this workgroup contracts over
-  const size_t lda = AK ? (size_t)ldk : (size_t)M;   // A stored [M,K] or [K,M]
+  // the length of the slice this workgroup contracts over, and where the caller gives A longer rows (GemmArgs::lda)
+  const size_t lda = (size_t)ldk;                    // A stored [M,K] or [K,M]
   const size_t ldb = BKC ? (size_t)ldk : (size_t)N;  // B stored [N,K] or [K,N]
   if constexpr (EPI == E_ACCUM && AK) {
     // Split-K launch of a forward / dgrad product (grid.y slices of K): slice y starts K elements further along the
@@ -264,6 +324,7 @@ __global__ __launch_bounds__(TL::NT * TL::KG) void gemm_mfma_kernel(int M, int N
     A += y * (size_t)K;
     B += y * (BKC ? (size_t)K : (size_t)K * N);
     C += y * (size_t)M * N;
+    if (EDGE) K = min(K, k_whole - (int)y * K);  // the last slice may be shorter
   }
 
   f32x4 acc[MI][NI];
@@ -538,7 +599,7 @@ __global__ __launch_bounds__(TL::NT * TL::KG) void gemm_mfma_kernel(int M, int N
       for (int q = 0; q < NQ; ++q) {
         const int c = tid + q * NT, lr = c / (BN / 8), lc = (c % (BN / 8)) * 8;
         const size_t row = m0 + p * PR + lr, col = n0 + lc, idx = row * (size_t)N + col;
-        if (EDGE && (grp != 0 || row >= (size_t)M || col >= (size_t)N)) continue;
+        if (EDGE && (grp != 0 || row >= (size_t)M || (EPI != E_LSE && EPI != E_DLOGITS && col >= (size_t)N))) continue;
         float v[8];
         *reinterpret_cast<f32x4*>(v) = *reinterpret_cast<const f32x4*>(cs + lr * LDC + lc);
         *reinterpret_cast<f32x4*>(v + 4) = *reinterpret_cast<const f32x4*>(cs + lr * LDC + lc + 4);
@@ -548,6 +609,10 @@ __global__ __launch_bounds__(TL::NT * TL::KG) void gemm_mfma_kernel(int M, int N
           for (int e = 0; e < 4; ++e) { v[e] += b0[e]; v[4 + e] += b1[e]; }
         }
         bf16x8 o;
+        if constexpr (EPI == E_LSE || EPI == E_DLOGITS) {
+          logit_epilogue<EPI, BN>(v, row, (int)col, N, M, bn, C, lg);
+          continue;
+        }
         if constexpr (EPI == E_BIAS_RES) {
           const bf16x8 rr = rpre[p][q];
 #pragma unroll
@@ -638,11 +703,16 @@ bf_status launch(const GemmArgs& a, hipStream_t st) {
   const int remap = (tiles_m * tiles_n) % 8 == 0 ? 1 : 0;
   // split-K (fp32 planes of partial results, forward / dgrad layouts only): a.K is the whole contraction, the kernel
   // gets the slice length and the row length of the K-contiguous operands separately
+  // (in the edge form slices are whole k-tiles, the last one what is left)
   const int slices = (EPI == E_ACCUM && AK && a.k_slices > 1) ? a.k_slices : 1;
+  const int k_slice = EDGE && slices > 1 ? ((a.K + slices - 1) / slices + BK - 1) / BK * BK : a.K / slices;
   const dim3 grid((unsigned)(tiles_m * tiles_n), (unsigned)slices);
-  kern<<<grid, TL::NT * TL::KG, lds, st>>>(a.M, a.N, a.K / slices, (const bf16_t*)a.A, (const bf16_t*)a.B, (TO*)a.C, a.bias,
+  typename LogitArgsOf<EPI>::type lg;
+  if constexpr (EPI == E_LSE || EPI == E_DLOGITS) lg = a.logit;
+  kern<<<grid, TL::NT * TL::KG, lds, st>>>(a.M, a.N, k_slice, (const bf16_t*)a.A, (const bf16_t*)a.B, (TO*)a.C, a.bias,
                                   (const TO*)a.R, (TO*)a.C2, a.accumulate, tiles_m, remap, a.n_seg > 1 ? a.n_seg : 1,
-                                  a.seg_stride_a, a.seg_stride_b, EPI == E_GELU_BWD ? a.colsum_part : nullptr, a.K);
+                                  a.seg_stride_a, a.seg_stride_b, EPI == E_GELU_BWD ? a.colsum_part : nullptr,
+                                  a.lda ? a.lda : AK ? a.K : a.M, a.K, lg);
   if (EPI == E_GELU_BWD && a.colsum_rows) *a.colsum_rows = tiles_m;
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_error("gemm_mfma launch failed: %s", hipGetErrorString(e)); return BF_EDEVICE; }
@@ -929,6 +999,105 @@ bf_status gemm_mfma(int layout, int epi, const GemmArgs& a, hipStream_t st) {
       if (epi == E_BIAS_RES) return launch<TileWide, true, false, E_BIAS_RES, bf16_t>(a, st);
       return launch<TileWide, true, false, E_NONE, bf16_t>(a, st);
     default: return by_layout<TileSmall>(layout, epi, a, st);
+  }
+}
+
+// ---- the products of the vocabulary loss ---------------------------------------------------------
+// The logits of a tile live in its accumulators and its epilogue's LDS only.  The edge form throughout: any number of rows and
+// columns.  Tiles as for a product of the same shape.
+namespace {
+
+inline int logit_tile(int rows, int cols) { return choose_edge_tile(L_NT, rows, cols); }  // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+
+template <int EPI>
+bf_status logits(const GemmArgs& a, hipStream_t st) {
+  switch (logit_tile(a.M, a.N)) {
+    case 0: return launch<TileBig, true, true, EPI, bf16_t, true>(a, st);
+    case 1: return launch<TileSmall, true, true, EPI, bf16_t, true>(a, st);
+    default: break;
+  }
+  switch (key_groups(L_NT, a.M, a.N, a.K, 1)) {
+    case G_FOUR: return launch<TileTiny4, true, true, EPI, bf16_t, true>(a, st);
+    case G_ONE: return launch<TileTiny, true, true, EPI, bf16_t, true>(a, st);
+    default: return launch<TileTiny2, true, true, EPI, bf16_t, true>(a, st);
+  }
+}
+
+bool logits_ok(int rows, int cols, int h, uintptr_t al) {
+  if (gemm_mfma_logits_supported(rows, cols, h) && !(al & 15)) return true;
+  set_error("gemm_mfma: product of the vocabulary loss not supported");
+  return false;
+}
+
+}  // namespace
+
+bool gemm_mfma_logits_supported(int rows, int cols, int h) {
+  const int most = 1 << 21;  // 32-bit lane offsets over 256 rows
+  return rows >= 1 && cols >= 1 && h >= 8 && h % 8 == 0 && rows <= most && cols <= most && h <= most;
+}
+
+int gemm_mfma_logits_tiles(int rows, int cols) {
+  const int bn[3] = {256, 128, 64}, t = bn[logit_tile(rows, cols)];
+  return (cols + t - 1) / t;
+}
+
+bf_status gemm_mfma_logits_lse(int rows, int cols, int h, const void* y, const void* w, const LogitArgs& l, int* tiles, hipStream_t st) {
+  if (!logits_ok(rows, cols, h, (uintptr_t)y | (uintptr_t)w)) return BF_EINVAL;
+  GemmArgs a{rows, cols, h, y, w, nullptr, nullptr, nullptr, nullptr, 0};
+  a.logit = l;
+  *tiles = gemm_mfma_logits_tiles(rows, cols);
+  return logits<E_LSE>(a, st);
+}
+
+bf_status gemm_mfma_logits_grad(int rows, int cols, int h, const void* y, const void* w, const LogitArgs& l, void* dz, hipStream_t st) {
+  if (!logits_ok(rows, cols, h, (uintptr_t)y | (uintptr_t)w | (uintptr_t)dz) || l.ldc % 8 || l.plane % 8) return BF_EINVAL;
+  GemmArgs a{rows, cols, h, y, w, dz, nullptr, nullptr, nullptr, 0};
+  a.logit = l;
+  return logits<E_DLOGITS>(a, st);
+}
+
+// Slices of the columns: enough workgroups to fill the chip where rows x h has few tiles
+int gemm_mfma_logits_dy_slices(int rows, int cols, int h) {
+  const int t = choose_edge_tile(L_NN, rows, h), e = t == 0 ? 256 : t == 1 ? 128 : 64;
+  const long tiles = (long)((rows + e - 1) / e) * ((h + e - 1) / e), slots = t == 0 ? 256 : 512;
+  long s = slots / tiles;
+  if (s > 16) s = 16;
+  if (s > cols / 1024) s = cols / 1024;
+  return s < 1 ? 1 : (int)s;
+}
+
+bf_status gemm_mfma_logits_dy(int rows, int cols, int h, const void* dz, int ldz, int parts, size_t plane, const void* w, float* planes, int slices,
+                              int accumulate, hipStream_t st) {
+  if (!logits_ok(rows, cols, h, (uintptr_t)dz | (uintptr_t)w | (uintptr_t)planes) || ldz % 8 || plane % 8 || slices < 1) return BF_EINVAL;
+  GemmArgs a{rows, h, cols, dz, w, planes, nullptr, nullptr, nullptr, accumulate};
+  a.lda = ldz;
+  // every slice has to have columns: a shorter piece may take fewer slices than the first one, which writes all planes
+  auto len = [&](int n) { return ((cols + n - 1) / n + BK - 1) / BK * BK; };
+  while (slices > 1 && (long)(slices - 1) * len(slices) >= cols) {
+    if (!accumulate) { set_error("gemm_mfma: %d slices of %d columns", slices, cols); return BF_EINVAL; }
+    --slices;
+  }
+  a.k_slices = slices;
+  a.n_seg = parts;
+  a.seg_stride_a = plane;
+  switch (choose_edge_tile(L_NN, rows, h)) {
+    case 0: return launch<TileBig, true, false, E_ACCUM, float, true>(a, st);
+    case 1: return launch<TileSmall, true, false, E_ACCUM, float, true>(a, st);
+    default: return launch<TileTiny, true, false, E_ACCUM, float, true>(a, st);
+  }
+}
+
+bf_status gemm_mfma_logits_dw(int rows, int cols, int h, const void* dz, int ldz, int parts, size_t plane, const void* y, float* dw, int accumulate,
+                              hipStream_t st) {
+  if (!logits_ok(rows, cols, h, (uintptr_t)dz | (uintptr_t)y | (uintptr_t)dw) || ldz % 8 || plane % 8) return BF_EINVAL;
+  GemmArgs a{cols, h, rows, dz, y, dw, nullptr, nullptr, nullptr, accumulate};
+  a.lda = ldz;
+  a.n_seg = parts;
+  a.seg_stride_a = plane;
+  switch (choose_edge_tile(L_TN, cols, h)) {
+    case 0: return launch<TileBig, false, false, E_ACCUM, float, true>(a, st);
+    case 1: return launch<TileSmall, false, false, E_ACCUM, float, true>(a, st);
+    default: return launch<TileTiny, false, false, E_ACCUM, float, true>(a, st);
   }
 }
 

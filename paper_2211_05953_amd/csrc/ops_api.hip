@@ -4,6 +4,12 @@
 #include "../../include/bf_ops.h"
 #include "common.h"
 
+namespace bf {
+// (takes a type of bf_ops.h)
+bf_status adam_clipped(int n_tensors, const bf_adam_tensor* x, const float* coef, int step, float lr, float beta1, float beta2, float eps, float wd,
+                       hipStream_t st);
+}  // namespace bf
+
 using namespace bf;
 
 static bool dtype_ok(int dtype, int kernels) {
@@ -196,6 +202,40 @@ bf_status bf_op_ce_loss(int dtype, int n_rows, int S_voc, void* z, const int32_t
 bf_status bf_op_adam(size_t n, float* w, float* m, float* v, const float* g, void* w_lp, int t, float lr, float beta1,
                      float beta2, float adam_eps, float weight_decay, void* stream) {
   return adam_step(n, w, m, v, g, (bf16_t*)w_lp, t, nullptr, lr, beta1, beta2, adam_eps, weight_decay, (hipStream_t)stream);
+}
+
+size_t bf_op_vocab_loss_work_bytes(int dtype, int n_rows, int S_hidden, int S_voc, int S_piece, int backward) {
+  return vocab_loss_work_bytes(dtype, n_rows, S_hidden, S_voc, S_piece, backward);
+}
+
+bf_status bf_op_vocab_loss_fwd(int dtype, int n_rows, int S_hidden, int S_voc, int S_piece, const void* y, const void* w_out, const int32_t* labels,
+                               float scale, float* lse, float* row_loss, float* loss_out, void* work, size_t work_bytes, void* stream) {
+  if (!dtype_ok(dtype, 0)) return BF_EINVAL;
+  return vocab_loss_fwd(dtype, n_rows, S_hidden, S_voc, S_piece, y, w_out, labels, scale, lse, row_loss, loss_out, work, work_bytes, (hipStream_t)stream);
+}
+
+bf_status bf_op_vocab_loss_bwd(int dtype, int n_rows, int S_hidden, int S_voc, int S_piece, const void* y, const void* w_out, const int32_t* labels,
+                               const float* lse, float scale, void* dy, float* dw, int accumulate, void* work, size_t work_bytes, void* stream) {
+  if (!dtype_ok(dtype, 0)) return BF_EINVAL;
+  return vocab_loss_bwd(dtype, n_rows, S_hidden, S_voc, S_piece, y, w_out, labels, lse, scale, dy, dw, accumulate, work, work_bytes, (hipStream_t)stream);
+}
+
+size_t bf_op_grad_norm_work_bytes(int n_tensors, const size_t* n) { return grad_norm_work_bytes(n_tensors, n); }
+
+bf_status bf_op_grad_norm(int dtype, int n_tensors, const void* const* g, const size_t* n, float max_norm, float* out, void* work,
+                          size_t work_bytes, void* stream) {
+  if (!dtype_ok(dtype, 0)) return BF_EINVAL;
+  return grad_norm(dtype, n_tensors, g, n, max_norm, out, work, work_bytes, (hipStream_t)stream);
+}
+
+bf_status bf_op_grad_scale(int dtype, int n_tensors, const void* const* g, void* const* dst, const size_t* n, const float* coef, void* stream) {
+  if (!dtype_ok(dtype, 0)) return BF_EINVAL;
+  return grad_scale(dtype, n_tensors, g, dst, n, coef, (hipStream_t)stream);
+}
+
+bf_status bf_op_adam_clipped(int n_tensors, const bf_adam_tensor* tensors, const float* coef, int t, float lr, float beta1, float beta2,
+                             float adam_eps, float weight_decay, void* stream) {
+  return adam_clipped(n_tensors, tensors, coef, t, lr, beta1, beta2, adam_eps, weight_decay, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,367 @@
+// Softmax cross entropy of a linear layer over a large vocabulary, in pieces of the vocabulary: z = y W^T is never kept.
+//
+//   lse_t = log sum_v exp z_tv,   row_loss_t = (lse_t - z_t,label) scale,   dz = scale (exp(z - lse) - onehot)
+//   dy = dz W,   dW = dz^T y
+//
+// Forward: the product's epilogue reduces each tile of logits to a maximum and a sum of exponentials per row (and picks the
+// label's logit); a second kernel merges the tiles in their order.  No logit reaches HBM.  Backward: piece by piece of the
+// vocabulary, the product again with dz as its epilogue, then the two gradient products on that piece: 6 T h V operations
+// beside the forward pass's 2.
+//
+// Precision.  dW is an fp32 main-grad: dz enters its product as two bf16 parts (16 bits and a sign; their error, 1.4e-6 of dz, is that
+// of the logits themselves), or three where the rows are few and the product waits for HBM anyway.  dy is stored in bf16: one
+// part, rounded once more than the result, as every bf16 tensor between kernels here.
+//
+// Rows whose label is outside the vocabulary have no loss and no gradient, whatever their y holds: dz is set to zero, and dW's
+// product reads a copy of y in which those rows are zero (a zero times an infinity is a NaN).
+#include <float.h>
+#include <math.h>
+
+#include "../../include/bf_ops.h"
+#include "common.h"
+
+namespace bf {
+
+namespace {
+
+constexpr int NT = 256;
+constexpr float LOG2E = 1.4426950408889634f;
+
+inline size_t up(size_t n, size_t m) { return (n + m - 1) / m * m; }
+
+bf_status launched() {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) { set_error("vocab_loss: launch failed: %s", hipGetErrorString(e)); return BF_EDEVICE; }
+  return BF_OK;
+}
+
+// (m, s) and (m2, s2): maxima, and sums of exponentials relative to them
+__device__ __forceinline__ void merge(float& m, float& s, float m2, float s2) {
+  const float top = fmaxf(m, m2);
+  s = s * __builtin_amdgcn_exp2f((m - top) * LOG2E) + s2 * __builtin_amdgcn_exp2f((m2 - top) * LOG2E);
+  m = top;
+}
+
+// 32 rows a workgroup, 8 threads to a row, each over every eighth tile in ascending order
+__global__ __launch_bounds__(NT) void lse_merge_kernel(int rows, int tiles, const float2* __restrict__ part, const float* __restrict__ at_label,
+                                                       const int32_t* __restrict__ label, int S_voc, float scale, float* __restrict__ lse,
+                                                       float* __restrict__ row_loss) {
+  __shared__ float2 red[8][32];
+  const int r = threadIdx.x & 31, g = threadIdx.x >> 5, row = blockIdx.x * 32 + r;
+  float m = -FLT_MAX, s = 0.f;
+  if (row < rows) {
+#pragma unroll 4
+    for (int k = g; k < tiles; k += 8) {
+      const float2 p = part[(size_t)k * rows + row];
+      merge(m, s, p.x, p.y);
+    }
+  }
+  red[g][r] = make_float2(m, s);
+  __syncthreads();
+  if (g || row >= rows) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) merge(m, s, red[k][r].x, red[k][r].y);
+  const float l = m + logf(s);
+  lse[row] = l;
+  const int v = label[row];
+  row_loss[row] = v >= 0 && v < S_voc ? (l - at_label[row]) * scale : 0.f;
+}
+
+__global__ __launch_bounds__(1024) void loss_sum_kernel(int rows, const float* __restrict__ row_loss, float* __restrict__ out) {
+  double s = 0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < rows; i += 1024) s += (double)row_loss[i];
+  __shared__ double red[16];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (int k = 1; k < 16; ++k) s += red[k];
+  out[0] = (float)s;
+}
+
+// dst = src, rows without a label in the vocabulary as zeros
+template <typename TS, typename TD>
+__global__ __launch_bounds__(NT) void labelled_rows_kernel(int h, const TS* __restrict__ src, const int32_t* __restrict__ label, int S_voc,
+                                                           TD* __restrict__ dst) {
+  const size_t row = blockIdx.x;
+  const int v = label[row];
+  const bool known = v >= 0 && v < S_voc;
+  const TS* s = src + row * (size_t)h;
+  TD* d = dst + row * (size_t)h;
+  for (int c = threadIdx.x; c < h; c += NT) d[c] = known ? (TD)(float)s[c] : (TD)0.f;
+}
+
+// the same for rows of whole 16-byte chunks of bf16
+__global__ __launch_bounds__(NT) void labelled_rows16_kernel(int chunks, const uint4* __restrict__ src, const int32_t* __restrict__ label, int S_voc,
+                                                             uint4* __restrict__ dst) {
+  const size_t row = blockIdx.x;
+  const int v = label[row];
+  const bool known = v >= 0 && v < S_voc;
+  for (int c = threadIdx.x; c < chunks; c += NT) dst[row * chunks + c] = known ? src[row * chunks + c] : make_uint4(0, 0, 0, 0);
+}
+
+template <typename TS, typename TD>
+__global__ __launch_bounds__(NT) void convert_kernel(size_t n, const TS* __restrict__ src, TD* __restrict__ dst) {
+  for (size_t i = (size_t)blockIdx.x * NT + threadIdx.x; i < n; i += (size_t)gridDim.x * NT) dst[i] = (TD)(float)src[i];
+}
+
+__global__ __launch_bounds__(NT) void add_kernel(size_t n, const float* __restrict__ src, float* __restrict__ dst) {
+  for (size_t i = (size_t)blockIdx.x * NT + threadIdx.x; i < n; i += (size_t)gridDim.x * NT) dst[i] += src[i];
+}
+
+inline unsigned grid_for(size_t n) {
+  const size_t g = (n + NT - 1) / NT;
+  return (unsigned)(g < 1 ? 1 : g > 4096 ? 4096 : g);
+}
+
+// ---- fp32 logits, a piece at a time (fp32 tensors, and bf16 ones whose rows are not whole 16-byte chunks)
+// statistics of a row of the piece, merged into what earlier pieces left
+__global__ __launch_bounds__(NT) void piece_lse_kernel(int rows, int cols, const float* __restrict__ z, const int32_t* __restrict__ label, int col0,
+                                                       int first, float2* __restrict__ stat, float* __restrict__ at_label) {
+  const int row = blockIdx.x;
+  const float* zr = z + (size_t)row * cols;
+  float m = -FLT_MAX, s = 0.f;
+  for (int c = threadIdx.x; c < cols; c += NT) m = fmaxf(m, zr[c]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  __shared__ float red[2][NT / 64];
+  if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = m;
+  __syncthreads();
+  m = fminf(fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3])), FLT_MAX);
+  for (int c = threadIdx.x; c < cols; c += NT) s += expf(zr[c] - m);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) red[1][threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x) return;
+  s = red[1][0] + red[1][1] + red[1][2] + red[1][3];
+  if (!first) merge(m, s, stat[row].x, stat[row].y);
+  stat[row] = make_float2(m, s);
+  const int at = label[row] - col0;
+  if (at >= 0 && at < cols) at_label[row] = zr[at];
+}
+
+__global__ __launch_bounds__(NT) void piece_dz_kernel(int cols, float* __restrict__ z, const int32_t* __restrict__ label, const float* __restrict__ lse,
+                                                      int col0, int S_voc, float scale) {
+  const size_t row = blockIdx.x;
+  float* zr = z + row * (size_t)cols;
+  const int v = label[row], at = v - col0;
+  const bool known = v >= 0 && v < S_voc;
+  const float l = lse[row];
+  for (int c = threadIdx.x; c < cols; c += NT) zr[c] = known ? (expf(zr[c] - l) - (c == at ? 1.f : 0.f)) * scale : 0.f;
+}
+
+// ---- sizes ---------------------------------------------------------------------------------------
+constexpr size_t PIECE_BYTES = (size_t)256 << 20;  // of dz: what the memory-side cache holds, and little beside 288 GB
+
+// dz's parts: see above.  Up to 64 rows dW's product is the writing of dW.
+inline int parts_of(int rows) { return rows <= 64 ? 3 : 2; }
+
+struct Plan {
+  bool matrix;   // bf16 matrix cores, else fp32 products
+  int piece;     // columns
+  int pieces;
+  // offsets into the scratch: copy of y, fp32 piece of W, z / dz, planes or sums of dy, statistics, labels' logits
+  size_t y, w, z, dy, stat, lab, total;
+  int slices;
+};
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+bool sizes_ok(int dtype, int rows, int h, int V, int piece) {
+  return (dtype == BF_FP32 || dtype == BF_BF16) && rows >= 1 && h >= 1 && V >= 1 && piece >= 0 && rows <= (1 << 21) && h <= (1 << 21) && V <= (1 << 21);
+}
+
+// `matrix` depends on the tensors' alignment too: the scratch is sized for the larger of the two
+Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool backward) {
+  Plan p{};
+  p.matrix = matrix;
+  const size_t per_col = (size_t)rows * (matrix ? 2 * (size_t)parts_of(rows) : 4);
+  size_t cols = piece ? (size_t)piece : PIECE_BYTES / per_col;
+  if (cols < 1024 && !piece) cols = 1024;
+  if (matrix && !backward) cols = (size_t)V;  // the forward product keeps nothing
+  if (cols > (size_t)V) cols = (size_t)V;
+  p.pieces = (int)((V + cols - 1) / cols);
+  if (!piece) cols = up((V + p.pieces - 1) / p.pieces, 512);  // pieces of about the same size
+  else if (matrix) cols = up(cols, 8);
+  if (cols > (size_t)V) cols = (size_t)V;
+  p.piece = (int)cols;
+  p.pieces = (int)((V + cols - 1) / cols);
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes, 256); return o; };
+  if (matrix) {
+    if (backward) {
+      p.slices = gemm_mfma_logits_dy_slices(rows, p.piece, h);
+      p.y = take((size_t)rows * h * 2);
+      p.z = take((size_t)rows * up(cols, 8) * 2 * parts_of(rows));
+      p.dy = take((size_t)p.slices * rows * h * 4);
+    } else {
+      p.stat = take((size_t)gemm_mfma_logits_tiles(rows, V) * rows * 8);
+      p.lab = take((size_t)rows * 4);
+    }
+  } else {
+    p.y = take((size_t)rows * h * 4);
+    if (dtype == BF_BF16) p.w = take(cols * h * 4);
+    p.z = take((size_t)rows * cols * 4);
+    if (backward) {
+      p.stat = take(p.pieces > 1 ? (size_t)rows * h * 4 : 0);  // a later piece's share of dy
+      if (dtype == BF_BF16) p.dy = take((size_t)rows * h * 4);
+    } else {
+      p.stat = take((size_t)rows * 8);
+      p.lab = take((size_t)rows * 4);
+    }
+  }
+  p.total = at;
+  return p;
+}
+
+bool matrix_possible(int dtype, int rows, int h, int V) { return dtype == BF_BF16 && gemm_mfma_logits_supported(rows, V, h); }
+
+// fp32 y and W piece of the fp32 products
+bf_status widen(int dtype, size_t n, const void* src, float* dst, hipStream_t st) {
+  if (dtype == BF_BF16) convert_kernel<bf16_t, float><<<grid_for(n), NT, 0, st>>>(n, (const bf16_t*)src, dst);
+  return launched();
+}
+
+bf_status product(int layout, int epi, GemmArgs a, hipStream_t st) { return gemm(BF_FP32, BF_KERNELS_AUTO, layout, epi, a, st); }
+
+}  // namespace
+
+size_t vocab_loss_work_bytes(int dtype, int rows, int h, int V, int piece, int backward) {
+  if (!sizes_ok(dtype, rows, h, V, piece)) return 0;
+  size_t n = plan_for(false, dtype, rows, h, V, piece, backward != 0).total;
+  if (matrix_possible(dtype, rows, h, V)) {
+    const size_t m = plan_for(true, dtype, rows, h, V, piece, backward != 0).total;
+    n = n > m ? n : m;
+  }
+  return n;
+}
+
+static bf_status check_args(const char* who, int dtype, int rows, int h, int V, int piece, const void* y, const void* w, const int32_t* label, const void* a,
+                            const void* b, const void* c, float scale, const void* work, size_t work_bytes, int backward) {
+  if (!sizes_ok(dtype, rows, h, V, piece)) { set_error("%s: bad type or sizes (1 .. 2^21)", who); return BF_EINVAL; }
+  if (!y || !w || !label || !a || !b || !c) { set_error("%s: null pointer", who); return BF_EINVAL; }
+  if (!(fabsf(scale) <= FLT_MAX)) { set_error("%s: scale is not finite", who); return BF_EINVAL; }
+  const size_t need = vocab_loss_work_bytes(dtype, rows, h, V, piece, backward);
+  if (!work || ((uintptr_t)work & 255) || work_bytes < need) { set_error("%s: needs %zu bytes of 256-byte aligned scratch", who, need); return BF_EINVAL; }
+  return BF_OK;
+}
+
+bf_status vocab_loss_fwd(int dtype, int rows, int h, int V, int piece, const void* y, const void* w, const int32_t* label, float scale, float* lse,
+                         float* row_loss, float* loss, void* work, size_t work_bytes, hipStream_t st) {
+  bf_status s = check_args("bf_op_vocab_loss_fwd", dtype, rows, h, V, piece, y, w, label, lse, row_loss, loss, scale, work, work_bytes, 0);
+  if (s != BF_OK) return s;
+  const Plan p = plan_for(matrix_possible(dtype, rows, h, V) && aligned16(y) && aligned16(w), dtype, rows, h, V, piece, false);
+  char* ws = (char*)work;
+  float* stat = (float*)(ws + p.stat);
+  int tiles = 1;
+  float* at_label = (float*)(ws + p.lab);
+  if (p.matrix) {
+    LogitArgs l;
+    l.label = label;
+    l.part = stat;
+    l.at_label = at_label;
+    s = gemm_mfma_logits_lse(rows, V, h, y, w, l, &tiles, st);
+    if (s != BF_OK) return s;
+  } else {
+    float* z = (float*)(ws + p.z);
+    const float* yf = (const float*)y;
+    if (dtype == BF_BF16) {
+      s = widen(dtype, (size_t)rows * h, y, (float*)(ws + p.y), st);
+      if (s != BF_OK) return s;
+      yf = (const float*)(ws + p.y);
+    }
+    for (int c0 = 0; c0 < V; c0 += p.piece) {
+      const int cols = V - c0 < p.piece ? V - c0 : p.piece;
+      const float* wf = (const float*)w + (size_t)c0 * h;
+      if (dtype == BF_BF16) {
+        s = widen(dtype, (size_t)cols * h, (const bf16_t*)w + (size_t)c0 * h, (float*)(ws + p.w), st);
+        if (s != BF_OK) return s;
+        wf = (const float*)(ws + p.w);
+      }
+      s = product(L_NT, E_NONE, GemmArgs{rows, cols, h, yf, wf, z, nullptr, nullptr, nullptr, 0}, st);
+      if (s != BF_OK) return s;
+      piece_lse_kernel<<<rows, NT, 0, st>>>(rows, cols, z, label, c0, c0 == 0, (float2*)stat, at_label);
+      s = launched();
+      if (s != BF_OK) return s;
+    }
+  }
+  lse_merge_kernel<<<(rows + 31) / 32, NT, 0, st>>>(rows, tiles, (const float2*)stat, at_label, label, V, scale, lse, row_loss);
+  s = launched();
+  if (s != BF_OK) return s;
+  loss_sum_kernel<<<1, 1024, 0, st>>>(rows, row_loss, loss);
+  return launched();
+}
+
+bf_status vocab_loss_bwd(int dtype, int rows, int h, int V, int piece, const void* y, const void* w, const int32_t* label, const float* lse, float scale,
+                         void* dy, float* dw, int accumulate, void* work, size_t work_bytes, hipStream_t st) {
+  bf_status s = check_args("bf_op_vocab_loss_bwd", dtype, rows, h, V, piece, y, w, label, lse, dy, dw, scale, work, work_bytes, 1);
+  if (s != BF_OK) return s;
+  const bool al = aligned16(y) && aligned16(w) && aligned16(dy) && aligned16(dw);
+  const Plan p = plan_for(matrix_possible(dtype, rows, h, V) && al, dtype, rows, h, V, piece, true);
+  char* ws = (char*)work;
+  if (p.matrix) {
+    bf16_t* yc = (bf16_t*)(ws + p.y);
+    float* planes = (float*)(ws + p.dy);
+    labelled_rows16_kernel<<<rows, NT, 0, st>>>(h / 8, (const uint4*)y, label, V, (uint4*)yc);
+    s = launched();
+    for (int c0 = 0; c0 < V && s == BF_OK; c0 += p.piece) {
+      const int cols = V - c0 < p.piece ? V - c0 : p.piece;
+      LogitArgs l;
+      l.label = label;
+      l.lse = lse;
+      l.scale = scale;
+      l.col0 = c0;
+      l.S_voc = V;
+      l.parts = parts_of(rows);
+      l.ldc = (int)up(cols, 8);
+      l.plane = (size_t)rows * l.ldc;
+      void* dz = ws + p.z;
+      const bf16_t* wp = (const bf16_t*)w + (size_t)c0 * h;
+      s = gemm_mfma_logits_grad(rows, cols, h, y, wp, l, dz, st);
+      if (s == BF_OK) s = gemm_mfma_logits_dw(rows, cols, h, dz, l.ldc, l.parts, l.plane, yc, dw + (size_t)c0 * h, accumulate, st);
+      if (s == BF_OK) s = gemm_mfma_logits_dy(rows, cols, h, dz, l.ldc, 1, l.plane, wp, planes, p.slices, c0 > 0, st);
+    }
+    if (s != BF_OK) return s;
+    if (p.slices > 1) return gemm_splitk_finish(E_NONE, rows, h, p.slices, planes, nullptr, nullptr, dy, st);
+    return cast_f32_to_bf16((size_t)rows * h, planes, (bf16_t*)dy, st);
+  }
+  float* yc = (float*)(ws + p.y);
+  float* z = (float*)(ws + p.z);
+  float* share = (float*)(ws + p.stat);
+  float* dyf = dtype == BF_BF16 ? (float*)(ws + p.dy) : (float*)dy;
+  for (int c0 = 0; c0 < V; c0 += p.piece) {
+    const int cols = V - c0 < p.piece ? V - c0 : p.piece;
+    const float *wf = (const float*)w + (size_t)c0 * h, *yf = (const float*)y;
+    if (dtype == BF_BF16) {
+      s = widen(dtype, (size_t)cols * h, (const bf16_t*)w + (size_t)c0 * h, (float*)(ws + p.w), st);
+      if (s != BF_OK) return s;
+      s = widen(dtype, (size_t)rows * h, y, yc, st);
+      if (s != BF_OK) return s;
+      wf = (const float*)(ws + p.w);
+      yf = yc;
+    }
+    s = product(L_NT, E_NONE, GemmArgs{rows, cols, h, yf, wf, z, nullptr, nullptr, nullptr, 0}, st);
+    if (s != BF_OK) return s;
+    piece_dz_kernel<<<rows, NT, 0, st>>>(cols, z, label, lse, c0, V, scale);
+    if (dtype == BF_BF16) labelled_rows_kernel<bf16_t, float><<<rows, NT, 0, st>>>(h, (const bf16_t*)y, label, V, yc);
+    else if (c0 == 0) labelled_rows_kernel<float, float><<<rows, NT, 0, st>>>(h, (const float*)y, label, V, yc);
+    s = launched();
+    if (s != BF_OK) return s;
+    s = product(L_NN, E_NONE, GemmArgs{rows, h, cols, z, wf, c0 ? share : dyf, nullptr, nullptr, nullptr, 0}, st);
+    if (s != BF_OK) return s;
+    if (c0) {
+      add_kernel<<<grid_for((size_t)rows * h), NT, 0, st>>>((size_t)rows * h, share, dyf);
+      s = launched();
+      if (s != BF_OK) return s;
+    }
+    s = product(L_TN, E_ACCUM, GemmArgs{cols, h, rows, z, yc, dw + (size_t)c0 * h, nullptr, nullptr, nullptr, accumulate}, st);
+    if (s != BF_OK) return s;
+  }
+  if (dtype == BF_BF16) return cast_f32_to_bf16((size_t)rows * h, dyf, (bf16_t*)dy, st);
+  return BF_OK;
+}
+
+}  // namespace bf
