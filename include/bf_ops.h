@@ -140,6 +140,46 @@ bf_status bf_op_attention_bwd_static(int dtype, int kernels, int S_mb, int S_seq
                                      void* dqkv, void* stream);
 int bf_op_attention_uses_mfma(int S_seq, int S_head);
 
+/* Attention under masks, with capped scores, a distance bias and shared key / value heads (for sequences that hold several
+ * documents).  A row's keys are one interval, its span:
+ *   _spans  from doc (device int32 [S_mb, S_seq], or NULL: a sequence is one document): a document is a run of equal ids; its
+ *           tokens see that document and nothing else.  A token of a negative id is padding: it sees nothing and no token
+ *           sees it.  causal = 1: keys j <= i only, or j < prefix[b] (device int32 [S_mb], or NULL) where that is more; the
+ *           first prefix[b] tokens of a sequence are then seen from in front of them too, inside their documents.
+ *           spans: device int32, 16-byte aligned, bf_op_attention_spans_elems(S_mb, S_seq) elements (0 for bad sizes): made once, used by
+ *           every layer's forward and backward.  S_seq is at most 2^24.
+ *   _fwd    ctx = softmax(b) V over each row's span with b_ij = c_ij - slopes[head] |i - j| (slopes: device fp32 [N_heads], or
+ *           NULL), c_ij = cap tanh(scale q_i.k_j / cap), or scale q_i.k_j where cap is 0.  lse [S_mb, N_heads, S_seq] (device fp32, may
+ *           be NULL) = log-sum-exp of a row's b.  A row without keys: ctx 0, lse -infinity.
+ *   _bwd    dq, dk, dv from dctx, with the ctx and lse of the forward pass; dk and dv are the sums over the N_heads / N_kv_heads
+ *           query heads of a key / value head, head a reading key / value head a / (N_heads / N_kv_heads).  A row
+ *           without keys has dq 0 and no part in dk and dv, whatever its q and dctx hold; a row of one key has no part in
+ *           dq and dk.  Slopes have no gradient.  work: device scratch, 256-byte aligned, of _bwd_work_bytes(cfg)
+ *           bytes (0 for a bad cfg), owned by the caller; calls that overlap need their own.
+ * Token t of sequence b starts (b S_seq + t) ld elements into its tensor, head a another a S_head elements on; ld_q, ld_k, ld_v (for
+ * q and dq, k and dk, v and dv) and ld_ctx (ctx, dctx) of 0 mean rows without gaps, so that a packed [Q | K | V] is three pointers
+ * into it and its row length.  Nothing between the rows is written.  What a mask hides never reaches a result, infinities and NaN
+ * included.  Sums have a fixed order: no atomics on memory.
+ * S_head 1 to 1024, S_mb * N_heads up to 65535.  S_head up to 128 on the matrix cores (bf16: probabilities and their gradients in bf16 as they enter the products;
+ * fp32: fp32 throughout), fastest where rows are whole 16-byte chunks; above, and with BF_KERNELS_PLAIN, on plain kernels. */
+typedef struct {
+  int32_t dtype, kernels;                            /* bf_dtype of all tensors but lse and slopes; bf_kernels */
+  int32_t S_mb, S_seq, N_heads, N_kv_heads, S_head;  /* N_kv_heads divides N_heads */
+  float scale;                                       /* 0: 1/sqrt(S_head) */
+  float cap;                                         /* 0: none */
+  int64_t ld_q, ld_k, ld_v, ld_ctx;
+} bf_attn_config;
+size_t bf_op_attention_spans_elems(int S_mb, int S_seq);
+bf_status bf_op_attention_spans(int S_mb, int S_seq, int causal, const int32_t* doc, const int32_t* prefix, int32_t* spans,
+                                void* stream);
+bf_status bf_op_attention_masked_fwd(const bf_attn_config* cfg, const void* q, const void* k, const void* v,
+                                     const int32_t* spans, const float* slopes, void* ctx, float* lse, void* stream);
+size_t bf_op_attention_masked_bwd_work_bytes(const bf_attn_config* cfg);
+bf_status bf_op_attention_masked_bwd(const bf_attn_config* cfg, const void* q, const void* k, const void* v,
+                                     const int32_t* spans, const float* slopes, const void* ctx, const float* lse,
+                                     const void* dctx, void* dq, void* dk, void* dv, void* work, size_t work_bytes,
+                                     void* stream);
+
 /* Input layer (App. A.1): x[t, :] = e_tok[tokens[t], :] + e_pos[t mod S_seq, :] for n_rows = S_mb * S_seq rows.
  * tokens: device int32 [n_rows]; e_tok [S_voc, S_hidden], e_pos [S_seq, S_hidden] device fp32; x in `dtype`.
  * An id outside 0..S_voc-1 contributes no token row. */

@@ -62,6 +62,11 @@ class bf_sched_stats(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("makespan", "busy", "bubble_num", "bubble_den", "peak_live")]
 
 
+class bf_attn_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "kernels", "S_mb", "S_seq", "N_heads", "N_kv_heads", "S_head")] + \
+               [("scale", C.c_float), ("cap", C.c_float)] + [(n, C.c_int64) for n in ("ld_q", "ld_k", "ld_v", "ld_ctx")]
+
+
 class bf_adam_tensor(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("w", "m", "v", "g", "w_lp")] + [("n", C.c_size_t)]
 
@@ -116,6 +121,11 @@ _SIGNATURES = {
     "bf_op_embedding_fwd": (C.c_int, [C.c_int] * 5 + [_P, _P, _P, _P, _P]),
     "bf_op_embedding_bwd": (C.c_int, [C.c_int] * 5 + [_P, _P, _P, _P, C.c_int, _P]),
     "bf_op_ce_loss": (C.c_int, [C.c_int] * 3 + [_P, _P, C.c_float, _P, _P, _P]),
+    "bf_op_attention_spans_elems": (C.c_size_t, [C.c_int] * 2),
+    "bf_op_attention_spans": (C.c_int, [C.c_int] * 3 + [_P] * 4),
+    "bf_op_attention_masked_fwd": (C.c_int, [_P] * 9),
+    "bf_op_attention_masked_bwd_work_bytes": (C.c_size_t, [_P]),
+    "bf_op_attention_masked_bwd": (C.c_int, [_P] * 13 + [C.c_size_t, _P]),
     "bf_op_vocab_loss_work_bytes": (C.c_size_t, [C.c_int] * 6),
     "bf_op_vocab_loss_fwd": (C.c_int, [C.c_int] * 5 + [_P, _P, _P, C.c_float, _P, _P, _P, _P, C.c_size_t, _P]),
     "bf_op_vocab_loss_bwd": (C.c_int, [C.c_int] * 5 + [_P, _P, _P, _P, C.c_float, _P, _P, C.c_int, _P, C.c_size_t, _P]),
@@ -463,6 +473,69 @@ def _list(tensors):
 def _elems(who, tensor, n):
     if tensor.numel() < n:
         raise ValueError("%s: a tensor of %d elements where %d are used" % (who, tensor.numel(), n))
+
+
+def make_attn_config(dtype, S_mb, S_seq, N_heads, N_kv_heads, S_head, scale=0.0, cap=0.0, ld_q=0, ld_k=0, ld_v=0, ld_ctx=0, kernels=BF_KERNELS_AUTO):
+    return bf_attn_config(dtype, kernels, S_mb, S_seq, N_heads, N_kv_heads, S_head, scale, cap, ld_q, ld_k, ld_v, ld_ctx)
+
+
+def bf_op_attention_spans_elems(S_mb, S_seq):
+    return load().bf_op_attention_spans_elems(S_mb, S_seq)
+
+
+def bf_op_attention_spans(S_mb, S_seq, causal, doc, prefix, spans):
+    """spans (int32, bf_op_attention_spans_elems) from document ids [S_mb, S_seq] and prefix lengths [S_mb], int32 or None each."""
+    import torch
+    who = "bf_op_attention_spans"
+    _tensors(who, [t for t in (doc, prefix, spans) if t is not None], torch.int32)
+    for t, n in ((doc, S_mb * S_seq), (prefix, S_mb), (spans, bf_op_attention_spans_elems(S_mb, S_seq))):
+        if t is not None:
+            _elems(who, t, n)
+    check(load().bf_op_attention_spans(S_mb, S_seq, causal, _ptr(doc), _ptr(prefix), _ptr(spans), _stream()))
+
+
+def _attn_tensors(who, cfg, spans, slopes, lse, rows):
+    """rows: (tensor, heads, step from a token to the next) each; the tensors may be views into longer rows."""
+    import torch
+    dev, dtype = torch.cuda.current_device(), _torch_dtype(cfg.dtype)
+    for t, heads, ld in rows:
+        n = heads * cfg.S_head
+        if t.dtype is not dtype or t.device.type != "cuda" or t.device.index != dev:
+            raise ValueError("%s: needs %s tensors on cuda:%d, got %s on %s" % (who, dtype, dev, t.dtype, t.device))
+        # what the kernels reach from the tensor's first element on has to lie in its storage
+        if ((cfg.S_mb * cfg.S_seq - 1) * (ld or n) + n + t.storage_offset()) * t.element_size() > t.untyped_storage().nbytes():
+            raise ValueError("%s: a tensor of shape %s does not hold %d rows of %d, %d apart" % (who, tuple(t.shape), cfg.S_mb * cfg.S_seq, n, ld or n))
+        if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError("%s: a token's row is not dense, strides %s" % (who, t.stride()))
+    _tensors(who, (spans,), torch.int32)
+    _elems(who, spans, bf_op_attention_spans_elems(cfg.S_mb, cfg.S_seq))
+    if slopes is not None:
+        _tensors(who, (slopes,), torch.float32)
+        _elems(who, slopes, cfg.N_heads)
+    if lse is not None:
+        _tensors(who, (lse,), torch.float32)
+        _elems(who, lse, cfg.S_mb * cfg.N_heads * cfg.S_seq)
+
+
+def bf_op_attention_masked_fwd(cfg, q, k, v, spans, slopes, ctx, lse=None):
+    _attn_tensors("bf_op_attention_masked_fwd", cfg, spans, slopes, lse,
+                  ((q, cfg.N_heads, cfg.ld_q), (k, cfg.N_kv_heads, cfg.ld_k), (v, cfg.N_kv_heads, cfg.ld_v), (ctx, cfg.N_heads, cfg.ld_ctx)))
+    check(load().bf_op_attention_masked_fwd(C.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), spans.data_ptr(), _ptr(slopes), ctx.data_ptr(), _ptr(lse),
+                                            _stream()))
+
+
+def bf_op_attention_masked_bwd_work_bytes(cfg):
+    return load().bf_op_attention_masked_bwd_work_bytes(C.byref(cfg))
+
+
+def bf_op_attention_masked_bwd(cfg, q, k, v, spans, slopes, ctx, lse, dctx, dq, dk, dv, work=None):
+    who, h, kv = "bf_op_attention_masked_bwd", cfg.N_heads, cfg.N_kv_heads
+    _attn_tensors(who, cfg, spans, slopes, lse, ((q, h, cfg.ld_q), (k, kv, cfg.ld_k), (v, kv, cfg.ld_v), (ctx, h, cfg.ld_ctx), (dctx, h, cfg.ld_ctx),
+                                                 (dq, h, cfg.ld_q), (dk, kv, cfg.ld_k), (dv, kv, cfg.ld_v)))
+    work = _work(who, work, bf_op_attention_masked_bwd_work_bytes(cfg))
+    check(load().bf_op_attention_masked_bwd(C.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), spans.data_ptr(), _ptr(slopes), ctx.data_ptr(),
+                                            lse.data_ptr(), dctx.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), work.data_ptr(),
+                                            work.numel() * work.element_size(), _stream()))
 
 
 def bf_op_vocab_loss_work_bytes(dtype, n_rows, S_hidden, S_voc, S_piece=0, backward=0):

@@ -5,7 +5,14 @@
 #include "common.h"
 
 namespace bf {
-// (takes a type of bf_ops.h)
+// (these take types of bf_ops.h)
+size_t attention_spans_elems(int S_mb, int S_seq);
+bf_status attention_spans(int S_mb, int S_seq, int causal, const int32_t* doc, const int32_t* prefix, int32_t* spans, hipStream_t st);
+bf_status attention_masked_fwd(const bf_attn_config* c, const void* q, const void* k, const void* v, const int32_t* spans, const float* slopes, void* ctx,
+                               float* lse, hipStream_t st);
+size_t attention_masked_bwd_work_bytes(const bf_attn_config* c);
+bf_status attention_masked_bwd(const bf_attn_config* c, const void* q, const void* k, const void* v, const int32_t* spans, const float* slopes, const void* ctx,
+                               const float* lse, const void* dctx, void* dq, void* dk, void* dv, void* work, size_t work_bytes, hipStream_t st);
 bf_status adam_clipped(int n_tensors, const bf_adam_tensor* x, const float* coef, int step, float lr, float beta1, float beta2, float eps, float wd,
                        hipStream_t st);
 }  // namespace bf
@@ -180,6 +187,25 @@ bf_status bf_op_attention_bwd_static(int dtype, int kernels, int S_mb, int S_seq
 }
 
 int bf_op_attention_uses_mfma(int S_seq, int S_head) { return attention_mfma_supported(S_seq, S_head) ? 1 : 0; }
+
+size_t bf_op_attention_spans_elems(int S_mb, int S_seq) { return attention_spans_elems(S_mb, S_seq); }
+
+bf_status bf_op_attention_spans(int S_mb, int S_seq, int causal, const int32_t* doc, const int32_t* prefix, int32_t* spans, void* stream) {
+  return attention_spans(S_mb, S_seq, causal, doc, prefix, spans, (hipStream_t)stream);
+}
+
+bf_status bf_op_attention_masked_fwd(const bf_attn_config* cfg, const void* q, const void* k, const void* v, const int32_t* spans, const float* slopes,
+                                     void* ctx, float* lse, void* stream) {
+  return attention_masked_fwd(cfg, q, k, v, spans, slopes, ctx, lse, (hipStream_t)stream);
+}
+
+size_t bf_op_attention_masked_bwd_work_bytes(const bf_attn_config* cfg) { return attention_masked_bwd_work_bytes(cfg); }
+
+bf_status bf_op_attention_masked_bwd(const bf_attn_config* cfg, const void* q, const void* k, const void* v, const int32_t* spans, const float* slopes,
+                                     const void* ctx, const float* lse, const void* dctx, void* dq, void* dk, void* dv, void* work, size_t work_bytes,
+                                     void* stream) {
+  return attention_masked_bwd(cfg, q, k, v, spans, slopes, ctx, lse, dctx, dq, dk, dv, work, work_bytes, (hipStream_t)stream);
+}
 
 bf_status bf_op_embedding_fwd(int dtype, int n_rows, int S_seq, int S_voc, int S_hidden, const int32_t* tokens,
                               const float* e_tok, const float* e_pos, void* x, void* stream) {

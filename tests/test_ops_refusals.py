@@ -73,3 +73,46 @@ def test_vocabulary_loss_scratch_does_not_grow_with_the_vocabulary(backward):
     assert at[0] == at[1] == at[2] < 2048 * 50304 * 4
     at = [bf.bf_op_vocab_loss_work_bytes(bf.BF_BF16, 2048, 1024, v, 8192, 1) for v in (50304, 150912, 2000000)]
     assert at[0] == at[1] == at[2] < 2048 * 50304 * 4
+
+
+def _attn(**k):
+    return bf.make_attn_config(**{**dict(dtype=bf.BF_BF16, S_mb=2, S_seq=100, N_heads=4, N_kv_heads=2, S_head=64), **k})
+
+
+BAD_ATTENTION = [dict(dtype=5), dict(kernels=9), dict(S_mb=0), dict(S_seq=0), dict(S_seq=(1 << 24) + 1), dict(N_heads=0), dict(N_kv_heads=0), dict(N_kv_heads=3),
+                 dict(S_head=0), dict(S_head=1025), dict(S_mb=20000), dict(scale=-1.0), dict(scale=math.inf), dict(scale=math.nan), dict(cap=-1.0),
+                 dict(cap=math.nan), dict(cap=math.inf), dict(ld_q=255), dict(ld_k=127), dict(ld_v=127), dict(ld_ctx=255), dict(ld_q=-256)]
+
+
+def test_masked_attention_refusals():
+    lib = bf.load()
+    good = _attn()
+    assert lib.bf_op_attention_masked_bwd_work_bytes(None) == 0
+    need = bf.bf_op_attention_masked_bwd_work_bytes(good)
+    assert need > 0
+    fwd = [C.byref(good), X, X, X, X, None, X, X, None]
+    bwd = [C.byref(good), X, X, X, X, None, X, X, X, X, X, X, X, need, None]
+    for bad in BAD_ATTENTION:
+        c = _attn(**bad)
+        assert bf.bf_op_attention_masked_bwd_work_bytes(c) == 0, bad
+        refused("bf_op_attention_masked_fwd", C.byref(c), *fwd[1:])
+        refused("bf_op_attention_masked_bwd", C.byref(c), *bwd[1:])
+    refused("bf_op_attention_masked_fwd", None, *fwd[1:])
+    refused("bf_op_attention_masked_bwd", None, *bwd[1:])
+    for at in (1, 2, 3, 4, 6):
+        refused("bf_op_attention_masked_fwd", *fwd[:at], None, *fwd[at + 1:])
+        refused("bf_op_attention_masked_fwd", *fwd[:at], X + 1, *fwd[at + 1:])
+    for at in (1, 2, 3, 4, 6, 7, 8, 9, 10, 11, 12):
+        refused("bf_op_attention_masked_bwd", *bwd[:at], None, *bwd[at + 1:])
+    for at, bad in ((4, X + 8), (12, X + 128), (13, need - 1)):
+        refused("bf_op_attention_masked_bwd", *bwd[:at], bad, *bwd[at + 1:])
+
+
+def test_attention_span_refusals():
+    assert bf.bf_op_attention_spans_elems(2, 100) > 400
+    for sizes in ((0, 5), (5, 0), (1, (1 << 24) + 1), (-1, 5)):
+        assert bf.bf_op_attention_spans_elems(*sizes) == 0
+        refused("bf_op_attention_spans", *sizes, 1, None, None, X, None)
+    refused("bf_op_attention_spans", 1, 100, 1, None, None, None, None)
+    refused("bf_op_attention_spans", 1, 100, 1, None, None, X + 4, None)
+    refused("bf_op_attention_spans", 70000, 10, 1, None, None, X, None)
