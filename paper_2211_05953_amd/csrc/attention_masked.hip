@@ -313,6 +313,25 @@ MaskedArgs args_of(const bf_attn_config& c, const void* q, const void* k, const 
   return a;
 }
 
+// rows of whole 16-byte chunks, in every tensor
+bool chunks(const bf_attn_config& c, const MaskedArgs& a, uintptr_t al) {
+  const size_t n = c.dtype == BF_BF16 ? 8 : 4;
+  return (al & 15) == 0 && (a.S_head | a.ldq | a.ldk | a.ldv | a.ldo) % n == 0;
+}
+
+bool matrix(const bf_attn_config& c) { return c.kernels == BF_KERNELS_AUTO && c.S_head <= 128 && c.dtype == BF_BF16; }
+
+// Shares of a key / value head's query heads in the dK / dV pass
+int splits_of(const bf_attn_config& c) {
+  if (!matrix(c)) return 1;
+  const int group = c.N_heads / c.N_kv_heads;
+  const long wgs = (long)((c.S_seq + 127) / 128) * c.N_kv_heads * c.S_mb;
+  int s = 1;
+  for (int k = 2; k <= group; ++k)
+    if (group % k == 0 && wgs * s < 1024) s = k;
+  return s;
+}
+
 bool element_aligned(int dtype, uintptr_t p) { return (p & (dtype == BF_BF16 ? 1 : 3)) == 0; }
 
 }  // namespace
@@ -339,7 +358,9 @@ bf_status attention_masked_fwd(const bf_attn_config* c, const void* q, const voi
     set_error("%s: a tensor is not aligned to its elements, or spans not to 16 bytes", who);
     return BF_EINVAL;
   }
-  const MaskedArgs a = args_of(*c, q, k, v, spans, slopes, ctx, lse);
+  MaskedArgs a = args_of(*c, q, k, v, spans, slopes, ctx, lse);
+  a.vec = chunks(*c, a, (uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)ctx);
+  if (matrix(*c)) return attention_masked_fwd_mfma(a, st);
   const dim3 grid(c->S_seq, c->S_mb * c->N_heads);
   if (c->dtype == BF_BF16) plain_fwd_kernel<bf16_t><<<grid, 64, 0, st>>>(a);
   else plain_fwd_kernel<float><<<grid, 64, 0, st>>>(a);
@@ -348,7 +369,9 @@ bf_status attention_masked_fwd(const bf_attn_config* c, const void* q, const voi
 
 size_t attention_masked_bwd_work_bytes(const bf_attn_config* c) {
   if (!cfg_ok("bf_op_attention_masked_bwd_work_bytes", c)) return 0;
-  return ((size_t)c->S_mb * c->N_heads * c->S_seq * 4 + 255) / 256 * 256;
+  const size_t delta = ((size_t)c->S_mb * c->N_heads * c->S_seq * 4 + 255) / 256 * 256;
+  const int splits = splits_of(*c);
+  return delta + (splits > 1 ? (size_t)splits * 2 * c->S_mb * c->S_seq * c->N_kv_heads * c->S_head * 4 : 0);
 }
 
 bf_status attention_masked_bwd(const bf_attn_config* c, const void* q, const void* k, const void* v, const int32_t* spans, const float* slopes, const void* ctx,
@@ -367,6 +390,10 @@ bf_status attention_masked_bwd(const bf_attn_config* c, const void* q, const voi
   a.dctx = dctx;
   a.dq = dq; a.dk = dk; a.dv = dv;
   a.delta = (float*)work;
+  a.splits = splits_of(*c);
+  a.planes = (float*)((char*)work + ((size_t)c->S_mb * c->N_heads * c->S_seq * 4 + 255) / 256 * 256);
+  a.vec = chunks(*c, a, al);
+  if (matrix(*c)) return attention_masked_bwd_mfma(a, st);
   const dim3 grid(c->S_seq, c->S_mb * c->N_heads), grid_kv(c->S_seq, c->S_mb * c->N_kv_heads);
   if (c->dtype == BF_BF16) {
     plain_dq_kernel<bf16_t><<<grid, 64, 0, st>>>(a);

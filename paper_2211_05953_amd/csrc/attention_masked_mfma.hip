@@ -1,0 +1,820 @@
+// Masked attention on the bf16 matrix cores, heads up to 128 (padded with zeros to 64 or 128 in LDS and registers).
+//
+// Layouts, LDS swizzle and the transposed score tiles are those of attention_mfma.hip: a lane owns one softmax row of a
+// forward or dQ tile and one key of a dK / dV tile, and its score registers are, rounded, the next product's operand.  What the
+// masks add: a workgroup walks only the tiles that its rows' spans reach; a wave skips a tile that none of its 32 rows sees
+// and applies no mask to one that all of them see whole; the others are masked by selection, after the score and before
+// anything is summed.  A tile that is masked in part and holds an infinity or a NaN takes a product for every column, over
+// the rows that the column sees (zero times infinity is a NaN in a matrix instruction).
+#include <float.h>
+#include <math.h>
+
+#include <type_traits>
+
+#include "attention_masked.h"
+#include "attention_tiles.h"
+
+namespace bf {
+
+namespace {
+
+// ---- loads and stores of token rows that may be shorter than D or off 16-byte alignment (EXACT: neither).
+// Tiles come through a buffer descriptor that ends with the last row there is: a lane keeps one 32-bit offset, and what lies
+// past the end, or past a short row, reads as zeros.
+constexpr uint32_t NOWHERE = 0x7fffff00u;
+
+template <int ROWS, int D, int NT, bool EXACT>
+struct Tile : TileRegs<ROWS, D, NT> {
+  static constexpr int CH = TileRegs<ROWS, D, NT>::CH, STEP = NT / (D / 8);  // rows between a thread's chunks
+  uint32_t off;
+  int col;
+  __device__ __forceinline__ void init(size_t ld, int tid, int d, bool vec) {
+    col = tid % (D / 8) * 8;
+    off = (uint32_t)(tid / (D / 8) * ld + col) * 2;
+    if (!EXACT && vec && col >= d) off = NOWHERE;
+  }
+  // g: the tile's first row, `valid` >= 1 of which are there (uniform)
+  __device__ __forceinline__ void fetch(const bf16_t* __restrict__ g, size_t ld, int valid, int d, bool vec) {
+    const uint32_t bytes = (uint32_t)(((valid < ROWS ? valid : ROWS) - 1) * ld + d) * 2;
+    __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)g, 0, (int)bytes, 0x00020000);
+    const uint32_t step = (uint32_t)(STEP * ld * 2);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      if (EXACT || vec) {
+        this->v[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off + i * step, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t at = off + i * step + 4 * e;
+          const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(rsrc, col + 2 * e < d ? at : NOWHERE, 0, 0);
+          const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(rsrc, col + 2 * e + 1 < d ? at + 2 : NOWHERE, 0, 0);
+          this->v[i][e] = lo | hi << 16;
+        }
+      }
+    }
+  }
+};
+
+template <int D, bool EXACT>
+__device__ __forceinline__ void load_row(const bf16_t* __restrict__ row, int lane, int d, bool vec, bf16x8 (&f)[D / 16]) {
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) {
+    const int c = kk * 16 + 8 * (lane >> 5);
+    if (EXACT || (vec && c < d)) {
+      f[kk] = *reinterpret_cast<const bf16x8*>(row + c);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[kk][e] = c + e < d ? row[c + e] : (bf16_t)0.f;
+    }
+  }
+}
+
+template <int D, bool EXACT>
+__device__ __forceinline__ void store_row(const f32x16 (&acc)[D / 32], bf16_t* __restrict__ row, int lane, float mul, int d, bool vec) {
+  if (EXACT) { store_rows<D>(acc, row, lane, mul); return; }
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const int c = dt * 32 + q4 * 8 + (lane >> 5) * 4;
+      if (vec && c < d) {  // d is a multiple of 8
+        bf16x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[dt][q4 * 4 + e] * mul);
+        *reinterpret_cast<bf16x4*>(row + c) = o;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < d) row[c + e] = (bf16_t)(acc[dt][q4 * 4 + e] * mul);
+      }
+    }
+}
+
+// ---- from a dot product to an exponent of two.  Without cap and bias the dot products stay as they are and the factor enters with
+// the exponential (one fma).  cap: tanh x = 1 - 2 r with r = 1 / (1 + e^2x), on the hardware exponential and reciprocal (1 ulp
+// each: an absolute error of 1e-7 of the cap); its derivative 1 - tanh^2 is 4 r (1 - r).
+struct ScoreFactors {
+  float c2;      // factor of an exponent: 1 where the score carries it already
+  float e2x;     // dot product to 2 x log2(e), x the tanh's argument
+  float capl;    // cap log2(e)
+  float mul;     // dot product to score (bias without cap)
+  float slopel;  // slope log2(e)
+};
+
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ ScoreFactors factors(const MaskedArgs& a, int head) {
+  ScoreFactors f;
+  f.c2 = CAP || BIAS ? 1.f : a.scale * LOG2E;
+  f.mul = a.scale * LOG2E;
+  f.capl = a.cap * LOG2E;
+  f.e2x = CAP ? 2.f * LOG2E * a.scale / a.cap : 0.f;
+  f.slopel = BIAS ? a.slope[head] * LOG2E : 0.f;
+  return f;
+}
+
+// dist: i - j as a float.  r: see above (CAP)
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ float exponent(float dot, float dist, const ScoreFactors& f, float& r) {
+  float t = dot;
+  if (CAP) {
+    r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(dot * f.e2x));
+    t = fmaf(r, -2.f * f.capl, f.capl);
+  } else if (BIAS) {
+    t *= f.mul;
+  }
+  if (BIAS) t = fmaf(-f.slopel, fabsf(dist), t);
+  return t;
+}
+
+// acc += tile^T p over a tile that is masked in part and holds an infinity or a NaN: column by column of p, with the tile's
+// rows that the column does not see taken as zeros.  rows_of(c): bit r is set where column c sees row r of the tile (uniform).
+template <int D, typename FA, typename F>
+__device__ __forceinline__ void accumulate_seen(f32x16 (&acc)[D / 32], const bf16x8 (&p)[4], int row0, int subs, const bf16_t* tile, const FA& fa, int lane,
+                                                F rows_of) {
+#pragma unroll 1
+  for (int c = 0; c < 32; ++c) {
+    const uint64_t seen = rows_of(c);
+    if (seen == 0) continue;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) {
+      f32x16 sum = zero16();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (k >= subs) continue;
+        bf16x8 v = fa.frag_t(tile, row0 + 16 * k, dt);
+        const uint32_t bits = (uint32_t)(seen >> (row0 + 16 * k + 4 * (lane >> 5)));  // rows 8 (e / 4) + e % 4 from there on
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = bits >> (8 * (e >> 2) + (e & 3)) & 1 ? v[e] : (bf16_t)0.f;
+        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[k], sum, 0, 0, 0);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[dt][r] = (lane & 31) == c ? acc[dt][r] + sum[r] : acc[dt][r];
+    }
+  }
+}
+
+// the rows of a tile at k0 that lie in [lo, hi)
+__device__ __forceinline__ uint64_t interval_bits(int k0, int lo, int hi) {
+  const int a = min(max(lo - k0, 0), 64), b = min(max(hi - k0, 0), 64);
+  if (a >= b) return 0;
+  return (~0ull >> (64 - (b - a))) << a;
+}
+
+// a wave's spans: which tiles it needs, and which of them whole.  Rows past the end count as neither.
+struct WaveSpan {
+  int lo_min, hi_max, lo_max, hi_min;
+  __device__ __forceinline__ void init(int2 sp, bool row) {
+    const bool any = sp.y > sp.x;
+    lo_min = row && any ? sp.x : INT_MAX;
+    hi_max = row && any ? sp.y : 0;
+    lo_max = !row ? 0 : any ? sp.x : INT_MAX;
+    hi_min = !row ? INT_MAX : any ? sp.y : 0;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {  // lanes l and l + 32 hold the same row
+      lo_min = min(lo_min, __shfl_xor(lo_min, o, 64));
+      hi_max = max(hi_max, __shfl_xor(hi_max, o, 64));
+      lo_max = max(lo_max, __shfl_xor(lo_max, o, 64));
+      hi_min = min(hi_min, __shfl_xor(hi_min, o, 64));
+    }
+    lo_min = __builtin_amdgcn_readfirstlane(lo_min);
+    hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+    lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+    hi_min = __builtin_amdgcn_readfirstlane(hi_min);
+  }
+  __device__ __forceinline__ bool skips(int k, int n) const { return k >= hi_max || k + n <= lo_min; }
+  __device__ __forceinline__ bool whole(int k, int n) const { return k >= lo_max && k + n <= hi_min; }
+};
+
+// of the query block's rows together
+template <int ROWS>
+__device__ __forceinline__ SpanBlock rows_of_block(const MaskedArgs& a, int b, int q0) {
+  const int blocks = (a.S_seq + SPAN_ROWS - 1) / SPAN_ROWS, at = q0 / SPAN_ROWS;
+  SpanBlock x = a.block[(size_t)b * blocks + at];
+#pragma unroll
+  for (int k = 1; k < ROWS / SPAN_ROWS; ++k)
+    if (at + k < blocks) {
+      const SpanBlock y = a.block[(size_t)b * blocks + at + k];
+      x = {min(x.lo_min, y.lo_min), max(x.hi_max, y.hi_max), max(x.lo_max, y.lo_max), min(x.hi_min, y.hi_min)};
+    }
+  x.hi_max = min(x.hi_max, a.S_seq);
+  return x;
+}
+
+// query block, head and sequence of a workgroup of a 1-D grid: the last query blocks first (under a causal mask the longest), and
+// neighbouring workgroups on different key / value heads, so that the query heads of one of them meet in one XCD's L2
+struct QueryBlock { int q0, head, kv, b; };
+__device__ __forceinline__ QueryBlock query_block(const MaskedArgs& a, int idx, int rows) {
+  const int nhb = a.N_heads * a.S_mb, blocks = (a.S_seq + rows - 1) / rows, group = a.N_heads / a.N_kv;
+  const int x = idx % nhb, hx = x % a.N_heads;
+  QueryBlock w;
+  w.q0 = (blocks - 1 - idx / nhb) * rows;
+  w.b = x / a.N_heads;
+  w.kv = hx % a.N_kv;
+  w.head = w.kv * group + hx / a.N_kv;
+  return w;
+}
+
+// ------------------------------------------------------------------------------ forward
+// SEEN: tiles that are masked in part by accumulate_seen.  Without it, returns whether one of those held a non-finite V.
+template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS, bool SEEN>
+__device__ __forceinline__ bool fwd_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2][BLK * D]) {
+  constexpr int NT = 2 * ROWS;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const QueryBlock wb = query_block(a, blockIdx.x, ROWS);
+  const int S = a.S_seq, d = a.S_head, q = wb.q0 + 32 * w + (lane & 31), ql = min(q, S - 1);
+  const size_t seq = (size_t)wb.b * S;
+  const bf16_t* kbase = (const bf16_t*)a.k + seq * a.ldk + (size_t)wb.kv * d;
+  const bf16_t* vbase = (const bf16_t*)a.v + seq * a.ldv + (size_t)wb.kv * d;
+  // (S_head 128: precomputed offsets would spill)
+  typename std::conditional<D == 64, FragAddr<D>, FragAddrXor<D>>::type fa;
+  fa.init(lane);
+  bf16x8 qf[D / 16];
+  load_row<D, EXACT>((const bf16_t*)a.q + (seq + ql) * a.ldq + (size_t)wb.head * d, lane, d, a.vec, qf);
+  int2 sp = a.span[seq + ql];
+  sp.x = max(sp.x, 0);
+  sp.y = min(sp.y, S);
+  WaveSpan ws;
+  ws.init(sp, q < S);
+  const SpanBlock wg = rows_of_block<ROWS>(a, wb.b, wb.q0);
+  const ScoreFactors f = factors<CAP, BIAS>(a, wb.head);
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) o[dt] = zero16();
+  // (a maximum of the lowest finite value, that its factor leaves finite: a row that has met only -inf adds exactly 0, no NaN)
+  float m = f.c2 > 1.f ? -FLT_MAX / f.c2 : -FLT_MAX, l = 0.f;
+
+  const int jbeg = wg.hi_max > 0 ? max(wg.lo_min, 0) / BLK : 0, jend = (wg.hi_max + BLK - 1) / BLK;
+  Tile<BLK, D, NT, EXACT> kr, vr;
+  bool bad = false;
+  kr.init(a.ldk, tid, d, a.vec);
+  vr.init(a.ldv, tid, d, a.vec);
+  // the next tile's K is on its way during the first half of a tile's work, its V during the second, in the same registers
+  auto fetch_k = [&](int j) { kr.fetch(kbase + (size_t)j * BLK * a.ldk, a.ldk, S - j * BLK, d, a.vec); };
+  auto fetch_v = [&](int j) { vr.fetch(vbase + (size_t)j * BLK * a.ldv, a.ldv, S - j * BLK, d, a.vec); };
+  auto note = [&](int j) {
+    const int kb = j * BLK;
+    if (!SEEN && !(kb >= wg.lo_max && kb + BLK <= wg.hi_min)) bad |= vr.non_finite();
+  };
+  typedef std::integral_constant<int, 0> I0;
+  typedef std::integral_constant<int, 1> I1;
+  if (jbeg < jend) {
+    fetch_k(jbeg);
+    fetch_v(jbeg);
+    kr.store(KVs[0][0], tid);
+    vr.store(KVs[0][1], tid);
+    note(jbeg);
+  }
+  __syncthreads();
+  // one key tile; PAR, its LDS stage, is a compile-time constant (the loop is unrolled by two)
+  auto body = [&](int j, auto parc) {
+    constexpr int PAR = decltype(parc)::value;
+    if constexpr (D == 128) fa.loop();
+    const bf16_t* Ks = KVs[PAR][0];
+    const bf16_t* Vs = KVs[PAR][1];
+    const int kb = j * BLK;
+    const bool next = j + 1 < jend, work = !ws.skips(kb, BLK), part = !ws.whole(kb, BLK);
+    if (next) fetch_k(j + 1);
+    f32x16 s[2] = {zero16(), zero16()};
+    if (work) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_k(Ks, 32 * t, kk), qf[kk], s[t], 0, 0, 0);
+    mfma_lds_pipeline<2 * (D / 16), 1, 4>();
+    if (CAP || BIAS) {
+      const float dist = (float)(q - kb - 4 * (lane >> 5));
+      float r_;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = exponent<CAP, BIAS>(s[t][r], dist - (float)(32 * t + (r >> 2) * 8 + (r & 3)), f, r_);
+    }
+    if (part) {
+      const int lo = sp.x - kb, n = sp.y - sp.x;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if ((unsigned)(32 * t + acc_row(r, lane) - lo) >= (unsigned)n) s[t][r] = -INFINITY;
+    }
+    float mx = m;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float nmx = -mx * f.c2;
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = __builtin_amdgcn_exp2f(CAP || BIAS ? s[t][r] + nmx : fmaf(s[t][r], f.c2, nmx));
+        s[t][r] = p;
+        sum += p;
+      }
+    if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {  // some row's maximum moved
+      const float alpha = __builtin_amdgcn_exp2f(CAP || BIAS ? m + nmx : fmaf(m, f.c2, nmx));
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+      m = mx;
+    }
+    l += sum;
+    }
+    bf16x8 pb[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) pb[k] = pack8(s[k >> 1], k & 1);
+    if (next) {
+      kr.store(KVs[PAR ^ 1][0], tid);
+      fetch_v(j + 1);
+    }
+    if (work) {
+      if (SEEN && part) {
+        accumulate_seen<D>(o, pb, 0, 4, Vs, fa, lane, [&](int c) {
+          return interval_bits(kb, __builtin_amdgcn_readlane(sp.x, c), __builtin_amdgcn_readlane(sp.y, c));
+        });
+      } else {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_t(Vs, 16 * k, dt), pb[k], o[dt], 0, 0, 0);
+        mfma_lds_pipeline<4 * (D / 32), 2, 4>();
+      }
+    }
+    if (next) {
+      vr.store(KVs[PAR ^ 1][1], tid);
+      note(j + 1);
+    }
+    __syncthreads();
+  };
+  for (int j = jbeg; j < jend; j += 2) {
+    body(j, I0{});
+    if (j + 1 < jend) body(j + 1, I1{});
+  }
+  if (!SEEN && __syncthreads_or(bad)) return true;
+  l += __shfl_xor(l, 32, 64);
+  if (q >= S) return false;
+  store_row<D, EXACT>(o, (bf16_t*)a.ctx + (seq + q) * a.ldo + (size_t)wb.head * d, lane, l == 0.f ? 0.f : 1.0f / l, d, a.vec);
+  if (lane < 32 && a.lse)
+    a.lse[((size_t)wb.b * a.N_heads + wb.head) * S + q] = l == 0.f ? -INFINITY : m * (CAP || BIAS ? LN2 : a.scale) + logf(l);
+  return false;
+}
+
+// The second way is a pass of its own, and a function: in the first one's loop, or behind it in the same body, what it needs
+// pushes the first one's registers out.
+template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS>
+__device__ __attribute__((noinline)) void fwd_rows_seen(MaskedArgs a, bf16_t (&KVs)[2][2][BLK * D]) {
+  fwd_rows<D, ROWS, EXACT, CAP, BIAS, true>(a, KVs);
+}
+
+template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS>
+__global__ __launch_bounds__(2 * ROWS, 2) void masked_fwd_kernel(MaskedArgs a) {
+  __shared__ __attribute__((aligned(16))) bf16_t KVs[2][2][BLK * D];
+  if (fwd_rows<D, ROWS, EXACT, CAP, BIAS, false>(a, KVs)) fwd_rows_seen<D, ROWS, EXACT, CAP, BIAS>(a, KVs);
+}
+
+// ------------------------------------------------------------------- backward, dQ pass
+// also takes delta = dctx . ctx of its rows, for the dK / dV pass
+template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS, bool SEEN>
+__device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2][BLK * D]) {
+  constexpr int NT = 2 * ROWS;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const QueryBlock wb = query_block(a, blockIdx.x, ROWS);
+  const int S = a.S_seq, d = a.S_head, q = wb.q0 + 32 * w + (lane & 31), ql = min(q, S - 1);
+  const size_t seq = (size_t)wb.b * S, orow = (seq + ql) * a.ldo + (size_t)wb.head * d;
+  const bf16_t* kbase = (const bf16_t*)a.k + seq * a.ldk + (size_t)wb.kv * d;
+  const bf16_t* vbase = (const bf16_t*)a.v + seq * a.ldv + (size_t)wb.kv * d;
+  // (S_head 128: precomputed offsets would spill)
+  typename std::conditional<D == 64, FragAddr<D>, FragAddrXor<D>>::type fa;
+  fa.init(lane);
+  bf16x8 qf[D / 16], dof[D / 16];
+  load_row<D, EXACT>((const bf16_t*)a.q + (seq + ql) * a.ldq + (size_t)wb.head * d, lane, d, a.vec, qf);
+  load_row<D, EXACT>((const bf16_t*)a.dctx + orow, lane, d, a.vec, dof);
+  const size_t st = ((size_t)wb.b * a.N_heads + wb.head) * S + ql;
+  float dl = 0.f;
+  {
+    bf16x8 cf[D / 16];
+    load_row<D, EXACT>((const bf16_t*)a.ctx + orow, lane, d, a.vec, cf);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dl = fmaf((float)dof[kk][e], (float)cf[kk][e], dl);
+    dl += __shfl_xor(dl, 32, 64);  // lanes l and l + 32 hold the two halves of the row
+    if (lane < 32 && q < S) a.delta[st] = dl;
+  }
+  // (a row without a finite score has no probabilities)
+  const float lse = a.lse[st], lse2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
+  int2 sp = a.span[seq + ql];
+  sp.x = max(sp.x, 0);
+  sp.y = min(sp.y, S);
+  WaveSpan ws;
+  ws.init(sp, q < S);
+  const SpanBlock wg = rows_of_block<ROWS>(a, wb.b, wb.q0);
+  const ScoreFactors f = factors<CAP, BIAS>(a, wb.head);
+  f32x16 dq[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) dq[dt] = zero16();
+
+  const int jbeg = wg.hi_max > 0 ? max(wg.lo_min, 0) / BLK : 0, jend = (wg.hi_max + BLK - 1) / BLK;
+  Tile<BLK, D, NT, EXACT> kr, vr;
+  bool bad = false;
+  kr.init(a.ldk, tid, d, a.vec);
+  vr.init(a.ldv, tid, d, a.vec);
+  // the next tile's K is on its way during the first half of a tile's work, its V during the second, in the same registers
+  auto fetch_k = [&](int j) { kr.fetch(kbase + (size_t)j * BLK * a.ldk, a.ldk, S - j * BLK, d, a.vec); };
+  auto fetch_v = [&](int j) { vr.fetch(vbase + (size_t)j * BLK * a.ldv, a.ldv, S - j * BLK, d, a.vec); };
+  auto note = [&](int j) {
+    const int kb = j * BLK;
+    if (!SEEN && !(kb >= wg.lo_max && kb + BLK <= wg.hi_min)) bad |= kr.non_finite();
+  };
+  if (jbeg < jend) {
+    fetch_k(jbeg);
+    fetch_v(jbeg);
+    kr.store(KVs[0][0], tid);
+    vr.store(KVs[0][1], tid);
+    note(jbeg);
+  }
+  __syncthreads();
+  auto body = [&](int j, auto par) {
+    const int p = par;
+    if constexpr (D == 128) fa.loop();
+    const bf16_t* Ks = KVs[p][0];
+    const bf16_t* Vs = KVs[p][1];
+    const int kb = j * BLK;
+    const bool next = j + 1 < jend, work = !ws.skips(kb, BLK), part = !ws.whole(kb, BLK);
+    if (next) fetch_k(j + 1);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (t == 1 && next) {
+        kr.store(KVs[p ^ 1][0], tid);
+        note(j + 1);
+        fetch_v(j + 1);
+      }
+      if (!work) continue;
+      f32x16 s = zero16(), dp = zero16();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_k(Ks, 32 * t, kk), qf[kk], s, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_k(Vs, 32 * t, kk), dof[kk], dp, 0, 0, 0);
+      }
+      mfma_lds_pipeline<2 * (D / 16), 1, 4>();
+      // p = exp(score - lse); dS = p (dP - delta) times the cap's derivative (the factor 1/sqrt(d) is applied once, to dQ)
+      const float dist = (float)(q - kb - 32 * t - 4 * (lane >> 5));
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float c = 0.f;
+        const float e = exponent<CAP, BIAS>(s[r], dist - (float)((r >> 2) * 8 + (r & 3)), f, c);
+        const float pr = __builtin_amdgcn_exp2f(CAP || BIAS ? e - lse2 : fmaf(e, f.c2, -lse2));
+        s[r] = pr * (dp[r] - dl);
+        if (CAP) s[r] *= 4.f * c * (1.f - c);
+      }
+      if (part) {
+        const int lo = sp.x - kb - 32 * t, n = sp.y - sp.x;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if ((unsigned)(acc_row(r, lane) - lo) >= (unsigned)n) s[r] = 0.f;
+      }
+      const bf16x8 dsb[4] = {pack8(s, 0), pack8(s, 1)};
+      if (SEEN && part) {
+        accumulate_seen<D>(dq, dsb, 32 * t, 2, Ks, fa, lane, [&](int c) {
+          return interval_bits(kb, __builtin_amdgcn_readlane(sp.x, c), __builtin_amdgcn_readlane(sp.y, c));
+        });
+        continue;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+          dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_t(Ks, 32 * t + 16 * k2, dt), dsb[k2], dq[dt], 0, 0, 0);
+      mfma_lds_pipeline<2 * (D / 32), 2, 4>();
+    }
+    if (next) vr.store(KVs[p ^ 1][1], tid);
+    __syncthreads();
+  };
+  if constexpr (D == 64) {
+    // unrolled by two: the LDS stage (and with it every fragment address) is a compile-time constant
+    for (int j = jbeg; j < jend; j += 2) {
+      body(j, std::integral_constant<int, 0>{});
+      if (j + 1 < jend) body(j + 1, std::integral_constant<int, 1>{});
+    }
+  } else {
+    for (int j = jbeg; j < jend; ++j) body(j, (j - jbeg) & 1);
+  }
+  if (!SEEN && __syncthreads_or(bad)) return true;
+  if (q >= S) return false;
+  if (sp.y - sp.x <= 1) {  // one key: its probability is 1 whatever the score
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) dq[dt] = zero16();
+  }
+  store_row<D, EXACT>(dq, (bf16_t*)a.dq + (seq + q) * a.ldq + (size_t)wb.head * d, lane, a.scale, d, a.vec);
+  return false;
+}
+
+template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS>
+__device__ __attribute__((noinline)) void dq_rows_seen(MaskedArgs a, bf16_t (&KVs)[2][2][BLK * D]) {
+  dq_rows<D, ROWS, EXACT, CAP, BIAS, true>(a, KVs);
+}
+
+template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS>
+__global__ __launch_bounds__(2 * ROWS, 2) void masked_dq_kernel(MaskedArgs a) {
+  __shared__ __attribute__((aligned(16))) bf16_t KVs[2][2][BLK * D];
+  if (dq_rows<D, ROWS, EXACT, CAP, BIAS, false>(a, KVs)) dq_rows_seen<D, ROWS, EXACT, CAP, BIAS>(a, KVs);
+}
+
+// ----------------------------------------------------------------- backward, dK / dV pass
+// 8 waves per 128 keys, in pairs as in attention_mfma.hip: waves 0-3 accumulate dV = P^T dctx, waves 4-7 the matching dK = dS^T Q.
+// The dV wave hands its partner P (times the cap's derivative) lane to lane through LDS, in fp32: rounded to bf16 there, dS
+// would be rounded twice.  A workgroup walks the query tiles whose spans reach its keys, for every query head of its share of
+// the key / value head's group, one after the other in one chain of sums.
+constexpr int NTHR_DKV = 512;
+
+template <int D>
+struct DkvShared {
+  bf16_t QOs[2][2][BLK * D];  // Q and dctx tiles
+  float stat[2][2][BLK];      // lse * log2(e) and delta of the tile's queries
+  int span[2][2][BLK];        // their spans
+  float Ps[2][4][4][64 * 4];  // [sub-tile][key group][register quarter][lane]
+  int range[2];
+};
+
+template <int D, bool EXACT, bool CAP, bool BIAS, bool SEEN>
+__device__ __forceinline__ bool dkv_keys(const MaskedArgs& a, DkvShared<D>& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kg = w & 3;
+  const bool dk_role = w >= 4;  // wave-uniform
+  const int S = a.S_seq, d = a.S_head, group = a.N_heads / a.N_kv, heads = group / a.splits;
+  const int per = a.N_kv * a.splits * a.S_mb, x = blockIdx.x % per;
+  const int k0 = blockIdx.x / per * WG_ROWS;  // earliest keys first: under a causal mask they see the most queries
+  const int kv = x % a.N_kv, split = x / a.N_kv % a.splits, b = x / (a.N_kv * a.splits);
+  const size_t seq = (size_t)b * S;
+  const int kw = k0 + 32 * kg, key = kw + (lane & 31), kl = min(key, S - 1);
+  const int blocks = (S + SPAN_ROWS - 1) / SPAN_ROWS;
+  const SpanBlock* tb = a.block + (size_t)b * blocks;
+
+  // the query tiles that see any of these keys lie between the first and the last of them
+  if (tid < 2) sh.range[tid] = tid ? 0 : INT_MAX;
+  __syncthreads();
+  for (int j = tid; j < blocks; j += NTHR_DKV) {
+    const SpanBlock y = tb[j];
+    if (y.hi_max > k0 && y.lo_min < k0 + WG_ROWS) { atomicMin(&sh.range[0], j); atomicMax(&sh.range[1], j + 1); }
+  }
+  __syncthreads();
+  const int jbeg = sh.range[0], jend = sh.range[1], tiles = jend > jbeg ? jend - jbeg : 0, total = tiles * heads;
+
+  typename std::conditional<D == 64, FragAddr<D>, FragAddrXor<D>>::type fa;
+  fa.init(lane);
+  bf16x8 kvf[D / 16];  // this wave's K rows (dV role) or V rows (dK role)
+  if (dk_role) load_row<D, EXACT>((const bf16_t*)a.v + (seq + kl) * a.ldv + (size_t)kv * d, lane, d, a.vec, kvf);
+  else load_row<D, EXACT>((const bf16_t*)a.k + (seq + kl) * a.ldk + (size_t)kv * d, lane, d, a.vec, kvf);
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
+
+  Tile<BLK, D, NTHR_DKV, EXACT> qr, dor;
+  qr.init(a.ldq, tid, d, a.vec);
+  dor.init(a.ldo, tid, d, a.vec);
+  bool bad = false;
+  float lnext = 0.f, dnext = 0.f;
+  int2 snext = make_int2(0, 0);
+  // step `it`: query head it / tiles of the share, tile jbeg + it % tiles
+  const int head0 = kv * group + split * heads;
+  int fh = 0, fj = jbeg;  // of the next fetch
+  auto fetch = [&]() {
+    const int head = head0 + fh;
+    qr.fetch((const bf16_t*)a.q + (seq + (size_t)fj * BLK) * a.ldq + (size_t)head * d, a.ldq, S - fj * BLK, d, a.vec);
+    dor.fetch((const bf16_t*)a.dctx + (seq + (size_t)fj * BLK) * a.ldo + (size_t)head * d, a.ldo, S - fj * BLK, d, a.vec);
+    if (tid < BLK) {
+      const int i = fj * BLK + tid;
+      const size_t st = ((size_t)b * a.N_heads + head) * S + i;
+      // past the end: no span, and exp2(score - inf) = 0
+      const float l = i < S ? a.lse[st] : -INFINITY;
+      lnext = l == -INFINITY ? INFINITY : l * LOG2E;
+      dnext = i < S ? a.delta[st] : 0.f;
+      snext = i < S ? a.span[seq + i] : make_int2(0, 0);
+    }
+    if (++fj == jend) { fj = jbeg; ++fh; }
+  };
+  auto put = [&](int it, int stage) {
+    qr.store(sh.QOs[stage][0], tid);
+    dor.store(sh.QOs[stage][1], tid);
+    if (tid < BLK) {
+      sh.stat[stage][0][tid] = lnext;
+      sh.stat[stage][1][tid] = dnext;
+      sh.span[stage][0][tid] = snext.x;
+      sh.span[stage][1][tid] = snext.y;
+    }
+    const int j = jbeg + it % tiles;
+    const bool whole = k0 >= tb[j].lo_max && k0 + WG_ROWS <= tb[j].hi_min && (j + 1) * BLK <= S;
+    if (!SEEN && !whole) bad |= qr.non_finite() || dor.non_finite();
+  };
+  if (total > 0) {
+    fetch();
+    put(0, 0);
+  }
+  if (total > 1) fetch();
+  __syncthreads();
+  int j = jbeg, hx = 0;
+  ScoreFactors f = factors<CAP, BIAS>(a, head0);
+  // every wave passes the same barriers: one at the hand-over of P and one at the end of the tile
+  for (int it = 0; it < total; ++it) {
+    const int cur = it & 1;
+    if constexpr (D == 128) fa.loop();
+    const bf16_t* Qs = sh.QOs[cur][0];
+    const bf16_t* dOs = sh.QOs[cur][1];
+    const float* lse_s = sh.stat[cur][0];
+    const float* delta_s = sh.stat[cur][1];
+    const int* lo_s = sh.span[cur][0];
+    const int* hi_s = sh.span[cur][1];
+    if (it + 1 < total) put(it + 1, cur ^ 1);
+    if (it + 2 < total) fetch();
+    const int qb = j * BLK;
+    const SpanBlock y = tb[j];
+    const bool skip = kw >= S || y.hi_max <= kw || y.lo_min >= kw + 32;
+    const bool part = !(kw >= y.lo_max && kw + 32 <= y.hi_min && qb + BLK <= S);
+    f32x16 s[2] = {zero16(), zero16()};  // scores, then P (dV role); dP, then dS (dK role)
+    if (!skip) {
+      __builtin_amdgcn_sched_barrier(0);
+      const bf16_t* tile = dk_role ? dOs : Qs;
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_k(tile, 32 * u, kk), kvf[kk], s[u], 0, 0, 0);
+      mfma_lds_pipeline<2 * (D / 16), 1, 4>();
+      if (!dk_role) {
+        const float dist = (float)(qb + 4 * (lane >> 5) - key);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const f32x4 ls = *reinterpret_cast<const f32x4*>(&lse_s[32 * u + acc_row(4 * q4, lane)]);
+            f32x4 give;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int r = 4 * q4 + e;
+              float c = 0.f;
+              const float ex = exponent<CAP, BIAS>(s[u][r], dist + (float)(32 * u + 8 * q4 + e), f, c);
+              s[u][r] = __builtin_amdgcn_exp2f(CAP || BIAS ? ex - ls[e] : fmaf(ex, f.c2, -ls[e]));
+              give[e] = CAP ? s[u][r] * (4.f * c * (1.f - c)) : s[u][r];
+            }
+            *reinterpret_cast<f32x4*>(&sh.Ps[u][kg][q4][lane * 4]) = give;
+          }
+        if (part) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+              const int4 lo = *reinterpret_cast<const int4*>(&lo_s[32 * u + acc_row(4 * q4, lane)]);
+              const int4 hi = *reinterpret_cast<const int4*>(&hi_s[32 * u + acc_row(4 * q4, lane)]);
+              if (key < lo.x || key >= hi.x) s[u][4 * q4] = 0.f;
+              if (key < lo.y || key >= hi.y) s[u][4 * q4 + 1] = 0.f;
+              if (key < lo.z || key >= hi.z) s[u][4 * q4 + 2] = 0.f;
+              if (key < lo.w || key >= hi.w) s[u][4 * q4 + 3] = 0.f;
+            }
+        }
+      }
+    }
+    __syncthreads();
+    if (!skip) {
+      if (dk_role) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const f32x4 pr = *reinterpret_cast<const f32x4*>(&sh.Ps[u][kg][q4][lane * 4]);
+            const f32x4 dl = *reinterpret_cast<const f32x4*>(&delta_s[32 * u + acc_row(4 * q4, lane)]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[u][4 * q4 + e] = pr[e] * (s[u][4 * q4 + e] - dl[e]);
+          }
+        if (part) {
+          // (a row of one key has no score gradient; it is never part of a tile taken whole)
+          auto out = [&](int lo, int hi) { return key < lo || key >= hi || hi - lo == 1; };
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+              const int4 lo = *reinterpret_cast<const int4*>(&lo_s[32 * u + acc_row(4 * q4, lane)]);
+              const int4 hi = *reinterpret_cast<const int4*>(&hi_s[32 * u + acc_row(4 * q4, lane)]);
+              if (out(lo.x, hi.x)) s[u][4 * q4] = 0.f;
+              if (out(lo.y, hi.y)) s[u][4 * q4 + 1] = 0.f;
+              if (out(lo.z, hi.z)) s[u][4 * q4 + 2] = 0.f;
+              if (out(lo.w, hi.w)) s[u][4 * q4 + 3] = 0.f;
+            }
+        }
+      }
+      const bf16_t* tile = dk_role ? Qs : dOs;
+      bf16x8 pb[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) pb[k] = pack8(s[k >> 1], k & 1);
+      if (SEEN && part) {
+        accumulate_seen<D>(acc, pb, 0, 4, tile, fa, lane, [&](int c) { return __builtin_amdgcn_ballot_w64(kw + c >= lo_s[lane] && kw + c < hi_s[lane]); });
+      } else {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_t(tile, 16 * k, dt), pb[k], acc[dt], 0, 0, 0);
+        mfma_lds_pipeline<4 * (D / 32), 2, 4>();
+      }
+    }
+    if (++j == jend) {
+      j = jbeg;
+      if (++hx < heads && BIAS) f = factors<CAP, BIAS>(a, head0 + hx);
+    }
+    __syncthreads();
+  }
+  if (!SEEN && __syncthreads_or(bad)) return true;
+  if (key >= S) return false;
+  const float mul = dk_role ? a.scale : 1.f;
+  if (a.splits > 1) {
+    // this share's plane: [split][dk, dv][token][key / value head][d]
+    const size_t width = (size_t)a.N_kv * d, plane = (size_t)a.S_mb * S * width;
+    float* out = a.planes + (2 * (size_t)split + (dk_role ? 0 : 1)) * plane + (seq + key) * width + (size_t)kv * d;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int c = dt * 32 + acc_row(r, lane);
+        if (EXACT || c < d) out[c] = acc[dt][r] * mul;
+      }
+    return false;
+  }
+  bf16_t* out = dk_role ? (bf16_t*)a.dk + (seq + key) * a.ldk + (size_t)kv * d : (bf16_t*)a.dv + (seq + key) * a.ldv + (size_t)kv * d;
+  store_row<D, EXACT>(acc, out, lane, mul, d, a.vec);
+  return false;
+}
+
+template <int D, bool EXACT, bool CAP, bool BIAS>
+__device__ __attribute__((noinline)) void dkv_keys_seen(MaskedArgs a, DkvShared<D>& sh) {
+  dkv_keys<D, EXACT, CAP, BIAS, true>(a, sh);
+}
+
+template <int D, bool EXACT, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NTHR_DKV, 2) void masked_dkv_kernel(MaskedArgs a) {
+  __shared__ __attribute__((aligned(16))) DkvShared<D> sh;
+  if (dkv_keys<D, EXACT, CAP, BIAS, false>(a, sh)) dkv_keys_seen<D, EXACT, CAP, BIAS>(a, sh);
+}
+
+
+// dk, dv = the shares' planes, added in ascending order
+__global__ __launch_bounds__(256) void masked_join_kernel(MaskedArgs a) {
+  const size_t width = (size_t)a.N_kv * a.S_head, plane = (size_t)a.S_mb * a.S_seq * width, n = 2 * plane;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
+    float t = 0.f;
+    for (int k = 0; k < a.splits; ++k) t += a.planes[(size_t)k * n + i];
+    const bool v = i >= plane;
+    const size_t e = v ? i - plane : i, row = e / width, c = e - row * width;
+    if (v) ((bf16_t*)a.dv)[row * a.ldv + c] = (bf16_t)t;
+    else ((bf16_t*)a.dk)[row * a.ldk + c] = (bf16_t)t;
+  }
+}
+
+bf_status launched() {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) { set_error("attention_masked_mfma: launch failed: %s", hipGetErrorString(e)); return BF_EDEVICE; }
+  return BF_OK;
+}
+
+inline unsigned query_grid(const MaskedArgs& a, int rows) { return (unsigned)((a.S_seq + rows - 1) / rows) * (unsigned)(a.N_heads * a.S_mb); }
+
+template <int D, bool EXACT, bool CAP, bool BIAS>
+void run(const MaskedArgs& a, bool backward, hipStream_t st) {
+  constexpr int ROWS = 128;
+  if (!backward) {
+    masked_fwd_kernel<D, ROWS, EXACT, CAP, BIAS><<<query_grid(a, ROWS), 2 * ROWS, 0, st>>>(a);
+    return;
+  }
+  masked_dq_kernel<D, ROWS, EXACT, CAP, BIAS><<<query_grid(a, ROWS), 2 * ROWS, 0, st>>>(a);
+  const unsigned grid = (unsigned)((a.S_seq + WG_ROWS - 1) / WG_ROWS) * (unsigned)(a.N_kv * a.splits * a.S_mb);
+  masked_dkv_kernel<D, EXACT, CAP, BIAS><<<grid, NTHR_DKV, 0, st>>>(a);
+  if (a.splits > 1) masked_join_kernel<<<2048, 256, 0, st>>>(a);
+}
+
+template <int D, bool EXACT>
+void by_score(const MaskedArgs& a, bool backward, hipStream_t st) {
+  if (a.cap > 0.f && a.slope) run<D, EXACT, true, true>(a, backward, st);
+  else if (a.cap > 0.f) run<D, EXACT, true, false>(a, backward, st);
+  else if (a.slope) run<D, EXACT, false, true>(a, backward, st);
+  else run<D, EXACT, false, false>(a, backward, st);
+}
+
+bf_status by_head(const MaskedArgs& a, bool backward, hipStream_t st) {
+  if (a.vec && a.S_head == 64) by_score<64, true>(a, backward, st);
+  else if (a.vec && a.S_head == 128) by_score<128, true>(a, backward, st);
+  else if (a.S_head <= 64) by_score<64, false>(a, backward, st);
+  else by_score<128, false>(a, backward, st);
+  return launched();
+}
+
+}  // namespace
+
+bf_status attention_masked_fwd_mfma(const MaskedArgs& a, hipStream_t st) { return by_head(a, false, st); }
+bf_status attention_masked_bwd_mfma(const MaskedArgs& a, hipStream_t st) { return by_head(a, true, st); }
+
+}  // namespace bf
