@@ -380,34 +380,27 @@ __global__ __launch_bounds__(2 * ROWS, 2) void masked_fwd_kernel(MaskedArgs a) {
 }
 
 // ------------------------------------------------------------------- backward, dQ pass
-// also takes delta = dctx . ctx of its rows, for the dK / dV pass
+// Walks the keys twice.  First for delta = sum of P dP, in fp32 and kept for the dK / dV pass; then for dS = P (dP - delta) and
+// dQ = dS K.  The usual delta = dctx . ctx takes a ctx that was rounded when it was stored, which puts as large an error on every score
+// gradient of the row as their own rounding does where few keys share a row (8192 tokens, 16 heads of 128, sharp rows: dQ and dK
+// 2.8e-3 off in the 2-norm, 2.3e-3 so); it is two products and no sums, against three and their sums.
 template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS, bool SEEN>
 __device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2][BLK * D]) {
   constexpr int NT = 2 * ROWS;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const QueryBlock wb = query_block(a, blockIdx.x, ROWS);
   const int S = a.S_seq, d = a.S_head, q = wb.q0 + 32 * w + (lane & 31), ql = min(q, S - 1);
-  const size_t seq = (size_t)wb.b * S, orow = (seq + ql) * a.ldo + (size_t)wb.head * d;
+  const size_t seq = (size_t)wb.b * S;
   const bf16_t* kbase = (const bf16_t*)a.k + seq * a.ldk + (size_t)wb.kv * d;
   const bf16_t* vbase = (const bf16_t*)a.v + seq * a.ldv + (size_t)wb.kv * d;
+
   // (S_head 128: precomputed offsets would spill)
   typename std::conditional<D == 64, FragAddr<D>, FragAddrXor<D>>::type fa;
   fa.init(lane);
   bf16x8 qf[D / 16], dof[D / 16];
   load_row<D, EXACT>((const bf16_t*)a.q + (seq + ql) * a.ldq + (size_t)wb.head * d, lane, d, a.vec, qf);
-  load_row<D, EXACT>((const bf16_t*)a.dctx + orow, lane, d, a.vec, dof);
+  load_row<D, EXACT>((const bf16_t*)a.dctx + (seq + ql) * a.ldo + (size_t)wb.head * d, lane, d, a.vec, dof);
   const size_t st = ((size_t)wb.b * a.N_heads + wb.head) * S + ql;
-  float dl = 0.f;
-  {
-    bf16x8 cf[D / 16];
-    load_row<D, EXACT>((const bf16_t*)a.ctx + orow, lane, d, a.vec, cf);
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) dl = fmaf((float)dof[kk][e], (float)cf[kk][e], dl);
-    dl += __shfl_xor(dl, 32, 64);  // lanes l and l + 32 hold the two halves of the row
-    if (lane < 32 && q < S) a.delta[st] = dl;
-  }
   // (a row without a finite score has no probabilities)
   const float lse = a.lse[st], lse2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
   int2 sp = a.span[seq + ql];
@@ -433,81 +426,100 @@ __device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2]
     const int kb = j * BLK;
     if (!SEEN && !(kb >= wg.lo_max && kb + BLK <= wg.hi_min)) bad |= kr.non_finite();
   };
-  if (jbeg < jend) {
-    fetch_k(jbeg);
-    fetch_v(jbeg);
-    kr.store(KVs[0][0], tid);
-    vr.store(KVs[0][1], tid);
-    note(jbeg);
-  }
-  __syncthreads();
-  auto body = [&](int j, auto par) {
-    const int p = par;
-    if constexpr (D == 128) fa.loop();
-    const bf16_t* Ks = KVs[p][0];
-    const bf16_t* Vs = KVs[p][1];
-    const int kb = j * BLK;
-    const bool next = j + 1 < jend, work = !ws.skips(kb, BLK), part = !ws.whole(kb, BLK);
-    if (next) fetch_k(j + 1);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if (t == 1 && next) {
-        kr.store(KVs[p ^ 1][0], tid);
-        note(j + 1);
-        fetch_v(j + 1);
-      }
-      if (!work) continue;
-      f32x16 s = zero16(), dp = zero16();
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) {
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_k(Ks, 32 * t, kk), qf[kk], s, 0, 0, 0);
-        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_k(Vs, 32 * t, kk), dof[kk], dp, 0, 0, 0);
-      }
-      mfma_lds_pipeline<2 * (D / 16), 1, 4>();
-      // p = exp(score - lse); dS = p (dP - delta) times the cap's derivative (the factor 1/sqrt(d) is applied once, to dQ)
-      const float dist = (float)(q - kb - 32 * t - 4 * (lane >> 5));
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float c = 0.f;
-        const float e = exponent<CAP, BIAS>(s[r], dist - (float)((r >> 2) * 8 + (r & 3)), f, c);
-        const float pr = __builtin_amdgcn_exp2f(CAP || BIAS ? e - lse2 : fmaf(e, f.c2, -lse2));
-        s[r] = pr * (dp[r] - dl);
-        if (CAP) s[r] *= 4.f * c * (1.f - c);
-      }
-      if (part) {
-        const int lo = sp.x - kb - 32 * t, n = sp.y - sp.x;
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if ((unsigned)(acc_row(r, lane) - lo) >= (unsigned)n) s[r] = 0.f;
-      }
-      const bf16x8 dsb[4] = {pack8(s, 0), pack8(s, 1)};
-      if (SEEN && part) {
-        accumulate_seen<D>(dq, dsb, 32 * t, 2, Ks, fa, lane, [&](int c) {
-          return interval_bits(kb, __builtin_amdgcn_readlane(sp.x, c), __builtin_amdgcn_readlane(sp.y, c));
-        });
-        continue;
-      }
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-          dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_t(Ks, 32 * t + 16 * k2, dt), dsb[k2], dq[dt], 0, 0, 0);
-      mfma_lds_pipeline<2 * (D / 32), 2, 4>();
+  float delta = 0.f;
+  auto walk = [&](auto second) {
+    constexpr bool GRAD = decltype(second)::value;
+    if (jbeg < jend) {
+      fetch_k(jbeg);
+      fetch_v(jbeg);
+      kr.store(KVs[0][0], tid);
+      vr.store(KVs[0][1], tid);
+      if (GRAD) note(jbeg);
     }
-    if (next) vr.store(KVs[p ^ 1][1], tid);
     __syncthreads();
-  };
-  if constexpr (D == 64) {
-    // unrolled by two: the LDS stage (and with it every fragment address) is a compile-time constant
-    for (int j = jbeg; j < jend; j += 2) {
-      body(j, std::integral_constant<int, 0>{});
-      if (j + 1 < jend) body(j + 1, std::integral_constant<int, 1>{});
+    auto body = [&](int j, auto par) {
+      const int p = par;
+      if constexpr (D == 128) fa.loop();
+      const bf16_t* Ks = KVs[p][0];
+      const bf16_t* Vs = KVs[p][1];
+      const int kb = j * BLK;
+      const bool next = j + 1 < jend, work = !ws.skips(kb, BLK), part = !ws.whole(kb, BLK);
+      if (next) fetch_k(j + 1);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (t == 1 && next) {
+          kr.store(KVs[p ^ 1][0], tid);
+          if (GRAD) note(j + 1);
+          fetch_v(j + 1);
+        }
+        if (!work) continue;
+        f32x16 s = zero16(), dp = zero16();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_k(Ks, 32 * t, kk), qf[kk], s, 0, 0, 0);
+          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_k(Vs, 32 * t, kk), dof[kk], dp, 0, 0, 0);
+        }
+        mfma_lds_pipeline<2 * (D / 16), 1, 4>();
+        // p = exp(score - lse); dS = p (dP - delta) times the cap's derivative (the factor 1/sqrt(d) is applied once, to dQ)
+        const float dist = (float)(q - kb - 32 * t - 4 * (lane >> 5));
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float c = 0.f;
+          const float e = exponent<CAP, BIAS>(s[r], dist - (float)((r >> 2) * 8 + (r & 3)), f, c);
+          const float pr = __builtin_amdgcn_exp2f(CAP || BIAS ? e - lse2 : fmaf(e, f.c2, -lse2));
+          if (GRAD) {
+            s[r] = pr * (dp[r] - delta);
+            if (CAP) s[r] *= 4.f * c * (1.f - c);
+          } else {
+            s[r] = pr * dp[r];
+          }
+        }
+        if (part) {
+          const int lo = sp.x - kb - 32 * t, n = sp.y - sp.x;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if ((unsigned)(acc_row(r, lane) - lo) >= (unsigned)n) s[r] = 0.f;
+        }
+        if constexpr (!GRAD) {
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum[r & 3] += s[r];
+          delta += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        } else {
+          const bf16x8 dsb[4] = {pack8(s, 0), pack8(s, 1)};
+          if (SEEN && part) {
+            accumulate_seen<D>(dq, dsb, 32 * t, 2, Ks, fa, lane, [&](int c) {
+              return interval_bits(kb, __builtin_amdgcn_readlane(sp.x, c), __builtin_amdgcn_readlane(sp.y, c));
+            });
+            continue;
+          }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+              dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa.frag_t(Ks, 32 * t + 16 * k2, dt), dsb[k2], dq[dt], 0, 0, 0);
+          mfma_lds_pipeline<2 * (D / 32), 2, 4>();
+        }
+      }
+      if (next) vr.store(KVs[p ^ 1][1], tid);
+      __syncthreads();
+    };
+    if constexpr (D == 64) {
+      // unrolled by two: the LDS stage (and with it every fragment address) is a compile-time constant
+      for (int j = jbeg; j < jend; j += 2) {
+        body(j, std::integral_constant<int, 0>{});
+        if (j + 1 < jend) body(j + 1, std::integral_constant<int, 1>{});
+      }
+    } else {
+      for (int j = jbeg; j < jend; ++j) body(j, (j - jbeg) & 1);
     }
-  } else {
-    for (int j = jbeg; j < jend; ++j) body(j, (j - jbeg) & 1);
-  }
+  };
+  walk(std::false_type{});
+  delta += __shfl_xor(delta, 32, 64);  // lanes l and l + 32 hold the two halves of a row
+  if (lane < 32 && q < S) a.delta[st] = delta;
+  walk(std::true_type{});
   if (!SEEN && __syncthreads_or(bad)) return true;
   if (q >= S) return false;
   if (sp.y - sp.x <= 1) {  // one key: its probability is 1 whatever the score

@@ -8,8 +8,7 @@
 // vocabulary, the product again with dz as its epilogue, then the two gradient products on that piece: 6 T h V operations
 // beside the forward pass's 2.
 //
-// Precision.  dW is an fp32 main-grad: dz enters its product as two bf16 parts (16 bits and a sign; their error, 1.4e-6 of dz, is that
-// of the logits themselves), or three where the rows are few and the product waits for HBM anyway.  dy is stored in bf16: one
+// Precision.  dW is an fp32 main-grad: dz enters its product as two or three bf16 parts (parts_of).  dy is stored in bf16: one
 // part, rounded once more than the result, as every bf16 tensor between kernels here.
 //
 // Rows whose label is outside the vocabulary have no loss and no gradient, whatever their y holds: dz is set to zero, and dW's
@@ -156,8 +155,10 @@ __global__ __launch_bounds__(NT) void piece_dz_kernel(int cols, float* __restric
 // ---- sizes ---------------------------------------------------------------------------------------
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;  // of dz: what the memory-side cache holds, and little beside 288 GB
 
-// dz's parts: see above.  Up to 64 rows dW's product is the writing of dW.
-inline int parts_of(int rows) { return rows <= 64 ? 3 : 2; }
+// dz's parts, as many as it takes for what they drop (1.4e-6 of dz with two) to stay under the fp32 error of the logits, which grows with the
+// root of their length: 5e-7 of dz at S_hidden 256, 1e-6 at 2048, 1.8e-6 at 8192.  Up to 64 rows dW's product is the writing of dW,
+// and the third part costs nothing.
+inline int parts_of(int rows, int h) { return rows <= 64 || h < 2048 ? 3 : 2; }
 
 struct Plan {
   bool matrix;   // bf16 matrix cores, else fp32 products
@@ -178,7 +179,7 @@ bool sizes_ok(int dtype, int rows, int h, int V, int piece) {
 Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool backward) {
   Plan p{};
   p.matrix = matrix;
-  const size_t per_col = (size_t)rows * (matrix ? 2 * (size_t)parts_of(rows) : 4);
+  const size_t per_col = (size_t)rows * (matrix ? 2 * (size_t)parts_of(rows, h) : 4);
   size_t cols = piece ? (size_t)piece : PIECE_BYTES / per_col;
   if (cols < 1024 && !piece) cols = 1024;
   if (matrix && !backward) cols = (size_t)V;  // the forward product keeps nothing
@@ -195,7 +196,7 @@ Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool ba
     if (backward) {
       p.slices = gemm_mfma_logits_dy_slices(rows, p.piece, h);
       p.y = take((size_t)rows * h * 2);
-      p.z = take((size_t)rows * up(cols, 8) * 2 * parts_of(rows));
+      p.z = take((size_t)rows * up(cols, 8) * 2 * parts_of(rows, h));
       p.dy = take((size_t)p.slices * rows * h * 4);
     } else {
       p.stat = take((size_t)gemm_mfma_logits_tiles(rows, V) * rows * 8);
@@ -315,7 +316,7 @@ bf_status vocab_loss_bwd(int dtype, int rows, int h, int V, int piece, const voi
       l.scale = scale;
       l.col0 = c0;
       l.S_voc = V;
-      l.parts = parts_of(rows);
+      l.parts = parts_of(rows, h);
       l.ldc = (int)up(cols, 8);
       l.plane = (size_t)rows * l.ldc;
       void* dz = ws + p.z;
