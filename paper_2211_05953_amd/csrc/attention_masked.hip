@@ -319,7 +319,12 @@ bool chunks(const bf_attn_config& c, const MaskedArgs& a, uintptr_t al) {
   return (al & 15) == 0 && (a.S_head | a.ldq | a.ldk | a.ldv | a.ldo) % n == 0;
 }
 
-bool matrix(const bf_attn_config& c) { return c.kernels == BF_KERNELS_AUTO && c.S_head <= 128 && c.dtype == BF_BF16; }
+// the matrix-core kernels: heads up to 128, and 32-bit offsets into a tile of 64 rows
+bool matrix(const bf_attn_config& c) {
+  const int64_t far = 1 << 22;
+  return c.kernels == BF_KERNELS_AUTO && c.S_head <= 128 && c.ld_q <= far && c.ld_k <= far && c.ld_v <= far && c.ld_ctx <= far &&
+         (int64_t)c.N_heads * c.S_head <= far;
+}
 
 // Shares of a key / value head's query heads in the dK / dV pass
 int splits_of(const bf_attn_config& c) {
@@ -360,7 +365,7 @@ bf_status attention_masked_fwd(const bf_attn_config* c, const void* q, const voi
   }
   MaskedArgs a = args_of(*c, q, k, v, spans, slopes, ctx, lse);
   a.vec = chunks(*c, a, (uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)ctx);
-  if (matrix(*c)) return attention_masked_fwd_mfma(a, st);
+  if (matrix(*c)) return c->dtype == BF_BF16 ? attention_masked_fwd_mfma(a, st) : attention_masked_fwd_f32(a, st);
   const dim3 grid(c->S_seq, c->S_mb * c->N_heads);
   if (c->dtype == BF_BF16) plain_fwd_kernel<bf16_t><<<grid, 64, 0, st>>>(a);
   else plain_fwd_kernel<float><<<grid, 64, 0, st>>>(a);
@@ -393,7 +398,7 @@ bf_status attention_masked_bwd(const bf_attn_config* c, const void* q, const voi
   a.splits = splits_of(*c);
   a.planes = (float*)((char*)work + ((size_t)c->S_mb * c->N_heads * c->S_seq * 4 + 255) / 256 * 256);
   a.vec = chunks(*c, a, al);
-  if (matrix(*c)) return attention_masked_bwd_mfma(a, st);
+  if (matrix(*c)) return c->dtype == BF_BF16 ? attention_masked_bwd_mfma(a, st) : attention_masked_bwd_f32(a, st);
   const dim3 grid(c->S_seq, c->S_mb * c->N_heads), grid_kv(c->S_seq, c->S_mb * c->N_kv_heads);
   if (c->dtype == BF_BF16) {
     plain_dq_kernel<bf16_t><<<grid, 64, 0, st>>>(a);

@@ -1,0 +1,567 @@
+// Masked attention in fp32 on the fp32 matrix cores (v_mfma_f32_32x32x2_f32), heads up to 128 (padded with zeros to 64 or 128).
+//
+// The passes are those of attention_masked_mfma.hip on tiles of 32 keys (queries).  An instruction contracts over two values,
+// one from each half of the wave.  Over head dimensions a lane holds four in a row, dimensions 8 c + 4 (lane / 32) .. + 3, for four
+// instructions.  Over the tile's rows instruction r takes rows (r / 4) 8 + r % 4 and the same + 4: register r of a score tile is then
+// the other operand as it stands.  157 TFLOP/s against 2.5 PFLOP/s in bf16: the matrix cores bound everything here (64 cycles an
+// instruction, one 4- or 16-byte LDS read for one or four of them).
+#include <float.h>
+#include <math.h>
+
+#include <type_traits>
+
+#include "attention_masked.h"
+
+namespace bf {
+
+namespace {
+
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr int BLK = 32;    // rows of a streamed tile
+constexpr int ROWS = 128;  // queries (keys) of a workgroup, 32 to a wave
+constexpr uint32_t NOWHERE = 0x7fffff00u;
+
+// a tile row's length: rows eight apart share banks in a 16-byte read, and the two rows of a 4-byte read do not
+template <int D> constexpr int LD = D + 8;
+
+__device__ __forceinline__ int acc_row(int r, int lane) { return (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3); }
+
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+
+// Tiles through a buffer descriptor that ends with the last row there is; what lies past it, or past a short row, reads as zeros.
+template <int D, int NT>
+struct Tile {
+  static constexpr int CH = BLK * D / 4 / NT, STEP = NT / (D / 4);
+  u32x4 v[CH];
+  uint32_t off;
+  int col;
+  __device__ __forceinline__ void init(size_t ld, int tid, int d, bool vec) {
+    col = tid % (D / 4) * 4;
+    off = (uint32_t)(tid / (D / 4) * ld + col) * 4;
+    if (vec && col >= d) off = NOWHERE;
+  }
+  __device__ __forceinline__ void fetch(const float* __restrict__ g, size_t ld, int valid, int d, bool vec) {
+    const uint32_t bytes = (uint32_t)(((valid < BLK ? valid : BLK) - 1) * ld + d) * 4;
+    __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)g, 0, (int)bytes, 0x00020000);
+    const uint32_t step = (uint32_t)(STEP * ld * 4);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      if (vec) {
+        v[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off + i * step, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[i][e] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, col + e < d ? off + i * step + 4 * e : NOWHERE, 0, 0);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(float* lds, int tid) const {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) *reinterpret_cast<u32x4*>(lds + (tid / (D / 4) + i * STEP) * LD<D> + col) = v[i];
+  }
+  __device__ __forceinline__ bool non_finite() const {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any |= (v[i][e] & 0x7fffffffu) >= 0x7f800000u;
+    return any;
+  }
+};
+
+// a token's row as the operand of a contraction over head dimensions
+template <int D>
+__device__ __forceinline__ void load_row(const float* __restrict__ row, int lane, int d, bool vec, f32x4 (&f)[D / 8]) {
+#pragma unroll
+  for (int c = 0; c < D / 8; ++c) {
+    const int at = 8 * c + 4 * (lane >> 5);
+    if (vec && at < d) {
+      f[c] = *reinterpret_cast<const f32x4*>(row + at);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[c][e] = at + e < d ? row[at + e] : 0.f;
+    }
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void store_row(const f32x16 (&acc)[D / 32], float* __restrict__ row, int lane, float mul, int d, bool vec) {
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const int c = dt * 32 + q4 * 8 + (lane >> 5) * 4;
+      if (vec && c < d) {
+        f32x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = acc[dt][q4 * 4 + e] * mul;
+        *reinterpret_cast<f32x4*>(row + c) = o;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < d) row[c + e] = acc[dt][q4 * 4 + e] * mul;
+      }
+    }
+}
+
+// s += tile (rows) x row^T over the head dimensions
+template <int D>
+__device__ __forceinline__ void dots(f32x16& s, const float* tile, const f32x4 (&f)[D / 8], int lane) {
+#pragma unroll
+  for (int c = 0; c < D / 8; ++c) {
+    const f32x4 t = *reinterpret_cast<const f32x4*>(tile + (lane & 31) * LD<D> + 8 * c + 4 * (lane >> 5));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(t[e], f[c][e], s, 0, 0, 0);
+  }
+}
+
+// acc += tile^T s over the tile's rows
+template <int D>
+__device__ __forceinline__ void sums(f32x16 (&acc)[D / 32], const f32x16& s, const float* tile, int lane) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+      acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[acc_row(r, lane) * LD<D> + 32 * dt + (lane & 31)], s[r], acc[dt], 0, 0, 0);
+}
+
+// the same, column by column of s over the tile's rows that the column sees (bit r of rows_of(c)): for tiles masked in part that
+// hold an infinity or a NaN
+template <int D, typename F>
+__device__ __forceinline__ void sums_seen(f32x16 (&acc)[D / 32], const f32x16& s, const float* tile, int lane, F rows_of) {
+#pragma unroll 1
+  for (int c = 0; c < 32; ++c) {
+    const uint32_t seen = rows_of(c);
+    if (seen == 0) continue;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) {
+      f32x16 sum = zero16();
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = acc_row(r, lane);
+        const float t = tile[row * LD<D> + 32 * dt + (lane & 31)];
+        sum = __builtin_amdgcn_mfma_f32_32x32x2f32(seen >> row & 1 ? t : 0.f, s[r], sum, 0, 0, 0);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[dt][r] = (lane & 31) == c ? acc[dt][r] + sum[r] : acc[dt][r];
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t interval_bits(int k0, int lo, int hi) {
+  const int a = min(max(lo - k0, 0), 32), b = min(max(hi - k0, 0), 32);
+  return a >= b ? 0u : (~0u >> (32 - (b - a))) << a;
+}
+
+// a score from a dot product; slack: the cap's derivative there
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ float score_of(float dot, float dist, const MaskedArgs& a, float inv_cap, float slope, float& slack) {
+  float s = dot * a.scale;
+  if (CAP) {
+    const float t = tanhf(s * inv_cap);
+    s = a.cap * t;
+    slack = 1.f - t * t;
+  }
+  if (BIAS) s = fmaf(-slope, fabsf(dist), s);
+  return s;
+}
+
+struct WaveSpan {
+  int lo_min, hi_max, lo_max, hi_min;
+  __device__ __forceinline__ void init(int2 sp, bool row) {
+    const bool any = sp.y > sp.x;
+    lo_min = row && any ? sp.x : INT_MAX;
+    hi_max = row && any ? sp.y : 0;
+    lo_max = !row ? 0 : any ? sp.x : INT_MAX;
+    hi_min = !row ? INT_MAX : any ? sp.y : 0;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      lo_min = min(lo_min, __shfl_xor(lo_min, o, 64));
+      hi_max = max(hi_max, __shfl_xor(hi_max, o, 64));
+      lo_max = max(lo_max, __shfl_xor(lo_max, o, 64));
+      hi_min = min(hi_min, __shfl_xor(hi_min, o, 64));
+    }
+    lo_min = __builtin_amdgcn_readfirstlane(lo_min);
+    hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+    lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+    hi_min = __builtin_amdgcn_readfirstlane(hi_min);
+  }
+  __device__ __forceinline__ bool skips(int k, int n) const { return k >= hi_max || k + n <= lo_min; }
+  __device__ __forceinline__ bool whole(int k, int n) const { return k >= lo_max && k + n <= hi_min; }
+};
+
+template <int D>
+struct QueryShared { float K[2][BLK * LD<D>], V[2][BLK * LD<D>]; };
+
+// Forward (GRAD false) and dQ (GRAD true): 128 queries, 32 to a wave.  SEEN: tiles that are masked in part by sums_seen; without it
+// returns whether one of those held a non-finite value that enters a sum.
+template <int D, bool CAP, bool BIAS, bool GRAD, bool SEEN>
+__device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D>& sh) {
+  constexpr int NT = 256;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int S = a.S_seq, d = a.S_head, nhb = a.N_heads * a.S_mb, blocks = (S + ROWS - 1) / ROWS, group = a.N_heads / a.N_kv;
+  const int x = blockIdx.x % nhb, hx = x % a.N_heads, b = x / a.N_heads, kv = hx % a.N_kv, head = kv * group + hx / a.N_kv;
+  const int q = (blocks - 1 - blockIdx.x / nhb) * ROWS + 32 * w + (lane & 31), ql = min(q, S - 1);
+  const size_t seq = (size_t)b * S, st = ((size_t)b * a.N_heads + head) * S + ql, orow = (seq + ql) * a.ldo + (size_t)head * d;
+  const float* kbase = (const float*)a.k + seq * a.ldk + (size_t)kv * d;
+  const float* vbase = (const float*)a.v + seq * a.ldv + (size_t)kv * d;
+
+  f32x4 qf[D / 8], dof[GRAD ? D / 8 : 1];
+  load_row<D>((const float*)a.q + (seq + ql) * a.ldq + (size_t)head * d, lane, d, a.vec, qf);
+  float lse = 0.f, dl = 0.f;
+  if constexpr (GRAD) {
+    load_row<D>((const float*)a.dctx + orow, lane, d, a.vec, dof);
+    f32x4 cf[D / 8];
+    load_row<D>((const float*)a.ctx + orow, lane, d, a.vec, cf);
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dl = fmaf(dof[c][e], cf[c][e], dl);
+    dl += __shfl_xor(dl, 32, 64);
+    if (lane < 32 && q < S) a.delta[st] = dl;
+    lse = a.lse[st] == -INFINITY ? INFINITY : a.lse[st];  // (a row without a finite score has no probabilities)
+  }
+  int2 sp = a.span[seq + ql];
+  sp.x = max(sp.x, 0);
+  sp.y = min(sp.y, S);
+  WaveSpan ws;
+  ws.init(sp, q < S);
+  const int sb = (S + SPAN_ROWS - 1) / SPAN_ROWS, at = (q - 32 * w - (lane & 31)) / SPAN_ROWS;
+  SpanBlock wg = a.block[(size_t)b * sb + at];
+  if (at + 1 < sb) {
+    const SpanBlock y = a.block[(size_t)b * sb + at + 1];
+    wg = {min(wg.lo_min, y.lo_min), max(wg.hi_max, y.hi_max), max(wg.lo_max, y.lo_max), min(wg.hi_min, y.hi_min)};
+  }
+  wg.hi_max = min(wg.hi_max, S);
+  const float slope = BIAS ? a.slope[head] : 0.f, inv_cap = CAP ? 1.f / a.cap : 0.f;
+  f32x16 o[D / 32];  // ctx, or dQ; transposed: rows = head dims, column = the lane's query
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) o[dt] = zero16();
+  float m = -FLT_MAX, l = 0.f;
+
+  const int jbeg = wg.hi_max > 0 ? max(wg.lo_min, 0) / BLK : 0, jend = (wg.hi_max + BLK - 1) / BLK;
+  Tile<D, NT> kr, vr;
+  kr.init(a.ldk, tid, d, a.vec);
+  vr.init(a.ldv, tid, d, a.vec);
+  bool bad = false;
+  auto fetch = [&](int j) {
+    kr.fetch(kbase + (size_t)j * BLK * a.ldk, a.ldk, S - j * BLK, d, a.vec);
+    vr.fetch(vbase + (size_t)j * BLK * a.ldv, a.ldv, S - j * BLK, d, a.vec);
+  };
+  auto put = [&](int j, int stage) {
+    kr.store(sh.K[stage], tid);
+    vr.store(sh.V[stage], tid);
+    const int kb = j * BLK;
+    if (!SEEN && !(kb >= wg.lo_max && kb + BLK <= wg.hi_min)) bad |= GRAD ? kr.non_finite() : vr.non_finite();
+  };
+  if (jbeg < jend) {
+    fetch(jbeg);
+    put(jbeg, 0);
+  }
+  __syncthreads();
+  for (int j = jbeg; j < jend; ++j) {
+    const int cur = (j - jbeg) & 1, kb = j * BLK;
+    if (j + 1 < jend) fetch(j + 1);
+    if (!ws.skips(kb, BLK)) {
+      const bool part = !ws.whole(kb, BLK);
+      f32x16 s = zero16();
+      dots<D>(s, sh.K[cur], qf, lane);
+      const float dist = (float)(q - kb - 4 * (lane >> 5));
+      const int lo = sp.x - kb, n = sp.y - sp.x;
+      if constexpr (!GRAD) {
+        float mx = m, slack;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = score_of<CAP, BIAS>(s[r], dist - (float)((r >> 2) * 8 + (r & 3)), a, inv_cap, slope, slack);
+          if (part && (unsigned)(acc_row(r, lane) - lo) >= (unsigned)n) s[r] = -INFINITY;
+          mx = fmaxf(mx, s[r]);
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {
+          const float alpha = __builtin_amdgcn_exp2f((m - mx) * LOG2E);
+          l *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+          m = mx;
+        }
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = __builtin_amdgcn_exp2f((s[r] - m) * LOG2E);
+          sum[r & 3] += s[r];
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      } else {
+        f32x16 dp = zero16();
+        dots<D>(dp, sh.V[cur], dof, lane);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float slack = 1.f;
+          const float t = score_of<CAP, BIAS>(s[r], dist - (float)((r >> 2) * 8 + (r & 3)), a, inv_cap, slope, slack);
+          s[r] = __builtin_amdgcn_exp2f((t - lse) * LOG2E) * (dp[r] - dl) * slack;
+          if (part && (unsigned)(acc_row(r, lane) - lo) >= (unsigned)n) s[r] = 0.f;
+        }
+      }
+      const float* tile = GRAD ? sh.K[cur] : sh.V[cur];
+      if (SEEN && part)
+        sums_seen<D>(o, s, tile, lane, [&](int c) { return interval_bits(kb, __builtin_amdgcn_readlane(sp.x, c), __builtin_amdgcn_readlane(sp.y, c)); });
+      else sums<D>(o, s, tile, lane);
+    }
+    if (j + 1 < jend) put(j + 1, cur ^ 1);
+    __syncthreads();
+  }
+  if (!SEEN && __syncthreads_or(bad)) return true;
+  l += __shfl_xor(l, 32, 64);
+  if (q >= S) return false;
+  if constexpr (GRAD) {
+    if (sp.y - sp.x <= 1) {  // one key: its probability is 1 whatever the score
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) o[dt] = zero16();
+    }
+    store_row<D>(o, (float*)a.dq + (seq + q) * a.ldq + (size_t)head * d, lane, a.scale, d, a.vec);
+  } else {
+    store_row<D>(o, (float*)a.ctx + orow, lane, l == 0.f ? 0.f : 1.0f / l, d, a.vec);
+    if (lane < 32 && a.lse) a.lse[st] = l == 0.f ? -INFINITY : m + logf(l);
+  }
+  return false;
+}
+
+// (a function of its own: see attention_masked_mfma.hip)
+template <int D, bool CAP, bool BIAS, bool GRAD>
+__device__ __attribute__((noinline)) void query_rows_seen(MaskedArgs a, QueryShared<D>& sh) {
+  query_rows<D, CAP, BIAS, GRAD, true>(a, sh);
+}
+
+template <int D, bool CAP, bool BIAS, bool GRAD>
+__global__ __launch_bounds__(256, 2) void masked_query_f32_kernel(MaskedArgs a) {
+  __shared__ __attribute__((aligned(16))) QueryShared<D> sh;
+  if (query_rows<D, CAP, BIAS, GRAD, false>(a, sh)) query_rows_seen<D, CAP, BIAS, GRAD>(a, sh);
+}
+
+// dK / dV: 8 waves per 128 keys in pairs, as in attention_masked_mfma.hip
+constexpr int NTHR_DKV = 512;
+template <int D>
+struct KeyShared {
+  float Q[2][BLK * LD<D>], O[2][BLK * LD<D>];
+  float stat[2][2][BLK];
+  int span[2][2][BLK];
+  float P[4][4][64 * 4];  // [key group][register quarter][lane]
+  int range[2];
+};
+
+template <int D, bool CAP, bool BIAS, bool SEEN>
+__device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D>& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kg = w & 3;
+  const bool dk_role = w >= 4;  // wave-uniform
+  const int S = a.S_seq, d = a.S_head, group = a.N_heads / a.N_kv, heads = group / a.splits;
+  const int per = a.N_kv * a.splits * a.S_mb, x = blockIdx.x % per, k0 = blockIdx.x / per * ROWS;
+  const int kv = x % a.N_kv, split = x / a.N_kv % a.splits, b = x / (a.N_kv * a.splits);
+  const size_t seq = (size_t)b * S;
+  const int kw = k0 + 32 * kg, key = kw + (lane & 31), kl = min(key, S - 1);
+  const int blocks = (S + SPAN_ROWS - 1) / SPAN_ROWS;
+  const SpanBlock* tb = a.block + (size_t)b * blocks;
+  if (tid < 2) sh.range[tid] = tid ? 0 : INT_MAX;
+  __syncthreads();
+  for (int j = tid; j < blocks; j += NTHR_DKV) {
+    const SpanBlock y = tb[j];
+    if (y.hi_max > k0 && y.lo_min < k0 + ROWS) { atomicMin(&sh.range[0], j); atomicMax(&sh.range[1], j + 1); }
+  }
+  __syncthreads();
+  // in tiles of 32 queries, two to a block of spans
+  const int jbeg = sh.range[0] == INT_MAX ? 0 : 2 * sh.range[0], jend = min(2 * sh.range[1], (S + BLK - 1) / BLK);
+  const int tiles = jend > jbeg ? jend - jbeg : 0, total = tiles * heads, head0 = kv * group + split * heads;
+
+  f32x4 kvf[D / 8];  // this wave's K rows (dV role) or V rows (dK role)
+  if (dk_role) load_row<D>((const float*)a.v + (seq + kl) * a.ldv + (size_t)kv * d, lane, d, a.vec, kvf);
+  else load_row<D>((const float*)a.k + (seq + kl) * a.ldk + (size_t)kv * d, lane, d, a.vec, kvf);
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
+  Tile<D, NTHR_DKV> qr, dor;
+  qr.init(a.ldq, tid, d, a.vec);
+  dor.init(a.ldo, tid, d, a.vec);
+  bool bad = false;
+  float lnext = 0.f, dnext = 0.f;
+  int2 snext = make_int2(0, 0);
+  int fh = 0, fj = jbeg, pj = jbeg;  // of the next fetch, and the next store
+  auto fetch = [&]() {
+    const int head = head0 + fh;
+    qr.fetch((const float*)a.q + (seq + (size_t)fj * BLK) * a.ldq + (size_t)head * d, a.ldq, S - fj * BLK, d, a.vec);
+    dor.fetch((const float*)a.dctx + (seq + (size_t)fj * BLK) * a.ldo + (size_t)head * d, a.ldo, S - fj * BLK, d, a.vec);
+    if (tid < BLK) {
+      const int i = fj * BLK + tid;
+      const size_t st = ((size_t)b * a.N_heads + head) * S + i;
+      const float l = i < S ? a.lse[st] : -INFINITY;
+      lnext = l == -INFINITY ? INFINITY : l;
+      dnext = i < S ? a.delta[st] : 0.f;
+      snext = i < S ? a.span[seq + i] : make_int2(0, 0);
+    }
+    if (++fj == jend) { fj = jbeg; ++fh; }
+  };
+  auto put = [&](int stage) {
+    qr.store(sh.Q[stage], tid);
+    dor.store(sh.O[stage], tid);
+    if (tid < BLK) {
+      sh.stat[stage][0][tid] = lnext;
+      sh.stat[stage][1][tid] = dnext;
+      sh.span[stage][0][tid] = snext.x;
+      sh.span[stage][1][tid] = snext.y;
+    }
+    const SpanBlock y = tb[pj >> 1];
+    const bool whole = k0 >= y.lo_max && k0 + ROWS <= y.hi_min && (pj + 1) * BLK <= S;
+    if (!SEEN && !whole) bad |= qr.non_finite() || dor.non_finite();
+    if (++pj == jend) pj = jbeg;
+  };
+  if (total > 0) {
+    fetch();
+    put(0);
+  }
+  __syncthreads();
+  int j = jbeg, hx = 0;
+  float slope = BIAS ? a.slope[head0] : 0.f;
+  const float inv_cap = CAP ? 1.f / a.cap : 0.f;
+  for (int it = 0; it < total; ++it) {
+    const int cur = it & 1, qb = j * BLK;
+    if (it + 1 < total) fetch();
+    const SpanBlock y = tb[j >> 1];
+    const bool skip = kw >= S || y.hi_max <= kw || y.lo_min >= kw + 32;
+    const bool part = !(kw >= y.lo_max && kw + 32 <= y.hi_min && qb + BLK <= S);
+    const int* lo_s = sh.span[cur][0];
+    const int* hi_s = sh.span[cur][1];
+    f32x16 s = zero16();
+    if (!skip) {
+      if (!dk_role) {
+        dots<D>(s, sh.Q[cur], kvf, lane);
+        const float dist = (float)(qb + 4 * (lane >> 5) - key);
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const f32x4 ls = *reinterpret_cast<const f32x4*>(&sh.stat[cur][0][acc_row(4 * q4, lane)]);
+          f32x4 give;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * q4 + e;
+            float slack = 1.f;
+            const float t = score_of<CAP, BIAS>(s[r], dist + (float)(8 * q4 + e), a, inv_cap, slope, slack);
+            s[r] = __builtin_amdgcn_exp2f((t - ls[e]) * LOG2E);
+            give[e] = s[r] * slack;
+            if (part && (key < lo_s[acc_row(r, lane)] || key >= hi_s[acc_row(r, lane)])) s[r] = 0.f;
+          }
+          *reinterpret_cast<f32x4*>(&sh.P[kg][q4][lane * 4]) = give;
+        }
+      } else {
+        dots<D>(s, sh.O[cur], kvf, lane);
+      }
+    }
+    __syncthreads();
+    if (!skip) {
+      if (dk_role) {
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const f32x4 pr = *reinterpret_cast<const f32x4*>(&sh.P[kg][q4][lane * 4]);
+          const f32x4 dl = *reinterpret_cast<const f32x4*>(&sh.stat[cur][1][acc_row(4 * q4, lane)]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * q4 + e;
+            s[r] = pr[e] * (s[r] - dl[e]);
+            if (part) {
+              const int lo = lo_s[acc_row(r, lane)], hi = hi_s[acc_row(r, lane)];
+              if (key < lo || key >= hi || hi - lo == 1) s[r] = 0.f;  // (a row of one key has no score gradient)
+            }
+          }
+        }
+      }
+      const float* tile = dk_role ? sh.Q[cur] : sh.O[cur];
+      if (SEEN && part)
+        sums_seen<D>(acc, s, tile, lane, [&](int c) {
+          return (uint32_t)__builtin_amdgcn_ballot_w64(kw + c >= lo_s[lane & 31] && kw + c < hi_s[lane & 31]);
+        });
+      else sums<D>(acc, s, tile, lane);
+    }
+    if (++j == jend) {
+      j = jbeg;
+      if (++hx < heads && BIAS) slope = a.slope[head0 + hx];
+    }
+    if (it + 1 < total) put(cur ^ 1);
+    __syncthreads();
+  }
+  if (!SEEN && __syncthreads_or(bad)) return true;
+  if (key >= S) return false;
+  const float mul = dk_role ? a.scale : 1.f;
+  if (a.splits > 1) {
+    // this share's plane: [split][dk, dv][token][key / value head][d]
+    const size_t width = (size_t)a.N_kv * d, plane = (size_t)a.S_mb * S * width;
+    float* out = a.planes + (2 * (size_t)split + (dk_role ? 0 : 1)) * plane + (seq + key) * width + (size_t)kv * d;
+    store_row<D>(acc, out, lane, mul, d, d % 4 == 0);
+    return false;
+  }
+  store_row<D>(acc, dk_role ? (float*)a.dk + (seq + key) * a.ldk + (size_t)kv * d : (float*)a.dv + (seq + key) * a.ldv + (size_t)kv * d, lane, mul, d, a.vec);
+  return false;
+}
+
+template <int D, bool CAP, bool BIAS>
+__device__ __attribute__((noinline)) void key_rows_seen(MaskedArgs a, KeyShared<D>& sh) {
+  key_rows<D, CAP, BIAS, true>(a, sh);
+}
+
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NTHR_DKV, 2) void masked_key_f32_kernel(MaskedArgs a) {
+  __shared__ __attribute__((aligned(16))) KeyShared<D> sh;
+  if (key_rows<D, CAP, BIAS, false>(a, sh)) key_rows_seen<D, CAP, BIAS>(a, sh);
+}
+
+__global__ __launch_bounds__(256) void masked_join_f32_kernel(MaskedArgs a) {
+  const size_t width = (size_t)a.N_kv * a.S_head, plane = (size_t)a.S_mb * a.S_seq * width, n = 2 * plane;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
+    float t = 0.f;
+    for (int k = 0; k < a.splits; ++k) t += a.planes[(size_t)k * n + i];
+    const bool v = i >= plane;
+    const size_t e = v ? i - plane : i, row = e / width, c = e - row * width;
+    if (v) ((float*)a.dv)[row * a.ldv + c] = t;
+    else ((float*)a.dk)[row * a.ldk + c] = t;
+  }
+}
+
+template <int D, bool CAP, bool BIAS>
+void run(const MaskedArgs& a, bool backward, hipStream_t st) {
+  const unsigned blocks = (unsigned)((a.S_seq + ROWS - 1) / ROWS), grid = blocks * (unsigned)(a.N_heads * a.S_mb);
+  if (!backward) {
+    masked_query_f32_kernel<D, CAP, BIAS, false><<<grid, 256, 0, st>>>(a);
+    return;
+  }
+  masked_query_f32_kernel<D, CAP, BIAS, true><<<grid, 256, 0, st>>>(a);
+  masked_key_f32_kernel<D, CAP, BIAS><<<blocks * (unsigned)(a.N_kv * a.splits * a.S_mb), NTHR_DKV, 0, st>>>(a);
+  if (a.splits > 1) masked_join_f32_kernel<<<2048, 256, 0, st>>>(a);
+}
+
+template <int D>
+void by_score(const MaskedArgs& a, bool backward, hipStream_t st) {
+  if (a.cap > 0.f && a.slope) run<D, true, true>(a, backward, st);
+  else if (a.cap > 0.f) run<D, true, false>(a, backward, st);
+  else if (a.slope) run<D, false, true>(a, backward, st);
+  else run<D, false, false>(a, backward, st);
+}
+
+bf_status both(const MaskedArgs& a, bool backward, hipStream_t st) {
+  if (a.S_head <= 64) by_score<64>(a, backward, st);
+  else by_score<128>(a, backward, st);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) { set_error("attention_masked_f32: launch failed: %s", hipGetErrorString(e)); return BF_EDEVICE; }
+  return BF_OK;
+}
+
+}  // namespace
+
+bf_status attention_masked_fwd_f32(const MaskedArgs& a, hipStream_t st) { return both(a, false, st); }
+bf_status attention_masked_bwd_f32(const MaskedArgs& a, hipStream_t st) { return both(a, true, st); }
+
+}  // namespace bf
