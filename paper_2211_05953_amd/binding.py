@@ -3,6 +3,7 @@ the library's HIP kernels; torch is used for device memory and streams.  There i
 fallback: a missing library is an ImportError at load()."""
 import ctypes as C
 import os
+from array import array as _array
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libbf.so")
@@ -443,36 +444,55 @@ def bf_op_adam(n, w, m, v, g, w_lp, t, lr, beta1, beta2, adam_eps, weight_decay)
                             weight_decay, _stream()))
 
 
-def _tensors(who, tensors, dtype):
-    """Checks tensors that a kernel is to work on: dense, of `dtype` (torch), on the current device."""
-    import torch
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t.dtype is not dtype or not t.is_contiguous() or t.device.type != "cuda" or t.device.index != dev:
-            raise ValueError("%s: needs contiguous %s tensors on cuda:%d, got %s on %s, strides %s" % (who, dtype, dev, t.dtype, t.device, t.stride()))
+_torch = None
+
+
+def _th():
+    """torch, imported on first use: the calculators and the schedule need none of it."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
 
 
 def _torch_dtype(dtype):
-    import torch
-    return torch.bfloat16 if dtype == BF_BF16 else torch.float32
+    return _th().bfloat16 if dtype == BF_BF16 else _th().float32
 
 
-def _work(who, work, n):
-    """The caller's scratch, or n bytes from torch's allocator (in the current stream's order)."""
-    import torch
-    if work is None:
-        return torch.empty(max(n, 1), dtype=torch.uint8, device="cuda")
-    _tensors(who, (work,), work.dtype)
-    return work
-
-
-def _list(tensors):
-    return (C.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors]), (C.c_size_t * len(tensors))(*[t.numel() for t in tensors])
+def _tensors(who, tensors, dtype):
+    """Checks tensors that a kernel is to work on: dense, of `dtype` (torch), on the current device."""
+    dev = _th()._C._cuda_getDevice()
+    for t in tensors:
+        if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+            raise ValueError("%s: needs contiguous %s tensors on cuda:%d, got %s on %s, strides %s" % (who, dtype, dev, t.dtype, t.device, t.stride()))
 
 
 def _elems(who, tensor, n):
     if tensor.numel() < n:
         raise ValueError("%s: a tensor of %d elements where %d are used" % (who, tensor.numel(), n))
+
+
+def _work(who, work, n):
+    """The caller's scratch, or n bytes from torch's allocator (in the current stream's order)."""
+    if work is None:
+        return _th().empty(n or 1, dtype=_th().uint8, device="cuda")
+    _tensors(who, (work,), work.dtype)
+    return work
+
+
+def _list(who, tensors, dtype):
+    """Host arrays of the addresses and sizes of a list of tensors, checked as by _tensors.  (Hundreds of tensors: the checks
+    of one kind together, a few calls into torch each.)"""
+    if [t.dtype for t in tensors].count(dtype) != len(tensors) or \
+            [t.get_device() for t in tensors].count(_th()._C._cuda_getDevice()) != len(tensors) or not all([t.is_contiguous() for t in tensors]):
+        _tensors(who, tensors, dtype)
+    return _array("Q", [t.data_ptr() for t in tensors]), _array("Q", [t.numel() for t in tensors])
+
+
+def _at(arr):
+    """Address of an array's elements, NULL for an empty one."""
+    return arr.buffer_info()[0] if len(arr) else None
 
 
 def make_attn_config(dtype, S_mb, S_seq, N_heads, N_kv_heads, S_head, scale=0.0, cap=0.0, ld_q=0, ld_k=0, ld_v=0, ld_ctx=0, kernels=BF_KERNELS_AUTO):
@@ -485,9 +505,8 @@ def bf_op_attention_spans_elems(S_mb, S_seq):
 
 def bf_op_attention_spans(S_mb, S_seq, causal, doc, prefix, spans):
     """spans (int32, bf_op_attention_spans_elems) from document ids [S_mb, S_seq] and prefix lengths [S_mb], int32 or None each."""
-    import torch
     who = "bf_op_attention_spans"
-    _tensors(who, [t for t in (doc, prefix, spans) if t is not None], torch.int32)
+    _tensors(who, [t for t in (doc, prefix, spans) if t is not None], _th().int32)
     for t, n in ((doc, S_mb * S_seq), (prefix, S_mb), (spans, bf_op_attention_spans_elems(S_mb, S_seq))):
         if t is not None:
             _elems(who, t, n)
@@ -496,25 +515,28 @@ def bf_op_attention_spans(S_mb, S_seq, causal, doc, prefix, spans):
 
 def _attn_tensors(who, cfg, spans, slopes, lse, rows):
     """rows: (tensor, heads, step from a token to the next) each; the tensors may be views into longer rows."""
-    import torch
-    dev, dtype = torch.cuda.current_device(), _torch_dtype(cfg.dtype)
+    torch = _th()
+    dev, dtype = torch._C._cuda_getDevice(), _torch_dtype(cfg.dtype)
+    S_mb, S_seq, S_head = cfg.S_mb, cfg.S_seq, cfg.S_head
     for t, heads, ld in rows:
-        n = heads * cfg.S_head
-        if t.dtype is not dtype or t.device.type != "cuda" or t.device.index != dev:
+        n = heads * S_head
+        if t.dtype is not dtype or t.get_device() != dev:
             raise ValueError("%s: needs %s tensors on cuda:%d, got %s on %s" % (who, dtype, dev, t.dtype, t.device))
-        # what the kernels reach from the tensor's first element on has to lie in its storage
-        if ((cfg.S_mb * cfg.S_seq - 1) * (ld or n) + n + t.storage_offset()) * t.element_size() > t.untyped_storage().nbytes():
-            raise ValueError("%s: a tensor of shape %s does not hold %d rows of %d, %d apart" % (who, tuple(t.shape), cfg.S_mb * cfg.S_seq, n, ld or n))
+        if t.dim() == 3 and t.shape == (S_mb, S_seq, n) and t.stride() == (S_seq * (ld or n), ld or n, 1):
+            continue
+        # another shape: what the kernels reach from the tensor's first element on has to lie in its storage
+        if ((S_mb * S_seq - 1) * (ld or n) + n + t.storage_offset()) * t.element_size() > t.untyped_storage().nbytes():
+            raise ValueError("%s: a tensor of shape %s does not hold %d rows of %d, %d apart" % (who, tuple(t.shape), S_mb * S_seq, n, ld or n))
         if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
             raise ValueError("%s: a token's row is not dense, strides %s" % (who, t.stride()))
     _tensors(who, (spans,), torch.int32)
-    _elems(who, spans, bf_op_attention_spans_elems(cfg.S_mb, cfg.S_seq))
+    _elems(who, spans, bf_op_attention_spans_elems(S_mb, S_seq))
     if slopes is not None:
         _tensors(who, (slopes,), torch.float32)
         _elems(who, slopes, cfg.N_heads)
     if lse is not None:
         _tensors(who, (lse,), torch.float32)
-        _elems(who, lse, cfg.S_mb * cfg.N_heads * cfg.S_seq)
+        _elems(who, lse, S_mb * cfg.N_heads * S_seq)
 
 
 def bf_op_attention_masked_fwd(cfg, q, k, v, spans, slopes, ctx, lse=None):
@@ -543,7 +565,7 @@ def bf_op_vocab_loss_work_bytes(dtype, n_rows, S_hidden, S_voc, S_piece=0, backw
 
 
 def _vocab_loss(who, dtype, n_rows, S_hidden, S_voc, S_piece, backward, y, w_out, labels, fp32, small, work):
-    import torch
+    torch = _th()
     _tensors(who, (y, w_out), _torch_dtype(dtype))
     _tensors(who, (labels,), torch.int32)
     _tensors(who, fp32, torch.float32)
@@ -551,7 +573,7 @@ def _vocab_loss(who, dtype, n_rows, S_hidden, S_voc, S_piece, backward, y, w_out
     _elems(who, w_out, S_voc * S_hidden)
     for t in (labels,) + small:
         _elems(who, t, n_rows)
-    return _work(who, work, bf_op_vocab_loss_work_bytes(dtype, n_rows, S_hidden, S_voc, S_piece, backward))
+    return _work(who, work, load().bf_op_vocab_loss_work_bytes(dtype, n_rows, S_hidden, S_voc, S_piece, backward))
 
 
 def bf_op_vocab_loss_fwd(dtype, n_rows, S_hidden, S_voc, y, w_out, labels, scale, lse, row_loss, loss_out, S_piece=0, work=None):
@@ -573,40 +595,40 @@ def bf_op_vocab_loss_bwd(dtype, n_rows, S_hidden, S_voc, y, w_out, labels, lse, 
 
 
 def bf_op_grad_norm_work_bytes(tensors):
-    return load().bf_op_grad_norm_work_bytes(len(tensors), _list(tensors)[1])
+    return load().bf_op_grad_norm_work_bytes(len(tensors), _at(_array("Q", [t.numel() for t in tensors])))
 
 
 def bf_op_grad_norm(dtype, tensors, max_norm, out, work=None):
     """out (fp32, 2 elements) = norm over a list of gradients, coefficient that clips it to max_norm."""
-    import torch
-    _tensors("bf_op_grad_norm", tensors, _torch_dtype(dtype))
-    _tensors("bf_op_grad_norm", (out,), torch.float32)
-    if out.numel() < 2:
-        raise ValueError("bf_op_grad_norm: out needs 2 elements")
-    lib, (g, n) = load(), _list(tensors)
-    work = _work("bf_op_grad_norm", work, lib.bf_op_grad_norm_work_bytes(len(tensors), n))
-    check(lib.bf_op_grad_norm(dtype, len(tensors), g, n, max_norm, out.data_ptr(), work.data_ptr(), work.numel() * work.element_size(), _stream()))
+    who = "bf_op_grad_norm"
+    lib, (g, n) = load(), _list(who, tensors, _torch_dtype(dtype))
+    _tensors(who, (out,), _th().float32)
+    _elems(who, out, 2)
+    work = _work(who, work, lib.bf_op_grad_norm_work_bytes(len(g), _at(n)))
+    check(lib.bf_op_grad_norm(dtype, len(g), _at(g), _at(n), max_norm, out.data_ptr(), work.data_ptr(), work.numel() * work.element_size(), _stream()))
 
 
 def bf_op_grad_scale(dtype, tensors, dst, coef):
     """dst[i] = tensors[i] * coef (device fp32); dst may be the tensors themselves."""
-    import torch
-    _tensors("bf_op_grad_scale", tensors, _torch_dtype(dtype))
-    _tensors("bf_op_grad_scale", dst, _torch_dtype(dtype))
-    _tensors("bf_op_grad_scale", (coef,), torch.float32)
-    (g, n), (d, m) = _list(tensors), _list(dst)
-    if list(n) != list(m) or not coef.numel():
-        raise ValueError("bf_op_grad_scale: the lists differ in their sizes, or coef is empty")
-    check(load().bf_op_grad_scale(dtype, len(tensors), g, d, n, coef.data_ptr(), _stream()))
+    who = "bf_op_grad_scale"
+    (g, n), (d, m) = _list(who, tensors, _torch_dtype(dtype)), _list(who, dst, _torch_dtype(dtype))
+    _tensors(who, (coef,), _th().float32)
+    _elems(who, coef, 1)
+    if n != m:
+        raise ValueError("%s: the lists differ in their sizes" % who)
+    check(load().bf_op_grad_scale(dtype, len(g), _at(g), _at(d), _at(n), coef.data_ptr(), _stream()))
 
 
 def bf_op_adam_clipped(tensors, coef, t, lr, beta1, beta2, adam_eps, weight_decay):
     """The Adam step number t on gradients times coef (device fp32).  tensors: (w, m, v, g, w_lp) each, w_lp bf16 or None."""
-    import torch
-    _tensors("bf_op_adam_clipped", [x for q in tensors for x in q[:4]] + [coef], torch.float32)
-    _tensors("bf_op_adam_clipped", [q[4] for q in tensors if q[4] is not None], torch.bfloat16)
-    if not coef.numel() or any(x is not None and x.numel() != q[0].numel() for q in tensors for x in q[1:]):
-        raise ValueError("bf_op_adam_clipped: tensors of different sizes in one entry, or an empty coef")
-    a = (bf_adam_tensor * len(tensors))(*[(w.data_ptr(), m.data_ptr(), v.data_ptr(), g.data_ptr(), None if lp is None else lp.data_ptr(), w.numel())
-                                          for w, m, v, g, lp in tensors])
-    check(load().bf_op_adam_clipped(len(tensors), a, coef.data_ptr(), t, lr, beta1, beta2, adam_eps, weight_decay, _stream()))
+    who, torch = "bf_op_adam_clipped", _th()
+    _tensors(who, (coef,), torch.float32)
+    _elems(who, coef, 1)
+    w, m, v, g, low = zip(*tensors) if tensors else ((),) * 5
+    (pw, n), (pm, n1), (pv, n2), (pg, n3) = (_list(who, x, torch.float32) for x in (w, m, v, g))
+    pl, n4 = _list(who, [x for x in low if x is not None], torch.bfloat16)
+    if not n == n1 == n2 == n3 or n4 != _array("Q", [k for k, x in zip(n, low) if x is not None]):
+        raise ValueError("%s: tensors of different sizes in one entry" % who)
+    rest = iter(pl)
+    a = _array("Q", [x for i, k in enumerate(n) for x in (pw[i], pm[i], pv[i], pg[i], 0 if low[i] is None else next(rest), k)])  # bf_adam_tensor
+    check(load().bf_op_adam_clipped(len(n), _at(a), coef.data_ptr(), t, lr, beta1, beta2, adam_eps, weight_decay, _stream()))

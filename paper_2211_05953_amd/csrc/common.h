@@ -133,11 +133,13 @@ bf_status gemm_splitk_finish(int epi, int M, int N, int slices, const float* par
                              void* C, hipStream_t st);
 // Products of the vocabulary loss on the bf16 matrix cores; 16-byte aligned operands, S_hidden % 8 == 0, any number of rows and
 // columns (gemm_mfma_logits_supported).  rows x cols logits = y[rows, h] w[cols, h]^T:
-//   _lse      leaves E_LSE's partial statistics in a.logit.part, *tiles rows of them (at most gemm_mfma_logits_tiles)
+//   _lse      leaves E_LSE's partial statistics in l.part, *tiles = gemm_mfma_logits_tiles rows of them
+//   _round    columns that are whole rounds of tiles over the chip (0: no such number)
 //   _grad     leaves E_DLOGITS' planes
 //   _dy       planes[slices][rows][h] (fp32) = (accumulate ? planes : 0) + dz[rows, cols] w[cols, h], slice y of the columns in plane y
 //   _dw       dw[cols, h] (fp32) = (accumulate ? dw : 0) + the sum over parts of dz_part^T y
 bool gemm_mfma_logits_supported(int rows, int cols, int h);
+int gemm_mfma_logits_round(int rows, int h);
 int gemm_mfma_logits_tiles(int rows, int cols);
 bf_status gemm_mfma_logits_lse(int rows, int cols, int h, const void* y, const void* w, const LogitArgs& l, int* tiles, hipStream_t st);
 bf_status gemm_mfma_logits_grad(int rows, int cols, int h, const void* y, const void* w, const LogitArgs& l, void* dz, hipStream_t st);

@@ -1003,16 +1003,19 @@ bf_status gemm_mfma(int layout, int epi, const GemmArgs& a, hipStream_t st) {
 }
 
 // ---- the products of the vocabulary loss ---------------------------------------------------------
-// The logits of a tile live in its accumulators and its epilogue's LDS only.  The edge form throughout: any number of rows and
-// columns.  Tiles as for a product of the same shape.
+// The logits of a tile live in its accumulators and its epilogue's LDS only.  Any number of rows and columns: whole 256 x 256 tiles where the
+// sizes are, the edge form elsewhere.
 namespace {
 
-inline int logit_tile(int rows, int cols) { return choose_edge_tile(L_NT, rows, cols); }  // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+// tile of the logits: 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+inline int logit_tile(int rows, int cols) { return choose_edge_tile(L_NT, rows, cols); }
 
 template <int EPI>
 bf_status logits(const GemmArgs& a, hipStream_t st) {
   switch (logit_tile(a.M, a.N)) {
-    case 0: return launch<TileBig, true, true, EPI, bf16_t, true>(a, st);
+    case 0:
+      if (a.M % 256 == 0 && a.N % 256 == 0 && a.K % BK == 0) return launch<TileBig, true, true, EPI, bf16_t>(a, st);
+      return launch<TileBig, true, true, EPI, bf16_t, true>(a, st);
     case 1: return launch<TileSmall, true, true, EPI, bf16_t, true>(a, st);
     default: break;
   }
@@ -1029,11 +1032,42 @@ bool logits_ok(int rows, int cols, int h, uintptr_t al) {
   return false;
 }
 
+// dy's tile and slices of the columns: 256 x 256 where a whole number of slices of at least 1024 columns fills the chip's 256
+// compute units, smaller ones where not.  2048 x 2048 from 24576 columns, us: 128 x 128 in two slices 232, 256 x 256 in four 172.
+struct DySplit { int tile, slices; };
+inline DySplit dy_split(int rows, int cols, int h) {
+  const long most = cols / 1024 < 1 ? 1 : cols / 1024 < 16 ? cols / 1024 : 16;
+  const long big = (long)((rows + 255) / 256) * ((h + 255) / 256);
+  if (big >= 256) return {0, 1};
+  if (256 % big == 0 && 256 / big <= most) return {0, (int)(256 / big)};
+  const int t = choose_edge_tile(L_NN, rows, h), e = t == 0 ? 256 : t == 1 ? 128 : 64;
+  const long tiles = (long)((rows + e - 1) / e) * ((h + e - 1) / e);
+  long s = (t == 0 ? 256 : 512) / tiles;
+  s = s < most ? s : most;
+  return {t, s < 1 ? 1 : (int)s};
+}
+
 }  // namespace
 
 bool gemm_mfma_logits_supported(int rows, int cols, int h) {
   const int most = 1 << 21;  // 32-bit lane offsets over 256 rows
   return rows >= 1 && cols >= 1 && h >= 8 && h % 8 == 0 && rows <= most && cols <= most && h <= most;
+}
+
+// Columns after which both the logits (rows x columns) and dw (columns x h) have filled the chip a whole number of times with 256 x 256
+// tiles; 0 where the rows or h are no whole tiles, or do not divide a round.
+int gemm_mfma_logits_round(int rows, int h) {
+  if (rows % 256 || h % 256) return 0;
+  int most = 0;
+  for (int across : {rows / 256, h / 256}) {
+    int unit = 256;
+    if (across < 256) {
+      if (256 % across) return 0;
+      unit = 256 / across * 256;
+    }
+    most = unit > most ? unit : most;
+  }
+  return most;
 }
 
 int gemm_mfma_logits_tiles(int rows, int cols) {
@@ -1056,15 +1090,7 @@ bf_status gemm_mfma_logits_grad(int rows, int cols, int h, const void* y, const 
   return logits<E_DLOGITS>(a, st);
 }
 
-// Slices of the columns: enough workgroups to fill the chip where rows x h has few tiles
-int gemm_mfma_logits_dy_slices(int rows, int cols, int h) {
-  const int t = choose_edge_tile(L_NN, rows, h), e = t == 0 ? 256 : t == 1 ? 128 : 64;
-  const long tiles = (long)((rows + e - 1) / e) * ((h + e - 1) / e), slots = t == 0 ? 256 : 512;
-  long s = slots / tiles;
-  if (s > 16) s = 16;
-  if (s > cols / 1024) s = cols / 1024;
-  return s < 1 ? 1 : (int)s;
-}
+int gemm_mfma_logits_dy_slices(int rows, int cols, int h) { return dy_split(rows, cols, h).slices; }
 
 bf_status gemm_mfma_logits_dy(int rows, int cols, int h, const void* dz, int ldz, int parts, size_t plane, const void* w, float* planes, int slices,
                               int accumulate, hipStream_t st) {
@@ -1073,6 +1099,7 @@ bf_status gemm_mfma_logits_dy(int rows, int cols, int h, const void* dz, int ldz
   a.lda = ldz;
   // every slice has to have columns: a shorter piece may take fewer slices than the first one, which writes all planes
   auto len = [&](int n) { return ((cols + n - 1) / n + BK - 1) / BK * BK; };
+  const int tile = slices == dy_split(rows, cols, h).slices ? dy_split(rows, cols, h).tile : choose_edge_tile(L_NN, rows, h);
   while (slices > 1 && (long)(slices - 1) * len(slices) >= cols) {
     if (!accumulate) { set_error("gemm_mfma: %d slices of %d columns", slices, cols); return BF_EINVAL; }
     --slices;
@@ -1080,8 +1107,10 @@ bf_status gemm_mfma_logits_dy(int rows, int cols, int h, const void* dz, int ldz
   a.k_slices = slices;
   a.n_seg = parts;
   a.seg_stride_a = plane;
-  switch (choose_edge_tile(L_NN, rows, h)) {
-    case 0: return launch<TileBig, true, false, E_ACCUM, float, true>(a, st);
+  switch (tile) {
+    case 0:
+      if (rows % 256 == 0 && h % 256 == 0 && cols % (BK * slices) == 0) return launch<TileBig, true, false, E_ACCUM, float>(a, st);
+      return launch<TileBig, true, false, E_ACCUM, float, true>(a, st);
     case 1: return launch<TileSmall, true, false, E_ACCUM, float, true>(a, st);
     default: return launch<TileTiny, true, false, E_ACCUM, float, true>(a, st);
   }
@@ -1095,7 +1124,9 @@ bf_status gemm_mfma_logits_dw(int rows, int cols, int h, const void* dz, int ldz
   a.n_seg = parts;
   a.seg_stride_a = plane;
   switch (choose_edge_tile(L_TN, cols, h)) {
-    case 0: return launch<TileBig, false, false, E_ACCUM, float, true>(a, st);
+    case 0:
+      if (cols % 256 == 0 && h % 256 == 0 && rows % BK == 0) return launch<TileBig, false, false, E_ACCUM, float>(a, st);
+      return launch<TileBig, false, false, E_ACCUM, float, true>(a, st);
     case 1: return launch<TileSmall, false, false, E_ACCUM, float, true>(a, st);
     default: return launch<TileTiny, false, false, E_ACCUM, float, true>(a, st);
   }

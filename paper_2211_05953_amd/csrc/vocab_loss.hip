@@ -156,14 +156,19 @@ __global__ __launch_bounds__(NT) void piece_dz_kernel(int cols, float* __restric
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;  // of dz: what the memory-side cache holds, and little beside 288 GB
 
 // dz's parts, as many as it takes for what they drop (1.4e-6 of dz with two) to stay under the fp32 error of the logits, which grows with the
-// root of their length: 5e-7 of dz at S_hidden 256, 1e-6 at 2048, 1.8e-6 at 8192.  Up to 64 rows dW's product is the writing of dW,
+// root of their length: 5e-7 of dz at S_hidden 256, 1e-6 at 2048, 1.8e-6 at 8192 (dw at 2048: 1.5e-6 off with two parts, 1e-6 with three).  Up to 64 rows dW's product is the writing of dW,
 // and the third part costs nothing.
-inline int parts_of(int rows, int h) { return rows <= 64 || h < 2048 ? 3 : 2; }
+inline int parts_of(int rows, int h) { return rows <= 64 || h < 4096 ? 3 : 2; }
+
+// dy is stored in bf16, one rounding more than its product's operand.  Of few rows the largest of their dz, the label's, may fall where
+// bf16 is coarsest for all of them (one row: 2.6e-3 off in the 2-norm, a rounding alone 1.7e-3); a second part costs little
+// where reading w bounds the product.
+inline int dy_parts_of(int rows) { return rows <= 256 ? 2 : 1; }
 
 struct Plan {
   bool matrix;   // bf16 matrix cores, else fp32 products
-  int piece;     // columns
-  int pieces;
+  int piece;     // columns of the largest piece
+  int unit;      // pieces are multiples of this, but for the last one
   // offsets into the scratch: copy of y, fp32 piece of W, z / dz, planes or sums of dy, statistics, labels' logits
   size_t y, w, z, dy, stat, lab, total;
   int slices;
@@ -175,6 +180,13 @@ bool sizes_ok(int dtype, int rows, int h, int V, int piece) {
   return (dtype == BF_FP32 || dtype == BF_BF16) && rows >= 1 && h >= 1 && V >= 1 && piece >= 0 && rows <= (1 << 21) && h <= (1 << 21) && V <= (1 << 21);
 }
 
+// columns of the piece at c0
+int cols_at(const Plan& p, int c0, int V) {
+  const int left = V - c0;
+  if (left >= p.piece) return p.piece;
+  return p.matrix && left > p.unit ? left / p.unit * p.unit : left;
+}
+
 // `matrix` depends on the tensors' alignment too: the scratch is sized for the larger of the two
 Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool backward) {
   Plan p{};
@@ -184,14 +196,24 @@ Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool ba
   if (cols < 1024 && !piece) cols = 1024;
   // fp32 dy: a product's sum over the columns is one chain in fp32, so it is cut (50304 columns in one: 1.1e-6 off, 6e-7 cut)
   if (!matrix && !piece && cols > 4096) cols = 4096;
-  if (matrix && !backward) cols = (size_t)V;  // the forward product keeps nothing
+  p.unit = 8;
+  if (matrix) {
+    // whole rounds of tiles and a rest: 2048 x 2048 x 50304 in pieces of 25600 (3.1 rounds of 256 x 256) and of 24576 (3), us for logits and dw of
+    // one: 250 + 429 and UNIT_FIGURE
+    const int round = gemm_mfma_logits_round(rows, h);
+    if (!piece && round) {
+      if (!backward) cols = (size_t)V;  // the forward product keeps nothing
+      if (cols >= (size_t)round) p.unit = round;
+    } else if (!backward) {
+      cols = (size_t)V;
+    } else if (!piece && cols < (size_t)V) {
+      cols = up((V + (V + cols - 1) / cols - 1) / ((V + cols - 1) / cols), 512);  // pieces of about the same size
+    }
+    cols = p.unit == 8 ? up(cols, 8) : cols / p.unit * p.unit;
+  }
   if (cols > (size_t)V) cols = (size_t)V;
-  p.pieces = (int)((V + cols - 1) / cols);
-  if (!piece) cols = up((V + p.pieces - 1) / p.pieces, 512);  // pieces of about the same size
-  else if (matrix) cols = up(cols, 8);
-  if (cols > (size_t)V) cols = (size_t)V;
+  if (p.unit > 8 && cols >= (size_t)p.unit) cols = cols / p.unit * p.unit;
   p.piece = (int)cols;
-  p.pieces = (int)((V + cols - 1) / cols);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes, 256); return o; };
   if (matrix) {
@@ -201,7 +223,9 @@ Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool ba
       p.z = take((size_t)rows * up(cols, 8) * 2 * parts_of(rows, h));
       p.dy = take((size_t)p.slices * rows * h * 4);
     } else {
-      p.stat = take((size_t)gemm_mfma_logits_tiles(rows, V) * rows * 8);
+      size_t tiles = 0;
+      for (int c0 = 0, n; c0 < V; c0 += n) tiles += gemm_mfma_logits_tiles(rows, n = cols_at(p, c0, V));
+      p.stat = take(tiles * rows * 8);
       p.lab = take((size_t)rows * 4);
     }
   } else {
@@ -209,7 +233,7 @@ Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool ba
     if (dtype == BF_BF16) p.w = take(cols * h * 4);
     p.z = take((size_t)rows * cols * 4);
     if (backward) {
-      p.stat = take(p.pieces > 1 ? (size_t)rows * h * 4 : 0);  // a later piece's share of dy
+      p.stat = take(p.piece < V ? (size_t)rows * h * 4 : 0);  // a later piece's share of dy
       if (dtype == BF_BF16) p.dy = take((size_t)rows * h * 4);
     } else {
       p.stat = take((size_t)rows * 8);
@@ -264,10 +288,17 @@ bf_status vocab_loss_fwd(int dtype, int rows, int h, int V, int piece, const voi
   if (p.matrix) {
     LogitArgs l;
     l.label = label;
-    l.part = stat;
     l.at_label = at_label;
-    s = gemm_mfma_logits_lse(rows, V, h, y, w, l, &tiles, st);
-    if (s != BF_OK) return s;
+    tiles = 0;
+    for (int c0 = 0, n; c0 < V; c0 += n) {
+      int done = 0;
+      n = cols_at(p, c0, V);
+      l.part = stat + (size_t)tiles * rows * 2;
+      l.col0 = c0;
+      s = gemm_mfma_logits_lse(rows, n, h, y, (const bf16_t*)w + (size_t)c0 * h, l, &done, st);
+      if (s != BF_OK) return s;
+      tiles += done;
+    }
   } else {
     float* z = (float*)(ws + p.z);
     const float* yf = (const float*)y;
@@ -276,8 +307,8 @@ bf_status vocab_loss_fwd(int dtype, int rows, int h, int V, int piece, const voi
       if (s != BF_OK) return s;
       yf = (const float*)(ws + p.y);
     }
-    for (int c0 = 0; c0 < V; c0 += p.piece) {
-      const int cols = V - c0 < p.piece ? V - c0 : p.piece;
+    for (int c0 = 0, n; c0 < V; c0 += n) {
+      const int cols = n = cols_at(p, c0, V);
       const float* wf = (const float*)w + (size_t)c0 * h;
       if (dtype == BF_BF16) {
         s = widen(dtype, (size_t)cols * h, (const bf16_t*)w + (size_t)c0 * h, (float*)(ws + p.w), st);
@@ -310,8 +341,8 @@ bf_status vocab_loss_bwd(int dtype, int rows, int h, int V, int piece, const voi
     float* planes = (float*)(ws + p.dy);
     labelled_rows16_kernel<<<rows, NT, 0, st>>>(h / 8, (const uint4*)y, label, V, (uint4*)yc);
     s = launched();
-    for (int c0 = 0; c0 < V && s == BF_OK; c0 += p.piece) {
-      const int cols = V - c0 < p.piece ? V - c0 : p.piece;
+    for (int c0 = 0, n; c0 < V && s == BF_OK; c0 += n) {
+      const int cols = n = cols_at(p, c0, V);
       LogitArgs l;
       l.label = label;
       l.lse = lse;
@@ -325,7 +356,7 @@ bf_status vocab_loss_bwd(int dtype, int rows, int h, int V, int piece, const voi
       const bf16_t* wp = (const bf16_t*)w + (size_t)c0 * h;
       s = gemm_mfma_logits_grad(rows, cols, h, y, wp, l, dz, st);
       if (s == BF_OK) s = gemm_mfma_logits_dw(rows, cols, h, dz, l.ldc, l.parts, l.plane, yc, dw + (size_t)c0 * h, accumulate, st);
-      if (s == BF_OK) s = gemm_mfma_logits_dy(rows, cols, h, dz, l.ldc, 1, l.plane, wp, planes, p.slices, c0 > 0, st);
+      if (s == BF_OK) s = gemm_mfma_logits_dy(rows, cols, h, dz, l.ldc, dy_parts_of(rows), l.plane, wp, planes, p.slices, c0 > 0, st);
     }
     if (s != BF_OK) return s;
     if (p.slices > 1) return gemm_splitk_finish(E_NONE, rows, h, p.slices, planes, nullptr, nullptr, dy, st);
@@ -335,8 +366,8 @@ bf_status vocab_loss_bwd(int dtype, int rows, int h, int V, int piece, const voi
   float* z = (float*)(ws + p.z);
   float* share = (float*)(ws + p.stat);
   float* dyf = dtype == BF_BF16 ? (float*)(ws + p.dy) : (float*)dy;
-  for (int c0 = 0; c0 < V; c0 += p.piece) {
-    const int cols = V - c0 < p.piece ? V - c0 : p.piece;
+  for (int c0 = 0, n; c0 < V; c0 += n) {
+    const int cols = n = cols_at(p, c0, V);
     const float *wf = (const float*)w + (size_t)c0 * h, *yf = (const float*)y;
     if (dtype == BF_BF16) {
       s = widen(dtype, (size_t)cols * h, (const bf16_t*)w + (size_t)c0 * h, (float*)(ws + p.w), st);
