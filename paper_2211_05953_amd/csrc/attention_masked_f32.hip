@@ -114,9 +114,10 @@ __device__ __forceinline__ void store_row(const f32x16 (&acc)[D / 32], float* __
 
 // s += tile (rows) x row^T over the head dimensions
 template <int D>
-__device__ __forceinline__ void dots(f32x16& s, const float* tile, const f32x4 (&f)[D / 8], int lane) {
+__device__ __forceinline__ void dots(f32x16& s, const float* tile, const f32x4 (&f)[D / 8], int lane, int d) {
 #pragma unroll
   for (int c = 0; c < D / 8; ++c) {
+    if (8 * c >= d) break;  // (uniform: nothing but zeros from here on)
     const f32x4 t = *reinterpret_cast<const f32x4*>(tile + (lane & 31) * LD<D> + 8 * c + 4 * (lane >> 5));
 #pragma unroll
     for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(t[e], f[c][e], s, 0, 0, 0);
@@ -125,24 +126,27 @@ __device__ __forceinline__ void dots(f32x16& s, const float* tile, const f32x4 (
 
 // acc += tile^T s over the tile's rows
 template <int D>
-__device__ __forceinline__ void sums(f32x16 (&acc)[D / 32], const f32x16& s, const float* tile, int lane) {
+__device__ __forceinline__ void sums(f32x16 (&acc)[D / 32], const f32x16& s, const float* tile, int lane, int d) {
 #pragma unroll
-  for (int r = 0; r < 16; ++r)
+  for (int dt = 0; dt < D / 32; ++dt) {
+    if (32 * dt >= d) break;
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
+    for (int r = 0; r < 16; ++r)
       acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[acc_row(r, lane) * LD<D> + 32 * dt + (lane & 31)], s[r], acc[dt], 0, 0, 0);
+  }
 }
 
 // the same, column by column of s over the tile's rows that the column sees (bit r of rows_of(c)): for tiles masked in part that
 // hold an infinity or a NaN
 template <int D, typename F>
-__device__ __forceinline__ void sums_seen(f32x16 (&acc)[D / 32], const f32x16& s, const float* tile, int lane, F rows_of) {
+__device__ __forceinline__ void sums_seen(f32x16 (&acc)[D / 32], const f32x16& s, const float* tile, int lane, int d, F rows_of) {
 #pragma unroll 1
   for (int c = 0; c < 32; ++c) {
     const uint32_t seen = rows_of(c);
     if (seen == 0) continue;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) {
+      if (32 * dt >= d) break;
       f32x16 sum = zero16();
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -161,12 +165,22 @@ __device__ __forceinline__ uint32_t interval_bits(int k0, int lo, int hi) {
   return a >= b ? 0u : (~0u >> (32 - (b - a))) << a;
 }
 
+// tanh to 3 ulp without a branch: a polynomial fitted to tanh(x) / x up to 0.55 (7e-9 off), 1 - 2 / (1 + e^2x) beyond, where the
+// difference costs no bits.  The library's function, inlined for every register of a tile, made the kernels long enough to
+// wait for their own instructions (two tiles to a wave: 61 us, TANH_FIGURE).
+__device__ __forceinline__ float tanh_f(float x) {
+  const float y = fabsf(x), u = x * x;
+  const float near = fmaf(x * u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, -0.00627260751f, 0.0210702536f), -0.0538518654f), 0.133325804f), -0.333333173f), x);
+  const float e = __builtin_amdgcn_exp2f(y * (2.f * LOG2E));
+  return y < 0.55f ? near : copysignf(fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f), x);
+}
+
 // a score from a dot product; slack: the cap's derivative there
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ float score_of(float dot, float dist, const MaskedArgs& a, float inv_cap, float slope, float& slack) {
   float s = dot * a.scale;
   if (CAP) {
-    const float t = tanhf(s * inv_cap);
+    const float t = tanh_f(s * inv_cap);
     s = a.cap * t;
     slack = 1.f - t * t;
   }
@@ -198,18 +212,24 @@ struct WaveSpan {
   __device__ __forceinline__ bool whole(int k, int n) const { return k >= lo_max && k + n <= hi_min; }
 };
 
-template <int D>
-struct QueryShared { float K[2][BLK * LD<D>], V[2][BLK * LD<D>]; };
+// KG key groups: 1: the four waves hold 32 rows each and share the tiles, in two LDS stages.  4: they hold the same 32 rows, every wave walks
+// every fourth tile through an LDS stage of its own, without barriers, and their sums meet at the end: for launches that
+// leave compute units idle.
+template <int D, int KG>
+struct QueryShared {
+  static constexpr int STAGES = KG == 1 ? 2 : 4;
+  float K[STAGES][BLK * LD<D>], V[STAGES][BLK * LD<D>];
+};
 
-// Forward (GRAD false) and dQ (GRAD true): 128 queries, 32 to a wave.  SEEN: tiles that are masked in part by sums_seen; without it
-// returns whether one of those held a non-finite value that enters a sum.
-template <int D, bool CAP, bool BIAS, bool GRAD, bool SEEN>
-__device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D>& sh) {
-  constexpr int NT = 256;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int S = a.S_seq, d = a.S_head, nhb = a.N_heads * a.S_mb, blocks = (S + ROWS - 1) / ROWS, group = a.N_heads / a.N_kv;
+// Forward (GRAD false) and dQ (GRAD true).  SEEN: tiles that are masked in part by sums_seen; without it returns whether one of
+// those held a non-finite value that enters a sum.
+template <int D, int KG, bool CAP, bool BIAS, bool GRAD, bool SEEN>
+__device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D, KG>& sh) {
+  constexpr int NT = KG == 1 ? 256 : 64, RB = KG == 1 ? ROWS : 32;  // threads that fetch a tile, rows of the workgroup
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, wr = KG == 1 ? w : 0, ft = KG == 1 ? tid : lane;
+  const int S = a.S_seq, d = a.S_head, nhb = a.N_heads * a.S_mb, blocks = (S + RB - 1) / RB, group = a.N_heads / a.N_kv;
   const int x = blockIdx.x % nhb, hx = x % a.N_heads, b = x / a.N_heads, kv = hx % a.N_kv, head = kv * group + hx / a.N_kv;
-  const int q = (blocks - 1 - blockIdx.x / nhb) * ROWS + 32 * w + (lane & 31), ql = min(q, S - 1);
+  const int q0 = (blocks - 1 - blockIdx.x / nhb) * RB, q = q0 + 32 * wr + (lane & 31), ql = min(q, S - 1);
   const size_t seq = (size_t)b * S, st = ((size_t)b * a.N_heads + head) * S + ql, orow = (seq + ql) * a.ldo + (size_t)head * d;
   const float* kbase = (const float*)a.k + seq * a.ldk + (size_t)kv * d;
   const float* vbase = (const float*)a.v + seq * a.ldv + (size_t)kv * d;
@@ -226,7 +246,7 @@ __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D>& 
 #pragma unroll
       for (int e = 0; e < 4; ++e) dl = fmaf(dof[c][e], cf[c][e], dl);
     dl += __shfl_xor(dl, 32, 64);
-    if (lane < 32 && q < S) a.delta[st] = dl;
+    if (lane < 32 && q < S && (KG == 1 || w == 0)) a.delta[st] = dl;
     lse = a.lse[st] == -INFINITY ? INFINITY : a.lse[st];  // (a row without a finite score has no probabilities)
   }
   int2 sp = a.span[seq + ql];
@@ -234,9 +254,11 @@ __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D>& 
   sp.y = min(sp.y, S);
   WaveSpan ws;
   ws.init(sp, q < S);
-  const int sb = (S + SPAN_ROWS - 1) / SPAN_ROWS, at = (q - 32 * w - (lane & 31)) / SPAN_ROWS;
+  const int sb = (S + SPAN_ROWS - 1) / SPAN_ROWS, at = q0 / SPAN_ROWS;
   SpanBlock wg = a.block[(size_t)b * sb + at];
-  if (at + 1 < sb) {
+  if (KG > 1) {
+    wg = {ws.lo_min, ws.hi_max, ws.lo_max, ws.hi_min};
+  } else if (at + 1 < sb) {
     const SpanBlock y = a.block[(size_t)b * sb + at + 1];
     wg = {min(wg.lo_min, y.lo_min), max(wg.hi_max, y.hi_max), max(wg.lo_max, y.lo_max), min(wg.hi_min, y.hi_min)};
   }
@@ -249,31 +271,38 @@ __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D>& 
 
   const int jbeg = wg.hi_max > 0 ? max(wg.lo_min, 0) / BLK : 0, jend = (wg.hi_max + BLK - 1) / BLK;
   Tile<D, NT> kr, vr;
-  kr.init(a.ldk, tid, d, a.vec);
-  vr.init(a.ldv, tid, d, a.vec);
+  kr.init(a.ldk, ft, d, a.vec);
+  vr.init(a.ldv, ft, d, a.vec);
   bool bad = false;
   auto fetch = [&](int j) {
     kr.fetch(kbase + (size_t)j * BLK * a.ldk, a.ldk, S - j * BLK, d, a.vec);
     vr.fetch(vbase + (size_t)j * BLK * a.ldv, a.ldv, S - j * BLK, d, a.vec);
   };
   auto put = [&](int j, int stage) {
-    kr.store(sh.K[stage], tid);
-    vr.store(sh.V[stage], tid);
+    kr.store(sh.K[stage], ft);
+    vr.store(sh.V[stage], ft);
     const int kb = j * BLK;
     if (!SEEN && !(kb >= wg.lo_max && kb + BLK <= wg.hi_min)) bad |= GRAD ? kr.non_finite() : vr.non_finite();
   };
-  if (jbeg < jend) {
-    fetch(jbeg);
-    put(jbeg, 0);
+  // (one wave's own stage: its LDS accesses are in order)
+  auto sync = [&]() {
+    if (KG == 1) __syncthreads();
+    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+  const int j0 = KG == 1 ? jbeg : jbeg + w;
+  if (j0 < jend) {
+    fetch(j0);
+    put(j0, KG == 1 ? 0 : w);
   }
-  __syncthreads();
-  for (int j = jbeg; j < jend; ++j) {
-    const int cur = (j - jbeg) & 1, kb = j * BLK;
-    if (j + 1 < jend) fetch(j + 1);
+  sync();
+  for (int j = j0; j < jend; j += KG) {
+    const int cur = KG == 1 ? (j - jbeg) & 1 : w, kb = j * BLK;
+    const float *K = sh.K[cur], *V = sh.V[cur];
+    if (j + KG < jend) fetch(j + KG);
     if (!ws.skips(kb, BLK)) {
       const bool part = !ws.whole(kb, BLK);
       f32x16 s = zero16();
-      dots<D>(s, sh.K[cur], qf, lane);
+      dots<D>(s, K, qf, lane, d);
       const float dist = (float)(q - kb - 4 * (lane >> 5));
       const int lo = sp.x - kb, n = sp.y - sp.x;
       if constexpr (!GRAD) {
@@ -303,7 +332,7 @@ __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D>& 
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       } else {
         f32x16 dp = zero16();
-        dots<D>(dp, sh.V[cur], dof, lane);
+        dots<D>(dp, V, dof, lane, d);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           float slack = 1.f;
@@ -312,16 +341,48 @@ __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D>& 
           if (part && (unsigned)(acc_row(r, lane) - lo) >= (unsigned)n) s[r] = 0.f;
         }
       }
-      const float* tile = GRAD ? sh.K[cur] : sh.V[cur];
+      const float* tile = GRAD ? K : V;
       if (SEEN && part)
-        sums_seen<D>(o, s, tile, lane, [&](int c) { return interval_bits(kb, __builtin_amdgcn_readlane(sp.x, c), __builtin_amdgcn_readlane(sp.y, c)); });
-      else sums<D>(o, s, tile, lane);
+        sums_seen<D>(o, s, tile, lane, d, [&](int c) { return interval_bits(kb, __builtin_amdgcn_readlane(sp.x, c), __builtin_amdgcn_readlane(sp.y, c)); });
+      else sums<D>(o, s, tile, lane, d);
     }
-    if (j + 1 < jend) put(j + 1, cur ^ 1);
-    __syncthreads();
+    if (KG > 1) sync();
+    if (j + KG < jend) put(j + KG, KG == 1 ? cur ^ 1 : w);
+    sync();
   }
   if (!SEEN && __syncthreads_or(bad)) return true;
   l += __shfl_xor(l, 32, 64);
+  if constexpr (KG > 1) {
+    // the other groups hand over their sums, lane to lane, in the stage that was theirs; added in order
+    constexpr int NV = D / 2 + 2;
+    static_assert(NV * 64 <= BLK * LD<D>, "the hand-over does not fit");
+    if (w > 0) {
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sh.K[w][(dt * 16 + r) * 64 + lane] = o[dt][r];
+      sh.K[w][(NV - 2) * 64 + lane] = m;
+      sh.K[w][(NV - 1) * 64 + lane] = l;
+    }
+    __syncthreads();
+    if (w > 0) return false;
+#pragma unroll 1
+    for (int g = 1; g < KG; ++g) {
+      const float* from = sh.K[g] + lane;
+      float a0 = 1.f, a1 = 1.f;
+      if (!GRAD) {
+        const float m1 = from[(NV - 2) * 64], M = fmaxf(m, m1);
+        a0 = __builtin_amdgcn_exp2f((m - M) * LOG2E);
+        a1 = __builtin_amdgcn_exp2f((m1 - M) * LOG2E);
+        l = l * a0 + from[(NV - 1) * 64] * a1;
+        m = M;
+      }
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] = GRAD ? o[dt][r] + from[(dt * 16 + r) * 64] : o[dt][r] * a0 + from[(dt * 16 + r) * 64] * a1;
+    }
+  }
   if (q >= S) return false;
   if constexpr (GRAD) {
     if (sp.y - sp.x <= 1) {  // one key: its probability is 1 whatever the score
@@ -337,34 +398,42 @@ __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D>& 
 }
 
 // (a function of its own: see attention_masked_mfma.hip)
-template <int D, bool CAP, bool BIAS, bool GRAD>
-__device__ __attribute__((noinline)) void query_rows_seen(MaskedArgs a, QueryShared<D>& sh) {
-  query_rows<D, CAP, BIAS, GRAD, true>(a, sh);
+template <int D, int KG, bool CAP, bool BIAS, bool GRAD>
+__device__ __attribute__((noinline)) void query_rows_seen(MaskedArgs a, QueryShared<D, KG>& sh) {
+  query_rows<D, KG, CAP, BIAS, GRAD, true>(a, sh);
 }
 
-template <int D, bool CAP, bool BIAS, bool GRAD>
-__global__ __launch_bounds__(256, 2) void masked_query_f32_kernel(MaskedArgs a) {
-  __shared__ __attribute__((aligned(16))) QueryShared<D> sh;
-  if (query_rows<D, CAP, BIAS, GRAD, false>(a, sh)) query_rows_seen<D, CAP, BIAS, GRAD>(a, sh);
+template <int D, int KG, bool CAP, bool BIAS, bool GRAD>
+__global__ __launch_bounds__(256, KG == 1 ? 2 : 1) void masked_query_f32_kernel(MaskedArgs a) {
+  __shared__ __attribute__((aligned(16))) QueryShared<D, KG> sh;
+  if (query_rows<D, KG, CAP, BIAS, GRAD, false>(a, sh)) {
+    __syncthreads();
+    query_rows_seen<D, KG, CAP, BIAS, GRAD>(a, sh);
+  }
 }
 
-// dK / dV: 8 waves per 128 keys in pairs, as in attention_masked_mfma.hip
+// dK / dV: 8 waves in pairs, as in attention_masked_mfma.hip.  QG query groups: 1: 32 keys to a pair, 128 to the workgroup, the tiles in
+// two LDS stages.  4: all pairs hold the same 32 keys, each takes every fourth tile through a stage of its own, and their sums
+// meet at the end.
 constexpr int NTHR_DKV = 512;
-template <int D>
+template <int D, int QG>
 struct KeyShared {
-  float Q[2][BLK * LD<D>], O[2][BLK * LD<D>];
-  float stat[2][2][BLK];
-  int span[2][2][BLK];
-  float P[4][4][64 * 4];  // [key group][register quarter][lane]
+  static constexpr int STAGES = QG == 1 ? 2 : 4;
+  float Q[STAGES][BLK * LD<D>], O[STAGES][BLK * LD<D>];
+  float stat[STAGES][2][BLK];
+  int span[STAGES][2][BLK];
+  float P[4][4][64 * 4];  // [pair][register quarter][lane]
   int range[2];
 };
 
-template <int D, bool CAP, bool BIAS, bool SEEN>
-__device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D>& sh) {
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kg = w & 3;
+template <int D, int QG, bool CAP, bool BIAS, bool SEEN>
+__device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D, QG>& sh) {
+  constexpr int KB = QG == 1 ? ROWS : 32, NT = NTHR_DKV / QG;  // keys of the workgroup, threads that fetch a tile
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, pair = w & 3;
+  const int kg = QG == 1 ? pair : 0, grp = QG == 1 ? 0 : pair, ft = QG == 1 ? tid : (w >> 2) * 64 + lane;
   const bool dk_role = w >= 4;  // wave-uniform
   const int S = a.S_seq, d = a.S_head, group = a.N_heads / a.N_kv, heads = group / a.splits;
-  const int per = a.N_kv * a.splits * a.S_mb, x = blockIdx.x % per, k0 = blockIdx.x / per * ROWS;
+  const int per = a.N_kv * a.splits * a.S_mb, x = blockIdx.x % per, k0 = blockIdx.x / per * KB;
   const int kv = x % a.N_kv, split = x / a.N_kv % a.splits, b = x / (a.N_kv * a.splits);
   const size_t seq = (size_t)b * S;
   const int kw = k0 + 32 * kg, key = kw + (lane & 31), kl = min(key, S - 1);
@@ -374,7 +443,7 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D>& sh) 
   __syncthreads();
   for (int j = tid; j < blocks; j += NTHR_DKV) {
     const SpanBlock y = tb[j];
-    if (y.hi_max > k0 && y.lo_min < k0 + ROWS) { atomicMin(&sh.range[0], j); atomicMax(&sh.range[1], j + 1); }
+    if (y.hi_max > k0 && y.lo_min < k0 + KB) { atomicMin(&sh.range[0], j); atomicMax(&sh.range[1], j + 1); }
   }
   __syncthreads();
   // in tiles of 32 queries, two to a block of spans
@@ -387,61 +456,62 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D>& sh) 
   f32x16 acc[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
-  Tile<D, NTHR_DKV> qr, dor;
-  qr.init(a.ldq, tid, d, a.vec);
-  dor.init(a.ldo, tid, d, a.vec);
+  Tile<D, NT> qr, dor;
+  qr.init(a.ldq, ft, d, a.vec);
+  dor.init(a.ldo, ft, d, a.vec);
   bool bad = false;
   float lnext = 0.f, dnext = 0.f;
   int2 snext = make_int2(0, 0);
-  int fh = 0, fj = jbeg, pj = jbeg;  // of the next fetch, and the next store
-  auto fetch = [&]() {
-    const int head = head0 + fh;
+  // step `it`: query head it / tiles of the share, tile jbeg + it % tiles
+  auto fetch = [&](int it) {
+    if (it >= total) return;
+    const int fj = jbeg + it % tiles, head = head0 + it / tiles;
     qr.fetch((const float*)a.q + (seq + (size_t)fj * BLK) * a.ldq + (size_t)head * d, a.ldq, S - fj * BLK, d, a.vec);
     dor.fetch((const float*)a.dctx + (seq + (size_t)fj * BLK) * a.ldo + (size_t)head * d, a.ldo, S - fj * BLK, d, a.vec);
-    if (tid < BLK) {
-      const int i = fj * BLK + tid;
+    if (ft < BLK) {
+      const int i = fj * BLK + ft;
       const size_t st = ((size_t)b * a.N_heads + head) * S + i;
       const float l = i < S ? a.lse[st] : -INFINITY;
       lnext = l == -INFINITY ? INFINITY : l;
       dnext = i < S ? a.delta[st] : 0.f;
       snext = i < S ? a.span[seq + i] : make_int2(0, 0);
     }
-    if (++fj == jend) { fj = jbeg; ++fh; }
   };
-  auto put = [&](int stage) {
-    qr.store(sh.Q[stage], tid);
-    dor.store(sh.O[stage], tid);
-    if (tid < BLK) {
-      sh.stat[stage][0][tid] = lnext;
-      sh.stat[stage][1][tid] = dnext;
-      sh.span[stage][0][tid] = snext.x;
-      sh.span[stage][1][tid] = snext.y;
+  auto put = [&](int it, int stage) {
+    if (it >= total) return;
+    qr.store(sh.Q[stage], ft);
+    dor.store(sh.O[stage], ft);
+    if (ft < BLK) {
+      sh.stat[stage][0][ft] = lnext;
+      sh.stat[stage][1][ft] = dnext;
+      sh.span[stage][0][ft] = snext.x;
+      sh.span[stage][1][ft] = snext.y;
     }
+    const int pj = jbeg + it % tiles;
     const SpanBlock y = tb[pj >> 1];
-    const bool whole = k0 >= y.lo_max && k0 + ROWS <= y.hi_min && (pj + 1) * BLK <= S;
+    const bool whole = k0 >= y.lo_max && k0 + KB <= y.hi_min && (pj + 1) * BLK <= S;
     if (!SEEN && !whole) bad |= qr.non_finite() || dor.non_finite();
-    if (++pj == jend) pj = jbeg;
   };
-  if (total > 0) {
-    fetch();
-    put(0);
-  }
+  fetch(grp);
+  put(grp, grp);
   __syncthreads();
-  int j = jbeg, hx = 0;
-  float slope = BIAS ? a.slope[head0] : 0.f;
   const float inv_cap = CAP ? 1.f / a.cap : 0.f;
-  for (int it = 0; it < total; ++it) {
-    const int cur = it & 1, qb = j * BLK;
-    if (it + 1 < total) fetch();
+  // every wave passes the same barriers, whether it has a tile or not
+  for (int step = 0; step < total; step += QG) {
+    const int it = step + grp, cur = QG == 1 ? it & 1 : grp;
+    const bool there = it < total;
+    const int j = jbeg + (there ? it % tiles : 0), qb = j * BLK;
+    const float slope = BIAS && there ? a.slope[head0 + it / tiles] : 0.f;
+    fetch(it + QG);
     const SpanBlock y = tb[j >> 1];
-    const bool skip = kw >= S || y.hi_max <= kw || y.lo_min >= kw + 32;
+    const bool skip = !there || kw >= S || y.hi_max <= kw || y.lo_min >= kw + 32;
     const bool part = !(kw >= y.lo_max && kw + 32 <= y.hi_min && qb + BLK <= S);
     const int* lo_s = sh.span[cur][0];
     const int* hi_s = sh.span[cur][1];
     f32x16 s = zero16();
     if (!skip) {
       if (!dk_role) {
-        dots<D>(s, sh.Q[cur], kvf, lane);
+        dots<D>(s, sh.Q[cur], kvf, lane, d);
         const float dist = (float)(qb + 4 * (lane >> 5) - key);
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
@@ -456,10 +526,10 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D>& sh) 
             give[e] = s[r] * slack;
             if (part && (key < lo_s[acc_row(r, lane)] || key >= hi_s[acc_row(r, lane)])) s[r] = 0.f;
           }
-          *reinterpret_cast<f32x4*>(&sh.P[kg][q4][lane * 4]) = give;
+          *reinterpret_cast<f32x4*>(&sh.P[pair][q4][lane * 4]) = give;
         }
       } else {
-        dots<D>(s, sh.O[cur], kvf, lane);
+        dots<D>(s, sh.O[cur], kvf, lane, d);
       }
     }
     __syncthreads();
@@ -467,7 +537,7 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D>& sh) 
       if (dk_role) {
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
-          const f32x4 pr = *reinterpret_cast<const f32x4*>(&sh.P[kg][q4][lane * 4]);
+          const f32x4 pr = *reinterpret_cast<const f32x4*>(&sh.P[pair][q4][lane * 4]);
           const f32x4 dl = *reinterpret_cast<const f32x4*>(&sh.stat[cur][1][acc_row(4 * q4, lane)]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -482,19 +552,37 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D>& sh) 
       }
       const float* tile = dk_role ? sh.Q[cur] : sh.O[cur];
       if (SEEN && part)
-        sums_seen<D>(acc, s, tile, lane, [&](int c) {
+        sums_seen<D>(acc, s, tile, lane, d, [&](int c) {
           return (uint32_t)__builtin_amdgcn_ballot_w64(kw + c >= lo_s[lane & 31] && kw + c < hi_s[lane & 31]);
         });
-      else sums<D>(acc, s, tile, lane);
+      else sums<D>(acc, s, tile, lane, d);
     }
-    if (++j == jend) {
-      j = jbeg;
-      if (++hx < heads && BIAS) slope = a.slope[head0 + hx];
-    }
-    if (it + 1 < total) put(cur ^ 1);
+    if (QG > 1) __syncthreads();  // its own stage is free
+    put(it + QG, QG == 1 ? cur ^ 1 : grp);
     __syncthreads();
   }
   if (!SEEN && __syncthreads_or(bad)) return true;
+  if constexpr (QG > 1) {
+    // the other pairs' sums, lane to lane, in the stages that were theirs; added in order
+    static_assert(D / 2 * 64 <= BLK * LD<D>, "the hand-over does not fit");
+    float* mine = (dk_role ? sh.Q : sh.O)[pair] + lane;
+    if (pair > 0) {
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mine[(dt * 16 + r) * 64] = acc[dt][r];
+    }
+    __syncthreads();
+    if (pair > 0) return false;
+#pragma unroll 1
+    for (int g = 1; g < QG; ++g) {
+      const float* from = (dk_role ? sh.Q : sh.O)[g] + lane;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[dt][r] += from[(dt * 16 + r) * 64];
+    }
+  }
   if (key >= S) return false;
   const float mul = dk_role ? a.scale : 1.f;
   if (a.splits > 1) {
@@ -508,15 +596,18 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D>& sh) 
   return false;
 }
 
-template <int D, bool CAP, bool BIAS>
-__device__ __attribute__((noinline)) void key_rows_seen(MaskedArgs a, KeyShared<D>& sh) {
-  key_rows<D, CAP, BIAS, true>(a, sh);
+template <int D, int QG, bool CAP, bool BIAS>
+__device__ __attribute__((noinline)) void key_rows_seen(MaskedArgs a, KeyShared<D, QG>& sh) {
+  key_rows<D, QG, CAP, BIAS, true>(a, sh);
 }
 
-template <int D, bool CAP, bool BIAS>
+template <int D, int QG, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NTHR_DKV, 2) void masked_key_f32_kernel(MaskedArgs a) {
-  __shared__ __attribute__((aligned(16))) KeyShared<D> sh;
-  if (key_rows<D, CAP, BIAS, false>(a, sh)) key_rows_seen<D, CAP, BIAS>(a, sh);
+  __shared__ __attribute__((aligned(16))) KeyShared<D, QG> sh;
+  if (key_rows<D, QG, CAP, BIAS, false>(a, sh)) {
+    __syncthreads();
+    key_rows_seen<D, QG, CAP, BIAS>(a, sh);
+  }
 }
 
 __global__ __launch_bounds__(256) void masked_join_f32_kernel(MaskedArgs a) {
@@ -531,15 +622,23 @@ __global__ __launch_bounds__(256) void masked_join_f32_kernel(MaskedArgs a) {
   }
 }
 
+// Workgroups of 128 rows below which the rows' keys (the keys' queries) are shared out over the waves instead
+constexpr unsigned FEW = 192;
+
+template <int D, bool CAP, bool BIAS, bool GRAD>
+void query(const MaskedArgs& a, hipStream_t st) {
+  const unsigned hb = (unsigned)(a.N_heads * a.S_mb), grid = (unsigned)((a.S_seq + ROWS - 1) / ROWS) * hb;
+  if (grid < FEW) masked_query_f32_kernel<D, 4, CAP, BIAS, GRAD><<<(unsigned)((a.S_seq + 31) / 32) * hb, 256, 0, st>>>(a);
+  else masked_query_f32_kernel<D, 1, CAP, BIAS, GRAD><<<grid, 256, 0, st>>>(a);
+}
+
 template <int D, bool CAP, bool BIAS>
 void run(const MaskedArgs& a, bool backward, hipStream_t st) {
-  const unsigned blocks = (unsigned)((a.S_seq + ROWS - 1) / ROWS), grid = blocks * (unsigned)(a.N_heads * a.S_mb);
-  if (!backward) {
-    masked_query_f32_kernel<D, CAP, BIAS, false><<<grid, 256, 0, st>>>(a);
-    return;
-  }
-  masked_query_f32_kernel<D, CAP, BIAS, true><<<grid, 256, 0, st>>>(a);
-  masked_key_f32_kernel<D, CAP, BIAS><<<blocks * (unsigned)(a.N_kv * a.splits * a.S_mb), NTHR_DKV, 0, st>>>(a);
+  if (!backward) { query<D, CAP, BIAS, false>(a, st); return; }
+  query<D, CAP, BIAS, true>(a, st);
+  const unsigned hb = (unsigned)(a.N_kv * a.splits * a.S_mb), grid = (unsigned)((a.S_seq + ROWS - 1) / ROWS) * hb;
+  if (grid < FEW) masked_key_f32_kernel<D, 4, CAP, BIAS><<<(unsigned)((a.S_seq + 31) / 32) * hb, NTHR_DKV, 0, st>>>(a);
+  else masked_key_f32_kernel<D, 1, CAP, BIAS><<<grid, NTHR_DKV, 0, st>>>(a);
   if (a.splits > 1) masked_join_f32_kernel<<<2048, 256, 0, st>>>(a);
 }
 

@@ -187,6 +187,14 @@ def test_forward_and_backward(dtype, B, S, H, KV, d, mask):
     Case(dtype, B, S, H, KV, d, **mask).check()
 
 
+# enough workgroups for the forms that share tiles between their waves
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("mask", MASKS[:6])
+@pytest.mark.parametrize("B,S,H,KV,d", [(3, 140, 72, 36, 64), (2, 140, 100, 25, 128), (2, 300, 64, 32, 72), (4, 100, 60, 60, 33)])
+def test_large_launches(dtype, mask, B, S, H, KV, d):
+    Case(dtype, B, S, H, KV, d, **mask).check()
+
+
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("mask", MASKS[2:6])
 @pytest.mark.parametrize("offset", [1, 3])
@@ -205,10 +213,10 @@ def test_plain_kernels(dtype, mask):
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("d", [64, 128, 200])
 @pytest.mark.parametrize("mask", [dict(causal=1), dict(causal=0), dict(causal=1, slopes=1, cap=10.0)])
-def test_what_a_mask_hides_reaches_no_result(dtype, value, d, mask):
+def test_what_a_mask_hides_reaches_no_result(dtype, value, d, mask, H=4, KV=2):
     """Padding in the middle and at the end, and a document of its own, hold infinities or NaN in q, k, v and dctx: the other
     documents' results are those of zeros in their place."""
-    c = Case(dtype, 2, 300, 4, 2, d, docs=40, pad=1, **mask)
+    c = Case(dtype, 2, 300, H, KV, d, docs=40, pad=1, **mask)
     c.doc[1, 100:130] = 5000
     bad = (c.doc < 0) | (c.doc == 5000)
     for x in (c.q, c.k, c.v, c.dctx):
@@ -226,6 +234,12 @@ def test_what_a_mask_hides_reaches_no_result(dtype, value, d, mask):
     none = c.doc < 0
     assert not ctx[none].any() and not dq[none].any() and not dk[none].any() and not dv[none].any()
     assert bool((lse.transpose(1, 2)[none] == -math.inf).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_what_a_mask_hides_in_large_launches(dtype):
+    test_what_a_mask_hides_reaches_no_result(dtype, math.nan, 64, dict(causal=1), H=96, KV=96)
+    test_what_a_mask_hides_reaches_no_result(dtype, math.inf, 128, dict(causal=0, cap=10.0), H=96, KV=48)
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
