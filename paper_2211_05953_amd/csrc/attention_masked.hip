@@ -313,10 +313,10 @@ MaskedArgs args_of(const bf_attn_config& c, const void* q, const void* k, const 
   return a;
 }
 
-// rows of whole 16-byte chunks, in every tensor
+// rows of whole 16-byte chunks that start at multiples of 4 bytes, in every tensor
 bool chunks(const bf_attn_config& c, const MaskedArgs& a, uintptr_t al) {
-  const size_t n = c.dtype == BF_BF16 ? 8 : 4;
-  return (al & 15) == 0 && (a.S_head | a.ldq | a.ldk | a.ldv | a.ldo) % n == 0;
+  if (c.dtype == BF_FP32) return a.S_head % 4 == 0;
+  return (al & 3) == 0 && a.S_head % 8 == 0 && ((a.ldq | a.ldk | a.ldv | a.ldo) & 1) == 0;
 }
 
 // the matrix-core kernels: heads up to 128, and 32-bit offsets into a tile of 64 rows

@@ -18,77 +18,83 @@ namespace bf {
 
 namespace {
 
-// ---- loads and stores of token rows that may be shorter than D or off 16-byte alignment (EXACT: neither).
-// Tiles come through a buffer descriptor that ends with the last row there is: a lane keeps one 32-bit offset, and what lies
-// past the end, or past a short row, reads as zeros.
+// ---- loads and stores of token rows, shorter than D or not.  Through buffer descriptors that end where the rows do: a lane keeps one
+// 32-bit offset, and what lies past the end, or past a short row, reads as zeros and is not written.  No branches: short
+// launches wait for their instructions, about 1 us for 600 bytes that run once.
+// VEC: rows of whole 16-byte chunks that start at multiples of 4 bytes; else element by element.
 constexpr uint32_t NOWHERE = 0x7fffff00u;
 
-template <int ROWS, int D, int NT, bool EXACT>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void* g, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)g, 0, (int)bytes, 0x00020000);
+}
+
+// eight elements at byte offset `off`, `left` of them inside the row (VEC: all or none)
+template <bool VEC>
+__device__ __forceinline__ u32x4 load_chunk(__amdgpu_buffer_rsrc_t rsrc, uint32_t off, int left) {
+  if (VEC) return __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0);
+  u32x4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(rsrc, 2 * e < left ? off + 4 * e : NOWHERE, 0, 0);
+    const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(rsrc, 2 * e + 1 < left ? off + 4 * e + 2 : NOWHERE, 0, 0);
+    v[e] = lo | hi << 16;
+  }
+  return v;
+}
+
+template <int ROWS, int D, int NT, bool VEC>
 struct Tile : TileRegs<ROWS, D, NT> {
   static constexpr int CH = TileRegs<ROWS, D, NT>::CH, STEP = NT / (D / 8);  // rows between a thread's chunks
   uint32_t off;
-  int col;
-  __device__ __forceinline__ void init(size_t ld, int tid, int d, bool vec) {
-    col = tid % (D / 8) * 8;
-    off = (uint32_t)(tid / (D / 8) * ld + col) * 2;
-    if (!EXACT && vec && col >= d) off = NOWHERE;
+  int left;
+  __device__ __forceinline__ void init(size_t ld, int tid, int d) {
+    const int col = tid % (D / 8) * 8;
+    left = d - col;
+    off = VEC && left <= 0 ? NOWHERE : (uint32_t)(tid / (D / 8) * ld + col) * 2;
   }
   // g: the tile's first row, `valid` >= 1 of which are there (uniform)
-  __device__ __forceinline__ void fetch(const bf16_t* __restrict__ g, size_t ld, int valid, int d, bool vec) {
-    const uint32_t bytes = (uint32_t)(((valid < ROWS ? valid : ROWS) - 1) * ld + d) * 2;
-    __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)g, 0, (int)bytes, 0x00020000);
+  __device__ __forceinline__ void fetch(const bf16_t* __restrict__ g, size_t ld, int valid, int d) {
+    const auto rsrc = rows_at(g, (uint32_t)(((valid < ROWS ? valid : ROWS) - 1) * ld + d) * 2);
     const uint32_t step = (uint32_t)(STEP * ld * 2);
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      if (EXACT || vec) {
-        this->v[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off + i * step, 0, 0);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t at = off + i * step + 4 * e;
-          const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(rsrc, col + 2 * e < d ? at : NOWHERE, 0, 0);
-          const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(rsrc, col + 2 * e + 1 < d ? at + 2 : NOWHERE, 0, 0);
-          this->v[i][e] = lo | hi << 16;
-        }
-      }
-    }
+    for (int i = 0; i < CH; ++i) this->v[i] = load_chunk<VEC>(rsrc, off + i * step, left);
   }
 };
 
-template <int D, bool EXACT>
-__device__ __forceinline__ void load_row(const bf16_t* __restrict__ row, int lane, int d, bool vec, bf16x8 (&f)[D / 16]) {
+// rows: the workgroup's first row and its bytes from there (uniform); off: the lane's row
+template <int D, bool VEC>
+__device__ __forceinline__ void load_row(__amdgpu_buffer_rsrc_t rows, uint32_t off, int lane, int d, bf16x8 (&f)[D / 16]) {
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) {
     const int c = kk * 16 + 8 * (lane >> 5);
-    if (EXACT || (vec && c < d)) {
-      f[kk] = *reinterpret_cast<const bf16x8*>(row + c);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[kk][e] = c + e < d ? row[c + e] : (bf16_t)0.f;
-    }
+    f[kk] = __builtin_bit_cast(bf16x8, load_chunk<VEC>(rows, !VEC || c < d ? off + 2 * c : NOWHERE, d - c));
   }
 }
 
-template <int D, bool EXACT>
-__device__ __forceinline__ void store_row(const f32x16 (&acc)[D / 32], bf16_t* __restrict__ row, int lane, float mul, int d, bool vec) {
-  if (EXACT) { store_rows<D>(acc, row, lane, mul); return; }
+template <int D, bool VEC>
+__device__ __forceinline__ void store_row(const f32x16 (&acc)[D / 32], __amdgpu_buffer_rsrc_t rows, uint32_t off, int lane, float mul, int d) {
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int q4 = 0; q4 < 4; ++q4) {
       const int c = dt * 32 + q4 * 8 + (lane >> 5) * 4;
-      if (vec && c < d) {  // d is a multiple of 8
-        bf16x4 o;
+      bf16x4 o;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[dt][q4 * 4 + e] * mul);
-        *reinterpret_cast<bf16x4*>(row + c) = o;
+      for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[dt][q4 * 4 + e] * mul);
+      typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
+      const u32x2 u = __builtin_bit_cast(u32x2, o);
+      if (VEC) {
+        __builtin_amdgcn_raw_buffer_store_b64(u, rows, c < d ? off + 2 * c : NOWHERE, 0, 0);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (c + e < d) row[c + e] = (bf16_t)(acc[dt][q4 * 4 + e] * mul);
+          __builtin_amdgcn_raw_buffer_store_b16((short)(u[e >> 1] >> 16 * (e & 1)), rows, c + e < d ? off + 2 * (c + e) : NOWHERE, 0, 0);
       }
     }
 }
+
+// bytes of up to n rows, those that are there of them
+__device__ __forceinline__ uint32_t row_bytes(int n, int there, size_t ld, int d) { return (uint32_t)(((there < n ? there : n) - 1) * ld + d) * 2; }
 
 // ---- from a dot product to an exponent of two.  Without cap and bias the dot products stay as they are and the factor enters with
 // the exponential (one fma).  cap: tanh x = 1 - 2 r with r = 1 / (1 + e^2x), on the hardware exponential and reciprocal (1 ulp
@@ -216,7 +222,7 @@ __device__ __forceinline__ QueryBlock query_block(const MaskedArgs& a, int idx, 
 
 // ------------------------------------------------------------------------------ forward
 // SEEN: tiles that are masked in part by accumulate_seen.  Without it, returns whether one of those held a non-finite V.
-template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS, bool SEEN>
+template <int D, int ROWS, bool VEC, bool CAP, bool BIAS, bool SEEN>
 __device__ __forceinline__ bool fwd_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2][BLK * D]) {
   constexpr int NT = 2 * ROWS;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -229,7 +235,10 @@ __device__ __forceinline__ bool fwd_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2
   typename std::conditional<D == 64, FragAddr<D>, FragAddrXor<D>>::type fa;
   fa.init(lane);
   bf16x8 qf[D / 16];
-  load_row<D, EXACT>((const bf16_t*)a.q + (seq + ql) * a.ldq + (size_t)wb.head * d, lane, d, a.vec, qf);
+  // (rows past the end read zeros)
+  const int r0 = 32 * w + (lane & 31);
+  load_row<D, VEC>(rows_at((const bf16_t*)a.q + (seq + wb.q0) * a.ldq + (size_t)wb.head * d, row_bytes(ROWS, S - wb.q0, a.ldq, d)), (uint32_t)(r0 * a.ldq) * 2, lane,
+                   d, qf);
   int2 sp = a.span[seq + ql];
   sp.x = max(sp.x, 0);
   sp.y = min(sp.y, S);
@@ -244,13 +253,13 @@ __device__ __forceinline__ bool fwd_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2
   float m = f.c2 > 1.f ? -FLT_MAX / f.c2 : -FLT_MAX, l = 0.f;
 
   const int jbeg = wg.hi_max > 0 ? max(wg.lo_min, 0) / BLK : 0, jend = (wg.hi_max + BLK - 1) / BLK;
-  Tile<BLK, D, NT, EXACT> kr, vr;
+  Tile<BLK, D, NT, VEC> kr, vr;
   bool bad = false;
-  kr.init(a.ldk, tid, d, a.vec);
-  vr.init(a.ldv, tid, d, a.vec);
+  kr.init(a.ldk, tid, d);
+  vr.init(a.ldv, tid, d);
   // the next tile's K is on its way during the first half of a tile's work, its V during the second, in the same registers
-  auto fetch_k = [&](int j) { kr.fetch(kbase + (size_t)j * BLK * a.ldk, a.ldk, S - j * BLK, d, a.vec); };
-  auto fetch_v = [&](int j) { vr.fetch(vbase + (size_t)j * BLK * a.ldv, a.ldv, S - j * BLK, d, a.vec); };
+  auto fetch_k = [&](int j) { kr.fetch(kbase + (size_t)j * BLK * a.ldk, a.ldk, S - j * BLK, d); };
+  auto fetch_v = [&](int j) { vr.fetch(vbase + (size_t)j * BLK * a.ldv, a.ldv, S - j * BLK, d); };
   auto note = [&](int j) {
     const int kb = j * BLK;
     if (!SEEN && !(kb >= wg.lo_max && kb + BLK <= wg.hi_min)) bad |= vr.non_finite();
@@ -359,24 +368,24 @@ __device__ __forceinline__ bool fwd_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2
   }
   if (!SEEN && __syncthreads_or(bad)) return true;
   l += __shfl_xor(l, 32, 64);
-  if (q >= S) return false;
-  store_row<D, EXACT>(o, (bf16_t*)a.ctx + (seq + q) * a.ldo + (size_t)wb.head * d, lane, l == 0.f ? 0.f : 1.0f / l, d, a.vec);
-  if (lane < 32 && a.lse)
+  store_row<D, VEC>(o, rows_at((bf16_t*)a.ctx + (seq + wb.q0) * a.ldo + (size_t)wb.head * d, row_bytes(ROWS, S - wb.q0, a.ldo, d)), (uint32_t)(r0 * a.ldo) * 2, lane,
+                    l == 0.f ? 0.f : 1.0f / l, d);
+  if (lane < 32 && q < S && a.lse)
     a.lse[((size_t)wb.b * a.N_heads + wb.head) * S + q] = l == 0.f ? -INFINITY : m * (CAP || BIAS ? LN2 : a.scale) + logf(l);
   return false;
 }
 
 // The second way is a pass of its own, and a function: in the first one's loop, or behind it in the same body, what it needs
 // pushes the first one's registers out.
-template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS>
+template <int D, int ROWS, bool VEC, bool CAP, bool BIAS>
 __device__ __attribute__((noinline)) void fwd_rows_seen(MaskedArgs a, bf16_t (&KVs)[2][2][BLK * D]) {
-  fwd_rows<D, ROWS, EXACT, CAP, BIAS, true>(a, KVs);
+  fwd_rows<D, ROWS, VEC, CAP, BIAS, true>(a, KVs);
 }
 
-template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS>
+template <int D, int ROWS, bool VEC, bool CAP, bool BIAS>
 __global__ __launch_bounds__(2 * ROWS, 2) void masked_fwd_kernel(MaskedArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t KVs[2][2][BLK * D];
-  if (fwd_rows<D, ROWS, EXACT, CAP, BIAS, false>(a, KVs)) fwd_rows_seen<D, ROWS, EXACT, CAP, BIAS>(a, KVs);
+  if (fwd_rows<D, ROWS, VEC, CAP, BIAS, false>(a, KVs)) fwd_rows_seen<D, ROWS, VEC, CAP, BIAS>(a, KVs);
 }
 
 // ------------------------------------------------------------------- backward, dQ pass
@@ -384,7 +393,7 @@ __global__ __launch_bounds__(2 * ROWS, 2) void masked_fwd_kernel(MaskedArgs a) {
 // dQ = dS K.  The usual delta = dctx . ctx takes a ctx that was rounded when it was stored, which puts as large an error on every score
 // gradient of the row as their own rounding does where few keys share a row (8192 tokens, 16 heads of 128, sharp rows: dQ and dK
 // 2.8e-3 off in the 2-norm, 2.3e-3 so); it is two products and no sums, against three and their sums.
-template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS, bool SEEN>
+template <int D, int ROWS, bool VEC, bool CAP, bool BIAS, bool SEEN>
 __device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2][BLK * D]) {
   constexpr int NT = 2 * ROWS;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -398,8 +407,11 @@ __device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2]
   typename std::conditional<D == 64, FragAddr<D>, FragAddrXor<D>>::type fa;
   fa.init(lane);
   bf16x8 qf[D / 16], dof[D / 16];
-  load_row<D, EXACT>((const bf16_t*)a.q + (seq + ql) * a.ldq + (size_t)wb.head * d, lane, d, a.vec, qf);
-  load_row<D, EXACT>((const bf16_t*)a.dctx + (seq + ql) * a.ldo + (size_t)wb.head * d, lane, d, a.vec, dof);
+  const int r0 = 32 * w + (lane & 31);
+  load_row<D, VEC>(rows_at((const bf16_t*)a.q + (seq + wb.q0) * a.ldq + (size_t)wb.head * d, row_bytes(ROWS, S - wb.q0, a.ldq, d)), (uint32_t)(r0 * a.ldq) * 2, lane,
+                   d, qf);
+  load_row<D, VEC>(rows_at((const bf16_t*)a.dctx + (seq + wb.q0) * a.ldo + (size_t)wb.head * d, row_bytes(ROWS, S - wb.q0, a.ldo, d)), (uint32_t)(r0 * a.ldo) * 2,
+                   lane, d, dof);
   const size_t st = ((size_t)wb.b * a.N_heads + wb.head) * S + ql;
   // (a row without a finite score has no probabilities)
   const float lse = a.lse[st], lse2 = lse == -INFINITY ? INFINITY : lse * LOG2E;
@@ -415,13 +427,13 @@ __device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2]
   for (int dt = 0; dt < D / 32; ++dt) dq[dt] = zero16();
 
   const int jbeg = wg.hi_max > 0 ? max(wg.lo_min, 0) / BLK : 0, jend = (wg.hi_max + BLK - 1) / BLK;
-  Tile<BLK, D, NT, EXACT> kr, vr;
+  Tile<BLK, D, NT, VEC> kr, vr;
   bool bad = false;
-  kr.init(a.ldk, tid, d, a.vec);
-  vr.init(a.ldv, tid, d, a.vec);
+  kr.init(a.ldk, tid, d);
+  vr.init(a.ldv, tid, d);
   // the next tile's K is on its way during the first half of a tile's work, its V during the second, in the same registers
-  auto fetch_k = [&](int j) { kr.fetch(kbase + (size_t)j * BLK * a.ldk, a.ldk, S - j * BLK, d, a.vec); };
-  auto fetch_v = [&](int j) { vr.fetch(vbase + (size_t)j * BLK * a.ldv, a.ldv, S - j * BLK, d, a.vec); };
+  auto fetch_k = [&](int j) { kr.fetch(kbase + (size_t)j * BLK * a.ldk, a.ldk, S - j * BLK, d); };
+  auto fetch_v = [&](int j) { vr.fetch(vbase + (size_t)j * BLK * a.ldv, a.ldv, S - j * BLK, d); };
   auto note = [&](int j) {
     const int kb = j * BLK;
     if (!SEEN && !(kb >= wg.lo_max && kb + BLK <= wg.hi_min)) bad |= kr.non_finite();
@@ -521,24 +533,24 @@ __device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2]
   if (lane < 32 && q < S) a.delta[st] = delta;
   walk(std::true_type{});
   if (!SEEN && __syncthreads_or(bad)) return true;
-  if (q >= S) return false;
   if (sp.y - sp.x <= 1) {  // one key: its probability is 1 whatever the score
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) dq[dt] = zero16();
   }
-  store_row<D, EXACT>(dq, (bf16_t*)a.dq + (seq + q) * a.ldq + (size_t)wb.head * d, lane, a.scale, d, a.vec);
+  store_row<D, VEC>(dq, rows_at((bf16_t*)a.dq + (seq + wb.q0) * a.ldq + (size_t)wb.head * d, row_bytes(ROWS, S - wb.q0, a.ldq, d)), (uint32_t)(r0 * a.ldq) * 2, lane,
+                    a.scale, d);
   return false;
 }
 
-template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS>
+template <int D, int ROWS, bool VEC, bool CAP, bool BIAS>
 __device__ __attribute__((noinline)) void dq_rows_seen(MaskedArgs a, bf16_t (&KVs)[2][2][BLK * D]) {
-  dq_rows<D, ROWS, EXACT, CAP, BIAS, true>(a, KVs);
+  dq_rows<D, ROWS, VEC, CAP, BIAS, true>(a, KVs);
 }
 
-template <int D, int ROWS, bool EXACT, bool CAP, bool BIAS>
+template <int D, int ROWS, bool VEC, bool CAP, bool BIAS>
 __global__ __launch_bounds__(2 * ROWS, 2) void masked_dq_kernel(MaskedArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t KVs[2][2][BLK * D];
-  if (dq_rows<D, ROWS, EXACT, CAP, BIAS, false>(a, KVs)) dq_rows_seen<D, ROWS, EXACT, CAP, BIAS>(a, KVs);
+  if (dq_rows<D, ROWS, VEC, CAP, BIAS, false>(a, KVs)) dq_rows_seen<D, ROWS, VEC, CAP, BIAS>(a, KVs);
 }
 
 // ----------------------------------------------------------------- backward, dK / dV pass
@@ -557,7 +569,7 @@ struct DkvShared {
   int range[2];
 };
 
-template <int D, bool EXACT, bool CAP, bool BIAS, bool SEEN>
+template <int D, bool VEC, bool CAP, bool BIAS, bool SEEN>
 __device__ __forceinline__ bool dkv_keys(const MaskedArgs& a, DkvShared<D>& sh) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kg = w & 3;
   const bool dk_role = w >= 4;  // wave-uniform
@@ -566,7 +578,7 @@ __device__ __forceinline__ bool dkv_keys(const MaskedArgs& a, DkvShared<D>& sh) 
   const int k0 = blockIdx.x / per * WG_ROWS;  // earliest keys first: under a causal mask they see the most queries
   const int kv = x % a.N_kv, split = x / a.N_kv % a.splits, b = x / (a.N_kv * a.splits);
   const size_t seq = (size_t)b * S;
-  const int kw = k0 + 32 * kg, key = kw + (lane & 31), kl = min(key, S - 1);
+  const int kw = k0 + 32 * kg, key = kw + (lane & 31);
   const int blocks = (S + SPAN_ROWS - 1) / SPAN_ROWS;
   const SpanBlock* tb = a.block + (size_t)b * blocks;
 
@@ -583,15 +595,16 @@ __device__ __forceinline__ bool dkv_keys(const MaskedArgs& a, DkvShared<D>& sh) 
   typename std::conditional<D == 64, FragAddr<D>, FragAddrXor<D>>::type fa;
   fa.init(lane);
   bf16x8 kvf[D / 16];  // this wave's K rows (dV role) or V rows (dK role)
-  if (dk_role) load_row<D, EXACT>((const bf16_t*)a.v + (seq + kl) * a.ldv + (size_t)kv * d, lane, d, a.vec, kvf);
-  else load_row<D, EXACT>((const bf16_t*)a.k + (seq + kl) * a.ldk + (size_t)kv * d, lane, d, a.vec, kvf);
+  const bf16_t* own = dk_role ? (const bf16_t*)a.v + (seq + k0) * a.ldv : (const bf16_t*)a.k + (seq + k0) * a.ldk;
+  const size_t ldo = dk_role ? a.ldv : a.ldk;
+  load_row<D, VEC>(rows_at(own + (size_t)kv * d, row_bytes(WG_ROWS, S - k0, ldo, d)), (uint32_t)((32 * kg + (lane & 31)) * ldo) * 2, lane, d, kvf);
   f32x16 acc[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
 
-  Tile<BLK, D, NTHR_DKV, EXACT> qr, dor;
-  qr.init(a.ldq, tid, d, a.vec);
-  dor.init(a.ldo, tid, d, a.vec);
+  Tile<BLK, D, NTHR_DKV, VEC> qr, dor;
+  qr.init(a.ldq, tid, d);
+  dor.init(a.ldo, tid, d);
   bool bad = false;
   float lnext = 0.f, dnext = 0.f;
   int2 snext = make_int2(0, 0);
@@ -600,8 +613,8 @@ __device__ __forceinline__ bool dkv_keys(const MaskedArgs& a, DkvShared<D>& sh) 
   int fh = 0, fj = jbeg;  // of the next fetch
   auto fetch = [&]() {
     const int head = head0 + fh;
-    qr.fetch((const bf16_t*)a.q + (seq + (size_t)fj * BLK) * a.ldq + (size_t)head * d, a.ldq, S - fj * BLK, d, a.vec);
-    dor.fetch((const bf16_t*)a.dctx + (seq + (size_t)fj * BLK) * a.ldo + (size_t)head * d, a.ldo, S - fj * BLK, d, a.vec);
+    qr.fetch((const bf16_t*)a.q + (seq + (size_t)fj * BLK) * a.ldq + (size_t)head * d, a.ldq, S - fj * BLK, d);
+    dor.fetch((const bf16_t*)a.dctx + (seq + (size_t)fj * BLK) * a.ldo + (size_t)head * d, a.ldo, S - fj * BLK, d);
     if (tid < BLK) {
       const int i = fj * BLK + tid;
       const size_t st = ((size_t)b * a.N_heads + head) * S + i;
@@ -742,9 +755,9 @@ __device__ __forceinline__ bool dkv_keys(const MaskedArgs& a, DkvShared<D>& sh) 
     __syncthreads();
   }
   if (!SEEN && __syncthreads_or(bad)) return true;
-  if (key >= S) return false;
   const float mul = dk_role ? a.scale : 1.f;
   if (a.splits > 1) {
+    if (key >= S) return false;
     // this share's plane: [split][dk, dv][token][key / value head][d]
     const size_t width = (size_t)a.N_kv * d, plane = (size_t)a.S_mb * S * width;
     float* out = a.planes + (2 * (size_t)split + (dk_role ? 0 : 1)) * plane + (seq + key) * width + (size_t)kv * d;
@@ -753,24 +766,25 @@ __device__ __forceinline__ bool dkv_keys(const MaskedArgs& a, DkvShared<D>& sh) 
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int c = dt * 32 + acc_row(r, lane);
-        if (EXACT || c < d) out[c] = acc[dt][r] * mul;
+        if (c < d) out[c] = acc[dt][r] * mul;
       }
     return false;
   }
-  bf16_t* out = dk_role ? (bf16_t*)a.dk + (seq + key) * a.ldk + (size_t)kv * d : (bf16_t*)a.dv + (seq + key) * a.ldv + (size_t)kv * d;
-  store_row<D, EXACT>(acc, out, lane, mul, d, a.vec);
+  bf16_t* out = dk_role ? (bf16_t*)a.dk + (seq + k0) * a.ldk : (bf16_t*)a.dv + (seq + k0) * a.ldv;
+  const size_t ldg = dk_role ? a.ldk : a.ldv;
+  store_row<D, VEC>(acc, rows_at(out + (size_t)kv * d, row_bytes(WG_ROWS, S - k0, ldg, d)), (uint32_t)((32 * kg + (lane & 31)) * ldg) * 2, lane, mul, d);
   return false;
 }
 
-template <int D, bool EXACT, bool CAP, bool BIAS>
+template <int D, bool VEC, bool CAP, bool BIAS>
 __device__ __attribute__((noinline)) void dkv_keys_seen(MaskedArgs a, DkvShared<D>& sh) {
-  dkv_keys<D, EXACT, CAP, BIAS, true>(a, sh);
+  dkv_keys<D, VEC, CAP, BIAS, true>(a, sh);
 }
 
-template <int D, bool EXACT, bool CAP, bool BIAS>
+template <int D, bool VEC, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NTHR_DKV, 2) void masked_dkv_kernel(MaskedArgs a) {
   __shared__ __attribute__((aligned(16))) DkvShared<D> sh;
-  if (dkv_keys<D, EXACT, CAP, BIAS, false>(a, sh)) dkv_keys_seen<D, EXACT, CAP, BIAS>(a, sh);
+  if (dkv_keys<D, VEC, CAP, BIAS, false>(a, sh)) dkv_keys_seen<D, VEC, CAP, BIAS>(a, sh);
 }
 
 
@@ -795,32 +809,30 @@ bf_status launched() {
 
 inline unsigned query_grid(const MaskedArgs& a, int rows) { return (unsigned)((a.S_seq + rows - 1) / rows) * (unsigned)(a.N_heads * a.S_mb); }
 
-template <int D, bool EXACT, bool CAP, bool BIAS>
+template <int D, bool VEC, bool CAP, bool BIAS>
 void run(const MaskedArgs& a, bool backward, hipStream_t st) {
   constexpr int ROWS = 128;
   if (!backward) {
-    masked_fwd_kernel<D, ROWS, EXACT, CAP, BIAS><<<query_grid(a, ROWS), 2 * ROWS, 0, st>>>(a);
+    masked_fwd_kernel<D, ROWS, VEC, CAP, BIAS><<<query_grid(a, ROWS), 2 * ROWS, 0, st>>>(a);
     return;
   }
-  masked_dq_kernel<D, ROWS, EXACT, CAP, BIAS><<<query_grid(a, ROWS), 2 * ROWS, 0, st>>>(a);
+  masked_dq_kernel<D, ROWS, VEC, CAP, BIAS><<<query_grid(a, ROWS), 2 * ROWS, 0, st>>>(a);
   const unsigned grid = (unsigned)((a.S_seq + WG_ROWS - 1) / WG_ROWS) * (unsigned)(a.N_kv * a.splits * a.S_mb);
-  masked_dkv_kernel<D, EXACT, CAP, BIAS><<<grid, NTHR_DKV, 0, st>>>(a);
+  masked_dkv_kernel<D, VEC, CAP, BIAS><<<grid, NTHR_DKV, 0, st>>>(a);
   if (a.splits > 1) masked_join_kernel<<<2048, 256, 0, st>>>(a);
 }
 
-template <int D, bool EXACT>
+template <int D, bool VEC>
 void by_score(const MaskedArgs& a, bool backward, hipStream_t st) {
-  if (a.cap > 0.f && a.slope) run<D, EXACT, true, true>(a, backward, st);
-  else if (a.cap > 0.f) run<D, EXACT, true, false>(a, backward, st);
-  else if (a.slope) run<D, EXACT, false, true>(a, backward, st);
-  else run<D, EXACT, false, false>(a, backward, st);
+  if (a.cap > 0.f && a.slope) run<D, VEC, true, true>(a, backward, st);
+  else if (a.cap > 0.f) run<D, VEC, true, false>(a, backward, st);
+  else if (a.slope) run<D, VEC, false, true>(a, backward, st);
+  else run<D, VEC, false, false>(a, backward, st);
 }
 
 bf_status by_head(const MaskedArgs& a, bool backward, hipStream_t st) {
-  if (a.vec && a.S_head == 64) by_score<64, true>(a, backward, st);
-  else if (a.vec && a.S_head == 128) by_score<128, true>(a, backward, st);
-  else if (a.S_head <= 64) by_score<64, false>(a, backward, st);
-  else by_score<128, false>(a, backward, st);
+  if (a.S_head <= 64) a.vec ? by_score<64, true>(a, backward, st) : by_score<64, false>(a, backward, st);
+  else a.vec ? by_score<128, true>(a, backward, st) : by_score<128, false>(a, backward, st);
   return launched();
 }
 
