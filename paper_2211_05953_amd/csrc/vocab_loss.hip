@@ -199,7 +199,7 @@ Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool ba
   p.unit = 8;
   if (matrix) {
     // whole rounds of tiles and a rest: 2048 x 2048 x 50304 in pieces of 25600 (3.1 rounds of 256 x 256) and of 24576 (3), us for logits and dw of
-    // one: 250 + 429 and UNIT_FIGURE
+    // one: 250 + 429 and 208 + 350
     const int round = gemm_mfma_logits_round(rows, h);
     if (!piece && round) {
       if (!backward) cols = (size_t)V;  // the forward product keeps nothing
