@@ -37,25 +37,34 @@ __device__ __forceinline__ f32x16 zero16() {
   return z;
 }
 
-// Tiles through a buffer descriptor that ends with the last row there is; what lies past it, or past a short row, reads as zeros.
-template <int D, int NT>
+// Rows go through buffer descriptors that end with the last row there is: what lies past it, or past a short row, reads as zeros and
+// is not written, without branches (a short launch waits for its instructions).  VEC: rows of whole 16-byte chunks that start at
+// multiples of 4 bytes; else element by element.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void* g, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)g, 0, (int)bytes, 0x00020000);
+}
+// bytes of up to 32 rows, those that are there of them
+__device__ __forceinline__ uint32_t row_bytes(int there, size_t ld, int d) {
+  return there < 1 ? 0 : (uint32_t)(((there < 32 ? there : 32) - 1) * ld + d) * 4;
+}
+
+template <int D, int NT, bool VEC>
 struct Tile {
   static constexpr int CH = BLK * D / 4 / NT, STEP = NT / (D / 4);
   u32x4 v[CH];
   uint32_t off;
   int col;
-  __device__ __forceinline__ void init(size_t ld, int tid, int d, bool vec) {
+  __device__ __forceinline__ void init(size_t ld, int tid, int d) {
     col = tid % (D / 4) * 4;
     off = (uint32_t)(tid / (D / 4) * ld + col) * 4;
-    if (vec && col >= d) off = NOWHERE;
+    if (VEC && col >= d) off = NOWHERE;
   }
-  __device__ __forceinline__ void fetch(const float* __restrict__ g, size_t ld, int valid, int d, bool vec) {
-    const uint32_t bytes = (uint32_t)(((valid < BLK ? valid : BLK) - 1) * ld + d) * 4;
-    __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)g, 0, (int)bytes, 0x00020000);
+  __device__ __forceinline__ void fetch(const float* __restrict__ g, size_t ld, int valid, int d) {
+    const auto rsrc = rows_at(g, row_bytes(valid, ld, d));
     const uint32_t step = (uint32_t)(STEP * ld * 4);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      if (vec) {
+      if (VEC) {
         v[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off + i * step, 0, 0);
       } else {
 #pragma unroll
@@ -77,37 +86,37 @@ struct Tile {
   }
 };
 
-// a token's row as the operand of a contraction over head dimensions
-template <int D>
-__device__ __forceinline__ void load_row(const float* __restrict__ row, int lane, int d, bool vec, f32x4 (&f)[D / 8]) {
+// A token's row as the operand of a contraction over head dimensions.  rows: the wave's 32 (uniform); off: the lane's
+template <int D, bool VEC>
+__device__ __forceinline__ void load_row(__amdgpu_buffer_rsrc_t rows, uint32_t off, int lane, int d, f32x4 (&f)[D / 8]) {
 #pragma unroll
   for (int c = 0; c < D / 8; ++c) {
     const int at = 8 * c + 4 * (lane >> 5);
-    if (vec && at < d) {
-      f[c] = *reinterpret_cast<const f32x4*>(row + at);
+    if (VEC) {
+      f[c] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at < d ? off + 4 * at : NOWHERE, 0, 0));
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f[c][e] = at + e < d ? row[at + e] : 0.f;
+      for (int e = 0; e < 4; ++e) f[c][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rows, at + e < d ? off + 4 * (at + e) : NOWHERE, 0, 0));
     }
   }
 }
 
-template <int D>
-__device__ __forceinline__ void store_row(const f32x16 (&acc)[D / 32], float* __restrict__ row, int lane, float mul, int d, bool vec) {
+template <int D, bool VEC>
+__device__ __forceinline__ void store_row(const f32x16 (&acc)[D / 32], __amdgpu_buffer_rsrc_t rows, uint32_t off, int lane, float mul, int d) {
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int q4 = 0; q4 < 4; ++q4) {
       const int c = dt * 32 + q4 * 8 + (lane >> 5) * 4;
-      if (vec && c < d) {
-        f32x4 o;
+      f32x4 o;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = acc[dt][q4 * 4 + e] * mul;
-        *reinterpret_cast<f32x4*>(row + c) = o;
+      for (int e = 0; e < 4; ++e) o[e] = acc[dt][q4 * 4 + e] * mul;
+      const u32x4 u = __builtin_bit_cast(u32x4, o);
+      if (VEC) {
+        __builtin_amdgcn_raw_buffer_store_b128(u, rows, c < d ? off + 4 * c : NOWHERE, 0, 0);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (c + e < d) row[c + e] = acc[dt][q4 * 4 + e] * mul;
+        for (int e = 0; e < 4; ++e) __builtin_amdgcn_raw_buffer_store_b32(u[e], rows, c + e < d ? off + 4 * (c + e) : NOWHERE, 0, 0);
       }
     }
 }
@@ -175,8 +184,9 @@ __device__ __forceinline__ float tanh_f(float x) {
   return y < 0.55f ? near : copysignf(fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f), x);
 }
 
-// a score from a dot product; slack: the cap's derivative there
-template <bool CAP, bool BIAS>
+// a score from a dot product; slack: the cap's derivative there.  (slope 0: no bias; not worth kernels of its own, 2 operations beside
+// 64 cycles of the matrix core for each of a dot product's pairs of dimensions)
+template <bool CAP>
 __device__ __forceinline__ float score_of(float dot, float dist, const MaskedArgs& a, float inv_cap, float slope, float& slack) {
   float s = dot * a.scale;
   if (CAP) {
@@ -184,8 +194,7 @@ __device__ __forceinline__ float score_of(float dot, float dist, const MaskedArg
     s = a.cap * t;
     slack = 1.f - t * t;
   }
-  if (BIAS) s = fmaf(-slope, fabsf(dist), s);
-  return s;
+  return fmaf(-slope, fabsf(dist), s);
 }
 
 struct WaveSpan {
@@ -223,24 +232,27 @@ struct QueryShared {
 
 // Forward (GRAD false) and dQ (GRAD true).  SEEN: tiles that are masked in part by sums_seen; without it returns whether one of
 // those held a non-finite value that enters a sum.
-template <int D, int KG, bool CAP, bool BIAS, bool GRAD, bool SEEN>
+template <int D, int KG, bool VEC, bool CAP, bool GRAD, bool SEEN>
 __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D, KG>& sh) {
   constexpr int NT = KG == 1 ? 256 : 64, RB = KG == 1 ? ROWS : 32;  // threads that fetch a tile, rows of the workgroup
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, wr = KG == 1 ? w : 0, ft = KG == 1 ? tid : lane;
   const int S = a.S_seq, d = a.S_head, nhb = a.N_heads * a.S_mb, blocks = (S + RB - 1) / RB, group = a.N_heads / a.N_kv;
   const int x = blockIdx.x % nhb, hx = x % a.N_heads, b = x / a.N_heads, kv = hx % a.N_kv, head = kv * group + hx / a.N_kv;
   const int q0 = (blocks - 1 - blockIdx.x / nhb) * RB, q = q0 + 32 * wr + (lane & 31), ql = min(q, S - 1);
-  const size_t seq = (size_t)b * S, st = ((size_t)b * a.N_heads + head) * S + ql, orow = (seq + ql) * a.ldo + (size_t)head * d;
+  const size_t seq = (size_t)b * S, st = ((size_t)b * a.N_heads + head) * S + ql;
   const float* kbase = (const float*)a.k + seq * a.ldk + (size_t)kv * d;
   const float* vbase = (const float*)a.v + seq * a.ldv + (size_t)kv * d;
 
   f32x4 qf[D / 8], dof[GRAD ? D / 8 : 1];
-  load_row<D>((const float*)a.q + (seq + ql) * a.ldq + (size_t)head * d, lane, d, a.vec, qf);
+  const int w0 = q0 + 32 * wr;  // the wave's first row
+  const auto rows_of = [&](const void* t, size_t ld) { return rows_at((const float*)t + (seq + w0) * ld + (size_t)head * d, row_bytes(S - w0, ld, d)); };
+  const uint32_t qat = (uint32_t)((lane & 31) * a.ldq) * 4, oat = (uint32_t)((lane & 31) * a.ldo) * 4;
+  load_row<D, VEC>(rows_of(a.q, a.ldq), qat, lane, d, qf);
   float lse = 0.f, dl = 0.f;
   if constexpr (GRAD) {
-    load_row<D>((const float*)a.dctx + orow, lane, d, a.vec, dof);
+    load_row<D, VEC>(rows_of(a.dctx, a.ldo), oat, lane, d, dof);
     f32x4 cf[D / 8];
-    load_row<D>((const float*)a.ctx + orow, lane, d, a.vec, cf);
+    load_row<D, VEC>(rows_of(a.ctx, a.ldo), oat, lane, d, cf);
 #pragma unroll
     for (int c = 0; c < D / 8; ++c)
 #pragma unroll
@@ -263,20 +275,20 @@ __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D, K
     wg = {min(wg.lo_min, y.lo_min), max(wg.hi_max, y.hi_max), max(wg.lo_max, y.lo_max), min(wg.hi_min, y.hi_min)};
   }
   wg.hi_max = min(wg.hi_max, S);
-  const float slope = BIAS ? a.slope[head] : 0.f, inv_cap = CAP ? 1.f / a.cap : 0.f;
+  const float slope = a.slope ? a.slope[head] : 0.f, inv_cap = CAP ? 1.f / a.cap : 0.f;
   f32x16 o[D / 32];  // ctx, or dQ; transposed: rows = head dims, column = the lane's query
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) o[dt] = zero16();
   float m = -FLT_MAX, l = 0.f;
 
   const int jbeg = wg.hi_max > 0 ? max(wg.lo_min, 0) / BLK : 0, jend = (wg.hi_max + BLK - 1) / BLK;
-  Tile<D, NT> kr, vr;
-  kr.init(a.ldk, ft, d, a.vec);
-  vr.init(a.ldv, ft, d, a.vec);
+  Tile<D, NT, VEC> kr, vr;
+  kr.init(a.ldk, ft, d);
+  vr.init(a.ldv, ft, d);
   bool bad = false;
   auto fetch = [&](int j) {
-    kr.fetch(kbase + (size_t)j * BLK * a.ldk, a.ldk, S - j * BLK, d, a.vec);
-    vr.fetch(vbase + (size_t)j * BLK * a.ldv, a.ldv, S - j * BLK, d, a.vec);
+    kr.fetch(kbase + (size_t)j * BLK * a.ldk, a.ldk, S - j * BLK, d);
+    vr.fetch(vbase + (size_t)j * BLK * a.ldv, a.ldv, S - j * BLK, d);
   };
   auto put = [&](int j, int stage) {
     kr.store(sh.K[stage], ft);
@@ -309,7 +321,7 @@ __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D, K
         float mx = m, slack;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = score_of<CAP, BIAS>(s[r], dist - (float)((r >> 2) * 8 + (r & 3)), a, inv_cap, slope, slack);
+          s[r] = score_of<CAP>(s[r], dist - (float)((r >> 2) * 8 + (r & 3)), a, inv_cap, slope, slack);
           if (part && (unsigned)(acc_row(r, lane) - lo) >= (unsigned)n) s[r] = -INFINITY;
           mx = fmaxf(mx, s[r]);
         }
@@ -336,7 +348,7 @@ __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D, K
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           float slack = 1.f;
-          const float t = score_of<CAP, BIAS>(s[r], dist - (float)((r >> 2) * 8 + (r & 3)), a, inv_cap, slope, slack);
+          const float t = score_of<CAP>(s[r], dist - (float)((r >> 2) * 8 + (r & 3)), a, inv_cap, slope, slack);
           s[r] = __builtin_amdgcn_exp2f((t - lse) * LOG2E) * (dp[r] - dl) * slack;
           if (part && (unsigned)(acc_row(r, lane) - lo) >= (unsigned)n) s[r] = 0.f;
         }
@@ -389,26 +401,26 @@ __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D, K
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt) o[dt] = zero16();
     }
-    store_row<D>(o, (float*)a.dq + (seq + q) * a.ldq + (size_t)head * d, lane, a.scale, d, a.vec);
+    store_row<D, VEC>(o, rows_of(a.dq, a.ldq), qat, lane, a.scale, d);
   } else {
-    store_row<D>(o, (float*)a.ctx + orow, lane, l == 0.f ? 0.f : 1.0f / l, d, a.vec);
+    store_row<D, VEC>(o, rows_of(a.ctx, a.ldo), oat, lane, l == 0.f ? 0.f : 1.0f / l, d);
     if (lane < 32 && a.lse) a.lse[st] = l == 0.f ? -INFINITY : m + logf(l);
   }
   return false;
 }
 
 // (a function of its own: see attention_masked_mfma.hip)
-template <int D, int KG, bool CAP, bool BIAS, bool GRAD>
+template <int D, int KG, bool VEC, bool CAP, bool GRAD>
 __device__ __attribute__((noinline)) void query_rows_seen(MaskedArgs a, QueryShared<D, KG>& sh) {
-  query_rows<D, KG, CAP, BIAS, GRAD, true>(a, sh);
+  query_rows<D, KG, VEC, CAP, GRAD, true>(a, sh);
 }
 
-template <int D, int KG, bool CAP, bool BIAS, bool GRAD>
+template <int D, int KG, bool VEC, bool CAP, bool GRAD>
 __global__ __launch_bounds__(256, KG == 1 ? 2 : 1) void masked_query_f32_kernel(MaskedArgs a) {
   __shared__ __attribute__((aligned(16))) QueryShared<D, KG> sh;
-  if (query_rows<D, KG, CAP, BIAS, GRAD, false>(a, sh)) {
+  if (query_rows<D, KG, VEC, CAP, GRAD, false>(a, sh)) {
     __syncthreads();
-    query_rows_seen<D, KG, CAP, BIAS, GRAD>(a, sh);
+    query_rows_seen<D, KG, VEC, CAP, GRAD>(a, sh);
   }
 }
 
@@ -426,7 +438,7 @@ struct KeyShared {
   int range[2];
 };
 
-template <int D, int QG, bool CAP, bool BIAS, bool SEEN>
+template <int D, int QG, bool VEC, bool CAP, bool SEEN>
 __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D, QG>& sh) {
   constexpr int KB = QG == 1 ? ROWS : 32, NT = NTHR_DKV / QG;  // keys of the workgroup, threads that fetch a tile
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, pair = w & 3;
@@ -436,7 +448,7 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D, QG>& 
   const int per = a.N_kv * a.splits * a.S_mb, x = blockIdx.x % per, k0 = blockIdx.x / per * KB;
   const int kv = x % a.N_kv, split = x / a.N_kv % a.splits, b = x / (a.N_kv * a.splits);
   const size_t seq = (size_t)b * S;
-  const int kw = k0 + 32 * kg, key = kw + (lane & 31), kl = min(key, S - 1);
+  const int kw = k0 + 32 * kg, key = kw + (lane & 31);
   const int blocks = (S + SPAN_ROWS - 1) / SPAN_ROWS;
   const SpanBlock* tb = a.block + (size_t)b * blocks;
   if (tid < 2) sh.range[tid] = tid ? 0 : INT_MAX;
@@ -451,14 +463,15 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D, QG>& 
   const int tiles = jend > jbeg ? jend - jbeg : 0, total = tiles * heads, head0 = kv * group + split * heads;
 
   f32x4 kvf[D / 8];  // this wave's K rows (dV role) or V rows (dK role)
-  if (dk_role) load_row<D>((const float*)a.v + (seq + kl) * a.ldv + (size_t)kv * d, lane, d, a.vec, kvf);
-  else load_row<D>((const float*)a.k + (seq + kl) * a.ldk + (size_t)kv * d, lane, d, a.vec, kvf);
+  const size_t ldkv = dk_role ? a.ldv : a.ldk;
+  load_row<D, VEC>(rows_at((const float*)(dk_role ? a.v : a.k) + (seq + kw) * ldkv + (size_t)kv * d, row_bytes(S - kw, ldkv, d)),
+                   (uint32_t)((lane & 31) * ldkv) * 4, lane, d, kvf);
   f32x16 acc[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
-  Tile<D, NT> qr, dor;
-  qr.init(a.ldq, ft, d, a.vec);
-  dor.init(a.ldo, ft, d, a.vec);
+  Tile<D, NT, VEC> qr, dor;
+  qr.init(a.ldq, ft, d);
+  dor.init(a.ldo, ft, d);
   bool bad = false;
   float lnext = 0.f, dnext = 0.f;
   int2 snext = make_int2(0, 0);
@@ -466,8 +479,8 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D, QG>& 
   auto fetch = [&](int it) {
     if (it >= total) return;
     const int fj = jbeg + it % tiles, head = head0 + it / tiles;
-    qr.fetch((const float*)a.q + (seq + (size_t)fj * BLK) * a.ldq + (size_t)head * d, a.ldq, S - fj * BLK, d, a.vec);
-    dor.fetch((const float*)a.dctx + (seq + (size_t)fj * BLK) * a.ldo + (size_t)head * d, a.ldo, S - fj * BLK, d, a.vec);
+    qr.fetch((const float*)a.q + (seq + (size_t)fj * BLK) * a.ldq + (size_t)head * d, a.ldq, S - fj * BLK, d);
+    dor.fetch((const float*)a.dctx + (seq + (size_t)fj * BLK) * a.ldo + (size_t)head * d, a.ldo, S - fj * BLK, d);
     if (ft < BLK) {
       const int i = fj * BLK + ft;
       const size_t st = ((size_t)b * a.N_heads + head) * S + i;
@@ -501,7 +514,7 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D, QG>& 
     const int it = step + grp, cur = QG == 1 ? it & 1 : grp;
     const bool there = it < total;
     const int j = jbeg + (there ? it % tiles : 0), qb = j * BLK;
-    const float slope = BIAS && there ? a.slope[head0 + it / tiles] : 0.f;
+    const float slope = a.slope && there ? a.slope[head0 + it / tiles] : 0.f;
     fetch(it + QG);
     const SpanBlock y = tb[j >> 1];
     const bool skip = !there || kw >= S || y.hi_max <= kw || y.lo_min >= kw + 32;
@@ -521,7 +534,7 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D, QG>& 
           for (int e = 0; e < 4; ++e) {
             const int r = 4 * q4 + e;
             float slack = 1.f;
-            const float t = score_of<CAP, BIAS>(s[r], dist + (float)(8 * q4 + e), a, inv_cap, slope, slack);
+            const float t = score_of<CAP>(s[r], dist + (float)(8 * q4 + e), a, inv_cap, slope, slack);
             s[r] = __builtin_amdgcn_exp2f((t - ls[e]) * LOG2E);
             give[e] = s[r] * slack;
             if (part && (key < lo_s[acc_row(r, lane)] || key >= hi_s[acc_row(r, lane)])) s[r] = 0.f;
@@ -583,30 +596,25 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D, QG>& 
         for (int r = 0; r < 16; ++r) acc[dt][r] += from[(dt * 16 + r) * 64];
     }
   }
-  if (key >= S) return false;
-  const float mul = dk_role ? a.scale : 1.f;
-  if (a.splits > 1) {
-    // this share's plane: [split][dk, dv][token][key / value head][d]
-    const size_t width = (size_t)a.N_kv * d, plane = (size_t)a.S_mb * S * width;
-    float* out = a.planes + (2 * (size_t)split + (dk_role ? 0 : 1)) * plane + (seq + key) * width + (size_t)kv * d;
-    store_row<D>(acc, out, lane, mul, d, d % 4 == 0);
-    return false;
-  }
-  store_row<D>(acc, dk_role ? (float*)a.dk + (seq + key) * a.ldk + (size_t)kv * d : (float*)a.dv + (seq + key) * a.ldv + (size_t)kv * d, lane, mul, d, a.vec);
+  // a share of several: its plane, [split][dk, dv][token][key / value head][d]
+  const size_t width = (size_t)a.N_kv * d, plane = (size_t)a.S_mb * S * width, ldg = a.splits > 1 ? width : dk_role ? a.ldk : a.ldv;
+  float* out = a.splits > 1 ? a.planes + (2 * (size_t)split + (dk_role ? 0 : 1)) * plane : (float*)(dk_role ? a.dk : a.dv);
+  store_row<D, VEC>(acc, rows_at(out + (seq + kw) * ldg + (size_t)kv * d, row_bytes(S - kw, ldg, d)), (uint32_t)((lane & 31) * ldg) * 4, lane,
+                    dk_role ? a.scale : 1.f, d);
   return false;
 }
 
-template <int D, int QG, bool CAP, bool BIAS>
+template <int D, int QG, bool VEC, bool CAP>
 __device__ __attribute__((noinline)) void key_rows_seen(MaskedArgs a, KeyShared<D, QG>& sh) {
-  key_rows<D, QG, CAP, BIAS, true>(a, sh);
+  key_rows<D, QG, VEC, CAP, true>(a, sh);
 }
 
-template <int D, int QG, bool CAP, bool BIAS>
+template <int D, int QG, bool VEC, bool CAP>
 __global__ __launch_bounds__(NTHR_DKV, 2) void masked_key_f32_kernel(MaskedArgs a) {
   __shared__ __attribute__((aligned(16))) KeyShared<D, QG> sh;
-  if (key_rows<D, QG, CAP, BIAS, false>(a, sh)) {
+  if (key_rows<D, QG, VEC, CAP, false>(a, sh)) {
     __syncthreads();
-    key_rows_seen<D, QG, CAP, BIAS>(a, sh);
+    key_rows_seen<D, QG, VEC, CAP>(a, sh);
   }
 }
 
@@ -625,34 +633,32 @@ __global__ __launch_bounds__(256) void masked_join_f32_kernel(MaskedArgs a) {
 // Workgroups of 128 rows below which the rows' keys (the keys' queries) are shared out over the waves instead
 constexpr unsigned FEW = 192;
 
-template <int D, bool CAP, bool BIAS, bool GRAD>
+template <int D, bool VEC, bool CAP, bool GRAD>
 void query(const MaskedArgs& a, hipStream_t st) {
   const unsigned hb = (unsigned)(a.N_heads * a.S_mb), grid = (unsigned)((a.S_seq + ROWS - 1) / ROWS) * hb;
-  if (grid < FEW) masked_query_f32_kernel<D, 4, CAP, BIAS, GRAD><<<(unsigned)((a.S_seq + 31) / 32) * hb, 256, 0, st>>>(a);
-  else masked_query_f32_kernel<D, 1, CAP, BIAS, GRAD><<<grid, 256, 0, st>>>(a);
+  if (grid < FEW) masked_query_f32_kernel<D, 4, VEC, CAP, GRAD><<<(unsigned)((a.S_seq + 31) / 32) * hb, 256, 0, st>>>(a);
+  else masked_query_f32_kernel<D, 1, VEC, CAP, GRAD><<<grid, 256, 0, st>>>(a);
 }
 
-template <int D, bool CAP, bool BIAS>
+template <int D, bool VEC, bool CAP>
 void run(const MaskedArgs& a, bool backward, hipStream_t st) {
-  if (!backward) { query<D, CAP, BIAS, false>(a, st); return; }
-  query<D, CAP, BIAS, true>(a, st);
+  if (!backward) { query<D, VEC, CAP, false>(a, st); return; }
+  query<D, VEC, CAP, true>(a, st);
   const unsigned hb = (unsigned)(a.N_kv * a.splits * a.S_mb), grid = (unsigned)((a.S_seq + ROWS - 1) / ROWS) * hb;
-  if (grid < FEW) masked_key_f32_kernel<D, 4, CAP, BIAS><<<(unsigned)((a.S_seq + 31) / 32) * hb, NTHR_DKV, 0, st>>>(a);
-  else masked_key_f32_kernel<D, 1, CAP, BIAS><<<grid, NTHR_DKV, 0, st>>>(a);
+  if (grid < FEW) masked_key_f32_kernel<D, 4, VEC, CAP><<<(unsigned)((a.S_seq + 31) / 32) * hb, NTHR_DKV, 0, st>>>(a);
+  else masked_key_f32_kernel<D, 1, VEC, CAP><<<grid, NTHR_DKV, 0, st>>>(a);
   if (a.splits > 1) masked_join_f32_kernel<<<2048, 256, 0, st>>>(a);
 }
 
-template <int D>
+template <int D, bool VEC>
 void by_score(const MaskedArgs& a, bool backward, hipStream_t st) {
-  if (a.cap > 0.f && a.slope) run<D, true, true>(a, backward, st);
-  else if (a.cap > 0.f) run<D, true, false>(a, backward, st);
-  else if (a.slope) run<D, false, true>(a, backward, st);
-  else run<D, false, false>(a, backward, st);
+  if (a.cap > 0.f) run<D, VEC, true>(a, backward, st);
+  else run<D, VEC, false>(a, backward, st);
 }
 
 bf_status both(const MaskedArgs& a, bool backward, hipStream_t st) {
-  if (a.S_head <= 64) by_score<64>(a, backward, st);
-  else by_score<128>(a, backward, st);
+  if (a.S_head <= 64) a.vec ? by_score<64, true>(a, backward, st) : by_score<64, false>(a, backward, st);
+  else a.vec ? by_score<128, true>(a, backward, st) : by_score<128, false>(a, backward, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_error("attention_masked_f32: launch failed: %s", hipGetErrorString(e)); return BF_EDEVICE; }
   return BF_OK;
