@@ -155,10 +155,11 @@ __global__ __launch_bounds__(NT) void piece_dz_kernel(int cols, float* __restric
 // ---- sizes ---------------------------------------------------------------------------------------
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;  // of dz: what the memory-side cache holds, and little beside 288 GB
 
-// dz's parts, as many as it takes for what they drop (1.4e-6 of dz with two) to stay under the fp32 error of the logits, which grows with the
-// root of their length: 5e-7 of dz at S_hidden 256, 1e-6 at 2048, 1.8e-6 at 8192 (dw at 2048: 1.5e-6 off with two parts, 1e-6 with three).  Up to 64 rows dW's product is the writing of dW,
-// and the third part costs nothing.
-inline int parts_of(int rows, int h) { return rows <= 64 || h < 4096 ? 3 : 2; }
+// dz's parts, as many as it takes for what they drop (1.4e-6 of dz with two) to stay under the fp32 error of the logits, which grows with
+// their length: 5e-7 of dz at S_hidden 256, 1e-6 at 2048 and, in short sums, at 4184, 1.8e-6 at 8192 (dw at 2048: 1.5e-6 off with two
+// parts, 1e-6 with three; the third costs a sixth of 2048 rows' gradient).  Up to some 200 rows dW's product is the writing of dW, and the
+// third part costs nothing.
+inline int parts_of(int rows, int h) { return rows <= 256 || h < 8192 ? 3 : 2; }
 
 // dy is stored in bf16, one rounding more than its product's operand.  Of few rows the largest of their dz, the label's, may fall where
 // bf16 is coarsest for all of them (one row: 2.6e-3 off in the 2-norm, a rounding alone 1.7e-3); a second part costs little
