@@ -319,9 +319,12 @@ bool chunks(const bf_attn_config& c, const MaskedArgs& a, uintptr_t al) {
   return (al & 3) == 0 && a.S_head % 8 == 0 && ((a.ldq | a.ldk | a.ldv | a.ldo) & 1) == 0;
 }
 
-// the matrix-core kernels: heads up to 128, and 32-bit offsets into a tile of 64 rows
+// The matrix-core kernels: heads up to 128, and 32-bit offsets into a tile of 64 rows.  Not up to four tokens without shared heads, where
+// the plain kernels are faster (forward and backward in bf16, heads of 128, us: 4 x 16 of 4 tokens 35 against 40, 256 x 16 214 against
+// 299; of 8 39 against 39 and 491 against 307) and keep dS, which sums of one or two terms would round in full view, in fp32.
 bool matrix(const bf_attn_config& c) {
   const int64_t far = 1 << 22;
+  if (c.S_seq <= 4 && c.N_heads == c.N_kv_heads) return false;
   return c.kernels == BF_KERNELS_AUTO && c.S_head <= 128 && c.ld_q <= far && c.ld_k <= far && c.ld_v <= far && c.ld_ctx <= far &&
          (int64_t)c.N_heads * c.S_head <= far;
 }
