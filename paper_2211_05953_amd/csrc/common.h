@@ -39,6 +39,7 @@ struct LogitArgs {
   int col0 = 0;                    // the vocabulary's column that the product's column 0 is
   int S_voc = 0;
   int parts = 0;                   // E_DLOGITS: bf16 parts, plane elements apart
+  int unscaled = 0;                // and behind them a plane without the scale, in one part
   size_t plane = 0;
   int ldc = 0;                     // row length of a plane, a multiple of 8 (columns past N are written as zeros)
 };

@@ -251,12 +251,16 @@ __device__ __forceinline__ void logit_epilogue(const float (&v)[8], size_t row, 
     const bool known = label >= 0 && label < lg.S_voc;
     const float lse = lg.lse[row];
     float d[8];
+    bf16_t* out = reinterpret_cast<bf16_t*>(C) + row * (size_t)lg.ldc + col;
+    bf16x8 one;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float p = __builtin_amdgcn_exp2f((v[e] - lse) * LOG2E) - (at == e ? 1.f : 0.f);
-      d[e] = known && col + e < N ? p * lg.scale : 0.f;
+      d[e] = known && col + e < N ? p : 0.f;
+      one[e] = (__bf16)d[e];
+      d[e] *= lg.scale;
     }
-    bf16_t* out = reinterpret_cast<bf16_t*>(C) + row * (size_t)lg.ldc + col;
+    if (lg.unscaled) *reinterpret_cast<bf16x8*>(out + lg.parts * lg.plane) = one;
     for (int k = 0; k < lg.parts; ++k, out += lg.plane) {
       bf16x8 o;
 #pragma unroll

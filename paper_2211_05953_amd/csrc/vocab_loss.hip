@@ -164,7 +164,26 @@ inline int parts_of(int rows, int h) { return rows <= 256 || h < 8192 ? 3 : 2; }
 // dy is stored in bf16, one rounding more than its product's operand.  Of few rows the largest of their dz, the label's, may fall where
 // bf16 is coarsest for all of them (one row: 2.6e-3 off in the 2-norm, a rounding alone 1.7e-3); a second part costs little
 // where reading w bounds the product.
+// One part is taken without the scale, which enters with dy's rounding: a label of small probability is then -1, whose rounding is none, and not
+// -scale, whose rounding all rows share (1720 rows of 64: 2.8e-3 off, 2.0e-3 so).  Its plane costs 2 to 4 % of the gradient.
 inline int dy_parts_of(int rows) { return rows <= 256 ? 2 : 1; }
+inline int planes_of(int rows, int h) { return parts_of(rows, h) + (dy_parts_of(rows) == 1); }
+
+// dy = factor * the sum of its slices' planes, in their order
+__global__ __launch_bounds__(NT) void dy_finish_kernel(size_t n8, int slices, const float4* __restrict__ planes, float factor, bf16_t* __restrict__ dy) {
+  typedef bf16_t V8 __attribute__((vector_size(16)));
+  for (size_t i = (size_t)blockIdx.x * NT + threadIdx.x; i < n8; i += (size_t)gridDim.x * NT) {
+    float4 a = planes[2 * i], b = planes[2 * i + 1];
+    for (int k = 1; k < slices; ++k) {
+      const float4 c = planes[2 * (k * n8 + i)], d = planes[2 * (k * n8 + i) + 1];
+      a.x += c.x; a.y += c.y; a.z += c.z; a.w += c.w;
+      b.x += d.x; b.y += d.y; b.z += d.z; b.w += d.w;
+    }
+    const V8 o = {(bf16_t)(a.x * factor), (bf16_t)(a.y * factor), (bf16_t)(a.z * factor), (bf16_t)(a.w * factor),
+                  (bf16_t)(b.x * factor), (bf16_t)(b.y * factor), (bf16_t)(b.z * factor), (bf16_t)(b.w * factor)};
+    reinterpret_cast<V8*>(dy)[i] = o;
+  }
+}
 
 struct Plan {
   bool matrix;   // bf16 matrix cores, else fp32 products
@@ -192,7 +211,7 @@ int cols_at(const Plan& p, int c0, int V) {
 Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool backward) {
   Plan p{};
   p.matrix = matrix;
-  const size_t per_col = (size_t)rows * (matrix ? 2 * (size_t)parts_of(rows, h) : 4);
+  const size_t per_col = (size_t)rows * (matrix ? 2 * (size_t)planes_of(rows, h) : 4);
   size_t cols = piece ? (size_t)piece : PIECE_BYTES / per_col;
   if (cols < 1024 && !piece) cols = 1024;
   // fp32 dy: a product's sum over the columns is one chain in fp32, so it is cut (50304 columns in one: 1.1e-6 off, 6e-7 cut)
@@ -221,7 +240,7 @@ Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool ba
     if (backward) {
       p.slices = gemm_mfma_logits_dy_slices(rows, p.piece, h);
       p.y = take((size_t)rows * h * 2);
-      p.z = take((size_t)rows * up(cols, 8) * 2 * parts_of(rows, h));
+      p.z = take((size_t)rows * up(cols, 8) * 2 * planes_of(rows, h));
       p.dy = take((size_t)p.slices * rows * h * 4);
     } else {
       size_t tiles = 0;
@@ -340,6 +359,7 @@ bf_status vocab_loss_bwd(int dtype, int rows, int h, int V, int piece, const voi
   if (p.matrix) {
     bf16_t* yc = (bf16_t*)(ws + p.y);
     float* planes = (float*)(ws + p.dy);
+    const bool unscaled = dy_parts_of(rows) == 1;
     labelled_rows16_kernel<<<rows, NT, 0, st>>>(h / 8, (const uint4*)y, label, V, (uint4*)yc);
     s = launched();
     for (int c0 = 0, n; c0 < V && s == BF_OK; c0 += n) {
@@ -351,17 +371,19 @@ bf_status vocab_loss_bwd(int dtype, int rows, int h, int V, int piece, const voi
       l.col0 = c0;
       l.S_voc = V;
       l.parts = parts_of(rows, h);
+      l.unscaled = unscaled;
       l.ldc = (int)up(cols, 8);
       l.plane = (size_t)rows * l.ldc;
       void* dz = ws + p.z;
       const bf16_t* wp = (const bf16_t*)w + (size_t)c0 * h;
       s = gemm_mfma_logits_grad(rows, cols, h, y, wp, l, dz, st);
       if (s == BF_OK) s = gemm_mfma_logits_dw(rows, cols, h, dz, l.ldc, l.parts, l.plane, yc, dw + (size_t)c0 * h, accumulate, st);
-      if (s == BF_OK) s = gemm_mfma_logits_dy(rows, cols, h, dz, l.ldc, dy_parts_of(rows), l.plane, wp, planes, p.slices, c0 > 0, st);
+      if (s == BF_OK) s = gemm_mfma_logits_dy(rows, cols, h, (bf16_t*)dz + (unscaled ? l.parts * l.plane : 0), l.ldc, dy_parts_of(rows), l.plane, wp, planes, p.slices, c0 > 0, st);
     }
     if (s != BF_OK) return s;
-    if (p.slices > 1) return gemm_splitk_finish(E_NONE, rows, h, p.slices, planes, nullptr, nullptr, dy, st);
-    return cast_f32_to_bf16((size_t)rows * h, planes, (bf16_t*)dy, st);
+    const size_t n8 = (size_t)rows * h / 8;
+    dy_finish_kernel<<<grid_for(n8), NT, 0, st>>>(n8, p.slices, (const float4*)planes, unscaled ? scale : 1.f, (bf16_t*)dy);
+    return launched();
   }
   float* yc = (float*)(ws + p.y);
   float* z = (float*)(ws + p.z);
