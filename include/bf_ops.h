@@ -201,8 +201,9 @@ bf_status bf_op_ce_loss(int dtype, int n_rows, int S_voc, void* z, const int32_t
  *   _bwd  from that lse: with dz = (softmax(z) - onehot(label)) * scale,
  *         dy[n_rows, S_hidden] (`dtype`) = dz w_out;  dw[S_voc, S_hidden] (fp32) = (accumulate ? dw : 0) + dz^T y
  * labels: device int32 [n_rows].  A row whose label is outside 0..S_voc-1 has row_loss 0, dy 0 and no part in dw, whatever
- * its y holds.  Sums have a fixed order: no atomics.  bf16 tensors of 16-byte aligned rows (S_hidden % 8 == 0) run on the
- * bf16 matrix cores with logits and statistics in fp32, dw to fp32 precision; fp32 tensors and other rows as fp32 products.
+ * its y holds.  Sums have a fixed order: no atomics.  bf16 tensors run on the
+ * bf16 matrix cores with logits and statistics in fp32, dw to fp32 precision (rows that are not 16-byte aligned, S_hidden % 8 or
+ * tensors that start elsewhere, through copies in the scratch); fp32 tensors as fp32 products.
  * S_piece: columns of a piece (0: the library's choice, 256 MiB of dz); work: device scratch, 256-byte aligned, of
  * bf_op_vocab_loss_work_bytes(..., backward = 0 or 1) bytes (0 for bad sizes), owned by the caller; calls that overlap need
  * their own.  Sizes are 1 to 2^21. */

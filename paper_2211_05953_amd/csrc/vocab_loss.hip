@@ -81,15 +81,12 @@ __global__ __launch_bounds__(1024) void loss_sum_kernel(int rows, const float* _
 }
 
 // dst = src, rows without a label in the vocabulary as zeros
-template <typename TS, typename TD>
-__global__ __launch_bounds__(NT) void labelled_rows_kernel(int h, const TS* __restrict__ src, const int32_t* __restrict__ label, int S_voc,
-                                                           TD* __restrict__ dst) {
+__global__ __launch_bounds__(NT) void labelled_rows_kernel(int h, const float* __restrict__ src, const int32_t* __restrict__ label, int S_voc,
+                                                           float* __restrict__ dst) {
   const size_t row = blockIdx.x;
   const int v = label[row];
   const bool known = v >= 0 && v < S_voc;
-  const TS* s = src + row * (size_t)h;
-  TD* d = dst + row * (size_t)h;
-  for (int c = threadIdx.x; c < h; c += NT) d[c] = known ? (TD)(float)s[c] : (TD)0.f;
+  for (int c = threadIdx.x; c < h; c += NT) dst[row * h + c] = known ? src[row * h + c] : 0.f;
 }
 
 // the same for rows of whole 16-byte chunks of bf16
@@ -101,9 +98,28 @@ __global__ __launch_bounds__(NT) void labelled_rows16_kernel(int chunks, const u
   for (int c = threadIdx.x; c < chunks; c += NT) dst[row * chunks + c] = known ? src[row * chunks + c] : make_uint4(0, 0, 0, 0);
 }
 
-template <typename TS, typename TD>
-__global__ __launch_bounds__(NT) void convert_kernel(size_t n, const TS* __restrict__ src, TD* __restrict__ dst) {
-  for (size_t i = (size_t)blockIdx.x * NT + threadIdx.x; i < n; i += (size_t)gridDim.x * NT) dst[i] = (TD)(float)src[i];
+// rows that are none: lengthened with zeros.  label: as above, or NULL: every row
+typedef bf16_t V8 __attribute__((vector_size(16)));
+__global__ __launch_bounds__(NT) void pad_rows_kernel(size_t n8, int h, int chunks, const bf16_t* __restrict__ src, const int32_t* __restrict__ label,
+                                                      int S_voc, V8* __restrict__ dst) {
+  for (size_t i = (size_t)blockIdx.x * NT + threadIdx.x; i < n8; i += (size_t)gridDim.x * NT) {
+    const size_t row = i / chunks;
+    const int c = (int)(i - row * chunks) * 8;
+    const bool known = !label || (label[row] >= 0 && label[row] < S_voc);
+    V8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = known && c + e < h ? src[row * h + c + e] : (bf16_t)0.f;
+    dst[i] = o;
+  }
+}
+
+// dw = (accumulate ? dw : 0) + a piece of lengthened rows
+__global__ __launch_bounds__(NT) void cut_rows_kernel(size_t n, int h, int ld, const float* __restrict__ src, int accumulate, float* __restrict__ dw) {
+  for (size_t i = (size_t)blockIdx.x * NT + threadIdx.x; i < n; i += (size_t)gridDim.x * NT) {
+    const size_t row = i / h, c = i - row * h;
+    const float v = src[row * ld + c];
+    dw[i] = accumulate ? dw[i] + v : v;
+  }
 }
 
 __global__ __launch_bounds__(NT) void add_kernel(size_t n, const float* __restrict__ src, float* __restrict__ dst) {
@@ -115,7 +131,7 @@ inline unsigned grid_for(size_t n) {
   return (unsigned)(g < 1 ? 1 : g > 4096 ? 4096 : g);
 }
 
-// ---- fp32 logits, a piece at a time (fp32 tensors, and bf16 ones whose rows are not whole 16-byte chunks)
+// ---- fp32 logits, a piece at a time
 // statistics of a row of the piece, merged into what earlier pieces left
 __global__ __launch_bounds__(NT) void piece_lse_kernel(int rows, int cols, const float* __restrict__ z, const int32_t* __restrict__ label, int col0,
                                                        int first, float2* __restrict__ stat, float* __restrict__ at_label) {
@@ -169,9 +185,10 @@ inline int parts_of(int rows, int h) { return rows <= 256 || h < 8192 ? 3 : 2; }
 inline int dy_parts_of(int rows) { return rows <= 256 ? 2 : 1; }
 inline int planes_of(int rows, int h) { return parts_of(rows, h) + (dy_parts_of(rows) == 1); }
 
-// dy = factor * the sum of its slices' planes, in their order
-__global__ __launch_bounds__(NT) void dy_finish_kernel(size_t n8, int slices, const float4* __restrict__ planes, float factor, bf16_t* __restrict__ dy) {
-  typedef bf16_t V8 __attribute__((vector_size(16)));
+// dy = factor * the sum of its slices' planes, in their order, of the h first of a plane's 8 * chunks columns
+template <bool CUT>
+__global__ __launch_bounds__(NT) void dy_finish_kernel(size_t n8, int h, int chunks, int slices, const float4* __restrict__ planes, float factor,
+                                                       bf16_t* __restrict__ dy) {
   for (size_t i = (size_t)blockIdx.x * NT + threadIdx.x; i < n8; i += (size_t)gridDim.x * NT) {
     float4 a = planes[2 * i], b = planes[2 * i + 1];
     for (int k = 1; k < slices; ++k) {
@@ -181,7 +198,15 @@ __global__ __launch_bounds__(NT) void dy_finish_kernel(size_t n8, int slices, co
     }
     const V8 o = {(bf16_t)(a.x * factor), (bf16_t)(a.y * factor), (bf16_t)(a.z * factor), (bf16_t)(a.w * factor),
                   (bf16_t)(b.x * factor), (bf16_t)(b.y * factor), (bf16_t)(b.z * factor), (bf16_t)(b.w * factor)};
-    reinterpret_cast<V8*>(dy)[i] = o;
+    if (!CUT) {
+      reinterpret_cast<V8*>(dy)[i] = o;
+    } else {
+      const size_t row = i / chunks;
+      const int c = (int)(i - row * chunks) * 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e < h) dy[row * h + c + e] = o[e];
+    }
   }
 }
 
@@ -189,8 +214,10 @@ struct Plan {
   bool matrix;   // bf16 matrix cores, else fp32 products
   int piece;     // columns of the largest piece
   int unit;      // pieces are multiples of this, but for the last one
-  // offsets into the scratch: copy of y, fp32 piece of W, z / dz, planes or sums of dy, statistics, labels' logits
-  size_t y, w, z, dy, stat, lab, total;
+  bool pad;      // lengthened rows
+  int h;         // row length of the products
+  // offsets into the scratch: copy of y, lengthened piece of W and its dw, z / dz, planes of dy, statistics (or a piece's dy), labels' logits
+  size_t y, w, dw, z, dy, stat, lab, total;
   int slices;
 };
 
@@ -207,10 +234,15 @@ int cols_at(const Plan& p, int c0, int V) {
   return p.matrix && left > p.unit ? left / p.unit * p.unit : left;
 }
 
-// `matrix` depends on the tensors' alignment too: the scratch is sized for the larger of the two
-Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool backward) {
+// bf16 rows that are not whole 16-byte chunks, or do not start at one, are lengthened: copies of y and of a piece of w, the piece's dw and
+// dy's planes in the scratch (142 rows of 170, 58496 columns, loss and gradient: as fp32 products 1358 us, so 181).  Where the tensors start is not known when the scratch is sized: the larger of the two
+Plan plan_for(bool pad, int dtype, int rows, int h_given, int V, int piece, bool backward) {
   Plan p{};
+  const bool matrix = dtype == BF_BF16;
+  const int h = matrix ? (int)up(h_given, 8) : h_given;
   p.matrix = matrix;
+  p.pad = pad;
+  p.h = h;
   const size_t per_col = (size_t)rows * (matrix ? 2 * (size_t)planes_of(rows, h) : 4);
   size_t cols = piece ? (size_t)piece : PIECE_BYTES / per_col;
   if (cols < 1024 && !piece) cols = 1024;
@@ -231,12 +263,18 @@ Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool ba
     }
     cols = p.unit == 8 ? up(cols, 8) : cols / p.unit * p.unit;
   }
+  if (pad && !piece && cols > PIECE_BYTES / 4 / h) cols = PIECE_BYTES / 4 / h < 1024 ? 1024 : PIECE_BYTES / 4 / h / 8 * 8;
   if (cols > (size_t)V) cols = (size_t)V;
   if (p.unit > 8 && cols >= (size_t)p.unit) cols = cols / p.unit * p.unit;
   p.piece = (int)cols;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes, 256); return o; };
   if (matrix) {
+    if (pad) {
+      p.w = take(cols * h * 2);
+      if (backward) p.dw = take(cols * h * 4);
+      else p.y = take((size_t)rows * h * 2);
+    }
     if (backward) {
       p.slices = gemm_mfma_logits_dy_slices(rows, p.piece, h);
       p.y = take((size_t)rows * h * 2);
@@ -250,11 +288,9 @@ Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool ba
     }
   } else {
     p.y = take((size_t)rows * h * 4);
-    if (dtype == BF_BF16) p.w = take(cols * h * 4);
     p.z = take((size_t)rows * cols * 4);
     if (backward) {
       p.stat = take(p.piece < V ? (size_t)rows * h * 4 : 0);  // a later piece's share of dy
-      if (dtype == BF_BF16) p.dy = take((size_t)rows * h * 4);
     } else {
       p.stat = take((size_t)rows * 8);
       p.lab = take((size_t)rows * 4);
@@ -264,11 +300,9 @@ Plan plan_for(bool matrix, int dtype, int rows, int h, int V, int piece, bool ba
   return p;
 }
 
-bool matrix_possible(int dtype, int rows, int h, int V) { return dtype == BF_BF16 && gemm_mfma_logits_supported(rows, V, h); }
-
-// fp32 y and W piece of the fp32 products
-bf_status widen(int dtype, size_t n, const void* src, float* dst, hipStream_t st) {
-  if (dtype == BF_BF16) convert_kernel<bf16_t, float><<<grid_for(n), NT, 0, st>>>(n, (const bf16_t*)src, dst);
+bf_status pad_rows(size_t n, int h, int h8, const bf16_t* src, const int32_t* label, int V, void* dst, hipStream_t st) {
+  const size_t n8 = n * (h8 / 8);
+  pad_rows_kernel<<<grid_for(n8), NT, 0, st>>>(n8, h, h8 / 8, src, label, V, (V8*)dst);
   return launched();
 }
 
@@ -279,7 +313,7 @@ bf_status product(int layout, int epi, GemmArgs a, hipStream_t st) { return gemm
 size_t vocab_loss_work_bytes(int dtype, int rows, int h, int V, int piece, int backward) {
   if (!sizes_ok(dtype, rows, h, V, piece)) return 0;
   size_t n = plan_for(false, dtype, rows, h, V, piece, backward != 0).total;
-  if (matrix_possible(dtype, rows, h, V)) {
+  if (dtype == BF_BF16) {
     const size_t m = plan_for(true, dtype, rows, h, V, piece, backward != 0).total;
     n = n > m ? n : m;
   }
@@ -300,7 +334,7 @@ bf_status vocab_loss_fwd(int dtype, int rows, int h, int V, int piece, const voi
                          float* row_loss, float* loss, void* work, size_t work_bytes, hipStream_t st) {
   bf_status s = check_args("bf_op_vocab_loss_fwd", dtype, rows, h, V, piece, y, w, label, lse, row_loss, loss, scale, work, work_bytes, 0);
   if (s != BF_OK) return s;
-  const Plan p = plan_for(matrix_possible(dtype, rows, h, V) && aligned16(y) && aligned16(w), dtype, rows, h, V, piece, false);
+  const Plan p = plan_for(h % 8 || !aligned16(y) || !aligned16(w), dtype, rows, h, V, piece, false);
   char* ws = (char*)work;
   float* stat = (float*)(ws + p.stat);
   int tiles = 1;
@@ -310,31 +344,33 @@ bf_status vocab_loss_fwd(int dtype, int rows, int h, int V, int piece, const voi
     l.label = label;
     l.at_label = at_label;
     tiles = 0;
+    const void* ym = y;
+    if (p.pad) {
+      s = pad_rows(rows, h, p.h, (const bf16_t*)y, nullptr, V, ws + p.y, st);
+      if (s != BF_OK) return s;
+      ym = ws + p.y;
+    }
     for (int c0 = 0, n; c0 < V; c0 += n) {
       int done = 0;
       n = cols_at(p, c0, V);
       l.part = stat + (size_t)tiles * rows * 2;
       l.col0 = c0;
-      s = gemm_mfma_logits_lse(rows, n, h, y, (const bf16_t*)w + (size_t)c0 * h, l, &done, st);
+      const void* wp = (const bf16_t*)w + (size_t)c0 * h;
+      if (p.pad) {
+        s = pad_rows(n, h, p.h, (const bf16_t*)wp, nullptr, V, ws + p.w, st);
+        if (s != BF_OK) return s;
+        wp = ws + p.w;
+      }
+      s = gemm_mfma_logits_lse(rows, n, p.h, ym, wp, l, &done, st);
       if (s != BF_OK) return s;
       tiles += done;
     }
   } else {
     float* z = (float*)(ws + p.z);
     const float* yf = (const float*)y;
-    if (dtype == BF_BF16) {
-      s = widen(dtype, (size_t)rows * h, y, (float*)(ws + p.y), st);
-      if (s != BF_OK) return s;
-      yf = (const float*)(ws + p.y);
-    }
     for (int c0 = 0, n; c0 < V; c0 += n) {
       const int cols = n = cols_at(p, c0, V);
       const float* wf = (const float*)w + (size_t)c0 * h;
-      if (dtype == BF_BF16) {
-        s = widen(dtype, (size_t)cols * h, (const bf16_t*)w + (size_t)c0 * h, (float*)(ws + p.w), st);
-        if (s != BF_OK) return s;
-        wf = (const float*)(ws + p.w);
-      }
       s = product(L_NT, E_NONE, GemmArgs{rows, cols, h, yf, wf, z, nullptr, nullptr, nullptr, 0}, st);
       if (s != BF_OK) return s;
       piece_lse_kernel<<<rows, NT, 0, st>>>(rows, cols, z, label, c0, c0 == 0, (float2*)stat, at_label);
@@ -354,14 +390,18 @@ bf_status vocab_loss_bwd(int dtype, int rows, int h, int V, int piece, const voi
   bf_status s = check_args("bf_op_vocab_loss_bwd", dtype, rows, h, V, piece, y, w, label, lse, dy, dw, scale, work, work_bytes, 1);
   if (s != BF_OK) return s;
   const bool al = aligned16(y) && aligned16(w) && aligned16(dy) && aligned16(dw);
-  const Plan p = plan_for(matrix_possible(dtype, rows, h, V) && al, dtype, rows, h, V, piece, true);
+  const Plan p = plan_for(h % 8 || !al, dtype, rows, h, V, piece, true);
   char* ws = (char*)work;
   if (p.matrix) {
     bf16_t* yc = (bf16_t*)(ws + p.y);
     float* planes = (float*)(ws + p.dy);
     const bool unscaled = dy_parts_of(rows) == 1;
-    labelled_rows16_kernel<<<rows, NT, 0, st>>>(h / 8, (const uint4*)y, label, V, (uint4*)yc);
-    s = launched();
+    if (p.pad) {
+      s = pad_rows(rows, h, p.h, (const bf16_t*)y, label, V, yc, st);
+    } else {
+      labelled_rows16_kernel<<<rows, NT, 0, st>>>(h / 8, (const uint4*)y, label, V, (uint4*)yc);
+      s = launched();
+    }
     for (int c0 = 0, n; c0 < V && s == BF_OK; c0 += n) {
       const int cols = n = cols_at(p, c0, V);
       LogitArgs l;
@@ -370,41 +410,46 @@ bf_status vocab_loss_bwd(int dtype, int rows, int h, int V, int piece, const voi
       l.scale = scale;
       l.col0 = c0;
       l.S_voc = V;
-      l.parts = parts_of(rows, h);
+      l.parts = parts_of(rows, p.h);
       l.unscaled = unscaled;
       l.ldc = (int)up(cols, 8);
       l.plane = (size_t)rows * l.ldc;
       void* dz = ws + p.z;
       const bf16_t* wp = (const bf16_t*)w + (size_t)c0 * h;
-      s = gemm_mfma_logits_grad(rows, cols, h, y, wp, l, dz, st);
-      if (s == BF_OK) s = gemm_mfma_logits_dw(rows, cols, h, dz, l.ldc, l.parts, l.plane, yc, dw + (size_t)c0 * h, accumulate, st);
-      if (s == BF_OK) s = gemm_mfma_logits_dy(rows, cols, h, (bf16_t*)dz + (unscaled ? l.parts * l.plane : 0), l.ldc, dy_parts_of(rows), l.plane, wp, planes, p.slices, c0 > 0, st);
+      float* dwp = dw + (size_t)c0 * h;
+      if (p.pad) {
+        s = pad_rows(cols, h, p.h, wp, nullptr, V, ws + p.w, st);
+        wp = (const bf16_t*)(ws + p.w);
+        dwp = (float*)(ws + p.dw);
+      }
+      // (rows without a label have dz = 0 whatever their logits are)
+      if (s == BF_OK) s = gemm_mfma_logits_grad(rows, cols, p.h, p.pad ? yc : y, wp, l, dz, st);
+      if (s == BF_OK) s = gemm_mfma_logits_dw(rows, cols, p.h, dz, l.ldc, l.parts, l.plane, yc, dwp, p.pad ? 0 : accumulate, st);
+      if (s == BF_OK && p.pad) {
+        cut_rows_kernel<<<grid_for((size_t)cols * h), NT, 0, st>>>((size_t)cols * h, h, p.h, dwp, accumulate, dw + (size_t)c0 * h);
+        s = launched();
+      }
+      if (s == BF_OK) s = gemm_mfma_logits_dy(rows, cols, p.h, (bf16_t*)dz + (unscaled ? l.parts * l.plane : 0), l.ldc, dy_parts_of(rows), l.plane, wp, planes,
+                                              p.slices, c0 > 0, st);
     }
     if (s != BF_OK) return s;
-    const size_t n8 = (size_t)rows * h / 8;
-    dy_finish_kernel<<<grid_for(n8), NT, 0, st>>>(n8, p.slices, (const float4*)planes, unscaled ? scale : 1.f, (bf16_t*)dy);
+    const size_t n8 = (size_t)rows * p.h / 8;
+    const float factor = unscaled ? scale : 1.f;
+    if (p.pad) dy_finish_kernel<true><<<grid_for(n8), NT, 0, st>>>(n8, h, p.h / 8, p.slices, (const float4*)planes, factor, (bf16_t*)dy);
+    else dy_finish_kernel<false><<<grid_for(n8), NT, 0, st>>>(n8, h, p.h / 8, p.slices, (const float4*)planes, factor, (bf16_t*)dy);
     return launched();
   }
   float* yc = (float*)(ws + p.y);
   float* z = (float*)(ws + p.z);
   float* share = (float*)(ws + p.stat);
-  float* dyf = dtype == BF_BF16 ? (float*)(ws + p.dy) : (float*)dy;
+  float* dyf = (float*)dy;
   for (int c0 = 0, n; c0 < V; c0 += n) {
     const int cols = n = cols_at(p, c0, V);
     const float *wf = (const float*)w + (size_t)c0 * h, *yf = (const float*)y;
-    if (dtype == BF_BF16) {
-      s = widen(dtype, (size_t)cols * h, (const bf16_t*)w + (size_t)c0 * h, (float*)(ws + p.w), st);
-      if (s != BF_OK) return s;
-      s = widen(dtype, (size_t)rows * h, y, yc, st);
-      if (s != BF_OK) return s;
-      wf = (const float*)(ws + p.w);
-      yf = yc;
-    }
     s = product(L_NT, E_NONE, GemmArgs{rows, cols, h, yf, wf, z, nullptr, nullptr, nullptr, 0}, st);
     if (s != BF_OK) return s;
     piece_dz_kernel<<<rows, NT, 0, st>>>(cols, z, label, lse, c0, V, scale);
-    if (dtype == BF_BF16) labelled_rows_kernel<bf16_t, float><<<rows, NT, 0, st>>>(h, (const bf16_t*)y, label, V, yc);
-    else if (c0 == 0) labelled_rows_kernel<float, float><<<rows, NT, 0, st>>>(h, (const float*)y, label, V, yc);
+    if (c0 == 0) labelled_rows_kernel<<<rows, NT, 0, st>>>(h, (const float*)y, label, V, yc);
     s = launched();
     if (s != BF_OK) return s;
     s = product(L_NN, E_NONE, GemmArgs{rows, h, cols, z, wf, c0 ? share : dyf, nullptr, nullptr, nullptr, 0}, st);
@@ -417,7 +462,6 @@ bf_status vocab_loss_bwd(int dtype, int rows, int h, int V, int piece, const voi
     s = product(L_TN, E_ACCUM, GemmArgs{cols, h, rows, z, yc, dw + (size_t)c0 * h, nullptr, nullptr, nullptr, accumulate}, st);
     if (s != BF_OK) return s;
   }
-  if (dtype == BF_BF16) return cast_f32_to_bf16((size_t)rows * h, dyf, (bf16_t*)dy, st);
   return BF_OK;
 }
 
