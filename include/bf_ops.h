@@ -236,7 +236,7 @@ bf_status bf_op_grad_norm(int dtype, int n_tensors, const void* const* g, const 
 bf_status bf_op_grad_scale(int dtype, int n_tensors, const void* const* g, void* const* dst, const size_t* n,
                            const float* coef, void* stream);
 /* bf_op_adam on g_i * coef[0] for a list of tensors in one go (the gradients themselves stay as they are).  A coefficient
- * that is not finite leaves the step out: w, m, v and w_lp stay as they were. */
+ * that is not finite leaves the step out: w, m, v and w_lp stay as they were.  No two tensors may overlap. */
 typedef struct {
   float *w, *m, *v;
   const float* g;

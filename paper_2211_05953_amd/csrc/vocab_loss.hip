@@ -247,7 +247,7 @@ Plan plan_for(bool pad, int dtype, int rows, int h_given, int V, int piece, bool
   size_t cols = piece ? (size_t)piece : PIECE_BYTES / per_col;
   if (cols < 1024 && !piece) cols = 1024;
   // fp32 dy: a product's sum over the columns is one chain in fp32, so it is cut (50304 columns in one: 1.1e-6 off, 6e-7 cut)
-  if (!matrix && !piece && cols > 4096) cols = 4096;
+  if (!matrix && backward && !piece && cols > 4096) cols = 4096;
   p.unit = 8;
   if (matrix) {
     // whole rounds of tiles and a rest: 2048 x 2048 x 50304 in pieces of 25600 (3.1 rounds of 256 x 256) and of 24576 (3), us for logits and dw of

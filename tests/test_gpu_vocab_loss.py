@@ -119,6 +119,19 @@ def test_rows_off_16_byte_alignment(dtype, offset):
     _check(dtype, 70, 96, 700, 256, offset, accumulate=1)
 
 
+# 1001 is no multiple of a 16-byte chunk: copies, of a vocabulary long enough for two pieces of them in both directions
+def test_long_vocabulary_of_rows_that_are_no_chunks():
+    _check(bf.BF_BF16, 4, 1001, 70001)
+    _check(bf.BF_BF16, 4, 1001, 70001, accumulate=1, seed=1)
+
+
+# an unscaled plane of dz beside the scaled ones (more than 256 rows), and rows of one element
+@pytest.mark.parametrize("T,h,V", [(257, 1, 3), (1, 1, 1), (300, 7, 9), (513, 4184, 70), (257, 8200, 66)])
+def test_narrow_and_wide_rows(T, h, V):
+    _check(bf.BF_BF16, T, h, V)
+    _check(bf.BF_BF16, T, h, V, accumulate=1, seed=1)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("T,h,V,piece", [(70, 96, 700, 0), (300, 257, 401, 100), (300, 128, 3000, 1024)])
 def test_rows_without_a_label_leave_no_trace(dtype, T, h, V, piece):
