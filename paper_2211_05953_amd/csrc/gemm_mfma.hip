@@ -318,8 +318,8 @@ __global__ __launch_bounds__(TL::NT * TL::KG) void gemm_mfma_kernel(int M, int N
   const int m0 = bm * BM, n0 = bn * BN;
   // ldk: row length of the operands that are stored K-contiguous; equal to K except in a split-K launch, where K is
   // the length of the slice this workgroup contracts over, and where the caller gives A longer rows (GemmArgs::lda)
-  const size_t lda = (size_t)ldk;                    // A stored [M,K] or [K,M]
-  const size_t ldb = BKC ? (size_t)ldk : (size_t)N;  // B stored [N,K] or [K,N]
+  const size_t lda = AK || EDGE ? (size_t)ldk : (size_t)M;  // A stored [M,K] or [K,M]; whole tiles of [K,M]: no longer rows
+  const size_t ldb = BKC ? (size_t)ldk : (size_t)N;         // B stored [N,K] or [K,N]
   if constexpr (EPI == E_ACCUM && AK) {
     // Split-K launch of a forward / dgrad product (grid.y slices of K): slice y starts K elements further along the
     // contraction and leaves its fp32 partial result in plane y of C ([slices][M][N]); a second kernel adds the
@@ -1129,7 +1129,7 @@ bf_status gemm_mfma_logits_dw(int rows, int cols, int h, const void* dz, int ldz
   a.seg_stride_a = plane;
   switch (choose_edge_tile(L_TN, cols, h)) {
     case 0:
-      if (cols % 256 == 0 && h % 256 == 0 && rows % BK == 0) return launch<TileBig, false, false, E_ACCUM, float>(a, st);
+      if (cols % 256 == 0 && ldz == cols && h % 256 == 0 && rows % BK == 0) return launch<TileBig, false, false, E_ACCUM, float>(a, st);
       return launch<TileBig, false, false, E_ACCUM, float, true>(a, st);
     case 1: return launch<TileSmall, false, false, E_ACCUM, float, true>(a, st);
     default: return launch<TileTiny, false, false, E_ACCUM, float, true>(a, st);
