@@ -1,6 +1,7 @@
 // Masked attention in fp32 on the fp32 matrix cores (v_mfma_f32_32x32x2_f32), heads up to 128 (padded with zeros to 64 or 128).
 //
-// The passes are those of attention_masked_mfma.hip on tiles of 32 keys (queries).  An instruction contracts over two values,
+// The passes are those of attention_masked_mfma.hip on tiles of 32 keys (queries), with dQ in one walk: ctx is fp32, and delta = dctx . ctx
+// as exact as any.  An instruction contracts over two values,
 // one from each half of the wave.  Over head dimensions a lane holds four in a row, dimensions 8 c + 4 (lane / 32) .. + 3, for four
 // instructions.  Over the tile's rows instruction r takes rows (r / 4) 8 + r % 4 and the same + 4: register r of a score tile is then
 // the other operand as it stands.  157 TFLOP/s against 2.5 PFLOP/s in bf16: the matrix cores bound everything here (64 cycles an
@@ -232,6 +233,8 @@ struct QueryShared {
 
 // Forward (GRAD false) and dQ (GRAD true).  SEEN: tiles that are masked in part by sums_seen; without it returns whether one of
 // those held a non-finite value that enters a sum.
+// 2 x 500 queries, 8 heads of 80 over 2, bias and capped scores: forward 54 us, dQ 60, and the keys 77 (12, 16 and 17 TFLOP/s of 154): 256
+// workgroups, each wave a chain of two to four tiles.  A launch of one tile takes 24 us at D 128: rows, instructions, hand-over.
 template <int D, int KG, bool VEC, bool CAP, bool GRAD, bool SEEN>
 __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D, KG>& sh) {
   constexpr int NT = KG == 1 ? 256 : 64, RB = KG == 1 ? ROWS : 32;  // threads that fetch a tile, rows of the workgroup
@@ -424,7 +427,8 @@ __global__ __launch_bounds__(256, KG == 1 ? 2 : 1) void masked_query_f32_kernel(
   }
 }
 
-// dK / dV: 8 waves in pairs, as in attention_masked_mfma.hip.  QG query groups: 1: 32 keys to a pair, 128 to the workgroup, the tiles in
+// dK / dV: 8 waves in pairs that share 32 keys: the first takes a tile's scores and P and sums dV, the second dP and, from the first's P
+// through LDS, dS and sums dK.  QG query groups: 1: 32 keys to a pair, 128 to the workgroup, the tiles in
 // two LDS stages.  4: all pairs hold the same 32 keys, each takes every fourth tile through a stage of its own, and their sums
 // meet at the end.
 constexpr int NTHR_DKV = 512;

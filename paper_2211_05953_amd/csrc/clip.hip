@@ -53,6 +53,7 @@ __device__ __forceinline__ int entry_of(const TB& t, uint32_t chunk) {
   return lo;
 }
 
+// 24 tensors of 4 to 16 Mi elements (0.94 GB) 159 us, 5.9 TB/s; 200 of 256 to 256 Ki (22 MB) 7.5 us and the last sums 3
 template <typename T>
 __global__ __launch_bounds__(NT) void norm_kernel(NormTable t, double* __restrict__ part) {
   typedef typename Chunk<T>::V V;
@@ -100,6 +101,7 @@ __global__ __launch_bounds__(NT) void norm_finish_kernel(const double* __restric
   out[1] = !(norm <= DBL_MAX) ? NAN : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
 }
 
+// (those 200: 44 MB read and written in two launches of 12 us)
 template <typename T>
 __global__ __launch_bounds__(NT) void scale_kernel(ScaleTable t, const float* __restrict__ coef) {
   typedef typename Chunk<T>::V V;
@@ -141,7 +143,7 @@ __device__ __forceinline__ void adam_one(float& w, float& m, float& v, float g, 
 // Eight streams over HBM: the fewer places they are at, the faster.  One workgroup to a compute unit, with all its loads in flight
 // at once (four streams of four vectors), and accesses that do not stay in the caches.  Norm and step of 24 tensors of 4 to 16
 // Mi elements, us: 2048 workgroups with two vectors a stream 1637, without caching 1545; 512 with four 1451; 256 1386
-// (256 with eight 1434; the norm alone does not change).
+// (256 with eight 1434; the norm alone does not change).  The step alone 1217 us, 5.8 TB/s.
 constexpr int ADAM_VECS = 4;
 constexpr unsigned ADAM_WG = 256;
 __global__ __launch_bounds__(NT) void adam_clipped_kernel(AdamTable t, const float* __restrict__ coef, AdamArgs a) {
