@@ -491,7 +491,7 @@ def _list(who, tensors, dtype):
 
 
 def _at(arr):
-    """Address of an array's elements, NULL for an empty one."""
+    """Address of an array's elements, NULL for an empty one.  The array itself has to live until the call is over."""
     return arr.buffer_info()[0] if len(arr) else None
 
 
@@ -595,7 +595,8 @@ def bf_op_vocab_loss_bwd(dtype, n_rows, S_hidden, S_voc, y, w_out, labels, lse, 
 
 
 def bf_op_grad_norm_work_bytes(tensors):
-    return load().bf_op_grad_norm_work_bytes(len(tensors), _at(_array("Q", [t.numel() for t in tensors])))
+    n = _array("Q", [t.numel() for t in tensors])
+    return load().bf_op_grad_norm_work_bytes(len(n), _at(n))
 
 
 def bf_op_grad_norm(dtype, tensors, max_norm, out, work=None):
