@@ -513,6 +513,25 @@ def bf_op_attention_spans(S_mb, S_seq, causal, doc, prefix, spans):
     check(load().bf_op_attention_spans(S_mb, S_seq, causal, _ptr(doc), _ptr(prefix), _ptr(spans), _stream()))
 
 
+def _token_rows(t, S_mb, S_seq, heads, S_head, ld):
+    """Whether token (b, s) of `t` starts where the kernels look for it, (b S_seq + s) ld elements in, its heads side by side.  The dimensions are
+    (sequences, tokens, row), (all tokens, row), either with the row as (heads, S_head), or one; there may be more
+    sequences, tokens or columns than are used."""
+    n = heads * S_head
+    step = ld or n
+
+    def fits(*dims):  # (used, step between them); a step is met by nothing if one is used
+        return t.dim() == len(dims) and all(size >= used and (used == 1 or stride == want) for size, stride, (used, want) in zip(t.shape, t.stride(), dims))
+
+    tokens, flat = (S_mb * S_seq, step), (n, 1)
+    if fits((S_mb, S_seq * step), (S_seq, step), flat) or fits(tokens, flat):
+        return True
+    if t.dim() and t.shape[-1] == S_head and (fits((S_mb, S_seq * step), (S_seq, step), (heads, S_head), (S_head, 1)) or
+                                              fits(tokens, (heads, S_head), (S_head, 1))):
+        return True
+    return fits(((S_mb * S_seq - 1) * step + n, 1))
+
+
 def _attn_tensors(who, cfg, spans, slopes, lse, rows):
     """rows: (tensor, heads, step from a token to the next) each; the tensors may be views into longer rows."""
     torch = _th()
@@ -524,11 +543,9 @@ def _attn_tensors(who, cfg, spans, slopes, lse, rows):
             raise ValueError("%s: needs %s tensors on cuda:%d, got %s on %s" % (who, dtype, dev, t.dtype, t.device))
         if t.dim() == 3 and t.shape == (S_mb, S_seq, n) and t.stride() == (S_seq * (ld or n), ld or n, 1):
             continue
-        # another shape: what the kernels reach from the tensor's first element on has to lie in its storage
-        if ((S_mb * S_seq - 1) * (ld or n) + n + t.storage_offset()) * t.element_size() > t.untyped_storage().nbytes():
-            raise ValueError("%s: a tensor of shape %s does not hold %d rows of %d, %d apart" % (who, tuple(t.shape), S_mb * S_seq, n, ld or n))
-        if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError("%s: a token's row is not dense, strides %s" % (who, t.stride()))
+        if not _token_rows(t, S_mb, S_seq, heads, S_head, ld):
+            raise ValueError("%s: a tensor of shape %s and strides %s is not %d x %d tokens of %d heads of %d, %d elements apart"
+                             % (who, tuple(t.shape), t.stride(), S_mb, S_seq, heads, S_head, ld or n))
     _tensors(who, (spans,), torch.int32)
     _elems(who, spans, bf_op_attention_spans_elems(S_mb, S_seq))
     if slopes is not None:

@@ -318,3 +318,33 @@ def test_binding_refuses_what_a_kernel_would_misread():
             bf.bf_op_attention_masked_fwd(c.cfg, *ok[:at], bad, *ok[at + 1:])
     with pytest.raises(ValueError):
         bf.bf_op_attention_spans(2, 50, 1, torch.zeros(2, 49, dtype=torch.int32, device="cuda"), None, c.spans)
+
+
+def test_binding_refuses_rows_that_are_not_where_the_configuration_says():
+    """Views into packed rows without their step, heads in front of tokens: refused as inputs and as outputs, with all that the
+    kernels would reach inside the storage, and nothing is written."""
+    B, S, H, d = 2, 50, 2, 64
+    n = H * d
+    cfg, packed = (bf.make_attn_config(BF16, B, S, H, H, d, ld_q=ld, ld_k=ld, ld_v=ld) for ld in (0, 3 * n))
+    qkv = torch.randn(B, S, 3 * n, device="cuda").to(torch.bfloat16)
+    own = [x.contiguous() for x in qkv.split(n, 2)]
+    spans = torch.zeros(bf.bf_op_attention_spans_elems(B, S), dtype=torch.int32, device="cuda")
+    bf.bf_op_attention_spans(B, S, 1, None, None, spans)
+    ctx, lse = torch.empty(B, S, n, dtype=torch.bfloat16, device="cuda"), torch.empty(B, H, S, device="cuda")
+    bf.bf_op_attention_masked_fwd(cfg, *own, spans, None, ctx, lse)
+    other = torch.empty(B, S, H, d, dtype=torch.bfloat16, device="cuda")
+    bf.bf_op_attention_masked_fwd(packed, *(x.unflatten(2, (H, d)) for x in qkv.split(n, 2)), spans, None, other, lse)
+    assert torch.equal(ctx, other.flatten(2))
+    heads_first = own[0].unflatten(2, (H, d)).transpose(1, 2).contiguous()
+    for at in range(3):
+        for bad in (qkv.split(n, 2)[at], heads_first, heads_first.transpose(1, 2)):
+            with pytest.raises(ValueError):
+                bf.bf_op_attention_masked_fwd(cfg, *own[:at], bad, *own[at + 1:], spans, None, ctx, lse)
+    with pytest.raises(ValueError):
+        bf.bf_op_attention_masked_fwd(packed, *own, spans, None, ctx, lse)
+    out = torch.full_like(qkv, 7.0)
+    grads = [torch.full_like(x, 7.0) for x in own]
+    for at, part in enumerate(out.split(n, 2)):
+        with pytest.raises(ValueError):
+            bf.bf_op_attention_masked_bwd(cfg, *own, spans, None, ctx, lse, ctx, *grads[:at], part, *grads[at + 1:])
+    assert bool((out == 7).all()) and all(bool((x == 7).all()) for x in grads)

@@ -16,3 +16,40 @@ def test_gradient_norm_scratch_is_that_of_the_list(count):
     assert want == max(1, -(-count // 220)) * 2048 * 8
     for _ in range(20):
         assert bf.bf_op_grad_norm_work_bytes(tensors) == want
+
+
+# attention's rows: (S_mb, S_seq, heads, S_head)
+@pytest.mark.parametrize("sizes", [(2, 50, 4, 16), (1, 50, 4, 16), (2, 1, 4, 16), (3, 7, 1, 16), (2, 5, 3, 1), (1, 1, 1, 1)])
+def test_attention_rows_that_the_kernels_read_as_they_are(sizes):
+    B, S, H, d = sizes
+    fits = lambda t, ld=0: bf.binding._token_rows(t, B, S, H, d, ld)  # noqa: E731
+    n = H * d
+    x = torch.zeros(B, S, n)
+    assert fits(x) and fits(x, n) and fits(x.view(B * S, n)) and fits(x.view(B, S, H, d)) and fits(x.view(B * S, H, d)) and fits(x.view(-1))
+    assert fits(torch.zeros(B + 1, S, n)) and fits(torch.zeros(B * S + 3, n)) and fits(torch.zeros(B * S * n + 7))
+    wide = torch.zeros(B, S, 3 * n + 5)
+    for at in (0, n, 2 * n):
+        q = wide[..., at:at + n]
+        assert fits(q, 3 * n + 5) and fits(q.unflatten(2, (H, d)), 3 * n + 5) and fits(wide.view(B * S, -1)[:, at:at + n], 3 * n + 5)
+    assert fits(wide, 3 * n + 5) and fits(torch.zeros(B * S, 3 * n + 5), 3 * n + 5)
+
+
+def test_attention_rows_that_the_kernels_would_misread():
+    B, S, H, d = 2, 50, 4, 16
+    n = H * d
+    fits = lambda t, ld=0: bf.binding._token_rows(t, B, S, H, d, ld)  # noqa: E731
+    q = torch.zeros(B, S, 3 * n).split(n, 2)[1]
+    assert fits(q, 3 * n)
+    # another step between the tokens than the configuration's, with all that the kernels would reach inside the storage
+    for ld in (0, n, 2 * n, 3 * n - 1, 3 * n + 1):
+        assert not fits(q, ld) and not fits(q.unflatten(2, (H, d)), ld) and not fits(torch.zeros(B * S, 3 * n)[:, :n], ld)
+    x = torch.zeros(B, S, n)
+    assert not fits(x, 2 * n)
+    # heads in front of tokens, whole or as a view; rows that are not dense; a step of 0; too few tokens, heads or sequences
+    assert not fits(torch.zeros(B, H, S, d)) and not fits(torch.zeros(B, H, S, d).transpose(1, 2)) and not fits(torch.zeros(B, S, d, H).transpose(2, 3))
+    assert not fits(x.transpose(0, 1)) and not fits(torch.zeros(B, n, S).transpose(1, 2)) and not fits(torch.zeros(B, S, 2 * n)[..., ::2])
+    assert not fits(torch.zeros(1, S, n).expand(B, S, n)) and not fits(torch.zeros(B, 1, n).expand(B, S, n))
+    assert not fits(torch.zeros(B, S, 2 * H, d)[:, :, ::2]) and not fits(torch.zeros(B, S, H, 2 * d)[..., :d])
+    assert not fits(torch.zeros(B, S - 1, n)) and not fits(torch.zeros(1, S, n)) and not fits(torch.zeros(B, S, n - 1))
+    assert not fits(torch.zeros(B, S + 1, n)) and not fits(torch.zeros(B * S * n - 1)) and not fits(torch.zeros(B, S * n))
+    assert not fits(torch.zeros(B, S, H + 1, d)) and not fits(torch.zeros(B, S, H, d + 1)) and not fits(torch.zeros(()))
