@@ -149,7 +149,8 @@ int bf_op_attention_uses_mfma(int S_seq, int S_head);
  *           spans: device int32, 16-byte aligned, bf_op_attention_spans_elems(S_mb, S_seq) elements (0 for bad sizes): made once, used by
  *           every layer's forward and backward.  S_seq is at most 2^24.
  *   _fwd    ctx = softmax(b) V over each row's span with b_ij = c_ij - slopes[head] |i - j| (slopes: device fp32 [N_heads], or
- *           NULL), c_ij = cap tanh(scale q_i.k_j / cap), or scale q_i.k_j where cap is 0.  lse [S_mb, N_heads, S_seq] (device fp32, may
+ *           NULL), c_ij = cap tanh(scale q_i.k_j / cap), or scale q_i.k_j where cap is 0 (any finite cap; bf16 caps past 1024
+ *           take a longer tanh).  lse [S_mb, N_heads, S_seq] (device fp32, may
  *           be NULL) = log-sum-exp of a row's b.  A row without keys: ctx 0, lse -infinity.
  *   _bwd    dq, dk, dv from dctx, with the ctx and lse of the forward pass; dk and dv are the sums over the N_heads / N_kv_heads
  *           query heads of a key / value head, head a reading key / value head a / (N_heads / N_kv_heads).  A row

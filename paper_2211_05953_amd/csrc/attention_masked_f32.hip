@@ -175,16 +175,6 @@ __device__ __forceinline__ uint32_t interval_bits(int k0, int lo, int hi) {
   return a >= b ? 0u : (~0u >> (32 - (b - a))) << a;
 }
 
-// tanh to 3 ulp without a branch: a polynomial fitted to tanh(x) / x up to 0.55 (7e-9 off), 1 - 2 / (1 + e^2x) beyond, where the
-// difference costs no bits.  The library's function, inlined for every register of a tile, made the kernels long enough to
-// wait for their own instructions (500 queries: dQ 71.2 us and 69.0 with this, keys 120.6 and 106.0).
-__device__ __forceinline__ float tanh_f(float x) {
-  const float y = fabsf(x), u = x * x;
-  const float near = fmaf(x * u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, -0.00627260751f, 0.0210702536f), -0.0538518654f), 0.133325804f), -0.333333173f), x);
-  const float e = __builtin_amdgcn_exp2f(y * (2.f * LOG2E));
-  return y < 0.55f ? near : copysignf(fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f), x);
-}
-
 // a score from a dot product; slack: the cap's derivative there.  (slope 0: no bias; not worth kernels of its own, 2 operations beside
 // 64 cycles of the matrix core for each of a dot product's pairs of dimensions)
 template <bool CAP>
@@ -278,7 +268,7 @@ __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D, K
     wg = {min(wg.lo_min, y.lo_min), max(wg.hi_max, y.hi_max), max(wg.lo_max, y.lo_max), min(wg.hi_min, y.hi_min)};
   }
   wg.hi_max = min(wg.hi_max, S);
-  const float slope = a.slope ? a.slope[head] : 0.f, inv_cap = CAP ? 1.f / a.cap : 0.f;
+  const float slope = a.slope ? a.slope[head] : 0.f, inv_cap = CAP ? inverse_cap(a.cap) : 0.f;
   f32x16 o[D / 32];  // ctx, or dQ; transposed: rows = head dims, column = the lane's query
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) o[dt] = zero16();
@@ -512,7 +502,7 @@ __device__ __forceinline__ bool key_rows(const MaskedArgs& a, KeyShared<D, QG>& 
   fetch(grp);
   put(grp, grp);
   __syncthreads();
-  const float inv_cap = CAP ? 1.f / a.cap : 0.f;
+  const float inv_cap = CAP ? inverse_cap(a.cap) : 0.f;
   // every wave passes the same barriers, whether it has a tile or not
   for (int step = 0; step < total; step += QG) {
     const int it = step + grp, cur = QG == 1 ? it & 1 : grp;

@@ -105,40 +105,55 @@ __device__ __forceinline__ void store_row(const f32x16 (&acc)[D / 32], __amdgpu_
 __device__ __forceinline__ uint32_t row_bytes(int n, int there, size_t ld, int d) { return (uint32_t)(((there < n ? there : n) - 1) * ld + d) * 2; }
 
 // ---- from a dot product to an exponent of two.  Without cap and bias the dot products stay as they are and the factor enters with
-// the exponential (one fma).  cap: tanh x = 1 - 2 r with r = 1 / (1 + e^2x), on the hardware exponential and reciprocal (1 ulp
-// each: an absolute error of 1e-7 of the cap); its derivative 1 - tanh^2 is 4 r (1 - r).
+// the exponential (one fma).  CAP 1: tanh x = 1 - 2 r with r = 1 / (1 + e^2x), on the hardware exponential and reciprocal (1 ulp
+// each); its derivative 1 - tanh^2 is 4 r (1 - r).  That is off by 1.2e-7 of the cap, not of the score: caps past 2^10, where it
+// would show beside P's rounding (cap 1e4: 1.2e-3 of a probability, 1e6: a tenth), take CAP 2, a tanh as exact for small scores as for large
+// (8192 tokens, 16 heads of 128 over 4, forward and backward, us: 405 + 1868 and 538 + 2851).  So do caps so small that e2x is no fp32 number.
 struct ScoreFactors {
   float c2;      // factor of an exponent: 1 where the score carries it already
   float e2x;     // dot product to 2 x log2(e), x the tanh's argument
   float capl;    // cap log2(e)
   float mul;     // dot product to score (bias without cap)
   float slopel;  // slope log2(e)
+  float scale, cap, inv_cap;  // CAP 2
 };
 
-template <bool CAP, bool BIAS>
+constexpr float CAP_FAST = 1024.f;
+
+template <int CAP, bool BIAS>
 __device__ __forceinline__ ScoreFactors factors(const MaskedArgs& a, int head) {
   ScoreFactors f;
   f.c2 = CAP || BIAS ? 1.f : a.scale * LOG2E;
   f.mul = a.scale * LOG2E;
   f.capl = a.cap * LOG2E;
   f.e2x = CAP ? 2.f * LOG2E * a.scale / a.cap : 0.f;
-  f.slopel = BIAS ? a.slope[head] * LOG2E : 0.f;
+  f.scale = a.scale;
+  f.cap = a.cap;
+  f.inv_cap = CAP == 2 ? inverse_cap(a.cap) : 0.f;
+  f.slopel = BIAS && (CAP != 2 || a.slope) ? a.slope[head] * LOG2E : 0.f;  // (CAP 2 has no form without the bias)
   return f;
 }
 
-// dist: i - j as a float.  r: see above (CAP)
-template <bool CAP, bool BIAS>
+// dist: i - j as a float.  r: what slack_of takes (CAP)
+template <int CAP, bool BIAS>
 __device__ __forceinline__ float exponent(float dot, float dist, const ScoreFactors& f, float& r) {
   float t = dot;
-  if (CAP) {
+  if (CAP == 1) {
     r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(dot * f.e2x));
     t = fmaf(r, -2.f * f.capl, f.capl);
+  } else if (CAP == 2) {
+    r = tanh_f(dot * f.scale * f.inv_cap);
+    t = f.cap * r * LOG2E;
   } else if (BIAS) {
     t *= f.mul;
   }
   if (BIAS) t = fmaf(-f.slopel, fabsf(dist), t);
   return t;
 }
+
+// the cap's derivative
+template <int CAP>
+__device__ __forceinline__ float slack_of(float r) { return CAP == 1 ? 4.f * r * (1.f - r) : fmaf(-r, r, 1.f); }
 
 // acc += tile^T p over a tile that is masked in part and holds an infinity or a NaN: column by column of p, with the tile's
 // rows that the column does not see taken as zeros.  rows_of(c): bit r is set where column c sees row r of the tile (uniform).
@@ -232,7 +247,7 @@ __device__ __forceinline__ QueryBlock query_block(const MaskedArgs& a, int idx, 
 // SEEN: tiles that are masked in part by accumulate_seen.  Without it, returns whether one of those held a non-finite V.
 // 64 heads of 128, 2048 tokens, causal: 113 us, 0.61 PFLOP/s of the unmasked half's products, matrix cores busy 20 % of the time: bound by each
 // wave's chain of product, exponential, product, two workgroups of four waves to a compute unit.
-template <int D, int ROWS, bool VEC, bool CAP, bool BIAS, bool SEEN>
+template <int D, int ROWS, bool VEC, int CAP, bool BIAS, bool SEEN>
 __device__ __forceinline__ bool fwd_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2][BLK * D]) {
   constexpr int NT = 2 * ROWS;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -387,12 +402,12 @@ __device__ __forceinline__ bool fwd_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2
 
 // The second way is a pass of its own, and a function: in the first one's loop, or behind it in the same body, what it needs
 // pushes the first one's registers out.
-template <int D, int ROWS, bool VEC, bool CAP, bool BIAS>
+template <int D, int ROWS, bool VEC, int CAP, bool BIAS>
 __device__ __attribute__((noinline)) void fwd_rows_seen(MaskedArgs a, bf16_t (&KVs)[2][2][BLK * D]) {
   fwd_rows<D, ROWS, VEC, CAP, BIAS, true>(a, KVs);
 }
 
-template <int D, int ROWS, bool VEC, bool CAP, bool BIAS>
+template <int D, int ROWS, bool VEC, int CAP, bool BIAS>
 __global__ __launch_bounds__(2 * ROWS, 2) void masked_fwd_kernel(MaskedArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t KVs[2][2][BLK * D];
   if (fwd_rows<D, ROWS, VEC, CAP, BIAS, false>(a, KVs)) fwd_rows_seen<D, ROWS, VEC, CAP, BIAS>(a, KVs);
@@ -404,7 +419,7 @@ __global__ __launch_bounds__(2 * ROWS, 2) void masked_fwd_kernel(MaskedArgs a) {
 // gradient of the row as their own rounding does where few keys share a row (8192 tokens, 16 heads of 128, sharp rows: dQ and dK
 // 2.8e-3 off in the 2-norm, 2.3e-3 so); it is two products and no sums, against three and their sums.
 // 64 heads of 128, 2048 tokens, causal: 209 us, matrix cores busy 41 %; 0.82 PFLOP/s with the first walk's products, 0.49 without.
-template <int D, int ROWS, bool VEC, bool CAP, bool BIAS, bool SEEN>
+template <int D, int ROWS, bool VEC, int CAP, bool BIAS, bool SEEN>
 __device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2][BLK * D]) {
   constexpr int NT = 2 * ROWS;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -493,7 +508,7 @@ __device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2]
           const float pr = __builtin_amdgcn_exp2f(CAP || BIAS ? e - lse2 : fmaf(e, f.c2, -lse2));
           if (GRAD) {
             s[r] = pr * (dp[r] - delta);
-            if (CAP) s[r] *= 4.f * c * (1.f - c);
+            if (CAP) s[r] *= slack_of<CAP>(c);
           } else {
             s[r] = pr * dp[r];
           }
@@ -553,12 +568,12 @@ __device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2]
   return false;
 }
 
-template <int D, int ROWS, bool VEC, bool CAP, bool BIAS>
+template <int D, int ROWS, bool VEC, int CAP, bool BIAS>
 __device__ __attribute__((noinline)) void dq_rows_seen(MaskedArgs a, bf16_t (&KVs)[2][2][BLK * D]) {
   dq_rows<D, ROWS, VEC, CAP, BIAS, true>(a, KVs);
 }
 
-template <int D, int ROWS, bool VEC, bool CAP, bool BIAS>
+template <int D, int ROWS, bool VEC, int CAP, bool BIAS>
 __global__ __launch_bounds__(2 * ROWS, 2) void masked_dq_kernel(MaskedArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t KVs[2][2][BLK * D];
   if (dq_rows<D, ROWS, VEC, CAP, BIAS, false>(a, KVs)) dq_rows_seen<D, ROWS, VEC, CAP, BIAS>(a, KVs);
@@ -610,7 +625,7 @@ struct DkvAddr {
   }
 };
 
-template <int D, bool VEC, bool CAP, bool BIAS, bool SEEN>
+template <int D, bool VEC, int CAP, bool BIAS, bool SEEN>
 __device__ __forceinline__ bool dkv_keys(const MaskedArgs& a, DkvShared<D>& sh) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, kg = w & 3;
   const int role = __builtin_amdgcn_readfirstlane(w >> 2);
@@ -770,7 +785,7 @@ __device__ __forceinline__ bool dkv_keys(const MaskedArgs& a, DkvShared<D>& sh) 
         const float ex = exponent<CAP, BIAS>(s[r], dist + (float)(8 * q4 + e), f, c);
         s[r] = __builtin_amdgcn_exp2f(CAP || BIAS ? ex - ls[e] : fmaf(ex, f.c2, -ls[e]));
         dp[r] = s[r] * (dp[r] - dl[e]);
-        if (CAP) dp[r] *= 4.f * c * (1.f - c);
+        if (CAP) dp[r] *= slack_of<CAP>(c);
       };
       if (sum_before && !(SEEN && part_before)) {
         // The tile before's products beside this one's exponentials, in an order fixed by hand: a step is one product, the fragment
@@ -853,12 +868,12 @@ __device__ __forceinline__ bool dkv_keys(const MaskedArgs& a, DkvShared<D>& sh) 
   return false;
 }
 
-template <int D, bool VEC, bool CAP, bool BIAS>
+template <int D, bool VEC, int CAP, bool BIAS>
 __device__ __attribute__((noinline)) void dkv_keys_seen(MaskedArgs a, DkvShared<D>& sh) {
   dkv_keys<D, VEC, CAP, BIAS, true>(a, sh);
 }
 
-template <int D, bool VEC, bool CAP, bool BIAS>
+template <int D, bool VEC, int CAP, bool BIAS>
 __global__ __launch_bounds__(NTHR_DKV, 2) void masked_dkv_kernel(MaskedArgs a) {
   __shared__ __attribute__((aligned(16))) DkvShared<D> sh;
   if (dkv_keys<D, VEC, CAP, BIAS, false>(a, sh)) dkv_keys_seen<D, VEC, CAP, BIAS>(a, sh);
@@ -885,7 +900,7 @@ bf_status launched() {
 
 inline unsigned query_grid(const MaskedArgs& a, int rows) { return (unsigned)((a.S_seq + rows - 1) / rows) * (unsigned)(a.N_heads * a.S_mb); }
 
-template <int D, bool VEC, bool CAP, bool BIAS>
+template <int D, bool VEC, int CAP, bool BIAS>
 void run(const MaskedArgs& a, bool backward, hipStream_t st) {
   constexpr int ROWS = 128;
   if (!backward) {
@@ -900,10 +915,12 @@ void run(const MaskedArgs& a, bool backward, hipStream_t st) {
 
 template <int D, bool VEC>
 void by_score(const MaskedArgs& a, bool backward, hipStream_t st) {
-  if (a.cap > 0.f && a.slope) run<D, VEC, true, true>(a, backward, st);
-  else if (a.cap > 0.f) run<D, VEC, true, false>(a, backward, st);
-  else if (a.slope) run<D, VEC, false, true>(a, backward, st);
-  else run<D, VEC, false, false>(a, backward, st);
+  // (see ScoreFactors)
+  if (a.cap > CAP_FAST || (a.cap > 0.f && 2.0 * LOG2E * a.scale / a.cap > FLT_MAX)) run<D, VEC, 2, true>(a, backward, st);
+  else if (a.cap > 0.f && a.slope) run<D, VEC, 1, true>(a, backward, st);
+  else if (a.cap > 0.f) run<D, VEC, 1, false>(a, backward, st);
+  else if (a.slope) run<D, VEC, 0, true>(a, backward, st);
+  else run<D, VEC, 0, false>(a, backward, st);
 }
 
 bf_status by_head(const MaskedArgs& a, bool backward, hipStream_t st) {
