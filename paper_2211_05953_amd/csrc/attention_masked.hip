@@ -3,7 +3,7 @@
 //
 //   c_ij = cap tanh(scale q_i.k_j / cap)   (or scale q_i.k_j),   b_ij = c_ij - slope |i - j|
 //   P = softmax of b over j in [lo_i, hi_i),   ctx = P V,   lse = log-sum-exp of b
-//   dB = P (dctx V^T - delta),  delta_i = dctx_i . ctx_i,   dS = dB (1 - tanh^2) scale
+//   dB = P (dctx V^T - delta),  delta_i = dctx_i . ctx_i = sum_j P_ij dP_ij,  dP = dctx V^T,   dS = dB (1 - tanh^2) scale
 //   dq = dS K,   dk = dS^T Q,   dv = P^T dctx,   dk and dv summed over the query heads of a key / value head
 // A row with one key has dB = 0 (its P is 1 whatever the score), taken as exactly that; a row with none has ctx = 0,
 // lse = -inf and no gradient.
@@ -177,9 +177,13 @@ __global__ __launch_bounds__(64) void plain_fwd_kernel(MaskedArgs a) {
   if (lane == 0 && a.lse) a.lse[((size_t)b * a.N_heads + head) * a.S_seq + i] = l == 0.f ? -INFINITY : m + logf(l);
 }
 
+// delta: fp32 dctx . ctx; bf16 the sum of P dP as it is, since ctx was rounded when it was stored, which would enter every score gradient of
+// a row of few keys as far as their own rounding.  A span of up to 64 keys keeps P and dP for what follows
+// (backward, us, and with the stored ctx: 256 x 16 heads of 128, 4 tokens 188 / 186; 8 heads of 256 over 4, 500 tokens 2765 / 2637).
 template <typename T>
 __global__ __launch_bounds__(64) void plain_dq_kernel(MaskedArgs a) {
   __shared__ float q_s[PLAIN_HEAD], do_s[PLAIN_HEAD];
+  constexpr bool STORED = sizeof(T) == 4;
   const int lane = threadIdx.x, i = blockIdx.x, head = blockIdx.y % a.N_heads, b = blockIdx.y / a.N_heads, d = a.S_head;
   const int kv = head / (a.N_heads / a.N_kv);
   const size_t row = (size_t)b * a.S_seq + i, st = ((size_t)b * a.N_heads + head) * a.S_seq + i;
@@ -190,25 +194,32 @@ __global__ __launch_bounds__(64) void plain_dq_kernel(MaskedArgs a) {
   for (int c = lane; c < d; c += 64) {
     q_s[c] = (float)q[c];
     do_s[c] = (float)dc[c];
-    dl = fmaf((float)dc[c], (float)ctx[c], dl);
+    if (STORED) dl = fmaf((float)dc[c], (float)ctx[c], dl);
   }
-  dl = wave_sum(dl);
-  if (lane == 0) a.delta[st] = dl;
   __syncthreads();
   const int2 sp = a.span[row];
   const int lo = max(sp.x, 0), hi = min(sp.y, a.S_seq);
   const float slope = a.slope ? a.slope[head] : 0.f, lse = lse_of(a.lse[st]);
+  float p = 0.f, dp = 0.f, slack = 0.f;
+  auto key = [&](int j) {
+    p = dp = 0.f;
+    if (j >= hi) return;
+    const size_t at = (size_t)b * a.S_seq + j;
+    p = expf(score_of(dot_row(q_s, (const T*)a.k + at * a.ldk + (size_t)kv * d, d), a, slope, i, j, slack) - lse);
+    dp = dot_row(do_s, (const T*)a.v + at * a.ldv + (size_t)kv * d, d);
+  };
+  if (!STORED)
+    for (int j0 = lo; j0 < hi; j0 += 64) {
+      key(j0 + lane);
+      dl = fmaf(p, dp, dl);
+    }
+  dl = wave_sum(dl);
+  if (lane == 0) a.delta[st] = dl;
   float o[PER];
   for (int c = 0; c < PER; ++c) o[c] = 0.f;
   for (int j0 = lo; j0 < hi && hi - lo > 1; j0 += 64) {
-    const int j = j0 + lane;
-    float ds = 0.f;
-    if (j < hi) {
-      const size_t key = (size_t)b * a.S_seq + j;
-      float slack;
-      const float s = score_of(dot_row(q_s, (const T*)a.k + key * a.ldk + (size_t)kv * d, d), a, slope, i, j, slack);
-      ds = expf(s - lse) * (dot_row(do_s, (const T*)a.v + key * a.ldv + (size_t)kv * d, d) - dl) * slack;
-    }
+    if (STORED || hi - lo > 64) key(j0 + lane);
+    const float ds = j0 + lane < hi ? p * (dp - dl) * slack : 0.f;
     for (int k = 0; k < 64 && j0 + k < hi; ++k) {
       const float dk = __shfl(ds, k, 64);
       const T* kr = (const T*)a.k + ((size_t)b * a.S_seq + j0 + k) * a.ldk + (size_t)kv * d;

@@ -89,6 +89,26 @@ def test_any_cap(dtype, B, S, H, KV, d, more, cap):
     Tight(dtype, B, S, H, KV, d, cap=cap, **more).check()
 
 
+PLAIN = dict(kernels=bf.BF_KERNELS_PLAIN)
+
+
+# rows of two, three, a few keys; one, two and three chunks of 64 keys on the plain kernels; heads of more than 128
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("mask", [dict(), dict(causal=0), dict(docs=4), dict(docs=4, slopes=1, cap=5.0, big=4.0), dict(prefix=1, pad=1, cap=1e6)])
+@pytest.mark.parametrize("B,S,H,KV,d,more", [(3, 2, 4, 4, 64, {}), (3, 3, 4, 4, 128, {}), (3, 4, 4, 4, 33, {}), (3, 2, 4, 2, 64, {}), (3, 4, 4, 1, 128, {}), (2, 9, 4, 4, 64, {}),
+                                             (2, 40, 2, 1, 160, {}), (1, 64, 2, 2, 64, PLAIN), (1, 65, 2, 1, 64, PLAIN), (1, 130, 2, 2, 72, PLAIN), (2, 150, 4, 2, 64, {}),
+                                             (1, 300, 2, 2, 128, {})])
+def test_score_gradients_of_few_keys(dtype, B, S, H, KV, d, more, mask):
+    Tight(dtype, B, S, H, KV, d, **mask, **more).check()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("cap", CAPS)
+@pytest.mark.parametrize("B,S,H,KV,d,more", [(1, 3, 2, 2, 64, {}), (1, 40, 2, 1, 160, {})])
+def test_any_cap_on_the_plain_kernels(dtype, B, S, H, KV, d, more, cap):
+    Tight(dtype, B, S, H, KV, d, cap=cap, **more).check()
+
+
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("cap", CAPS)
 def test_scores_of_zero_under_any_cap(dtype, cap):
