@@ -205,7 +205,8 @@ bf_status bf_op_ce_loss(int dtype, int n_rows, int S_voc, void* z, const int32_t
  * its y holds.  Sums have a fixed order: no atomics.  bf16 tensors run on the
  * bf16 matrix cores with logits and statistics in fp32, dw to fp32 precision (rows that are not 16-byte aligned, S_hidden % 8 or
  * tensors that start elsewhere, through copies in the scratch); fp32 tensors as fp32 products.
- * S_piece: columns of a piece (0: the library's choice, 256 MiB of dz); work: device scratch, 256-byte aligned, of
+ * S_piece: columns of a piece, in bf16 rounded up to whole chunks of 8 (0: the library's choice, 256 MiB of dz, and a bf16 forward, which
+ * keeps nothing of a piece, in one; given, the scratch does not grow with the vocabulary); work: device scratch, 256-byte aligned, of
  * bf_op_vocab_loss_work_bytes(..., backward = 0 or 1) bytes (0 for bad sizes), owned by the caller; calls that overlap need
  * their own.  Sizes are 1 to 2^21. */
 size_t bf_op_vocab_loss_work_bytes(int dtype, int n_rows, int S_hidden, int S_voc, int S_piece, int backward);

@@ -43,10 +43,11 @@ __device__ __forceinline__ void merge(float& m, float& s, float m2, float s2) {
   m = top;
 }
 
-// 32 rows a workgroup, 8 threads to a row, each over every eighth tile in ascending order
+// 32 rows a workgroup, 8 threads to a row, each over every eighth tile in ascending order.  run (or NULL): what earlier pieces' tiles came
+// to (unless first), and where these go with them (unless last)
 __global__ __launch_bounds__(NT) void lse_merge_kernel(int rows, int tiles, const float2* __restrict__ part, const float* __restrict__ at_label,
                                                        const int32_t* __restrict__ label, int S_voc, float scale, float* __restrict__ lse,
-                                                       float* __restrict__ row_loss) {
+                                                       float* __restrict__ row_loss, float2* __restrict__ run, int first, int last) {
   __shared__ float2 red[8][32];
   const int r = threadIdx.x & 31, g = threadIdx.x >> 5, row = blockIdx.x * 32 + r;
   float m = -FLT_MAX, s = 0.f;
@@ -62,6 +63,11 @@ __global__ __launch_bounds__(NT) void lse_merge_kernel(int rows, int tiles, cons
   if (g || row >= rows) return;
 #pragma unroll
   for (int k = 1; k < 8; ++k) merge(m, s, red[k][r].x, red[k][r].y);
+  if (run && !first) merge(m, s, run[row].x, run[row].y);
+  if (run && !last) {
+    run[row] = make_float2(m, s);
+    return;
+  }
   const float l = m + logf(s);
   lse[row] = l;
   const int v = label[row];
@@ -218,8 +224,10 @@ struct Plan {
   int unit;      // pieces are multiples of this, but for the last one
   bool pad;      // lengthened rows
   int h;         // row length of the products
-  // offsets into the scratch: copy of y, lengthened piece of W and its dw, z / dz, planes of dy, statistics (or a piece's dy), labels' logits
-  size_t y, w, dw, z, dy, stat, lab, total;
+  bool merge;    // bf16 forward: statistics merged piece by piece, so that they do not grow with the vocabulary
+  // offsets into the scratch: copy of y, lengthened piece of W and its dw, z / dz, planes of dy, statistics (or a piece's dy), those of
+  // earlier pieces, labels' logits
+  size_t y, w, dw, z, dy, stat, run, lab, total;
   int slices;
 };
 
@@ -258,7 +266,7 @@ Plan plan_for(bool pad, int dtype, int rows, int h_given, int V, int piece, bool
     if (!piece && round) {
       if (!backward) cols = (size_t)V;  // the forward product keeps nothing
       if (cols >= (size_t)round) p.unit = round;
-    } else if (!backward) {
+    } else if (!backward && !piece) {
       cols = (size_t)V;
     } else if (!piece && cols < (size_t)V) {
       cols = up((V + (V + cols - 1) / cols - 1) / ((V + cols - 1) / cols), 512);  // pieces of about the same size
@@ -284,8 +292,11 @@ Plan plan_for(bool pad, int dtype, int rows, int h_given, int V, int piece, bool
       p.dy = take((size_t)p.slices * rows * h * 4);
     } else {
       size_t tiles = 0;
-      for (int c0 = 0, n; c0 < V; c0 += n) tiles += gemm_mfma_logits_tiles(rows, n = cols_at(p, c0, V));
+      p.merge = piece != 0;
+      if (p.merge) tiles = (cols + 63) / 64;  // of any piece: the smallest tile is 64 wide
+      else for (int c0 = 0, n; c0 < V; c0 += n) tiles += gemm_mfma_logits_tiles(rows, n = cols_at(p, c0, V));
       p.stat = take(tiles * rows * 8);
+      if (p.merge) p.run = take((size_t)rows * 8);
       p.lab = take((size_t)rows * 4);
     }
   } else {
@@ -340,7 +351,9 @@ bf_status vocab_loss_fwd(int dtype, int rows, int h, int V, int piece, const voi
   char* ws = (char*)work;
   float* stat = (float*)(ws + p.stat);
   int tiles = 1;
+  bool pieces = false;  // some of the vocabulary is in `run` already
   float* at_label = (float*)(ws + p.lab);
+  float2* run = p.matrix && p.merge ? (float2*)(ws + p.run) : nullptr;
   if (p.matrix) {
     LogitArgs l;
     l.label = label;
@@ -366,6 +379,13 @@ bf_status vocab_loss_fwd(int dtype, int rows, int h, int V, int piece, const voi
       s = gemm_mfma_logits_lse(rows, n, p.h, ym, wp, l, &done, st);
       if (s != BF_OK) return s;
       tiles += done;
+      if (run && c0 + n < V) {
+        lse_merge_kernel<<<(rows + 31) / 32, NT, 0, st>>>(rows, tiles, (const float2*)stat, at_label, label, V, scale, lse, row_loss, run, c0 == 0, 0);
+        s = launched();
+        if (s != BF_OK) return s;
+        tiles = 0;
+        pieces = true;
+      }
     }
   } else {
     float* z = (float*)(ws + p.z);
@@ -380,7 +400,7 @@ bf_status vocab_loss_fwd(int dtype, int rows, int h, int V, int piece, const voi
       if (s != BF_OK) return s;
     }
   }
-  lse_merge_kernel<<<(rows + 31) / 32, NT, 0, st>>>(rows, tiles, (const float2*)stat, at_label, label, V, scale, lse, row_loss);
+  lse_merge_kernel<<<(rows + 31) / 32, NT, 0, st>>>(rows, tiles, (const float2*)stat, at_label, label, V, scale, lse, row_loss, run, !pieces, 1);
   s = launched();
   if (s != BF_OK) return s;
   loss_sum_kernel<<<1, 1024, 0, st>>>(rows, row_loss, loss);

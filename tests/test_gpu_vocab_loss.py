@@ -229,3 +229,23 @@ def test_binding_refuses_what_a_kernel_would_misread():
             bf.bf_op_vocab_loss_fwd(dtype, T, h, V, *ok[:at], bad, *ok[at + 1:])
     with pytest.raises(bf.BfError):
         bf.bf_op_vocab_loss_fwd(dtype, T, h, V, *ok, work=torch.empty(8, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,h,V,piece,offset", [(33, 256, 1003, 0, 0), (300, 128, 5001, 2049, 0), (300, 128, 5001, 8, 0), (70, 96, 3000, 100, 3), (257, 250, 9000, 1024, 0),
+                                                (1030, 64, 20000, 9999, 0)])
+def test_nothing_past_the_scratch(dtype, T, h, V, piece, offset):
+    """Pieces large and small, with and without lengthened rows, in scratch of exactly the size asked for; the same call with more
+    scratch gives the same bits."""
+    y, w, label = _inputs(dtype, T, h, V, offset=offset)
+    outs = []
+    for more in (0, 4096):
+        lse, rows, loss = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty(1, device="cuda")
+        dy, dw = torch.empty_like(y), torch.empty(V, h, device="cuda")
+        need = [bf.bf_op_vocab_loss_work_bytes(dtype, T, h, V, piece, k) for k in (0, 1)]
+        flat = [torch.full((n + 8192,), 0xA5, dtype=torch.uint8, device="cuda") for n in need]
+        bf.bf_op_vocab_loss_fwd(dtype, T, h, V, y, w, label, 1 / T, lse, rows, loss, S_piece=piece, work=flat[0][:need[0] + more])
+        bf.bf_op_vocab_loss_bwd(dtype, T, h, V, y, w, label, lse, 1 / T, dy, dw, S_piece=piece, work=flat[1][:need[1] + more])
+        assert all(bool((f[n:] == 0xA5).all()) for f, n in zip(flat, need))
+        outs.append((lse, rows, loss, dy, dw))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))

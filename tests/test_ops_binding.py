@@ -53,3 +53,18 @@ def test_attention_rows_that_the_kernels_would_misread():
     assert not fits(torch.zeros(B, S - 1, n)) and not fits(torch.zeros(1, S, n)) and not fits(torch.zeros(B, S, n - 1))
     assert not fits(torch.zeros(B, S + 1, n)) and not fits(torch.zeros(B * S * n - 1)) and not fits(torch.zeros(B, S * n))
     assert not fits(torch.zeros(B, S, H + 1, d)) and not fits(torch.zeros(B, S, H, d + 1)) and not fits(torch.zeros(()))
+
+
+@pytest.mark.parametrize("rows,h", [(2048, 8192), (2048, 1024), (2000, 1000), (33, 256), (8192, 64), (1, 8)])
+def test_forward_scratch_of_the_vocabulary_loss_is_a_piece_s(rows, h):
+    """bf16: asking for pieces costs no more scratch than the library's choice, less the smaller they are, and the same for any vocabulary."""
+    need = lambda V, piece: bf.bf_op_vocab_loss_work_bytes(bf.BF_BF16, rows, h, V, piece, 0)  # noqa: E731
+    for V in (50304, 50257, 150912):
+        at = [need(V, piece) for piece in (256, 1024, 8192)] + [need(V, 0)]
+        assert at == sorted(at)
+    for piece in (8, 1000, 8192):
+        at = [need(V, piece) for V in (50304, 50257, 150912, 2000000)]
+        assert at[0] == at[1] == at[2] == at[3]
+        # y and a piece of w lengthened to whole chunks, 8 bytes a row and 64 columns, and two of each row's numbers
+        h8, cols = -(-h // 8) * 8, -(-piece // 8) * 8
+        assert at[0] <= 2 * h8 * (rows + cols) + 8 * rows * (-(-cols // 64) + 2) + 5 * 256
