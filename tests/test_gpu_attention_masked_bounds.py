@@ -122,3 +122,12 @@ def test_scores_of_zero_under_any_cap(dtype, cap):
 def test_what_a_mask_hides_under_a_large_cap(dtype, d):
     _hidden(dtype, math.nan, d, dict(causal=1, cap=1e6))
     _hidden(dtype, math.inf, d, dict(causal=0, cap=1e6, slopes=1))
+
+
+# dozens of tiles in a row: several steps of the maximum, spans that begin and end far from their rows, prefixes longer than a workgroup's keys
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("B,S,H,KV,d,mask", [(1, 2048, 4, 2, 128, dict(docs=300, pad=1)), (1, 4100, 1, 1, 64, dict()), (1, 3001, 4, 1, 80, dict(cap=50.0, big=3.0)),
+                                             (2, 1500, 2, 2, 128, dict(prefix=1, slopes=1)), (1, 2500, 2, 1, 64, dict(causal=0, docs=900, slopes=1)),
+                                             (1, 1200, 1, 1, 192, dict(docs=500, cap=30.0))])
+def test_long_sequences(dtype, B, S, H, KV, d, mask):
+    Tight(dtype, B, S, H, KV, d, **mask).check()

@@ -249,3 +249,21 @@ def test_nothing_past_the_scratch(dtype, T, h, V, piece, offset):
         assert all(bool((f[n:] == 0xA5).all()) for f, n in zip(flat, need))
         outs.append((lse, rows, loss, dy, dw))
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+# Rows and hidden sizes of whole 256 x 256 tiles: pieces of whole rounds of them and an odd rest (logits, dw and dy with no bounds checks, sums in
+# slices, shorter pieces added to the planes of longer ones); dz in three parts and two, dy's in two (up to 256 rows) and one; pieces
+# as given, whole tiles too; a number of k-tiles that is no power of two
+WHOLE = [(256, 256, 65536 + 1003, 0), (1024, 1024, 16384 + 1003, 0), (2048, 1024, 2 * 16384 + 77, 0), (2048, 8192, 8192 + 300, 0), (1536, 1024, 16384, 0),
+         (1024, 1024, 40003, 16384), (1024, 1024, 16384, 0)]
+
+
+@pytest.mark.parametrize("accumulate", [0, 1])
+@pytest.mark.parametrize("T,h,V,piece", WHOLE)
+def test_whole_tiles(T, h, V, piece, accumulate):
+    _check(bf.BF_BF16, T, h, V, piece, accumulate=accumulate, seed=accumulate)
+
+
+@pytest.mark.parametrize("T,h,V,piece", [WHOLE[0], WHOLE[2], WHOLE[5]])
+def test_rows_without_a_label_leave_no_trace_on_whole_tiles(T, h, V, piece):
+    _check(bf.BF_BF16, T, h, V, piece, poison=True)
