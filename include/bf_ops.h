@@ -159,7 +159,7 @@ int bf_op_attention_uses_mfma(int S_seq, int S_head);
  *           bytes (0 for a bad cfg), owned by the caller; calls that overlap need their own.
  * Token t of sequence b starts (b S_seq + t) ld elements into its tensor, head a another a S_head elements on; ld_q, ld_k, ld_v (for
  * q and dq, k and dk, v and dv) and ld_ctx (ctx, dctx) of 0 mean rows without gaps, so that a packed [Q | K | V] is three pointers
- * into it and its row length.  Nothing between the rows is written.  What a mask hides never reaches a result, infinities and NaN
+ * into it and its row length.  Tensors are aligned to their elements.  Nothing between the rows is written.  What a mask hides never reaches a result, infinities and NaN
  * included.  Sums have a fixed order: no atomics on memory.
  * S_head 1 to 1024, S_mb * N_heads up to 65535.  S_head up to 128 on the matrix cores (bf16: probabilities and their gradients in bf16 as they enter the products;
  * fp32: fp32 throughout), fastest where rows are whole 16-byte chunks; above, for up to 4 tokens, and with BF_KERNELS_PLAIN, on plain kernels. */
@@ -208,7 +208,7 @@ bf_status bf_op_ce_loss(int dtype, int n_rows, int S_voc, void* z, const int32_t
  * S_piece: columns of a piece, in bf16 rounded up to whole chunks of 8 (0: the library's choice, 256 MiB of dz, and a bf16 forward, which
  * keeps nothing of a piece, in one; given, the scratch does not grow with the vocabulary); work: device scratch, 256-byte aligned, of
  * bf_op_vocab_loss_work_bytes(..., backward = 0 or 1) bytes (0 for bad sizes), owned by the caller; calls that overlap need
- * their own.  Sizes are 1 to 2^21. */
+ * their own.  Sizes are 1 to 2^21; tensors are aligned to their elements. */
 size_t bf_op_vocab_loss_work_bytes(int dtype, int n_rows, int S_hidden, int S_voc, int S_piece, int backward);
 bf_status bf_op_vocab_loss_fwd(int dtype, int n_rows, int S_hidden, int S_voc, int S_piece, const void* y, const void* w_out,
                                const int32_t* labels, float scale, float* lse, float* row_loss, float* loss_out, void* work,

@@ -353,6 +353,8 @@ int splits_of(const bf_attn_config& c) {
 
 bool element_aligned(int dtype, uintptr_t p) { return (p & (dtype == BF_BF16 ? 1 : 3)) == 0; }
 
+bool word_aligned(uintptr_t p) { return (p & 3) == 0; }
+
 }  // namespace
 
 size_t attention_spans_elems(int S_mb, int S_seq) {
@@ -363,6 +365,7 @@ size_t attention_spans_elems(int S_mb, int S_seq) {
 bf_status attention_spans(int S_mb, int S_seq, int causal, const int32_t* doc, const int32_t* prefix, int32_t* spans, hipStream_t st) {
   if (!attention_spans_elems(S_mb, S_seq) || S_mb > 65535) { set_error("bf_op_attention_spans: bad sizes"); return BF_EINVAL; }
   if (!spans || ((uintptr_t)spans & 15)) { set_error("bf_op_attention_spans: spans is null or not 16-byte aligned"); return BF_EINVAL; }
+  if (!word_aligned((uintptr_t)doc | (uintptr_t)prefix)) { set_error("bf_op_attention_spans: doc or prefix is not aligned to its elements"); return BF_EINVAL; }
   spans_kernel<<<dim3((S_seq + TOKENS - 1) / TOKENS, S_mb), TOKENS, 0, st>>>(S_seq, causal != 0, doc, prefix, (int2*)spans,
                                                                             (SpanBlock*)(spans + up4((size_t)S_mb * S_seq * 2)), (int)span_blocks(S_seq));
   return launched();
@@ -373,7 +376,8 @@ bf_status attention_masked_fwd(const bf_attn_config* c, const void* q, const voi
   const char* who = "bf_op_attention_masked_fwd";
   if (!cfg_ok(who, c)) return BF_EINVAL;
   if (!q || !k || !v || !spans || !ctx) { set_error("%s: null pointer", who); return BF_EINVAL; }
-  if (!element_aligned(c->dtype, (uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)ctx) || ((uintptr_t)spans & 15)) {
+  if (!element_aligned(c->dtype, (uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)ctx) || ((uintptr_t)spans & 15) ||
+      !word_aligned((uintptr_t)slopes | (uintptr_t)lse)) {
     set_error("%s: a tensor is not aligned to its elements, or spans not to 16 bytes", who);
     return BF_EINVAL;
   }
@@ -399,7 +403,7 @@ bf_status attention_masked_bwd(const bf_attn_config* c, const void* q, const voi
   if (!cfg_ok(who, c)) return BF_EINVAL;
   if (!q || !k || !v || !spans || !ctx || !lse || !dctx || !dq || !dk || !dv) { set_error("%s: null pointer", who); return BF_EINVAL; }
   const uintptr_t al = (uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)ctx | (uintptr_t)dctx | (uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv;
-  if (!element_aligned(c->dtype, al) || ((uintptr_t)spans & 15)) {
+  if (!element_aligned(c->dtype, al) || ((uintptr_t)spans & 15) || !word_aligned((uintptr_t)slopes | (uintptr_t)lse)) {
     set_error("%s: a tensor is not aligned to its elements, or spans not to 16 bytes", who);
     return BF_EINVAL;
   }

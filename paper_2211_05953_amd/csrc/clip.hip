@@ -246,7 +246,7 @@ bf_status grad_norm(int dtype, int n_tensors, const void* const* g, const size_t
                     hipStream_t st) {
   if (!list_ok("bf_op_grad_norm", n_tensors, g, n)) return BF_EINVAL;
   if (!(max_norm > 0.f)) { set_error("bf_op_grad_norm: max_norm must be above 0"); return BF_EINVAL; }
-  if (!out) { set_error("bf_op_grad_norm: out is null"); return BF_EINVAL; }
+  if (!out || ((uintptr_t)out & 3)) { set_error("bf_op_grad_norm: out is null or not aligned to its elements"); return BF_EINVAL; }
   if (!work || ((uintptr_t)work & 7) || work_bytes < grad_norm_work_bytes(n_tensors, n)) {
     set_error("bf_op_grad_norm: needs %zu bytes of 8-byte aligned scratch", grad_norm_work_bytes(n_tensors, n));
     return BF_EINVAL;
@@ -273,7 +273,7 @@ bf_status grad_norm(int dtype, int n_tensors, const void* const* g, const size_t
 
 bf_status grad_scale(int dtype, int n_tensors, const void* const* g, void* const* dst, const size_t* n, const float* coef, hipStream_t st) {
   if (!list_ok("bf_op_grad_scale", n_tensors, g, n) || !list_ok("bf_op_grad_scale", n_tensors, dst, n)) return BF_EINVAL;
-  if (!coef) { set_error("bf_op_grad_scale: coef is null"); return BF_EINVAL; }
+  if (!coef || ((uintptr_t)coef & 3)) { set_error("bf_op_grad_scale: coef is null or not aligned to its elements"); return BF_EINVAL; }
   const size_t es = dtype == BF_BF16 ? 2 : 4;
   for (int i = 0; i < n_tensors; ++i)
     if (n[i] && (!g[i] || !dst[i] || (((uintptr_t)g[i] | (uintptr_t)dst[i]) & (es - 1)))) {
@@ -298,7 +298,7 @@ bf_status grad_scale(int dtype, int n_tensors, const void* const* g, void* const
 bf_status adam_clipped(int n_tensors, const bf_adam_tensor* x, const float* coef, int step, float lr, float beta1, float beta2, float eps, float wd,
                        hipStream_t st) {
   if (n_tensors < 0 || (n_tensors > 0 && !x)) { set_error("bf_op_adam_clipped: bad list of tensors"); return BF_EINVAL; }
-  if (!coef || step < 1) { set_error("bf_op_adam_clipped: coef is null or step below 1"); return BF_EINVAL; }
+  if (!coef || ((uintptr_t)coef & 3) || step < 1) { set_error("bf_op_adam_clipped: coef is null or not aligned to its elements, or step below 1"); return BF_EINVAL; }
   for (int i = 0; i < n_tensors; ++i) {
     if (!x[i].n) continue;
     const uintptr_t al = (uintptr_t)x[i].w | (uintptr_t)x[i].m | (uintptr_t)x[i].v | (uintptr_t)x[i].g;

@@ -337,6 +337,9 @@ static bf_status check_args(const char* who, int dtype, int rows, int h, int V, 
                             const void* b, const void* c, float scale, const void* work, size_t work_bytes, int backward) {
   if (!sizes_ok(dtype, rows, h, V, piece)) { set_error("%s: bad type or sizes (1 .. 2^21)", who); return BF_EINVAL; }
   if (!y || !w || !label || !a || !b || !c) { set_error("%s: null pointer", who); return BF_EINVAL; }
+  // (a, b and c: fp32, but for a backward call's b, which is dy)
+  const uintptr_t wide = (uintptr_t)label | (uintptr_t)a | (uintptr_t)c | (backward ? 0 : (uintptr_t)b), stored = (uintptr_t)y | (uintptr_t)w | (backward ? (uintptr_t)b : 0);
+  if ((wide & 3) || (stored & (dtype == BF_BF16 ? 1 : 3))) { set_error("%s: a tensor is not aligned to its elements", who); return BF_EINVAL; }
   if (!(fabsf(scale) <= FLT_MAX)) { set_error("%s: scale is not finite", who); return BF_EINVAL; }
   const size_t need = vocab_loss_work_bytes(dtype, rows, h, V, piece, backward);
   if (!work || ((uintptr_t)work & 255) || work_bytes < need) { set_error("%s: needs %zu bytes of 256-byte aligned scratch", who, need); return BF_EINVAL; }

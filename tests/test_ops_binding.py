@@ -68,3 +68,39 @@ def test_forward_scratch_of_the_vocabulary_loss_is_a_piece_s(rows, h):
         # y and a piece of w lengthened to whole chunks, 8 bytes a row and 64 columns, and two of each row's numbers
         h8, cols = -(-h // 8) * 8, -(-piece // 8) * 8
         assert at[0] <= 2 * h8 * (rows + cols) + 8 * rows * (-(-cols // 64) + 2) + 5 * 256
+
+
+X = 1 << 20  # an aligned address that nothing may read
+
+
+def refused(name, *args):
+    lib = bf.load()
+    assert getattr(lib, name)(*args) == bf.BF_EINVAL, (name, args)
+    assert bf.binding.last_error()
+
+
+def test_pointers_that_are_not_aligned_to_their_elements_are_refused():
+    lib = bf.load()
+    one = (C.c_void_p * 1)(X), (C.c_size_t * 1)(100)
+    need = lib.bf_op_grad_norm_work_bytes(1, one[1])
+    refused("bf_op_grad_norm", bf.BF_FP32, 1, one[0], one[1], 1.0, X + 2, X, need, None)
+    refused("bf_op_grad_scale", bf.BF_FP32, 1, one[0], one[0], one[1], X + 1, None)
+    entry = (bf.bf_adam_tensor * 1)(bf.bf_adam_tensor(w=X, m=X, v=X, g=X, w_lp=X, n=10))
+    refused("bf_op_adam_clipped", 1, entry, X + 2, 1, 1e-3, 0.9, 0.99, 1e-8, 0.0, None)
+    for dtype, half in ((bf.BF_FP32, 2), (bf.BF_BF16, 1)):  # an address between two elements
+        need = [bf.bf_op_vocab_loss_work_bytes(dtype, 10, 64, 1000, 0, k) for k in (0, 1)]
+        fwd = [dtype, 10, 64, 1000, 0, X, X, X, 1.0, X, X, X, X, need[0], None]
+        bwd = [dtype, 10, 64, 1000, 0, X, X, X, X, 1.0, X, X, 0, X, need[1], None]
+        for at, off in ((5, half), (6, half), (7, 2), (9, 2), (10, 2), (11, 2)):
+            refused("bf_op_vocab_loss_fwd", *fwd[:at], X + off, *fwd[at + 1:])
+        for at, off in ((5, half), (6, half), (7, 2), (8, 2), (10, half), (11, 2)):
+            refused("bf_op_vocab_loss_bwd", *bwd[:at], X + off, *bwd[at + 1:])
+        cfg = bf.make_attn_config(dtype, 2, 100, 4, 2, 64)
+        fwd = [C.byref(cfg), X, X, X, X, X, X, X, None]
+        bwd = [C.byref(cfg), X, X, X, X, X, X, X, X, X, X, X, X, bf.bf_op_attention_masked_bwd_work_bytes(cfg), None]
+        for at, off in ((1, half), (2, half), (3, half), (5, 2), (6, half), (7, 2)):
+            refused("bf_op_attention_masked_fwd", *fwd[:at], X + off, *fwd[at + 1:])
+        for at, off in ((5, 2), (6, half), (7, 2), (8, half), (11, half)):
+            refused("bf_op_attention_masked_bwd", *bwd[:at], X + off, *bwd[at + 1:])
+    refused("bf_op_attention_spans", 2, 100, 1, X + 2, None, X, None)
+    refused("bf_op_attention_spans", 2, 100, 1, None, X + 1, X, None)
