@@ -161,7 +161,7 @@ int bf_op_attention_uses_mfma(int S_seq, int S_head);
  * q and dq, k and dk, v and dv) and ld_ctx (ctx, dctx) of 0 mean rows without gaps, so that a packed [Q | K | V] is three pointers
  * into it and its row length.  Tensors are aligned to their elements.  Nothing between the rows is written.  What a mask hides never reaches a result, infinities and NaN
  * included.  Sums have a fixed order: no atomics on memory.
- * S_head 1 to 1024, S_mb * N_heads up to 65535.  S_head up to 128 on the matrix cores (bf16: probabilities and their gradients in bf16 as they enter the products;
+ * S_head 1 to 1024, S_mb * N_heads up to 65535, and on the matrix cores times S_seq / 128 under 2^24 (backward 2^23).  S_head up to 128 on the matrix cores (bf16: probabilities and their gradients in bf16 as they enter the products;
  * fp32: fp32 throughout), fastest where rows are whole 16-byte chunks; above, for up to 4 tokens, and with BF_KERNELS_PLAIN, on plain kernels. */
 typedef struct {
   int32_t dtype, kernels;                            /* bf_dtype of all tensors but lse and slopes; bf_kernels */

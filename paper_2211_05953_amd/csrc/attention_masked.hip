@@ -340,6 +340,15 @@ bool matrix(const bf_attn_config& c) {
          (int64_t)c.N_heads * c.S_head <= far;
 }
 
+// A launch has fewer than 2^32 threads along its grid: 256 to 128 queries of a head, 512 to 128 keys (no more of those workgroups than of
+// the queries').
+bool launches_fit(const char* who, const bf_attn_config& c, bool backward) {
+  const long long wgs = (long long)((c.S_seq + 127) / 128) * c.S_mb * c.N_heads;
+  if (!matrix(c) || wgs < (backward ? 1 << 23 : 1 << 24)) return true;
+  set_error("%s: %d x %d tokens of %d heads are more than a launch holds", who, c.S_mb, c.S_seq, c.N_heads);
+  return false;
+}
+
 // Shares of a key / value head's query heads in the dK / dV pass
 int splits_of(const bf_attn_config& c) {
   if (!matrix(c)) return 1;
@@ -374,7 +383,7 @@ bf_status attention_spans(int S_mb, int S_seq, int causal, const int32_t* doc, c
 bf_status attention_masked_fwd(const bf_attn_config* c, const void* q, const void* k, const void* v, const int32_t* spans, const float* slopes, void* ctx,
                                float* lse, hipStream_t st) {
   const char* who = "bf_op_attention_masked_fwd";
-  if (!cfg_ok(who, c)) return BF_EINVAL;
+  if (!cfg_ok(who, c) || !launches_fit(who, *c, false)) return BF_EINVAL;
   if (!q || !k || !v || !spans || !ctx) { set_error("%s: null pointer", who); return BF_EINVAL; }
   if (!element_aligned(c->dtype, (uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)ctx) || ((uintptr_t)spans & 15) ||
       !word_aligned((uintptr_t)slopes | (uintptr_t)lse)) {
@@ -391,7 +400,8 @@ bf_status attention_masked_fwd(const bf_attn_config* c, const void* q, const voi
 }
 
 size_t attention_masked_bwd_work_bytes(const bf_attn_config* c) {
-  if (!cfg_ok("bf_op_attention_masked_bwd_work_bytes", c)) return 0;
+  const char* who = "bf_op_attention_masked_bwd_work_bytes";
+  if (!cfg_ok(who, c) || !launches_fit(who, *c, true)) return 0;
   const size_t delta = ((size_t)c->S_mb * c->N_heads * c->S_seq * 4 + 255) / 256 * 256;
   const int splits = splits_of(*c);
   return delta + (splits > 1 ? (size_t)splits * 2 * c->S_mb * c->S_seq * c->N_kv_heads * c->S_head * 4 : 0);
@@ -400,7 +410,7 @@ size_t attention_masked_bwd_work_bytes(const bf_attn_config* c) {
 bf_status attention_masked_bwd(const bf_attn_config* c, const void* q, const void* k, const void* v, const int32_t* spans, const float* slopes, const void* ctx,
                                const float* lse, const void* dctx, void* dq, void* dk, void* dv, void* work, size_t work_bytes, hipStream_t st) {
   const char* who = "bf_op_attention_masked_bwd";
-  if (!cfg_ok(who, c)) return BF_EINVAL;
+  if (!cfg_ok(who, c) || !launches_fit(who, *c, true)) return BF_EINVAL;
   if (!q || !k || !v || !spans || !ctx || !lse || !dctx || !dq || !dk || !dv) { set_error("%s: null pointer", who); return BF_EINVAL; }
   const uintptr_t al = (uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)ctx | (uintptr_t)dctx | (uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv;
   if (!element_aligned(c->dtype, al) || ((uintptr_t)spans & 15) || !word_aligned((uintptr_t)slopes | (uintptr_t)lse)) {

@@ -104,3 +104,18 @@ def test_pointers_that_are_not_aligned_to_their_elements_are_refused():
             refused("bf_op_attention_masked_bwd", *bwd[:at], X + off, *bwd[at + 1:])
     refused("bf_op_attention_spans", 2, 100, 1, X + 2, None, X, None)
     refused("bf_op_attention_spans", 2, 100, 1, None, X + 1, X, None)
+
+
+@pytest.mark.parametrize("dtype", [bf.BF_FP32, bf.BF_BF16])
+def test_attention_that_no_launch_holds_is_refused(dtype):
+    """2^32 threads along a grid: 256 to 128 queries of a head forward, 512 to 128 keys backward."""
+    make = lambda seq, heads, kernels=bf.BF_KERNELS_AUTO: bf.make_attn_config(dtype, 1, seq, heads, 1, 8, kernels=kernels)  # noqa: E731
+    tail = lambda n: (X,) * n  # noqa: E731
+    for seq, heads in ((1 << 24, 128), ((1 << 24) - 127, 128), (1 << 20, 2048), ((1 << 15) + 1, 65535)):
+        refused("bf_op_attention_masked_fwd", C.byref(make(seq, heads)), *tail(4), None, X, X, None)
+    for seq, heads in ((1 << 24, 64), ((1 << 24) - 127, 64), (1 << 20, 1024), ((1 << 14) + 1, 65535)):
+        cfg = make(seq, heads)
+        assert bf.bf_op_attention_masked_bwd_work_bytes(cfg) == 0
+        refused("bf_op_attention_masked_bwd", C.byref(cfg), *tail(4), None, *tail(7), 1 << 62, None)
+        assert bf.bf_op_attention_masked_bwd_work_bytes(make(seq, heads, bf.BF_KERNELS_PLAIN)) > 0
+    assert bf.bf_op_attention_masked_bwd_work_bytes(make((1 << 24) - 128, 64)) > 0
