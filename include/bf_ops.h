@@ -166,7 +166,7 @@ int bf_op_attention_uses_mfma(int S_seq, int S_head);
 typedef struct {
   int32_t dtype, kernels;                            /* bf_dtype of all tensors but lse and slopes; bf_kernels */
   int32_t S_mb, S_seq, N_heads, N_kv_heads, S_head;  /* N_kv_heads divides N_heads */
-  float scale;                                       /* 0: 1/sqrt(S_head) */
+  float scale;                                       /* up to 2^126; 0: 1/sqrt(S_head) */
   float cap;                                         /* 0: none */
   int64_t ld_q, ld_k, ld_v, ld_ctx;
 } bf_attn_config;

@@ -304,7 +304,11 @@ bool cfg_ok(const char* who, const bf_attn_config* c) {
     set_error("%s: a token's row is longer than the step to the next", who);
     return false;
   }
-  if (!(c->scale >= 0.f && c->scale <= FLT_MAX) || !(c->cap >= 0.f && c->cap <= FLT_MAX)) { set_error("%s: scale and cap must be finite and not negative", who); return false; }
+  // (the scale enters exponents of two: times log2(e), and the cap's tanh twice that, it has to be a finite fp32 number)
+  if (!(c->scale >= 0.f && c->scale <= 0x1p126f) || !(c->cap >= 0.f && c->cap <= FLT_MAX)) {
+    set_error("%s: scale must be 0 to 2^126, cap finite and not negative", who);
+    return false;
+  }
   return true;
 }
 

@@ -124,6 +124,24 @@ def test_what_a_mask_hides_under_a_large_cap(dtype, d):
     _hidden(dtype, math.inf, d, dict(causal=0, cap=1e6, slopes=1))
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("cap", [0.0, 1.0, 1e4])
+def test_scores_of_zero_under_the_largest_scale(dtype, cap):
+    """2^126: no product with a score of 0 is a NaN.  Keys of zeros, so every key has the same share: ctx and dv are means, dq is 0."""
+    B, S, H, KV, d = 1, 70, 2, 2, 64
+    c = Case(dtype, B, S, H, KV, d, causal=0, packed=0, cap=cap)
+    c.cfg.scale = 2.0**126
+    c.k.zero_()
+    ctx, lse, dq, dk, dv = c.run()
+    torch.cuda.synchronize()
+    u = 2.0**-8 if dtype == BF16 else 2.0**-22
+    for got, x in ((ctx, c.v), (dv, c.dctx)):
+        mean, size = x.double().mean(1, keepdim=True), x.double().abs().mean(1, keepdim=True)
+        # P rounded once, and the result; sums of 70 terms
+        assert float(((got.double() - mean).abs() - 2.1 * u * size - 2.0**-17 * size).max()) <= 0
+    assert float((lse.double() - math.log(S)).abs().max()) <= 2.0**-20 and not dq.any()
+
+
 # dozens of tiles in a row: several steps of the maximum, spans that begin and end far from their rows, prefixes longer than a workgroup's keys
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("B,S,H,KV,d,mask", [(1, 2048, 4, 2, 128, dict(docs=300, pad=1)), (1, 4100, 1, 1, 64, dict()), (1, 3001, 4, 1, 80, dict(cap=50.0, big=3.0)),

@@ -119,3 +119,12 @@ def test_attention_that_no_launch_holds_is_refused(dtype):
         refused("bf_op_attention_masked_bwd", C.byref(cfg), *tail(4), None, *tail(7), 1 << 62, None)
         assert bf.bf_op_attention_masked_bwd_work_bytes(make(seq, heads, bf.BF_KERNELS_PLAIN)) > 0
     assert bf.bf_op_attention_masked_bwd_work_bytes(make((1 << 24) - 128, 64)) > 0
+
+
+@pytest.mark.parametrize("dtype", [bf.BF_FP32, bf.BF_BF16])
+def test_attention_scales_that_are_infinite_as_exponents_are_refused(dtype):
+    for scale, good in ((2.0**126, True), (2.0**126 * 1.0001, False), (3e38, False), (1e-45, True)):
+        cfg = bf.make_attn_config(dtype, 2, 100, 4, 2, 64, scale=scale)
+        assert (bf.bf_op_attention_masked_bwd_work_bytes(cfg) > 0) == good
+        if not good:
+            refused("bf_op_attention_masked_fwd", C.byref(cfg), X, X, X, X, None, X, X, None)
