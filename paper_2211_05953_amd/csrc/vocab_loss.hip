@@ -260,15 +260,15 @@ Plan plan_for(bool pad, int dtype, int rows, int h_given, int V, int piece, bool
   if (!matrix && backward && !piece && cols > 4096) cols = 4096;
   p.unit = 8;
   if (matrix) {
+    // a forward product keeps nothing: the vocabulary in one, but for the 2^32 threads of a launch (512 to 256 x 256, 256 to 128 x 128 logits)
+    const size_t most = ((size_t)1 << 37) / rows / 256 * 256;
+    if (!backward && (!piece || cols > most)) cols = !piece && (size_t)V < most ? (size_t)V : most;
     // whole rounds of tiles and a rest: 2048 x 2048 x 50304 in pieces of 25600 (3.1 rounds of 256 x 256) and of 24576 (3), us for logits and dw of
     // one: 250 + 429 and 208 + 350
     const int round = gemm_mfma_logits_round(rows, h);
     if (!piece && round) {
-      if (!backward) cols = (size_t)V;  // the forward product keeps nothing
       if (cols >= (size_t)round) p.unit = round;
-    } else if (!backward && !piece) {
-      cols = (size_t)V;
-    } else if (!piece && cols < (size_t)V) {
+    } else if (backward && !piece && cols < (size_t)V) {
       cols = up((V + (V + cols - 1) / cols - 1) / ((V + cols - 1) / cols), 512);  // pieces of about the same size
     }
     cols = p.unit == 8 ? up(cols, 8) : cols / p.unit * p.unit;

@@ -267,3 +267,20 @@ def test_whole_tiles(T, h, V, piece, accumulate):
 @pytest.mark.parametrize("T,h,V,piece", [WHOLE[0], WHOLE[2], WHOLE[5]])
 def test_rows_without_a_label_leave_no_trace_on_whole_tiles(T, h, V, piece):
     _check(bf.BF_BF16, T, h, V, piece, poison=True)
+
+
+def test_the_most_rows():
+    """2^21 rows over a vocabulary whose tiles one launch does not hold: every 30011th row against fp64 (rows are independent)."""
+    T, h, V = 1 << 21, 8, (1 << 18) + 100
+    g = torch.Generator("cuda").manual_seed(5)
+    y, w = torch.randn(T, h, generator=g, device="cuda").bfloat16(), torch.randn(V, h, generator=g, device="cuda").bfloat16()
+    label = torch.randint(0, V, (T,), generator=g, device="cuda").int()
+    some = torch.arange(0, T, 30011, device="cuda")
+    label[some[0]], label[some[1]], label[some[2]] = V - 1, -1, 0
+    lse, rows, loss = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty(1, device="cuda")
+    bf.bf_op_vocab_loss_fwd(bf.BF_BF16, T, h, V, y, w, label, 1 / T, lse, rows, loss)
+    ref = _reference(y[some], w, label[some], 1 / T)
+    eps_z = (h + 64) * 2.0**-24 * float((y[some].double().abs() @ w.double().abs().t()).max()) + 2.0**-18
+    _within(lse[some], ref["lse"], eps_z + 2.0**-22 * ref["lse"].abs(), "lse")
+    _within(rows[some], ref["rows"], (2 * eps_z + 2.0**-21 * ref["lse"].abs()) / T, "rows")
+    assert abs(float(loss) - float(rows.double().sum())) <= 2.0**-23 * abs(float(loss))
