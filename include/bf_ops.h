@@ -140,7 +140,11 @@ bf_status bf_op_attention_bwd_static(int dtype, int kernels, int S_mb, int S_seq
                                      void* dqkv, void* stream);
 int bf_op_attention_uses_mfma(int S_seq, int S_head);
 
-/* Attention under masks, with capped scores, a distance bias and shared key / value heads (for sequences that hold several
+/* Masked attention here, and below the loss without logits and the clipping of gradients, are for training loops that call single kernels: the
+ * stack's own steps (bf.h) take no masks, keep their logits and clip nothing.  No output of these three overlaps an input or another output
+ * but where it says so.
+ *
+ * Attention under masks, with capped scores, a distance bias and shared key / value heads (for sequences that hold several
  * documents).  A row's keys are one interval, its span:
  *   _spans  from doc (device int32 [S_mb, S_seq], or NULL: a sequence is one document): a document is a run of equal ids; its
  *           tokens see that document and nothing else.  A token of a negative id is padding: it sees nothing and no token
@@ -203,8 +207,10 @@ bf_status bf_op_ce_loss(int dtype, int n_rows, int S_voc, void* z, const int32_t
  *         dy[n_rows, S_hidden] (`dtype`) = dz w_out;  dw[S_voc, S_hidden] (fp32) = (accumulate ? dw : 0) + dz^T y
  * labels: device int32 [n_rows].  A row whose label is outside 0..S_voc-1 has row_loss 0, dy 0 and no part in dw, whatever
  * its y holds.  Sums have a fixed order: no atomics.  bf16 tensors run on the
- * bf16 matrix cores with logits and statistics in fp32, dw to fp32 precision (rows that are not 16-byte aligned, S_hidden % 8 or
- * tensors that start elsewhere, through copies in the scratch); fp32 tensors as fp32 products.
+ * bf16 matrix cores with logits and statistics in fp32 (rows that are not 16-byte aligned, S_hidden % 8 or
+ * tensors that start elsewhere, through copies in the scratch); fp32 tensors as fp32 products.  dz enters the bf16 gradient products in bf16
+ * parts: dw's in three, from S_hidden 8192 and 257 rows on in two (dw 1e-6 and 1.7e-6 off), dy's in one, up to 256 rows in two (dy 1.9e-3 off, or its
+ * storage's rounding of 1.7e-3 alone).
  * S_piece: columns of a piece, in bf16 rounded up to whole chunks of 8 (0: the library's choice, 256 MiB of dz, and a bf16 forward, which
  * keeps nothing of a piece, in one; given, the scratch does not grow with the vocabulary); work: device scratch, 256-byte aligned, of
  * bf_op_vocab_loss_work_bytes(..., backward = 0 or 1) bytes (0 for bad sizes), owned by the caller; calls that overlap need
@@ -222,8 +228,9 @@ bf_status bf_op_vocab_loss_bwd(int dtype, int n_rows, int S_hidden, int S_voc, i
 bf_status bf_op_adam(size_t n, float* w, float* m, float* v, const float* g, void* w_lp, int t,
                      float lr, float beta1, float beta2, float adam_eps, float weight_decay, void* stream);
 
-/* Global gradient norm and clipping, over a list of tensors of one type (`dtype`: fp32 main-grads or bf16 gradients).  The
- * lists (g, dst, n, tensors) are host arrays, read during the call; the tensors they name are device memory, aligned to their
+/* Gradient norm and clipping, global over a list of tensors of one type (`dtype`: fp32 main-grads or bf16 gradients).  The list is
+ * what this process holds: where ranks hold parts of a model, the squares of their out[0] add up to the whole norm's, and the
+ * coefficient from that sum is the caller's to make (_scale and _adam_clipped take any).  The lists (g, dst, n, tensors) are host arrays, read during the call; the tensors they name are device memory, aligned to their
  * elements and no more.  A tensor of no elements is skipped, its pointers may be NULL.
  *
  *   out[0] = norm = sqrt(sum over all tensors and elements of g^2), squares and sums in fp64 and in a fixed order

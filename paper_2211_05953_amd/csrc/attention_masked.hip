@@ -108,6 +108,8 @@ __global__ __launch_bounds__(TOKENS) void spans_kernel(int S, int causal, const 
 }
 
 // ---- plain kernels: one wave per row, any head size up to 1024 -------------------------------------
+// Scalar products, a lane to a key: 500 tokens, 8 heads of 256 over 4, causal, bf16: forward 338 us (3 TFLOP/s), backward 2765.  For the sizes that the
+// matrix-core kernels have no form for, and to check them against.
 constexpr int PLAIN_HEAD = 1024, PER = PLAIN_HEAD / 64;
 
 __device__ __forceinline__ float wave_sum(float v) {

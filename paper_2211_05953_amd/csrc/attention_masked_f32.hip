@@ -224,7 +224,8 @@ struct QueryShared {
 // Forward (GRAD false) and dQ (GRAD true).  SEEN: tiles that are masked in part by sums_seen; without it returns whether one of
 // those held a non-finite value that enters a sum.
 // 2 x 500 queries, 8 heads of 80 over 2, bias and capped scores: forward 54 us, dQ 60, and the keys 77 (12, 16 and 17 TFLOP/s of 154): 256
-// workgroups, each wave a chain of two to four tiles.  A launch of one tile takes 24 us at D 128: rows, instructions, hand-over.
+// workgroups, each wave a chain of two to four tiles.  A launch of one tile takes 24 us at D 128: rows, instructions, hand-over.  dQ at D 128 on KG 1
+// keeps ten registers in scratch inside its loop, and rows that are no 16-byte chunks 20 to 80 in every form of D 128.
 template <int D, int KG, bool VEC, bool CAP, bool GRAD, bool SEEN>
 __device__ __forceinline__ bool query_rows(const MaskedArgs& a, QueryShared<D, KG>& sh) {
   constexpr int NT = KG == 1 ? 256 : 64, RB = KG == 1 ? ROWS : 32;  // threads that fetch a tile, rows of the workgroup

@@ -417,7 +417,7 @@ __global__ __launch_bounds__(2 * ROWS, 2) void masked_fwd_kernel(MaskedArgs a) {
 // Walks the keys twice.  First for delta = sum of P dP, in fp32 and kept for the dK / dV pass; then for dS = P (dP - delta) and
 // dQ = dS K.  The usual delta = dctx . ctx takes a ctx that was rounded when it was stored, which puts as large an error on every score
 // gradient of the row as their own rounding does where few keys share a row (8192 tokens, 16 heads of 128, sharp rows: dQ and dK
-// 2.8e-3 off in the 2-norm, 2.3e-3 so); it is two products and no sums, against three and their sums.
+// 2.8e-3 off in the 2-norm, 2.3e-3 so, the results' own rounding 1.7e-3); it is two products and no sums, against three and their sums, 35 % of the pass.
 // 64 heads of 128, 2048 tokens, causal: 209 us, matrix cores busy 41 %; 0.82 PFLOP/s with the first walk's products, 0.49 without.
 template <int D, int ROWS, bool VEC, int CAP, bool BIAS, bool SEEN>
 __device__ __forceinline__ bool dq_rows(const MaskedArgs& a, bf16_t (&KVs)[2][2][BLK * D]) {
@@ -586,7 +586,8 @@ __global__ __launch_bounds__(2 * ROWS, 2) void masked_dq_kernel(MaskedArgs a) {
 // have its successor's exponentials beside them, and a tile has one barrier; three LDS stages.
 // (One wave for the scores and P of both halves, the other for dP and dS, in fp32 through LDS and two barriers: 64 heads of 128,
 // 2048 tokens, causal 283 us, here 272, 0.51 PFLOP/s of the unmasked half's products; 2 x 16 heads of packed documents 119 and 94;
-// 8192 tokens with capped scores 967 and 1027, where each wave's exponentials and not the barriers set the time.)
+// 8192 tokens with capped scores 967 and 1027, where each wave's exponentials and not the barriers set the time: one form for all, as the others gain
+// more.)  Heads of 128 leave 8 registers in scratch around the loop's products, 16 and more where rows are no 16-byte chunks.
 // A workgroup walks the query tiles whose spans reach its keys, for every query head of its share of the key / value head's
 // group, one after the other in one chain of sums.
 constexpr int NTHR_DKV = 512;

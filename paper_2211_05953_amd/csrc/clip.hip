@@ -53,7 +53,7 @@ __device__ __forceinline__ int entry_of(const TB& t, uint32_t chunk) {
   return lo;
 }
 
-// 24 tensors of 4 to 16 Mi elements (0.94 GB) 159 us, 5.9 TB/s; 200 of 256 to 256 Ki (22 MB) 7.5 us and the last sums 3
+// 24 tensors of 4 to 16 Mi elements (0.94 GB) 159 us, 5.9 TB/s, in bf16 (0.43 GB) 80 us, 5.4; 200 of 256 to 256 Ki (22 MB) 7.5 us and the last sums 3
 template <typename T>
 __global__ __launch_bounds__(NT) void norm_kernel(NormTable t, double* __restrict__ part) {
   typedef typename Chunk<T>::V V;
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(NT) void norm_finish_kernel(const double* __restric
   out[1] = !(norm <= DBL_MAX) ? NAN : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
 }
 
-// (those 200: 44 MB read and written in two launches of 12 us)
+// (those 200: 44 MB read and written in two launches of 12 us; 24 tensors of 4 to 16 Mi 333 us in fp32 and 173 in bf16, 5.2 and 5.0 TB/s)
 template <typename T>
 __global__ __launch_bounds__(NT) void scale_kernel(ScaleTable t, const float* __restrict__ coef) {
   typedef typename Chunk<T>::V V;

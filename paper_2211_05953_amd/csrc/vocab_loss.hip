@@ -7,11 +7,11 @@
 // label's logit); a second kernel merges the tiles in their order.  No logit reaches HBM.  Backward: piece by piece of the
 // vocabulary, the product again with dz as its epilogue, then the two gradient products on that piece: 6 T h V operations
 // beside the forward pass's 2.
-// 2048 rows, 2048 x 50304, us in kernels: forward 436 (0.97 PFLOP/s), logits again 522, dW in three parts 1131 (1.12), dy 437.  8192 x 50304:
-// 1367 (1.23), 1469, 2991 in two parts (1.13), 1349.  Bound by the products: their rates are those of the same products elsewhere.
+// 2048 rows, 2048 x 50304, us in kernels: forward 402 (1.05 PFLOP/s), logits again 495, dW in three parts 1016 (1.25), dy 410.  8192 x 50304:
+// 1292 (1.31), 1379, 2766 in two parts (1.22), 1328.  Bound by the products: their rates are those of the same products elsewhere.
 //
-// Precision.  dW is an fp32 main-grad: dz enters its product as two or three bf16 parts (parts_of).  dy is stored in bf16: one
-// part, rounded once more than the result, as every bf16 tensor between kernels here.
+// Precision.  dW is an fp32 main-grad: dz enters its product as two or three bf16 parts (parts_of).  dy is stored in bf16: dz enters in
+// one part, rounded once more than the result, as every bf16 tensor between kernels here, or of few rows in two (dy_parts_of).
 //
 // Rows whose label is outside the vocabulary have no loss and no gradient, whatever their y holds: dz is set to zero, and dW's
 // product reads a copy of y in which those rows are zero (a zero times an infinity is a NaN).
@@ -179,15 +179,17 @@ __global__ __launch_bounds__(NT) void piece_dz_kernel(int cols, float* __restric
 // ---- sizes ---------------------------------------------------------------------------------------
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;  // of dz: what the memory-side cache holds, and little beside 288 GB
 
-// dz's parts, as many as it takes for what they drop (1.4e-6 of dz with two) to stay under the fp32 error of the logits, which grows with
-// their length: 5e-7 of dz at S_hidden 256, 1e-6 at 2048 and, in short sums, at 4184, 1.8e-6 at 8192 (dw at 2048: 1.5e-6 off with two
-// parts, 1e-6 with three; the third costs a sixth of 2048 rows' gradient).  Up to some 200 rows dW's product is the writing of dW, and the
+// dz's parts in dw's product.  Error of dw in the 2-norm and gradient's time, 2048 rows, 16384 columns: two parts 1.6e-6 to 1.75e-6 whatever
+// S_hidden; three, which leave the fp32 error of the logits and of the sums, 5.8e-7 at 1024 (388 us, two 320), 7.4e-7 at 4096 (1140, 925), 8.4e-7 at
+// 6144 (1697, 1383), 8.8e-7 at 7168 (1950, 1568), 9.3e-7 at 8192 (2162, 1763).  So the third part costs a fifth of the gradient at any size, and
+// is taken while it makes dw twice as exact, which ends between 7168 and 8192.  Up to some 200 rows dw's product is the writing of dw, and the
 // third part costs nothing.
 inline int parts_of(int rows, int h) { return rows <= 256 || h < 8192 ? 3 : 2; }
 
-// dy is stored in bf16, one rounding more than its product's operand.  Of few rows the largest of their dz, the label's, may fall where
-// bf16 is coarsest for all of them (one row: 2.6e-3 off in the 2-norm, a rounding alone 1.7e-3); a second part costs little
-// where reading w bounds the product.
+// dy is stored in bf16, and dz's rounding in one part is one more: 1.95e-3 off in the 2-norm at any number of rows, 1.66e-3, a rounding alone, with
+// two.  Of few rows the largest dz, the label's, may fall where bf16 is coarsest for all of them: at most over 60 draws 3.3e-3 (1.9e-3 with two parts) for
+// one row, 2.5e-3 for four, 2.2e-3 for 16, 2.0e-3 for 64 and more.  Two parts cost 13 % of the gradient up to 64 rows, where reading w bounds
+// the product, 23 % at 128, 27 % at 256 (2048 x 16384: 142 us, 180), and then buy the mean's seventh alone: 16 % at 300, 11 % at 1024.
 // One part is taken without the scale, which enters with dy's rounding: a label of small probability is then -1, whose rounding is none, and not
 // -scale, whose rounding all rows share (1720 rows of 64: 2.8e-3 off, 2.0e-3 so).  Its plane costs 2 to 4 % of the gradient.
 inline int dy_parts_of(int rows) { return rows <= 256 ? 2 : 1; }
@@ -245,7 +247,7 @@ int cols_at(const Plan& p, int c0, int V) {
 }
 
 // bf16 rows that are not whole 16-byte chunks, or do not start at one, are lengthened: copies of y and of a piece of w, the piece's dw and
-// dy's planes in the scratch (142 rows of 170, 58496 columns, loss and gradient: as fp32 products 1358 us, so 181).  Where the tensors start is not known when the scratch is sized: the larger of the two
+// dy's planes in the scratch (142 rows of 170, 58496 columns, loss and gradient: as fp32 products 1358 us, so 186; 138 for rows of 176, which are whole chunks).  Where the tensors start is not known when the scratch is sized: the larger of the two
 Plan plan_for(bool pad, int dtype, int rows, int h_given, int V, int piece, bool backward) {
   Plan p{};
   const bool matrix = dtype == BF_BF16;
