@@ -515,21 +515,23 @@ def bf_op_attention_spans(S_mb, S_seq, causal, doc, prefix, spans):
 
 def _token_rows(t, S_mb, S_seq, heads, S_head, ld):
     """Whether token (b, s) of `t` starts where the kernels look for it, (b S_seq + s) ld elements in, its heads side by side.  The dimensions are
-    (sequences, tokens, row), (all tokens, row), either with the row as (heads, S_head), or one; there may be more
+    (sequences, tokens, row) or (all tokens, row), the row one or several that end in S_head, or one for everything; there may be more
     sequences, tokens or columns than are used."""
     n = heads * S_head
     step = ld or n
-
-    def fits(*dims):  # (used, step between them); a step is met by nothing if one is used
-        return t.dim() == len(dims) and all(size >= used and (used == 1 or stride == want) for size, stride, (used, want) in zip(t.shape, t.stride(), dims))
-
-    tokens, flat = (S_mb * S_seq, step), (n, 1)
-    if fits((S_mb, S_seq * step), (S_seq, step), flat) or fits(tokens, flat):
-        return True
-    if t.dim() and t.shape[-1] == S_head and (fits((S_mb, S_seq * step), (S_seq, step), (heads, S_head), (S_head, 1)) or
-                                              fits(tokens, (heads, S_head), (S_head, 1))):
-        return True
-    return fits(((S_mb * S_seq - 1) * step + n, 1))
+    shape, stride = t.shape, t.stride()
+    for lead in (((S_mb, S_seq * step), (S_seq, step)), ((S_mb * S_seq, step),)):
+        at = len(lead)
+        if t.dim() <= at or (t.dim() > at + 1 and shape[-1] != S_head):
+            continue
+        dense = 1  # elements of the row's inner dimensions; a step is met by nothing if one is used
+        fits = all(size >= used and (used == 1 or x == want) for size, x, (used, want) in zip(shape, stride, lead))
+        for size, x in zip(reversed(shape[at:]), reversed(stride[at:])):
+            fits = fits and (size == 1 or x == dense)
+            dense *= size
+        if fits and dense >= n:
+            return True
+    return t.dim() == 1 and shape[0] >= (S_mb * S_seq - 1) * step + n and (shape[0] == 1 or stride[0] == 1)
 
 
 def _attn_tensors(who, cfg, spans, slopes, lse, rows):

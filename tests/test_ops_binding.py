@@ -27,6 +27,8 @@ def test_attention_rows_that_the_kernels_read_as_they_are(sizes):
     x = torch.zeros(B, S, n)
     assert fits(x) and fits(x, n) and fits(x.view(B * S, n)) and fits(x.view(B, S, H, d)) and fits(x.view(B * S, H, d)) and fits(x.view(-1))
     assert fits(torch.zeros(B + 1, S, n)) and fits(torch.zeros(B * S + 3, n)) and fits(torch.zeros(B * S * n + 7))
+    if H % 2 == 0:  # query heads by key / value head
+        assert fits(x.view(B, S, 2, H // 2, d)) and fits(x.view(B * S, H // 2, 2, d))
     wide = torch.zeros(B, S, 3 * n + 5)
     for at in (0, n, 2 * n):
         q = wide[..., at:at + n]
@@ -45,8 +47,11 @@ def test_attention_rows_that_the_kernels_would_misread():
         assert not fits(q, ld) and not fits(q.unflatten(2, (H, d)), ld) and not fits(torch.zeros(B * S, 3 * n)[:, :n], ld)
     x = torch.zeros(B, S, n)
     assert not fits(x, 2 * n)
+    # tokens in front of sequences, in their order and as a view
+    assert not fits(torch.zeros(S, B, n)) and not fits(torch.zeros(S, B, n).transpose(0, 1)) and not fits(torch.zeros(S, B, H, d))
     # heads in front of tokens, whole or as a view; rows that are not dense; a step of 0; too few tokens, heads or sequences
     assert not fits(torch.zeros(B, H, S, d)) and not fits(torch.zeros(B, H, S, d).transpose(1, 2)) and not fits(torch.zeros(B, S, d, H).transpose(2, 3))
+    assert not fits(torch.zeros(B, 2, S, H // 2, d)) and not fits(torch.zeros(B, S, H // 2, 2, d).transpose(2, 3)) and not fits(torch.zeros(B, S, d, H))
     assert not fits(x.transpose(0, 1)) and not fits(torch.zeros(B, n, S).transpose(1, 2)) and not fits(torch.zeros(B, S, 2 * n)[..., ::2])
     assert not fits(torch.zeros(1, S, n).expand(B, S, n)) and not fits(torch.zeros(B, 1, n).expand(B, S, n))
     assert not fits(torch.zeros(B, S, 2 * H, d)[:, :, ::2]) and not fits(torch.zeros(B, S, H, 2 * d)[..., :d])
