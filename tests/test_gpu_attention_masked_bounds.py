@@ -149,3 +149,38 @@ def test_scores_of_zero_under_the_largest_scale(dtype, cap):
                                              (1, 1200, 1, 1, 192, dict(docs=500, cap=30.0))])
 def test_long_sequences(dtype, B, S, H, KV, d, mask):
     Tight(dtype, B, S, H, KV, d, **mask).check()
+
+
+@pytest.mark.parametrize("dtype,S", [(BF16, 1 << 20), (FP32, 1 << 19)])
+def test_offsets_past_32_bits(dtype, S):
+    """Packed rows of 5.4 GB: documents of some hundred tokens at the beginning, across 2^32 bytes and at the end against fp64, each by itself."""
+    H, KV, d, t = 32, 4, 64, torch.bfloat16 if dtype == BF16 else torch.float32
+    widths = (H * d, KV * d, KV * d)
+    ld = sum(widths)
+    g = torch.Generator("cuda").manual_seed(3)
+    doc = (torch.rand(1, S, generator=g, device="cuda") < 1 / 200).int().cumsum(1).int()
+    qkv, dqkv = (torch.empty(1, S, ld, dtype=t, device="cuda") for _ in range(2))
+    ctx, dctx = (torch.empty(1, S, H * d, dtype=t, device="cuda") for _ in range(2))
+    for x in (qkv, dctx):
+        for part in x.split(1 << 17, 1):
+            part.copy_(torch.randn(part.shape, generator=g, device="cuda"))
+    (q, k, v), grads = qkv.split(widths, 2), dqkv.split(widths, 2)
+    cfg = bf.make_attn_config(dtype, 1, S, H, KV, d, ld_q=ld, ld_k=ld, ld_v=ld)
+    spans = torch.empty(bf.bf_op_attention_spans_elems(1, S), dtype=torch.int32, device="cuda")
+    bf.bf_op_attention_spans(1, S, 1, doc, None, spans)
+    lse = torch.empty(1, H, S, device="cuda")
+    bf.bf_op_attention_masked_fwd(cfg, q, k, v, spans, None, ctx, lse)
+    bf.bf_op_attention_masked_bwd(cfg, q, k, v, spans, None, ctx, lse, dctx, *grads)
+    past = 2**32 // (ld * qkv.element_size())
+    for at in (0, past, S - 1):
+        one = (doc[0] == doc[0, at]).nonzero()[:, 0]
+        a, b = int(one[0]), int(one[-1]) + 1
+        c = Tight(dtype, 1, b - a, H, KV, d, packed=0)
+        for mine, whole in ((c.q, q), (c.k, k), (c.v, v), (c.dctx, dctx)):
+            mine.copy_(whole[:, a:b])
+        want = c.want()
+        for name, x in zip(("ctx", "dq", "dk", "dv"), (ctx, *grads)):
+            w, bound = want[name]
+            assert float(((x[:, a:b].double() - w).abs() - bound).max()) <= 1e-30, (name, a, b)
+        w, bound = want["lse"]
+        assert float(((lse[:, :, a:b].double() - w).abs() - bound).max()) <= 0

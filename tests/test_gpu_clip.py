@@ -185,3 +185,35 @@ def test_captured_and_on_another_stream():
         torch.cuda.synchronize()
         assert torch.equal(o, out) and all(torch.equal(a, b) for a, b in zip(d, dst))
         assert all(torch.equal(a, b) for p, q in zip(first, state) for a, b in zip(p, q))
+
+
+def test_a_tensor_of_more_elements_than_an_entry_of_the_table_holds():
+    """2^30 and some elements: norm, scaled copy and Adam step, element by element on both sides of the cut and at the ends."""
+    n = (1 << 30) + 12345
+    g = torch.empty(n, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator("cuda").manual_seed(9)
+    for part in g.split(1 << 26):
+        part.copy_(torch.randn(part.numel(), generator=gen, device="cuda"))
+    out = torch.empty(2, device="cuda")
+    bf.bf_op_grad_norm(bf.BF_BF16, [g], 1000.0, out)
+    ref = math.sqrt(sum(float((p.double() ** 2).sum()) for p in g.split(1 << 26)))
+    coef = float(out[1])
+    assert abs(float(out[0]) - ref) <= 2.0**-23 * ref and abs(coef - 1000.0 / ref) <= 2.0**-23 * coef and coef < 1
+    dst = torch.zeros_like(g)
+    bf.bf_op_grad_scale(bf.BF_BF16, [g], [dst], out[1:])
+    for a, b in zip(g.split(1 << 26), dst.split(1 << 26)):
+        w = a.double() * coef
+        assert bool(((b.double() - w).abs() <= (2.0**-8 + 2.0**-23) * w.abs()).all())
+    del dst
+    w, m, v, f = (torch.zeros(n, device="cuda") for _ in range(4))
+    f.copy_(g)
+    del g
+    args = (1, 1e-2, 0.9, 0.99, 1e-8, 0.0)
+    bf.bf_op_adam_clipped([(w, m, v, f, None)], out[1:], *args)
+    for at in (0, (1 << 30) - 5000, n - 5000):
+        s = slice(at, at + 5000)
+        z = torch.zeros(5000, dtype=torch.float64, device="cuda")
+        rw, rm, rv = _adam_ref(z, z, z, (f[s] * out[1]).double(), *args)
+        assert bool(((m[s].double() - rm).abs() <= 2.0**-22 * rm.abs()).all()) and bool(((v[s].double() - rv).abs() <= 2.0**-21 * rv.abs()).all())
+        # the first step is lr g / (|g| + eps): a handful of roundings, and those of the square root's argument halved
+        assert bool(((w[s].double() - rw).abs() <= 2.0**-20 * rw.abs() + 1e-12).all())

@@ -284,3 +284,38 @@ def test_the_most_rows():
     _within(lse[some], ref["lse"], eps_z + 2.0**-22 * ref["lse"].abs(), "lse")
     _within(rows[some], ref["rows"], (2 * eps_z + 2.0**-21 * ref["lse"].abs()) / T, "rows")
     assert abs(float(loss) - float(rows.double().sum())) <= 2.0**-23 * abs(float(loss))
+
+
+def test_offsets_past_32_bits():
+    """w of 4.9 GB and dw of 9.8: the loss of every row, dy, and every 7919th row of dw and its last ones, against fp64."""
+    T, h, V = 5, 2048, 1200003
+    g = torch.Generator("cuda").manual_seed(6)
+    w = torch.empty(V, h, dtype=torch.bfloat16, device="cuda")
+    for part in w.split(1 << 18):
+        part.copy_(torch.randn(part.shape, generator=g, device="cuda") * (2 / math.sqrt(h)))
+    label = torch.tensor([V - 1, 0, -1, 1048577, 7], device="cuda").int()
+    y = torch.randn(T, h, generator=g, device="cuda").bfloat16()
+    lse, rows, loss = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty(1, device="cuda")
+    dy, dw = torch.empty_like(y), torch.empty(V, h, device="cuda")
+    bf.bf_op_vocab_loss_fwd(bf.BF_BF16, T, h, V, y, w, label, 0.5, lse, rows, loss)
+    bf.bf_op_vocab_loss_bwd(bf.BF_BF16, T, h, V, y, w, label, lse, 0.5, dy, dw)
+    yd, known = y.double(), label >= 0
+    z = torch.cat([yd @ part.double().t() for part in w.split(1 << 17)], 1)
+    eps_z = (h + 64) * 2.0**-24 * max(float((yd.abs() @ part.double().abs().t()).max()) for part in w.split(1 << 17)) + 2.0**-18
+    want = torch.logsumexp(z, 1)
+    _within(lse, want, eps_z + 2.0**-22 * want.abs(), "lse")
+    at = label.long().clamp_min(0)
+    row = torch.where(known, (want - z.gather(1, at[:, None])[:, 0]) * 0.5, 0.0)
+    _within(rows, row, (2 * eps_z + 2.0**-21 * want.abs()) * 0.5, "rows")
+    p = torch.exp(z - want[:, None]) * (0.5 * known)[:, None]
+    hot = torch.zeros_like(p).scatter_(1, at[:, None], (0.5 * known.double())[:, None])
+    dz, a = p - hot, p + hot
+    some = torch.cat([torch.arange(0, V, 7919, device="cuda"), torch.arange(V - 300, V, device="cuda"), at])
+    _within(dw[some], dz[:, some].t() @ yd, (eps_z + 2.0**-17 + (T + 64) * 2.0**-24) * (a[:, some].t() @ yd.abs()) + 1e-30, "dw")
+    want = b = 0
+    for i in range(0, V, 1 << 17):
+        s = slice(i, i + (1 << 17))
+        wd = w[s].double()
+        want = want + dz[:, s] @ wd
+        b = b + (eps_z + (V + 64) * 2.0**-24) * (a[:, s] @ wd.abs()) + 2.0**-8 * (dz[:, s].abs() @ wd.abs()) * 1.01
+    _within(dy, want, b + 2.0**-8 * want.abs() * 1.01, "dy")
