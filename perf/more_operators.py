@@ -1,0 +1,433 @@
+"""Operators of a training step that holds its products' operands and its optimizer states in 8 bits, as a program calls them.
+
+Four kinds: the forward pass of a linear layer (quantise the activations, multiply with kept weights), its backward pass (quantise
+the output's gradient both ways, input gradient, weight gradient), quantising a tensor both ways as the weights are after each
+optimizer step, and the clipped Adam step on 8-bit moments over many tensors.
+
+The 8-bit form of a tensor [rows, n]: codes [rows, n rounded up to 128] and one scale byte b = 127 + e for each 128 elements of a row,
+[n / 128 rounded up, rows rounded up to 16], e the smallest power of two that brings the block's largest value into the codes' range.
+
+With `own` set, run() makes the calls of paper_2211_05953_amd; without, it computes the same in elementary torch operations in
+32 bits.  exact() computes it from the definitions in 64 bits."""
+import math
+import random
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+CODES = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+BLOCK = 128
+LR, BETA1, BETA2, ADAM_EPS, DECAY, STEP, SEED = 1e-4, 0.9, 0.95, 1e-8, 0.1, 3, 0x5EED00000001
+V_TOP = 31744.0  # the largest code of a second moment: 4 bits of exponent, 4 of mantissa, no sign
+
+
+def _linear(**more):
+    return {"kind": "linear", "dtype": "bf16", "tokens": 1, "n_in": 1, "n_out": 1, "bias": 1, **more}
+
+
+def _back(**more):
+    return {"kind": "back", "dtype": "bf16", "tokens": 1, "n_in": 1, "n_out": 1, "grads": "e4m3", "dw": "fp32", **more}
+
+
+def listed():
+    return [
+        # A few tokens through a small layer of an odd width: launches and latency.
+        _linear(name="linear_small", tokens=33, n_in=250, n_out=1003),
+        # One token through a square layer of the 8192-wide stack: the weights are read once.
+        _linear(name="linear_token", n_in=8192, n_out=8192),
+        # The QKV projection of the 2048-wide stack on one sequence.
+        _linear(name="linear_2048", tokens=2048, n_in=2048, n_out=6144),
+        # The first linear layer of the MLP of the 8192-wide stack.
+        _linear(name="linear_8192", tokens=2048, n_in=8192, n_out=32768),
+        # Full precision around the product, sizes nobody rounded up.
+        _linear(name="linear_fp32_1000", dtype="fp32", tokens=1000, n_in=1000, n_out=4004, bias=0),
+        # Backward of a small model's layer on a short sequence, gradients in the format of wider range.
+        _back(name="back_small", tokens=60, n_in=256, n_out=1024, grads="e5m2"),
+        # Backward of the first MLP layer of the 2048-wide stack, weight gradient as fp32 main-grads are.
+        _back(name="back_2048", tokens=2048, n_in=2048, n_out=8192),
+        # Backward of the first MLP layer of the 8192-wide stack, weight gradient in bf16: taken once for a stage and stepped on at once.
+        _back(name="back_8192", tokens=2048, n_in=8192, n_out=32768, dw="bf16"),
+        # A master weight of odd sizes, both ways.
+        {"name": "pack_odd", "kind": "pack", "dtype": "fp32", "rows": 250, "cols": 1003, "format": "e4m3"},
+        # A weight of the 8192-wide stack after the optimizer step, both ways.
+        {"name": "pack_8192", "kind": "pack", "dtype": "bf16", "rows": 8192, "cols": 32768, "format": "e4m3"},
+        # The many small tensors of a small model.
+        {"name": "adam_small", "kind": "adam", "dtype": "fp32", "tensors": 200, "low": 256, "high": 262144, "odd": 1},
+        # A rank's share of the parameters.
+        {"name": "adam_large", "kind": "adam", "dtype": "fp32", "tensors": 24, "low": 4194304, "high": 16777216, "odd": 0},
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind, dtype = rng.choice(["linear", "linear", "back", "back", "pack", "adam"]), rng.choice(["bf16", "bf16", "fp32"])
+    width = lambda: rng.choice([_log(rng, 16, 32768), _log(rng, 64, 32768) // 64 * 64, _log(rng, 128, 32768) // 128 * 128])  # noqa: E731
+    if kind in ("linear", "back"):
+        n_in, n_out = width(), width()
+        tokens = _log(rng, 1, max(1, min(8192, 2**39 // (n_in * n_out))))
+        sizes = {"dtype": dtype, "tokens": tokens, "n_in": n_in, "n_out": n_out}
+        return _linear(bias=rng.choice([0, 1]), **sizes) if kind == "linear" else _back(grads=rng.choice(["e4m3", "e5m2"]), dw=rng.choice(["bf16", "fp32"]), **sizes)
+    if kind == "pack":
+        rows = rng.choice([width(), _log(rng, 1, 8192)])
+        cols = min(width(), 2**27 // rows)
+        return {"kind": kind, "dtype": dtype, "rows": rows, "cols": cols, "format": rng.choice(["e4m3", "e4m3", "e5m2"])}
+    tensors = _log(rng, 1, 300)
+    high = min(_log(rng, 16, 2**24), 2**27 // tensors)
+    return {"kind": kind, "dtype": dtype, "tensors": tensors, "low": rng.randint(1, max(1, high // 4)), "high": high, "odd": rng.choice([0, 1])}
+
+
+def _up(n, to):
+    return -(-n // to) * to
+
+
+def _sizes(case):
+    """Elements of the tensors of an Adam case, the same ones for every seed, where each starts in its arena, and its length."""
+    rng = random.Random(case["tensors"] * 1000003 + case["high"])
+    sizes = [_log(rng, case["low"], case["high"]) for _ in range(case["tensors"])]
+    if not case["odd"]:
+        sizes = [max(1, n // 64 * 64) for n in sizes]
+    starts, at = [], 0
+    for n in sizes:
+        starts.append(at)
+        at += n if case["odd"] else _up(n, 128)
+    return sizes, starts, at
+
+
+def work(case):
+    """Every input read once, every output written once, two operations per multiplication and addition of the products."""
+    size = 2 if case["dtype"] == "bf16" else 4
+    if case["kind"] in ("linear", "back"):
+        t, k, n = case["tokens"], case["n_in"], case["n_out"]
+        if case["kind"] == "linear":
+            return {"bytes": size * t * (k + n) + k * n, "flops": 2 * t * k * n}
+        return {"bytes": size * t * (k + n) + k * n + t * k + (2 if case["dw"] == "bf16" else 4) * k * n, "flops": 4 * t * k * n}
+    if case["kind"] == "pack":
+        n = case["rows"] * case["cols"]
+        return {"bytes": n * (size + 2), "flops": 4 * n}
+    n = sum(_sizes(case)[0])
+    return {"bytes": n * (8 + size + 4 + 2 + 4), "flops": n * 40}
+
+
+# ---- 8-bit forms, elementwise ---------------------------------------------------------------------
+def _two(e):
+    """2^e of whole numbers, exactly, down to the smallest numbers of 32 bits (exp2 is off by a rounding on the GPU)."""
+    a = e.int() // 2
+    return ((a + 127) << 23).view(torch.float32) * ((e.int() - a + 127) << 23).view(torch.float32)
+
+
+def _pack(x, fmt):
+    """Codes (as numbers of the 8-bit type) and scale bytes of the rows of x."""
+    rows, n = x.shape
+    lines = _up(n, BLOCK) // BLOCK
+    x = torch.nn.functional.pad(x.float(), (0, lines * BLOCK - n)).view(rows, lines, BLOCK)
+    top = x.abs().amax(2)
+    part, power = torch.frexp(top)  # 448 = 0.875 * 2^9, 57344 = 0.875 * 2^16
+    e = power - (9 if fmt == "e4m3" else 16) + (part > 0.875).int()
+    e = torch.where(top == 0, 0, e.clamp(min=-127))
+    q = (x * _two(-e)[:, :, None]).to(CODES[fmt]).view(rows, lines * BLOCK)
+    scale = torch.full((lines, _up(rows, 16)), 127, dtype=torch.uint8, device=x.device)
+    scale[:, :rows] = (e.t() + 127).to(torch.uint8)
+    return q, scale
+
+
+def _values(q, scale, n):
+    """What codes and scales stand for, in 32 bits."""
+    rows, lines = q.shape[0], scale.shape[0]
+    return (q.float().view(rows, lines, BLOCK) * _two(scale[:, :rows].t().int() - 127)[:, :, None]).view(rows, lines * BLOCK)[:, :n]
+
+
+def _state_bytes(n):
+    return _up(n, BLOCK) // BLOCK * 258
+
+
+def _pack_state(m, v):
+    """The 8-bit state of the moments of one tensor: blocks of 128 codes of m and 128 of v, then the blocks' scale bytes in pairs."""
+    n = m.numel()
+    lines = _up(n, BLOCK) // BLOCK
+    q, scale = _pack(torch.nn.functional.pad(m, (0, lines * BLOCK - n)).view(lines, BLOCK), "e4m3")
+    v = torch.nn.functional.pad(v, (0, lines * BLOCK - n)).view(lines, BLOCK)
+    part, power = torch.frexp(v.amax(1))
+    e = (power - 15 + (part > 0.96875).int()).clamp(min=-127)
+    y = v * _two(-e)[:, None]
+    ey = (torch.frexp(y)[1] - 1).clamp(min=0)
+    codes = (ey * 16 + torch.round(y * _two(4 - ey)).int()).to(torch.uint8)
+    codes = torch.stack([q.view(torch.uint8), codes], 1).view(-1)
+    return torch.cat([codes, torch.stack([scale[0, :lines], (e + 127).to(torch.uint8)], 1).view(-1)])
+
+
+def _moments(state):
+    """The moments that a state stands for, whole blocks of them, in 32 bits."""
+    lines = state.numel() // 258
+    codes, scales = state[: lines * 256].view(lines, 2, BLOCK), _two(state[lines * 256 :].view(lines, 2).int() - 127)
+    m = codes[:, 0].contiguous().view(torch.float8_e4m3fn).float() * scales[:, :1]
+    c = codes[:, 1].int()
+    v = torch.where(c < 16, c / 16, (16 + c % 16) * _two(c // 16 - 5)) * scales[:, 1:]
+    return m, v
+
+
+def _hash(x):
+    """A mixing of 32-bit whole numbers (held in 64): xor shifts and odd multipliers (32 bits of the fractions of sqrt 2 and sqrt 3)."""
+    x = x ^ (x >> 15)
+    x = (x * 0x6A09E667) & 0xFFFFFFFF
+    x = x ^ (x >> 13)
+    x = (x * 0xBB67AE85) & 0xFFFFFFFF
+    return x ^ (x >> 16)
+
+
+def _random(tensor, lines):
+    """Two random numbers of 16 bits for each element of a tensor's blocks, from seed, step and place."""
+    key = _hash(_hash(_hash(_hash(SEED & 0xFFFFFFFF) ^ (SEED >> 32)) ^ STEP) ^ tensor)
+    h = _hash((torch.arange(lines * BLOCK, device=DEV) + key) & 0xFFFFFFFF).view(lines, BLOCK)
+    return h & 0xFFFF, h >> 16
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    normal = lambda *shape: torch.randn(shape, generator=g, device=DEV)  # noqa: E731
+    uniform = lambda *shape: torch.rand(shape, generator=g, device=DEV)  # noqa: E731
+    dtype = TYPES[case["dtype"]]
+    s = dict(case)
+    if case["kind"] in ("linear", "back"):
+        t, k, n = case["tokens"], case["n_in"], case["n_out"]
+        # activations after a norm with a gain, a few channels of them large; gradients whose size differs from token to token
+        x = (normal(t, k) * (1 + 20 * (uniform(k) < 0.01))).to(dtype)
+        w = normal(k, n) / math.sqrt(k)
+        if case["kind"] == "linear":
+            s["x"], s["w8"] = x, _pack(w.t(), "e4m3")
+            s["b"] = normal(n) if case["bias"] else None
+        else:
+            s["dy"] = (normal(t, n) * (1e-4 * 10.0 ** (-3 * uniform(t, 1)))).to(dtype)
+            s["w8"], s["x8"] = _pack(w, "e4m3"), _pack(x.t(), "e4m3")
+    elif case["kind"] == "pack":
+        s["x"] = (normal(case["rows"], case["cols"]) * (0.02 * (1 + 10 * uniform(1, case["cols"])))).to(dtype)
+    else:
+        sizes, starts, total = _sizes(case)
+        cut = lambda x: [x[a : a + n] for a, n in zip(starts, sizes)]  # noqa: E731
+        s["grads"] = cut((normal(total) * 1e-3 * (1 + 3 * uniform(total))).to(dtype))
+        w, m, v = normal(total) * 0.02, normal(total) * 1e-4, uniform(total) * 1e-8
+        s["arena"] = {"w": w, "w_lp": w.to(torch.bfloat16)}
+        s["state"] = list(zip(cut(w), cut(s["arena"]["w_lp"]), [_pack_state(a, b) for a, b in zip(cut(m), cut(v))]))
+        s["coef"] = torch.full((1,), 0.75, device=DEV)
+        s["m"], s["v"] = torch.zeros(total, dtype=torch.bfloat16, device=DEV), torch.zeros(total, dtype=torch.bfloat16, device=DEV)
+        s["moments"] = list(zip(cut(s["m"]), cut(s["v"])))
+    return s
+
+
+# ---- the framework's calls ----------------------------------------------------------------------
+def _own_quantize(bf, x, fmt, along, down):
+    """The 8-bit forms of x along its rows and down its columns, where asked for."""
+    rows, cols = x.shape
+    new = lambda r, n: (torch.empty(r, bf.bf_op_fp8_row_bytes(n), dtype=torch.uint8, device=DEV),  # noqa: E731
+                        torch.empty(bf.bf_op_fp8_scale_elems(r, n), dtype=torch.uint8, device=DEV))
+    a, d = new(rows, cols) if along else (None, None), new(cols, rows) if down else (None, None)
+    bf.bf_op_fp8_quantize(bf.BF_BF16 if x.dtype is torch.bfloat16 else bf.BF_FP32, bf.BF_E4M3 if fmt == "e4m3" else bf.BF_E5M2, rows, cols, x, *a, *d)
+    return a, d
+
+
+def _own_linear(s):
+    import paper_2211_05953_amd as bf
+
+    t, k, n = s["tokens"], s["n_in"], s["n_out"]
+    (q, scale), _ = _own_quantize(bf, s["x"], "e4m3", True, False)
+    y = torch.empty(t, n, dtype=s["x"].dtype, device=DEV)
+    bf.bf_op_fp8_gemm(bf.BF_E4M3, bf.BF_E4M3, bf.BF_BF16 if s["dtype"] == "bf16" else bf.BF_FP32, t, n, k, q, scale, *s["w8"], y, bias=s["b"])
+    return {"y": y}
+
+
+def _own_back(s):
+    import paper_2211_05953_amd as bf
+
+    t, k, n = s["tokens"], s["n_in"], s["n_out"]
+    fmt = bf.BF_E4M3 if s["grads"] == "e4m3" else bf.BF_E5M2
+    a, d = _own_quantize(bf, s["dy"], s["grads"], True, True)
+    dx, dw = torch.empty(t, k, dtype=s["dy"].dtype, device=DEV), torch.empty(k, n, dtype=TYPES[s["dw"]], device=DEV)
+    bf.bf_op_fp8_gemm(fmt, bf.BF_E4M3, bf.BF_BF16 if s["dtype"] == "bf16" else bf.BF_FP32, t, k, n, *a, *s["w8"], dx)
+    bf.bf_op_fp8_gemm(bf.BF_E4M3, fmt, bf.BF_BF16 if s["dw"] == "bf16" else bf.BF_FP32, k, n, t, *s["x8"], *d, dw)
+    return {"dx": dx, "dw": dw}
+
+
+def _whole(q, scale, fmt, rows, cols):
+    """Codes as the numbers that they are, and the scales of their blocks."""
+    lines = _up(cols, BLOCK) // BLOCK
+    return {"q": q.view(CODES[fmt]).view(rows, lines * BLOCK), "scale": scale.view(lines, _up(rows, 16))}
+
+
+def _own_pack(s):
+    import paper_2211_05953_amd as bf
+
+    a, d = _own_quantize(bf, s["x"], s["format"], True, True)
+    return {"along": _whole(*a, s["format"], s["rows"], s["cols"]), "down": _whole(*d, s["format"], s["cols"], s["rows"])}
+
+
+def _own_adam(s):
+    import paper_2211_05953_amd as bf
+
+    bf.bf_op_adam8(bf.BF_BF16 if s["dtype"] == "bf16" else bf.BF_FP32, [(w, state, g, lp) for (w, lp, state), g in zip(s["state"], s["grads"])], s["coef"],
+                   SEED, STEP, LR, BETA1, BETA2, ADAM_EPS, DECAY)
+    bf.bf_op_adam8_moments(bf.BF_BF16, [(state, m, v) for (_, _, state), (m, v) in zip(s["state"], s["moments"])])
+    return {**s["arena"], "m": s["m"], "v": s["v"]}
+
+
+# ---- the plain form ---------------------------------------------------------------------------------
+def _plain_linear(s):
+    y = _values(*_pack(s["x"], "e4m3"), s["n_in"]) @ _values(*s["w8"], s["n_in"]).t()
+    return {"y": (y if s["b"] is None else y + s["b"]).to(s["x"].dtype)}
+
+
+def _plain_back(s):
+    dy, down = _values(*_pack(s["dy"], s["grads"]), s["n_out"]), _values(*_pack(s["dy"].t(), s["grads"]), s["tokens"])
+    dx, dw = dy @ _values(*s["w8"], s["n_out"]).t(), _values(*s["x8"], s["tokens"]) @ down.t()
+    return {"dx": dx.to(s["dy"].dtype), "dw": dw.to(TYPES[s["dw"]])}
+
+
+def _plain_pack(s):
+    return {"along": dict(zip(("q", "scale"), _pack(s["x"], s["format"]))), "down": dict(zip(("q", "scale"), _pack(s["x"].t(), s["format"])))}
+
+
+def _at_random(y, lowest, bits, r):
+    """y >= 0 on a grid of `bits` bits of mantissa down to 2^lowest and even below, up where the random number says so."""
+    step = _two((torch.frexp(y)[1] - 1).clamp(min=lowest) - bits)
+    return (((y / step * 65536).floor().long() + r) >> 16).float() * step
+
+
+def _adam_one(w, w_lp, state, g, coef, tensor, out_m, out_v):
+    n, lines = w.numel(), state.numel() // 258
+    m, v = _moments(state)
+    gg = torch.nn.functional.pad(g.float() * coef, (0, lines * BLOCK - n)).view(lines, BLOCK)
+    m = BETA1 * m + (1 - BETA1) * gg
+    v = BETA2 * v + (1 - BETA2) * gg * gg
+    step = ((m / (1 - BETA1**STEP)) / ((v / (1 - BETA2**STEP)).sqrt() + ADAM_EPS)).view(-1)[:n]
+    w.sub_(LR * (step + DECAY * w))
+    w_lp.copy_(w)
+    # back into 8 bits
+    rm, rv = _random(tensor, lines)
+    part, power = torch.frexp(m.abs().amax(1))
+    em = (power - 9 + (part > 0.875).int()).clamp(min=-127)
+    part, power = torch.frexp(v.amax(1))
+    ev = (power - 15 + (part > 0.96875).int()).clamp(min=-127)
+    unit_m, unit_v = _two(em)[:, None], _two(ev)[:, None]
+    qm = _at_random(m.abs() / unit_m, -6, 3, rm).clamp(max=448).copysign(m)
+    qv = _at_random(v / unit_v, 0, 4, rv).clamp(max=V_TOP)
+    qv = torch.where((v > 0) & (qv == 0), 0.0625, qv)  # a second moment above zero stays above it
+    ey = (torch.frexp(qv)[1] - 1).clamp(min=0)
+    codes = torch.stack([qm.to(torch.float8_e4m3fn).view(torch.uint8), (ey * 16 + qv * _two(4 - ey)).to(torch.uint8)], 1)
+    state[: lines * 256] = codes.view(-1)
+    state[lines * 256 :] = torch.stack([em + 127, ev + 127], 1).to(torch.uint8).view(-1)
+    out_m.copy_((qm * unit_m).view(-1)[:n])
+    out_v.copy_((qv * unit_v).view(-1)[:n])
+
+
+def _plain_adam(s):
+    _ = [_adam_one(*x, g, s["coef"], i, *o) for i, (x, g, o) in enumerate(zip(s["state"], s["grads"], s["moments"]))]
+    return {**s["arena"], "m": s["m"], "v": s["v"]}
+
+
+def run(state):
+    if own:
+        return {"linear": _own_linear, "back": _own_back, "pack": _own_pack, "adam": _own_adam}[state["kind"]](state)
+    return {"linear": _plain_linear, "back": _plain_back, "pack": _plain_pack, "adam": _plain_adam}[state["kind"]](state)
+
+
+# ---- the definitions in 64 bits -----------------------------------------------------------------------
+def _power(e):
+    """2^e of whole numbers held in 64 bits, exactly."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
+def _exact_codes(x, fmt):
+    """(the 8-bit numbers of the blocks of x's rows, the blocks' powers of two), [rows, blocks, 128] and [rows, blocks], in 64 bits."""
+    top, lowest, bits = (448.0, -6, 3) if fmt == "e4m3" else (57344.0, -14, 2)
+    rows, n = x.shape
+    blocks = torch.zeros(rows, -(-n // 128) * 128, dtype=torch.float64, device=x.device)
+    blocks[:, :n] = x
+    blocks = blocks.reshape(rows, -1, 128)
+    most = blocks.abs().max(2).values
+    e = torch.where(most > 0, torch.ceil(torch.log2(most / top)).clamp(min=-127), 0.0)
+    y = blocks / _power(e)[:, :, None]
+    grid = _power(torch.floor(torch.log2(y.abs())).clamp(min=lowest) - bits)
+    return torch.round(y / grid) * grid, e
+
+
+def _exact_values(x, fmt):
+    y, e = _exact_codes(x, fmt)
+    return (y * _power(e)[:, :, None]).reshape(x.shape[0], -1)[:, : x.shape[1]]
+
+
+def _exact_kept(kept, n):
+    q, scale = kept
+    unit = _power(scale[:, : q.shape[0]].t().long() - 127)
+    return (q.double() * unit.repeat_interleave(128, 1))[:, :n]
+
+
+def _exact_linear(s):
+    y = _exact_values(s["x"].double(), "e4m3").mm(_exact_kept(s["w8"], s["n_in"]).t())
+    return {"y": y if s["b"] is None else y + s["b"].double()}
+
+
+def _exact_back(s):
+    dy = s["dy"].double()
+    dx = _exact_values(dy, s["grads"]).mm(_exact_kept(s["w8"], s["n_out"]).t())
+    return {"dx": dx, "dw": _exact_kept(s["x8"], s["tokens"]).mm(_exact_values(dy.t(), s["grads"]).t())}
+
+
+def _exact_pack(s):
+    x = s["x"].double()
+    return {"along": {"q": _exact_codes(x, s["format"])[0], "scale": None}, "down": {"q": _exact_codes(x.t(), s["format"])[0], "scale": None}}
+
+
+def _mixed(x):
+    for shift, factor in ((15, 0x6A09E667), (13, 0xBB67AE85), (16, 1)):
+        x = ((x ^ (x >> shift)) * factor) % 2**32
+    return x
+
+
+def _rounded(y, bits, lowest, top, chance):
+    """y on the 8-bit grid, up with the chance of its distance from the value below (as whole 65536ths)."""
+    grid = _power(torch.floor(torch.log2(y)).clamp(min=lowest) - bits)
+    below = torch.floor(y / grid)
+    part = torch.floor((y / grid - below) * 65536)
+    return ((below + (part + chance >= 65536)) * grid).clamp(max=top)
+
+
+def _exact_adam(s):
+    sizes, starts, total = _sizes(s)
+    out = {k: torch.zeros(total, dtype=torch.float64, device=DEV) for k in ("w", "w_lp", "m", "v")}
+    for k in ("w", "w_lp"):
+        out[k] += s["arena"][k].double()
+    key = 0
+    for word in (SEED % 2**32, SEED // 2**32, STEP):
+        key = _mixed(key ^ word)
+    for i, (at, n) in enumerate(zip(starts, sizes)):
+        part, blocks, state = slice(at, at + n), -(-n // 128), s["state"][i][2]
+        codes, scales = state[: 256 * blocks].reshape(blocks, 256), state[256 * blocks :].reshape(blocks, 2).double()
+        c = codes[:, 128:].double()
+        field, low = torch.floor(c / 16), c % 16
+        m = codes[:, :128].contiguous().view(torch.float8_e4m3fn).double() * _power(scales[:, :1] - 127)
+        v = torch.where(field > 0, (1 + low / 16) * _power(field - 1), low / 16) * _power(scales[:, 1:] - 127)
+        g = torch.zeros(blocks * 128, dtype=torch.float64, device=DEV)
+        g[:n] = s["grads"][i].double() * s["coef"].double()
+        g = g.reshape(blocks, 128)
+        m, v = m + (1 - BETA1) * (g - m), v + (1 - BETA2) * (g * g - v)
+        w = out["w"][part]
+        rate = m / (1 - BETA1**STEP) / (torch.sqrt(v / (1 - BETA2**STEP)) + ADAM_EPS)
+        w = w - LR * (rate.reshape(-1)[:n] + DECAY * w)
+        h = _mixed((torch.arange(blocks * 128, device=DEV) + _mixed(key ^ i)) % 2**32).reshape(blocks, 128)
+        unit_m = _power(torch.ceil(torch.log2(m.abs().max(1).values / 448)).clamp(min=-127))[:, None]
+        unit_v = _power(torch.ceil(torch.log2(v.max(1).values / 31744)).clamp(min=-127))[:, None]
+        qm = torch.sign(m) * _rounded(m.abs() / unit_m, 3, -6, 448, h % 65536)
+        qv = _rounded(v / unit_v, 4, 0, 31744, h // 65536)
+        qv = torch.where((v > 0) & (qv == 0), 1 / 16, qv)
+        out["w"][part], out["w_lp"][part], out["m"][part], out["v"][part] = w, w, (qm * unit_m).reshape(-1)[:n], (qv * unit_v).reshape(-1)[:n]
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"linear": _exact_linear, "back": _exact_back, "pack": _exact_pack, "adam": _exact_adam}[case["kind"]](s)
