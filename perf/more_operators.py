@@ -200,11 +200,11 @@ def prepare(case, seed):
         x = (normal(t, k) * (1 + 20 * (uniform(k) < 0.01))).to(dtype)
         w = normal(k, n) / math.sqrt(k)
         if case["kind"] == "linear":
-            s["x"], s["w8"] = x, _pack(w.t(), "e4m3")
+            s["x"], s["w8"] = x, _pack(w.t().contiguous(), "e4m3")
             s["b"] = normal(n) if case["bias"] else None
         else:
             s["dy"] = (normal(t, n) * (1e-4 * 10.0 ** (-3 * uniform(t, 1)))).to(dtype)
-            s["w8"], s["x8"] = _pack(w, "e4m3"), _pack(x.t(), "e4m3")
+            s["w8"], s["x8"] = _pack(w, "e4m3"), _pack(x.t().contiguous(), "e4m3")
     elif case["kind"] == "pack":
         s["x"] = (normal(case["rows"], case["cols"]) * (0.02 * (1 + 10 * uniform(1, case["cols"])))).to(dtype)
     else:
