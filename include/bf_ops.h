@@ -255,6 +255,66 @@ typedef struct {
 bf_status bf_op_adam_clipped(int n_tensors, const bf_adam_tensor* tensors, const float* coef, int t, float lr, float beta1,
                              float beta2, float adam_eps, float weight_decay, void* stream);
 
+/* Training in 8 bits: operands of products as 8-bit floating-point codes with a scale for each block of 128, and Adam's moments in 8 bits.
+ * These are for training loops that call single kernels, beside bf_op_gemm and bf_op_adam_clipped; the stack's own steps do not use them.
+ *
+ * The 8-bit form of a matrix of `rows` rows of n elements, blocks along its rows:
+ *   codes   [rows][bf_op_fp8_row_bytes(n)] bytes (n rounded up to 128; zeros behind element n): BF_E4M3 (largest value 448) or
+ *           BF_E5M2 (57344; its infinities are not used)
+ *   scales  [ceil(n / 128)][rows rounded up to 16] bytes, bf_op_fp8_scale_elems(rows, n) in all: byte b stands for 2^(b - 127); element k of row r
+ *           is code[r][k] * 2^(scale[k / 128][r] - 127).  Bytes behind the last row are 127.
+ * Both 16-byte aligned.  A linear layer y = x W (x [T, h_in], W [h_in, h_out]) takes, as A and B of bf_op_fp8_gemm:
+ *   forward          y  [T, h_out]      x along its rows      W down its columns
+ *   input gradient   dx [T, h_in]       dy along its rows     W along its rows
+ *   weight gradient  dW [h_in, h_out]   x down its columns    dy down its columns
+ *
+ * _quantize  the forms of x [rows, cols] (`dtype`, rows ld_x elements apart, 0: cols) along its rows (q, scale) and down its columns (qt, scale_t: the
+ *            form of the transpose), either pair or both in one pass over x; NULL: not that one.  The scale is the smallest power of two, 2^-127 or
+ *            more, that brings the block's largest finite value into the format's range (of a block of zeros 2^0), codes are rounded once, to nearest
+ *            even; infinities and NaN become NaN codes and leave the others as they are.  rows, cols up to 2^21.
+ * _gemm      C[M,N] = A B^T + bias + R from the forms A [M, K] and B [N, K], dense C and R [M, N] in `dtype`, bias fp32 [N]; bias, R may be NULL,
+ *            R may be C.  accumulate = 1 (fp32 only): C += that.  A bf16 C comes from the 8-bit matrix instructions, whose sums inside a block keep about 16
+ *            bits (1.5e-5 of the result for normal operands, 8e-5 with large outliers in every block: under bf16's rounding of 1.7e-3); an fp32 C
+ *            from operands widened to bf16, exactly, with fp32 sums.  Sums have a fixed order: no atomics.  work: device scratch, 256-byte
+ *            aligned, of _work_bytes(M, N, K) bytes (0: none needed, or bad sizes), owned by the caller; calls that overlap need their own.
+ *            Sizes are 1 to 2^21. */
+typedef enum { BF_E4M3 = 0, BF_E5M2 = 1 } bf_fp8_format;
+size_t bf_op_fp8_row_bytes(int n);
+size_t bf_op_fp8_scale_elems(int rows, int n);
+bf_status bf_op_fp8_quantize(int dtype, int format, int rows, int cols, const void* x, size_t ld_x, void* q, void* scale, void* qt, void* scale_t,
+                             void* stream);
+size_t bf_op_fp8_gemm_work_bytes(int M, int N, int K);
+bf_status bf_op_fp8_gemm(int format_a, int format_b, int dtype, int M, int N, int K, const void* A, const void* scale_a, const void* B,
+                         const void* scale_b, void* C, const float* bias, const void* R, int accumulate, void* work, size_t work_bytes, void* stream);
+
+/* bf_op_adam_clipped with both moments of a tensor in 8 bits (2 1/64 bytes per parameter instead of 8):
+ *   state   device, 16-byte aligned, bf_op_adam8_state_bytes(n) bytes: for each 128 elements 128 codes of m (BF_E4M3) and 128 of v, and
+ *           behind all blocks two scale bytes for each (m's and v's; 2^(b - 127) as above).  v's codes have no sign: 4 bits of exponent, 4 of mantissa,
+ *           code c below 16 is c / 16, above (1 + c % 16 / 16) 2^(c / 16 - 1).  All zero bytes: moments of zero.
+ *   g       fp32 or bf16 (`dtype`), used times coef[0]
+ * The step is taken from the moments before they are rounded.  They are then rounded at random, up with the chance of their distance from the code below
+ * (in 65536ths): a mean that moves by less than half a code each step still moves.  The random numbers are a hash of (seed, t, the tensor's place
+ * in the list, element): the same call gives the same bits.  A v above zero is kept at the smallest code or more, 2^-18.95 of the block's
+ * largest, so that no step is divided by a v that was rounded away.  t and seed are values of the call: a captured graph repeats them.
+ * A coefficient that is not finite leaves the step out.  No two tensors may overlap. */
+typedef struct {
+  float* w;
+  void* state;
+  const void* g;
+  void* w_lp; /* bf16 copy of w to refresh, or NULL */
+  size_t n;
+} bf_adam8_tensor;
+size_t bf_op_adam8_state_bytes(size_t n);
+bf_status bf_op_adam8(int dtype, int n_tensors, const bf_adam8_tensor* tensors, const float* coef, uint64_t seed, int t, float lr, float beta1, float beta2,
+                      float adam_eps, float weight_decay, void* stream);
+/* What states stand for: m and v of n elements each in `dtype` (bf16 holds every code times its scale exactly, but under 2^-126), either may be NULL. */
+typedef struct {
+  const void* state;
+  void *m, *v;
+  size_t n;
+} bf_adam8_moments_tensor;
+bf_status bf_op_adam8_moments(int dtype, int n_tensors, const bf_adam8_moments_tensor* tensors, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

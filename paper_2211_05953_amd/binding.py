@@ -14,6 +14,7 @@ BF_FP32, BF_BF16 = 0, 1
 BF_CKPT_NONE, BF_CKPT_LAYER = 0, 1
 BF_KERNELS_AUTO, BF_KERNELS_PLAIN = 0, 1
 BF_NN, BF_NT, BF_TN = 0, 1, 2
+BF_E4M3, BF_E5M2 = 0, 1
 BF_EPI_NONE, BF_EPI_BIAS, BF_EPI_BIAS_RES, BF_EPI_BIAS_GELU, BF_EPI_GELU_BWD, BF_EPI_ACCUM = range(6)
 VOCAB_TENSOR_IDS = {"e_tok": 12, "e_pos": 13, "lnf_g": 14, "lnf_b": 15, "w_out": 16}
 TENSOR_IDS = {"ln1_g": 0, "ln1_b": 1, "w_qkv": 2, "b_qkv": 3, "w_o": 4, "b_o": 5,
@@ -70,6 +71,14 @@ class bf_attn_config(C.Structure):
 
 class bf_adam_tensor(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("w", "m", "v", "g", "w_lp")] + [("n", C.c_size_t)]
+
+
+class bf_adam8_tensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("w", "state", "g", "w_lp")] + [("n", C.c_size_t)]
+
+
+class bf_adam8_moments_tensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("state", "m", "v")] + [("n", C.c_size_t)]
 
 
 _P = C.c_void_p
@@ -134,6 +143,14 @@ _SIGNATURES = {
     "bf_op_grad_norm": (C.c_int, [C.c_int, C.c_int, _P, _P, C.c_float, _P, _P, C.c_size_t, _P]),
     "bf_op_grad_scale": (C.c_int, [C.c_int, C.c_int, _P, _P, _P, _P, _P]),
     "bf_op_adam_clipped": (C.c_int, [C.c_int, _P, _P, C.c_int] + [C.c_float] * 5 + [_P]),
+    "bf_op_fp8_row_bytes": (C.c_size_t, [C.c_int]),
+    "bf_op_fp8_scale_elems": (C.c_size_t, [C.c_int] * 2),
+    "bf_op_fp8_quantize": (C.c_int, [C.c_int] * 4 + [_P, C.c_size_t] + [_P] * 5),
+    "bf_op_fp8_gemm_work_bytes": (C.c_size_t, [C.c_int] * 3),
+    "bf_op_fp8_gemm": (C.c_int, [C.c_int] * 6 + [_P] * 7 + [C.c_int, _P, C.c_size_t, _P]),
+    "bf_op_adam8_state_bytes": (C.c_size_t, [C.c_size_t]),
+    "bf_op_adam8": (C.c_int, [C.c_int, C.c_int, _P, _P, C.c_uint64, C.c_int] + [C.c_float] * 5 + [_P]),
+    "bf_op_adam8_moments": (C.c_int, [C.c_int, C.c_int, _P, _P]),
     "bf_op_adam": (C.c_int, [C.c_size_t, _P, _P, _P, _P, _P, C.c_int] + [C.c_float] * 5 + [_P]),
 }
 
@@ -652,3 +669,111 @@ def bf_op_adam_clipped(tensors, coef, t, lr, beta1, beta2, adam_eps, weight_deca
     rest = iter(pl)
     a = _array("Q", [x for i, k in enumerate(n) for x in (pw[i], pm[i], pv[i], pg[i], 0 if low[i] is None else next(rest), k)])  # bf_adam_tensor
     check(load().bf_op_adam_clipped(len(n), _at(a), coef.data_ptr(), t, lr, beta1, beta2, adam_eps, weight_decay, _stream()))
+
+
+def bf_op_fp8_row_bytes(n):
+    return load().bf_op_fp8_row_bytes(n)
+
+
+def bf_op_fp8_scale_elems(rows, n):
+    return load().bf_op_fp8_scale_elems(rows, n)
+
+
+def _bytes(who, t, n):
+    """Checks a tensor of codes, scales or state: dense, of one-byte elements (uint8 or an 8-bit float), n of them at least, on the current device."""
+    if t.element_size() != 1:
+        raise ValueError("%s: needs tensors of bytes, got %s" % (who, t.dtype))
+    _tensors(who, (t,), t.dtype)
+    _elems(who, t, n)
+
+
+def _form(who, codes, scale, rows, n):
+    lib = load()
+    _bytes(who, codes, rows * lib.bf_op_fp8_row_bytes(n))
+    _bytes(who, scale, lib.bf_op_fp8_scale_elems(rows, n))
+
+
+def bf_op_fp8_quantize(dtype, format, rows, cols, x, q=None, scale=None, qt=None, scale_t=None, ld_x=0):
+    """8-bit forms of x [rows, cols] along its rows (q, scale) and down its columns (qt, scale_t).  x: dense, or a view of two dimensions whose rows are
+    dense (their distance is ld_x, taken from the view where ld_x is 0)."""
+    who = "bf_op_fp8_quantize"
+    if x.is_contiguous() and (x.dim() != 2 or ld_x or x.shape[1] == cols):
+        _tensors(who, (x,), _torch_dtype(dtype))
+        _elems(who, x, (rows - 1) * (ld_x or cols) + cols)
+    else:
+        _tensors(who, (x[:0],), _torch_dtype(dtype))
+        if x.dim() != 2 or x.shape[0] < rows or x.shape[1] < cols or x.stride(1) != 1 or x.stride(0) < cols or ld_x not in (0, x.stride(0)):
+            raise ValueError("%s: %d x %d elements in rows %d apart of a tensor of shape %s, strides %s" % (who, rows, cols, ld_x, tuple(x.shape), x.stride()))
+        ld_x = x.stride(0)
+    if q is not None and scale is not None:
+        _form(who, q, scale, rows, cols)
+    if qt is not None and scale_t is not None:
+        _form(who, qt, scale_t, cols, rows)
+    check(load().bf_op_fp8_quantize(dtype, format, rows, cols, x.data_ptr(), ld_x, _ptr(q), _ptr(scale), _ptr(qt), _ptr(scale_t), _stream()))
+
+
+def bf_op_fp8_gemm_work_bytes(M, N, K):
+    return load().bf_op_fp8_gemm_work_bytes(M, N, K)
+
+
+def bf_op_fp8_gemm(format_a, format_b, dtype, M, N, K, A, scale_a, B, scale_b, Cout, bias=None, R=None, accumulate=0, work=None):
+    """Cout[M, N] = A B^T + bias + R (or += in fp32) from 8-bit forms A [M, K] and B [N, K]."""
+    who, lib = "bf_op_fp8_gemm", load()
+    _form(who, A, scale_a, M, K)
+    _form(who, B, scale_b, N, K)
+    out = [t for t in (Cout, R) if t is not None]
+    _tensors(who, out, _torch_dtype(dtype))
+    for t in out:
+        _elems(who, t, M * N)
+    if bias is not None:
+        _tensors(who, (bias,), _th().float32)
+        _elems(who, bias, N)
+    n = lib.bf_op_fp8_gemm_work_bytes(M, N, K)
+    if n or work is not None:
+        work = _work(who, work, n)
+    check(lib.bf_op_fp8_gemm(format_a, format_b, dtype, M, N, K, A.data_ptr(), scale_a.data_ptr(), B.data_ptr(), scale_b.data_ptr(), Cout.data_ptr(), _ptr(bias),
+                             _ptr(R), accumulate, _ptr(work), 0 if work is None else work.numel() * work.element_size(), _stream()))
+
+
+def bf_op_adam8_state_bytes(n):
+    return load().bf_op_adam8_state_bytes(n)
+
+
+def _states(who, states, n):
+    """Addresses of the states of tensors of n[i] elements."""
+    if states:
+        p, have = _list(who, states, states[0].dtype)
+        for t, h, k in zip(states, have, n):
+            if t.element_size() != 1 or h < (k + 127) // 128 * 258:
+                raise ValueError("%s: a state of %d bytes and more for %d elements, got %d of %s" % (who, (k + 127) // 128 * 258, k, h, t.dtype))
+        return p
+    return _array("Q")
+
+
+def bf_op_adam8(dtype, tensors, coef, seed, t, lr, beta1, beta2, adam_eps, weight_decay):
+    """The Adam step number t on gradients (`dtype`) times coef (device fp32), moments in 8 bits.  tensors: (w, state, g, w_lp) each, w_lp bf16 or None; state: uint8,
+    bf_op_adam8_state_bytes(elements of w), zeros for moments of zero."""
+    who, torch = "bf_op_adam8", _th()
+    _tensors(who, (coef,), torch.float32)
+    _elems(who, coef, 1)
+    w, state, g, low = zip(*tensors) if tensors else ((),) * 4
+    (pw, n), (pg, n1) = _list(who, w, torch.float32), _list(who, g, _torch_dtype(dtype))
+    pl, n2 = _list(who, [x for x in low if x is not None], torch.bfloat16)
+    if n != n1 or n2 != _array("Q", [k for k, x in zip(n, low) if x is not None]):
+        raise ValueError("%s: tensors of different sizes in one entry" % who)
+    ps, rest = _states(who, state, n), iter(pl)
+    a = _array("Q", [x for i, k in enumerate(n) for x in (pw[i], ps[i], pg[i], 0 if low[i] is None else next(rest), k)])  # bf_adam8_tensor
+    check(load().bf_op_adam8(dtype, len(n), _at(a), coef.data_ptr(), seed, t, lr, beta1, beta2, adam_eps, weight_decay, _stream()))
+
+
+def bf_op_adam8_moments(dtype, tensors):
+    """m and v (`dtype`) that states stand for.  tensors: (state, m, v) each, m or v or both."""
+    who, want = "bf_op_adam8_moments", _torch_dtype(dtype)
+    n = _array("Q", [(v if m is None else m).numel() for _, m, v in tensors])
+    ms, vs = [m for _, m, _ in tensors if m is not None], [v for _, _, v in tensors if v is not None]
+    (pm, n1), (pv, n2) = _list(who, ms, want), _list(who, vs, want)
+    if n1 != _array("Q", [k for k, x in zip(n, tensors) if x[1] is not None]) or n2 != _array("Q", [k for k, x in zip(n, tensors) if x[2] is not None]):
+        raise ValueError("%s: tensors of different sizes in one entry" % who)
+    ps, rm, rv = _states(who, [s for s, _, _ in tensors], n), iter(pm), iter(pv)
+    a = _array("Q", [x for i, (_, m, v) in enumerate(tensors) for x in (ps[i], 0 if m is None else next(rm), 0 if v is None else next(rv), n[i])])
+    check(load().bf_op_adam8_moments(dtype, len(n), _at(a), _stream()))

@@ -15,6 +15,14 @@ bf_status attention_masked_bwd(const bf_attn_config* c, const void* q, const voi
                                const float* lse, const void* dctx, void* dq, void* dk, void* dv, void* work, size_t work_bytes, hipStream_t st);
 bf_status adam_clipped(int n_tensors, const bf_adam_tensor* x, const float* coef, int step, float lr, float beta1, float beta2, float eps, float wd,
                        hipStream_t st);
+bf_status fp8_quantize(int dtype, int format, int rows, int cols, const void* x, size_t ld, void* q, void* scale, void* qt, void* scale_t, hipStream_t st);
+size_t fp8_gemm_work_bytes(int M, int N, int K);
+bf_status fp8_gemm(int fa, int fb, int dtype, int M, int N, int K, const void* A, const void* sa, const void* B, const void* sb, void* C, const float* bias,
+                   const void* R, int accumulate, void* work, size_t work_bytes, hipStream_t st);
+size_t adam8_state_bytes(size_t n);
+bf_status adam8_step(int dtype, int n_tensors, const bf_adam8_tensor* x, const float* coef, uint64_t seed, int step, float lr, float beta1, float beta2, float eps,
+                     float wd, hipStream_t st);
+bf_status adam8_moments(int dtype, int n_tensors, const bf_adam8_moments_tensor* x, hipStream_t st);
 }  // namespace bf
 
 using namespace bf;
@@ -262,6 +270,37 @@ bf_status bf_op_grad_scale(int dtype, int n_tensors, const void* const* g, void*
 bf_status bf_op_adam_clipped(int n_tensors, const bf_adam_tensor* tensors, const float* coef, int t, float lr, float beta1, float beta2,
                              float adam_eps, float weight_decay, void* stream) {
   return adam_clipped(n_tensors, tensors, coef, t, lr, beta1, beta2, adam_eps, weight_decay, (hipStream_t)stream);
+}
+
+size_t bf_op_fp8_row_bytes(int n) { return n > 0 ? ((size_t)n + 127) / 128 * 128 : 0; }
+
+size_t bf_op_fp8_scale_elems(int rows, int n) { return rows > 0 && n > 0 ? ((size_t)n + 127) / 128 * (((size_t)rows + 15) / 16 * 16) : 0; }
+
+bf_status bf_op_fp8_quantize(int dtype, int format, int rows, int cols, const void* x, size_t ld_x, void* q, void* scale, void* qt, void* scale_t,
+                             void* stream) {
+  if (!dtype_ok(dtype, 0)) return BF_EINVAL;
+  return fp8_quantize(dtype, format, rows, cols, x, ld_x, q, scale, qt, scale_t, (hipStream_t)stream);
+}
+
+size_t bf_op_fp8_gemm_work_bytes(int M, int N, int K) { return fp8_gemm_work_bytes(M, N, K); }
+
+bf_status bf_op_fp8_gemm(int format_a, int format_b, int dtype, int M, int N, int K, const void* A, const void* scale_a, const void* B,
+                         const void* scale_b, void* C, const float* bias, const void* R, int accumulate, void* work, size_t work_bytes, void* stream) {
+  if (!dtype_ok(dtype, 0)) return BF_EINVAL;
+  return fp8_gemm(format_a, format_b, dtype, M, N, K, A, scale_a, B, scale_b, C, bias, R, accumulate, work, work_bytes, (hipStream_t)stream);
+}
+
+size_t bf_op_adam8_state_bytes(size_t n) { return adam8_state_bytes(n); }
+
+bf_status bf_op_adam8(int dtype, int n_tensors, const bf_adam8_tensor* tensors, const float* coef, uint64_t seed, int t, float lr, float beta1, float beta2,
+                      float adam_eps, float weight_decay, void* stream) {
+  if (!dtype_ok(dtype, 0)) return BF_EINVAL;
+  return adam8_step(dtype, n_tensors, tensors, coef, seed, t, lr, beta1, beta2, adam_eps, weight_decay, (hipStream_t)stream);
+}
+
+bf_status bf_op_adam8_moments(int dtype, int n_tensors, const bf_adam8_moments_tensor* tensors, void* stream) {
+  if (!dtype_ok(dtype, 0)) return BF_EINVAL;
+  return adam8_moments(dtype, n_tensors, tensors, (hipStream_t)stream);
 }
 
 }  // extern "C"
