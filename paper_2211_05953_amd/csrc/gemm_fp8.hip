@@ -46,11 +46,12 @@ struct Fp8Args {
   const float* bias;
   const void* R;
   int accumulate;
-  int tiles_m, remap, slice;   // slice: blocks that a workgroup takes; grid.y slices, slice y into plane y of C
+  int tiles_m, slice;          // slice: blocks that a workgroup takes; grid.y slices, slice y into plane y of C
 };
 
-template <int BM_, int BN_, int WM_, int WN_>
+template <int BM_, int BN_, int WM_, int WN_, int NS_ = 2>
 struct Tile8 {
+  static constexpr int NS = NS_;  // stages
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NT = WM * WN * 64;
   static constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
   static constexpr int GA = MI < 4 ? MI : 4, GB = NI < 4 ? NI : 4;  // fragments that share a load of scale bytes
@@ -65,7 +66,7 @@ __device__ __forceinline__ int kswz8(int row) {
 
 // row of the tile that LDS row r holds
 template <int G>
-__device__ __forceinline__ int row_of(int r) { return (r / (16 * G)) * (16 * G) + (r % 16) * G + (r / 16) % G; }
+__host__ __device__ __forceinline__ constexpr int row_of(int r) { return (r / (16 * G)) * (16 * G) + (r % 16) * G + (r / 16) % G; }
 
 template <int G>
 __device__ __forceinline__ int load_scales(const uint8_t* p) {
@@ -74,9 +75,12 @@ __device__ __forceinline__ int load_scales(const uint8_t* p) {
   else return *p;
 }
 
+// c += a b with scales, c in place.  (Written out: from the builtin the compiler gives accumulators new registers, and a 128 x 128 sub-tile, whose
+// accumulators are half of all registers there are, spends as long on moving them as on products.)
 template <int SEL_A, int SEL_B, int FA, int FB>
-__device__ __forceinline__ f32x4 mma_scaled(v8i a, v8i b, f32x4 c, int sa, int sb) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, FA, FB, SEL_A, sa, SEL_B, sb);
+__device__ __forceinline__ void mma_scaled(const v8i& a, const v8i& b, f32x4& c, int sa, int sb) {
+  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%c5,%c6,0] op_sel_hi:[%c7,%c8,0] cbsz:%c9 blgp:%c10"
+               : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb), "n"(SEL_A & 1), "n"(SEL_B & 1), "n"(SEL_A >> 1), "n"(SEL_B >> 1), "n"(FA), "n"(FB));
 }
 
 template <int I, int N, typename F>
@@ -151,18 +155,29 @@ __device__ __forceinline__ void put(float (&v)[G], int row, int col, const Fp8Ar
 template <typename TL, int FA, int FB, bool WIDE, typename TO>
 __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's pass drops the whole kernel over the builtins that load into LDS)
+  static_assert((TL::NT & (TL::NT - 1)) == 0, "a power of two");
   constexpr int BM = TL::BM, BN = TL::BN, NT = TL::NT, MI = TL::MI, NI = TL::NI, GA = TL::GA, GB = TL::GB, CA = TL::CA, CB = TL::CB;
-  // (two arrays and not one: the compiler then knows that reads of a stage need not wait for loads into the other)
-  __shared__ __attribute__((aligned(128))) uint8_t stage0[(BM + BN) * BKB];
-  __shared__ __attribute__((aligned(128))) uint8_t stage1[(BM + BN) * BKB];
+  // (an array for each and not one: the compiler then knows that reads of a stage need not wait for loads into the others)
+  constexpr int NS = TL::NS, STAGE = (BM + BN) * BKB + 512;
+  static_assert(NS == 2 || NS == 4, "two or four stages");
+  __shared__ __attribute__((aligned(128))) uint8_t stage0[STAGE];
+  __shared__ __attribute__((aligned(128))) uint8_t stage1[STAGE];
+  __shared__ __attribute__((aligned(128))) uint8_t stage2[NS == 4 ? STAGE : 16];
+  __shared__ __attribute__((aligned(128))) uint8_t stage3[NS == 4 ? STAGE : 16];
+  auto stage = [&](auto i) -> uint8_t* {
+    constexpr int S = decltype(i)::value % NS;
+    if constexpr (S == 0) return stage0;
+    else if constexpr (S == 1) return stage1;
+    else if constexpr (S == 2) return stage2;
+    else return stage3;
+  };
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w % TL::WM, wn = w / TL::WM;
 
   // each XCD (its own L2) a contiguous range of the tile order, which walks groups of 8 row-tiles
-  int lin = blockIdx.x;
-  if (p.remap) lin = (lin & 7) * (gridDim.x >> 3) + (lin >> 3);
   const int tiles_n = gridDim.x / p.tiles_m;
-  int bm, bn;
-  if (p.remap && p.tiles_m % 8 == 0) {
+  int lin = blockIdx.x, bm, bn;
+  if (gridDim.x % 8 == 0) lin = (lin & 7) * (gridDim.x >> 3) + (lin >> 3);
+  if (p.tiles_m % 8 == 0) {
     const int in_group = 8 * tiles_n, gi = lin / in_group, rem = lin % in_group;
     bm = gi * 8 + (rem & 7);
     bn = rem >> 3;
@@ -173,47 +188,47 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
   const int m0 = bm * BM, n0 = bn * BN;
   const int kb0 = blockIdx.y * p.slice, nk = min(p.slice, p.blocks - kb0);
   const size_t ld = (size_t)p.blocks * BKB;
-  const uint8_t *ga = p.A + (size_t)m0 * ld + (size_t)kb0 * BKB, *gb = p.B + (size_t)n0 * ld + (size_t)kb0 * BKB;
   TO* C = reinterpret_cast<TO*>(p.C) + (size_t)blockIdx.y * p.M * p.N;
 
-  // Lanes whose row lies behind the matrix read its last row instead: what they compute is not stored.
-  const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)ga, 0, 0x7fffffff, 0x00020000);
-  const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)gb, 0, 0x7fffffff, 0x00020000);
-  int off_a[CA], off_b[CB];
-#pragma unroll
-  for (int i = 0; i < CA; ++i) {
-    const int c = i * NT + tid, r = c >> 3, ch = (c & 7) ^ kswz8(r);
-    off_a[i] = min(row_of<GA>(r), p.M - 1 - m0) * (int)ld + ch * 16;
-  }
-#pragma unroll
-  for (int i = 0; i < CB; ++i) {
-    const int c = i * NT + tid, r = c >> 3, ch = (c & 7) ^ kswz8(r);
-    off_b[i] = min(row_of<GB>(r), p.N - 1 - n0) * (int)ld + ch * 16;
-  }
+  // What is loaded: a tile's operands by 32-bit lane offsets from its first byte.  The descriptors end where the matrices end, and lanes whose row lies
+  // behind it get nothing: what they compute is not stored.
   typedef __attribute__((address_space(3))) void* lds_ptr;
-  auto issue = [&](uint8_t* st, int kt) {
-#pragma unroll
-    for (int i = 0; i < CA; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(st + (i * NT + w * 64) * 16), 16, off_a[i], kt * BKB, 0, 0);
-#pragma unroll
-    for (int i = 0; i < CB; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(st + BM * BKB + (i * NT + w * 64) * 16), 16, off_b[i], kt * BKB, 0, 0);
+  auto rest = [&](int rows) {
+    const size_t n = (size_t)rows * ld - (size_t)kb0 * BKB;
+    return (int)(n < 0x7fffff00u ? n : 0x7fffff00u);
   };
-  // scale bytes of the lane's rows / columns, G to a load
+  const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)(p.A + (size_t)m0 * ld + (size_t)kb0 * BKB), 0, rest(p.M - m0), 0x00020000);
+  const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)(p.B + (size_t)n0 * ld + (size_t)kb0 * BKB), 0, rest(p.N - n0), 0x00020000);
+  int sld = w & 1 ? p.ldsb : p.ldsa;
+  const uint8_t* sp = (w & 1 ? p.sb : p.sa) + (size_t)kb0 * sld;
+  asm("" : "+s"(sld), "+s"(sp));  // held in registers: a load of arguments in the loop would wait for everything that is read from LDS
+  const int off_s = min((w & 1 ? n0 : m0) + 4 * lane, sld - 4);
+  // chunk i of a thread is NT / 8 LDS rows, a power of two, further on: the bits of row_of are those of the two parts
+  const int ch = (tid & 7) ^ kswz8(tid >> 3);
+  const int off_a = row_of<GA>(tid >> 3) * (int)ld + ch * 16, off_b = GA == GB ? off_a : row_of<GB>(tid >> 3) * (int)ld + ch * 16;
+  auto issue_chunk = [&](uint8_t* st, int kt, int i) {
+    if (i < CA) __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(st + (i * NT + w * 64) * 16), 16, off_a + (kt * BKB + row_of<GA>(i * (NT / 8)) * (int)ld), 0, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(st + BM * BKB + ((i - CA) * NT + w * 64) * 16), 16, off_b + (kt * BKB + row_of<GB>((i - CA) * (NT / 8)) * (int)ld), 0, 0, 0);
+  };
+  // The block's scale bytes behind the tiles, 256 of A's rows (even waves, all the same) and 256 of B's (odd ones): every wave has the same number of loads
+  // on its way.  Lanes behind the last row repeat its neighbours'.
+  constexpr int SCALES = (BM + BN) * BKB;
+  auto issue_scales = [&](uint8_t* st, int kt) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)(sp + (int64_t)kt * sld), 0, 0x7fffffff, 0x00020000), (lds_ptr)(st + SCALES + (w & 1) * 256), 4, off_s, 0, 0, 0);
+  };
+  auto issue = [&](uint8_t* st, int kt) {
+    issue_scales(st, kt);
+#pragma unroll
+    for (int i = 0; i < CA + CB; ++i) issue_chunk(st, kt, i);
+  };
+  // the lane's: G rows / columns to a load
   constexpr int SA = MI / GA, SB = NI / GB;
-  const uint8_t *psa = p.sa + (size_t)kb0 * p.ldsa, *psb = p.sb + (size_t)kb0 * p.ldsb;
-  int oa[SA], ob[SB];
+  int sca[SA], scb[SB];
+  auto scales = [&](const uint8_t* st, int (&a)[SA], int (&b)[SB]) {
 #pragma unroll
-  for (int s = 0; s < SA; ++s) oa[s] = min(m0 + wm * TL::TM + s * 16 * GA + (lane & 15) * GA, p.ldsa - GA);
+    for (int s = 0; s < SA; ++s) a[s] = load_scales<GA>(st + SCALES + wm * TL::TM + s * 16 * GA + (lane & 15) * GA);
 #pragma unroll
-  for (int s = 0; s < SB; ++s) ob[s] = min(n0 + wn * TL::TN + s * 16 * GB + (lane & 15) * GB, p.ldsb - GB);
-  int sca[SA], scb[SB], nsa[SA], nsb[SB];
-  auto scales = [&](int kt, int (&a)[SA], int (&b)[SB]) {
-    const uint8_t *qa = psa + (size_t)kt * p.ldsa, *qb = psb + (size_t)kt * p.ldsb;
-#pragma unroll
-    for (int s = 0; s < SA; ++s) a[s] = load_scales<GA>(qa + oa[s]);
-#pragma unroll
-    for (int s = 0; s < SB; ++s) b[s] = load_scales<GB>(qb + ob[s]);
+    for (int s = 0; s < SB; ++s) b[s] = load_scales<GB>(st + SCALES + 256 + wn * TL::TN + s * 16 * GB + (lane & 15) * GB);
   };
 
   f32x4 acc[MI][NI];
@@ -228,21 +243,24 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
   for (int kk = 0; kk < 2; ++kk) fo[kk] = (lane & 15) * BKB + (((kk * 4 + (lane >> 4)) ^ kswz8(lane & 15)) << 4);
   const int fa = wm * TL::TM * BKB, fb = BM * BKB + wn * TL::TN * BKB;
   auto chunk = [&](const uint8_t* st, int base, int t, int kk) { return *reinterpret_cast<const v4i*>(st + base + t * 16 * BKB + fo[kk]); };
-  auto arrived = [] {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+  // Everything but the last `left` blocks' loads is there, for all waves, and their reads of LDS are over.
+  auto arrived = [](auto left) {
+    constexpr int VM = decltype(left)::value * (CA + CB + 1);
+    static_assert(VM < 64, "the counter's range");
+    __builtin_amdgcn_s_waitcnt((VM & 15) | (VM >> 4) << 14 | 7 << 4);  // vmcnt(VM) lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
+  typedef std::integral_constant<int, 0> H0;
+  typedef std::integral_constant<int, 1> H1;
 
-  issue(stage0, 0);
-  scales(0, sca, scb);
   if constexpr (WIDE) {
     // One barrier per block: behind it the tile is there and the other stage is free.
     auto body = [&](uint8_t* cur, uint8_t* nxt, int kt) {
-      arrived();
-      if (kt + 1 < nk) {
-        issue(nxt, kt + 1);
-        scales(kt + 1, nsa, nsb);
-      }
+      arrived(H0{});
+      if (kt + 1 < nk) issue(nxt, kt + 1);
+      scales(cur, sca, scb);
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
         bf16x8 b[NI][2];
@@ -260,11 +278,8 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
             for (int h = 0; h < 2; ++h) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[h], b[j][h], acc[i][j], 0, 0, 0);
         });
       }
-#pragma unroll
-      for (int s = 0; s < SA; ++s) sca[s] = nsa[s];
-#pragma unroll
-      for (int s = 0; s < SB; ++s) scb[s] = nsb[s];
     };
+    issue(stage0, 0);
     for (int kt = 0; kt < nk; kt += 2) {
       body(stage0, stage1, kt);
       if (kt + 1 < nk) body(stage1, stage0, kt + 1);
@@ -281,67 +296,67 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
       const v4i x = chunk(st, base, t, 0), y = chunk(st, base, t, 1);
       return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    auto get_a = [&](const uint8_t* st, int half, v8i (&f)[MH]) {
-#pragma unroll
-      for (int i = 0; i < MH; ++i) f[i] = whole(st, fa, half * MH + i);
-    };
-    auto get_b = [&](const uint8_t* st, int half) {
-#pragma unroll
-      for (int j = 0; j < NH; ++j) bx[half][j] = whole(st, fb, half * NH + j);
-    };
-    auto mma = [&](auto ha, auto hb, v8i (&f)[MH]) {
-      unrolled<0, MH>([&](auto i) {
-        unrolled<0, NH>([&](auto jj) {
-          constexpr int I = decltype(i)::value, J = I & 1 ? NH - 1 - decltype(jj)::value : decltype(jj)::value;  // serpentine: one operand changes
-          constexpr int TI = decltype(ha)::value * MH + I, TJ = decltype(hb)::value * NH + J;
-          acc[TI][TJ] = mma_scaled<TI % GA, TJ % GB, FA, FB>(f[I], bx[decltype(hb)::value][J], acc[TI][TJ], sca[TI / GA], scb[TJ / GB]);
-        });
+    auto read_a = [&](const uint8_t* st, int half, v8i (&f)[MH], int i) { f[i] = whole(st, fa, half * MH + i); };
+    auto read_b = [&](const uint8_t* st, int half, int j) { bx[half][j] = whole(st, fb, half * NH + j); };
+    // The instructions of a phase in the order that they are issued in: an MFMA, then what `side` has for its place.
+    auto phase = [&](auto ha, auto hb, v8i (&f)[MH], auto&& side) {
+      unrolled<0, MH * NH>([&](auto n) {
+        constexpr int I = decltype(n)::value / NH, JJ = decltype(n)::value % NH, J = I & 1 ? NH - 1 - JJ : JJ;  // serpentine: one operand changes
+        constexpr int TI = decltype(ha)::value * MH + I, TJ = decltype(hb)::value * NH + J;
+        mma_scaled<TI % GA, TJ % GB, FA, FB>(f[I], bx[decltype(hb)::value][J], acc[TI][TJ], sca[TI / GA], scb[TJ / GB]);
+        side(decltype(n)::value);
+        __builtin_amdgcn_sched_barrier(0);
       });
     };
-    typedef std::integral_constant<int, 0> H0;
-    typedef std::integral_constant<int, 1> H1;
-    // one phase's instructions in turn: an MFMA, then a share of the reads from LDS (0x100)
-    auto interleave = [&](auto reads) {
-      constexpr int NMMA = MH * NH, NR = decltype(reads)::value, PER = (NR + NMMA - 1) / NMMA;
+    // loads of a tile: one after every EACH matrix instructions of the last two phases, or PER after each
+    constexpr int NMMA = MH * NH, FIT = 2 * NMMA / (CA + CB), EACH = FIT > 3 ? 3 : FIT < 1 ? 1 : FIT, PER = (CA + CB + 2 * NMMA - 1) / (2 * NMMA);
+    auto share = [&](uint8_t* st, int kt, int n) {
+      if (n % EACH) return;
 #pragma unroll
-      for (int i = 0; i < NMMA; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        if (i * PER < NR) __builtin_amdgcn_sched_group_barrier(0x100, PER, 0);
-      }
-      __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < PER; ++i)
+        if (n / EACH * PER + i < CA + CB) issue_chunk(st, kt, n / EACH * PER + i);
     };
-    typedef std::integral_constant<int, 2 * MH> RA;
-    typedef std::integral_constant<int, 2 * NH> RB;
-    auto body = [&](uint8_t* cur, uint8_t* nxt, int kt, auto first, auto second) {
-      constexpr int F = decltype(first)::value, S = decltype(second)::value;
-      if (kt + 1 < nk) scales(kt + 1, nsa, nsb);
-      get_b(cur, S);
-      mma(H0{}, first, a0);
-      interleave(RB{});
-      get_a(cur, 1, a1);
-      mma(H0{}, second, a0);
-      interleave(RA{});
-      arrived();
-      if (kt + 2 < nk) issue(cur, kt + 2);
-      get_a(nxt, 0, a0);
-      mma(H1{}, second, a1);
-      interleave(RA{});
-      get_b(nxt, S);
-      mma(H1{}, first, a1);
-      interleave(RB{});
+    // works on block kt in stage U and loads block kt + NS into it (behind the last one: the last again, which nothing reads)
+    auto body = [&](auto u, int kt) {
+      constexpr int U = decltype(u)::value, S = U & 1 ? 0 : 1;
+      const std::integral_constant<int, U & 1> first_half{};
+      const std::integral_constant<int, S> second_half{};
+      uint8_t *const cur = stage(u), *const nxt = stage(std::integral_constant<int, U + 1>{});
+      const int lk = min(kt + NS, nk - 1);
+      int na[SA], nb[SB];
+      phase(H0{}, first_half, a0, [&](int n) { if (n < NH) read_b(cur, S, n); });
+      phase(H0{}, second_half, a0, [&](int n) { if (n < MH) read_a(cur, 1, a1, n); });
+      arrived(std::integral_constant<int, NS - 2>{});
+      scales(nxt, na, nb);
+      issue_scales(cur, lk);
+      phase(H1{}, second_half, a1, [&](int n) {
+        if (n < MH) read_a(nxt, 0, a0, n);
+        share(cur, lk, n);
+      });
+      phase(H1{}, first_half, a1, [&](int n) {
+        if (n < NH) read_b(nxt, S, n);
+        share(cur, lk, NMMA + n);
+      });
 #pragma unroll
-      for (int s = 0; s < SA; ++s) sca[s] = nsa[s];
+      for (int s = 0; s < SA; ++s) sca[s] = na[s];
 #pragma unroll
-      for (int s = 0; s < SB; ++s) scb[s] = nsb[s];
+      for (int s = 0; s < SB; ++s) scb[s] = nb[s];
+      asm volatile("s_nop 1");  // between a move and a matrix instruction that reads it
     };
-    arrived();
-    if (nk > 1) issue(stage1, 1);
-    get_a(stage0, 0, a0);
-    get_b(stage0, 0);
-    for (int kt = 0; kt < nk; kt += 2) {
-      body(stage0, stage1, kt, H0{}, H1{});
-      if (kt + 1 < nk) body(stage1, stage0, kt + 1, H1{}, H0{});
-    }
+    unrolled<0, NS>([&](auto u) { issue(stage(u), min((int)decltype(u)::value, nk - 1)); });
+    arrived(std::integral_constant<int, NS - 1>{});
+    scales(stage0, sca, scb);
+#pragma unroll
+    for (int i = 0; i < MH; ++i) read_a(stage0, 0, a0, i);
+#pragma unroll
+    for (int j = 0; j < NH; ++j) read_b(stage0, 0, j);
+    int kt = 0;
+    for (; kt + NS <= nk; kt += NS) unrolled<0, NS>([&](auto u) { body(u, kt + decltype(u)::value); });
+    unrolled<0, NS - 1>([&](auto u) {
+      if (kt + decltype(u)::value < nk) body(u, kt + decltype(u)::value);
+    });
+    // nothing is on its way into LDS when the workgroup ends, and the last results are there (16 passes and some)
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
   }
 
   // lane l, register r of a fragment: row 4 (l / 16) + r, column l % 16 of it
@@ -378,10 +393,10 @@ __global__ __launch_bounds__(256) void fp8_finish_kernel(size_t n, int N, int sl
   }
 }
 
-typedef Tile8<256, 256, 2, 4> Big8;
+typedef Tile8<256, 256, 4, 2> Big8;
 typedef Tile8<256, 256, 2, 4> Wide8;  // widened operands: smaller sub-tiles, two waves to a SIMD
-typedef Tile8<128, 128, 2, 2> Mid8;
-typedef Tile8<64, 64, 2, 2> Small8;
+typedef Tile8<128, 128, 2, 2, 4> Mid8;
+typedef Tile8<64, 64, 2, 2, 4> Small8;
 
 struct Plan { int tile, slices, slice; };  // tile 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
 
@@ -404,7 +419,6 @@ bf_status launch8(Fp8Args a, int slices, hipStream_t st) {
   a.tiles_m = (a.M + TL::BM - 1) / TL::BM;
   const long tiles = (long)a.tiles_m * ((a.N + TL::BN - 1) / TL::BN);
   if (tiles * TL::NT >= (1l << 32)) { set_error("bf_op_fp8_gemm: more than 2^32 threads"); return BF_EINVAL; }
-  a.remap = tiles % 8 == 0;
   gemm_fp8_kernel<TL, FA, FB, WIDE, TO><<<dim3((unsigned)tiles, (unsigned)slices), TL::NT, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) { set_error("bf_op_fp8_gemm: launch failed: %s", hipGetErrorString(e)); return BF_EDEVICE; }
@@ -455,7 +469,7 @@ bf_status fp8_gemm(int fa, int fb, int dtype, int M, int N, int K, const void* A
     return BF_EINVAL;
   }
   Fp8Args a{M, N, blocks, (const uint8_t*)A, (const uint8_t*)B, (const uint8_t*)sa, (const uint8_t*)sb, (M + 15) / 16 * 16, (N + 15) / 16 * 16, C, bias, R,
-            accumulate, 0, 0, q.slice};
+            accumulate, 0, q.slice};
   if (split) {
     a.C = work;
     a.bias = nullptr;
