@@ -500,11 +500,34 @@ def _work(who, work, n):
 
 def _list(who, tensors, dtype):
     """Host arrays of the addresses and sizes of a list of tensors, checked as by _tensors.  (Hundreds of tensors: the checks
-    of one kind together, a few calls into torch each.)"""
-    if [t.dtype for t in tensors].count(dtype) != len(tensors) or \
-            [t.get_device() for t in tensors].count(_th()._C._cuda_getDevice()) != len(tensors) or not all([t.is_contiguous() for t in tensors]):
+    of one kind together, a few calls into torch each, most of them by map, without steps of the interpreter.)"""
+    T = _th().Tensor
+    if [t.dtype for t in tensors].count(dtype) != len(tensors) or set(map(T.get_device, tensors)) - {_th()._C._cuda_getDevice()} or \
+            not all(map(T.is_contiguous, tensors)):
         _tensors(who, tensors, dtype)
-    return _array("Q", [t.data_ptr() for t in tensors]), _array("Q", [t.numel() for t in tensors])
+    return _array("Q", list(map(T.data_ptr, tensors))), _array("Q", list(map(T.numel, tensors)))
+
+
+def _table(*columns):
+    """The columns (arrays of 8-byte numbers of one length) side by side: an array of structures."""
+    t = _array("Q", bytes(8 * len(columns) * len(columns[0])))
+    for k, c in enumerate(columns):
+        t[k::len(columns)] = c
+    return t
+
+
+def _optional(who, tensors, dtype, n):
+    """Addresses of tensors of n[i] elements, 0 where there is none."""
+    if not any([t is None for t in tensors]):
+        p, m = _list(who, tensors, dtype)
+        if m != n:
+            raise ValueError("%s: tensors of different sizes in one entry" % who)
+        return p
+    p, m = _list(who, [t for t in tensors if t is not None], dtype)
+    if m != _array("Q", [k for k, t in zip(n, tensors) if t is not None]):
+        raise ValueError("%s: tensors of different sizes in one entry" % who)
+    rest = iter(p)
+    return _array("Q", [0 if t is None else next(rest) for t in tensors])
 
 
 def _at(arr):
@@ -672,11 +695,11 @@ def bf_op_adam_clipped(tensors, coef, t, lr, beta1, beta2, adam_eps, weight_deca
 
 
 def bf_op_fp8_row_bytes(n):
-    return load().bf_op_fp8_row_bytes(n)
+    return (n + 127) // 128 * 128 if n > 0 else 0
 
 
 def bf_op_fp8_scale_elems(rows, n):
-    return load().bf_op_fp8_scale_elems(rows, n)
+    return (n + 127) // 128 * ((rows + 15) // 16 * 16) if rows > 0 and n > 0 else 0
 
 
 def _bytes(who, t, n):
@@ -687,28 +710,32 @@ def _bytes(who, t, n):
     _elems(who, t, n)
 
 
-def _form(who, codes, scale, rows, n):
-    lib = load()
-    _bytes(who, codes, rows * lib.bf_op_fp8_row_bytes(n))
-    _bytes(who, scale, lib.bf_op_fp8_scale_elems(rows, n))
+def _form(who, codes, scale, rows, n, dev):
+    """Checks the form of a matrix [rows, n].  (Small calls are bound by the host: what is right is seen in one expression.)"""
+    lines = (n + 127) // 128
+    if codes.element_size() != 1 or scale.element_size() != 1 or codes.numel() < rows * lines * 128 or scale.numel() < lines * ((rows + 15) // 16 * 16) or \
+            codes.get_device() != dev or scale.get_device() != dev or not codes.is_contiguous() or not scale.is_contiguous():
+        _bytes(who, codes, rows * bf_op_fp8_row_bytes(n))
+        _bytes(who, scale, bf_op_fp8_scale_elems(rows, n))
 
 
 def bf_op_fp8_quantize(dtype, format, rows, cols, x, q=None, scale=None, qt=None, scale_t=None, ld_x=0):
     """8-bit forms of x [rows, cols] along its rows (q, scale) and down its columns (qt, scale_t).  x: dense, or a view of two dimensions whose rows are
     dense (their distance is ld_x, taken from the view where ld_x is 0)."""
-    who = "bf_op_fp8_quantize"
-    if x.is_contiguous() and (x.dim() != 2 or ld_x or x.shape[1] == cols):
-        _tensors(who, (x,), _torch_dtype(dtype))
+    who, torch = "bf_op_fp8_quantize", _th()
+    dev = torch._C._cuda_getDevice()
+    if x.dtype is not _torch_dtype(dtype) or x.get_device() != dev:
+        _tensors(who, (x[:0],), _torch_dtype(dtype))
+    if x.is_contiguous() and (ld_x or x.dim() != 2 or x.shape[1] == cols):
         _elems(who, x, (rows - 1) * (ld_x or cols) + cols)
     else:
-        _tensors(who, (x[:0],), _torch_dtype(dtype))
         if x.dim() != 2 or x.shape[0] < rows or x.shape[1] < cols or x.stride(1) != 1 or x.stride(0) < cols or ld_x not in (0, x.stride(0)):
             raise ValueError("%s: %d x %d elements in rows %d apart of a tensor of shape %s, strides %s" % (who, rows, cols, ld_x, tuple(x.shape), x.stride()))
         ld_x = x.stride(0)
     if q is not None and scale is not None:
-        _form(who, q, scale, rows, cols)
+        _form(who, q, scale, rows, cols, dev)
     if qt is not None and scale_t is not None:
-        _form(who, qt, scale_t, cols, rows)
+        _form(who, qt, scale_t, cols, rows, dev)
     check(load().bf_op_fp8_quantize(dtype, format, rows, cols, x.data_ptr(), ld_x, _ptr(q), _ptr(scale), _ptr(qt), _ptr(scale_t), _stream()))
 
 
@@ -718,15 +745,16 @@ def bf_op_fp8_gemm_work_bytes(M, N, K):
 
 def bf_op_fp8_gemm(format_a, format_b, dtype, M, N, K, A, scale_a, B, scale_b, Cout, bias=None, R=None, accumulate=0, work=None):
     """Cout[M, N] = A B^T + bias + R (or += in fp32) from 8-bit forms A [M, K] and B [N, K]."""
-    who, lib = "bf_op_fp8_gemm", load()
-    _form(who, A, scale_a, M, K)
-    _form(who, B, scale_b, N, K)
-    out = [t for t in (Cout, R) if t is not None]
-    _tensors(who, out, _torch_dtype(dtype))
-    for t in out:
-        _elems(who, t, M * N)
+    who, lib, torch = "bf_op_fp8_gemm", load(), _th()
+    dev, want = torch._C._cuda_getDevice(), _torch_dtype(dtype)
+    _form(who, A, scale_a, M, K, dev)
+    _form(who, B, scale_b, N, K, dev)
+    for t in (Cout,) if R is None else (Cout, R):
+        if t.dtype is not want or t.get_device() != dev or not t.is_contiguous() or t.numel() < M * N:
+            _tensors(who, (t,), want)
+            _elems(who, t, M * N)
     if bias is not None:
-        _tensors(who, (bias,), _th().float32)
+        _tensors(who, (bias,), torch.float32)
         _elems(who, bias, N)
     n = lib.bf_op_fp8_gemm_work_bytes(M, N, K)
     if n or work is not None:
@@ -741,13 +769,12 @@ def bf_op_adam8_state_bytes(n):
 
 def _states(who, states, n):
     """Addresses of the states of tensors of n[i] elements."""
-    if states:
-        p, have = _list(who, states, states[0].dtype)
-        for t, h, k in zip(states, have, n):
-            if t.element_size() != 1 or h < (k + 127) // 128 * 258:
-                raise ValueError("%s: a state of %d bytes and more for %d elements, got %d of %s" % (who, (k + 127) // 128 * 258, k, h, t.dtype))
-        return p
-    return _array("Q")
+    if not states:
+        return _array("Q")
+    p, have = _list(who, states, states[0].dtype)
+    if states[0].element_size() != 1 or any([h < (k + 127) // 128 * 258 for h, k in zip(have, n)]):
+        raise ValueError("%s: a state is bf_op_adam8_state_bytes(n) bytes, 258 for each 128 elements" % who)
+    return p
 
 
 def bf_op_adam8(dtype, tensors, coef, seed, t, lr, beta1, beta2, adam_eps, weight_decay):
@@ -758,22 +785,16 @@ def bf_op_adam8(dtype, tensors, coef, seed, t, lr, beta1, beta2, adam_eps, weigh
     _elems(who, coef, 1)
     w, state, g, low = zip(*tensors) if tensors else ((),) * 4
     (pw, n), (pg, n1) = _list(who, w, torch.float32), _list(who, g, _torch_dtype(dtype))
-    pl, n2 = _list(who, [x for x in low if x is not None], torch.bfloat16)
-    if n != n1 or n2 != _array("Q", [k for k, x in zip(n, low) if x is not None]):
+    if n != n1:
         raise ValueError("%s: tensors of different sizes in one entry" % who)
-    ps, rest = _states(who, state, n), iter(pl)
-    a = _array("Q", [x for i, k in enumerate(n) for x in (pw[i], ps[i], pg[i], 0 if low[i] is None else next(rest), k)])  # bf_adam8_tensor
+    a = _table(pw, _states(who, state, n), pg, _optional(who, low, torch.bfloat16, n), n)  # bf_adam8_tensor
     check(load().bf_op_adam8(dtype, len(n), _at(a), coef.data_ptr(), seed, t, lr, beta1, beta2, adam_eps, weight_decay, _stream()))
 
 
 def bf_op_adam8_moments(dtype, tensors):
     """m and v (`dtype`) that states stand for.  tensors: (state, m, v) each, m or v or both."""
     who, want = "bf_op_adam8_moments", _torch_dtype(dtype)
-    n = _array("Q", [(v if m is None else m).numel() for _, m, v in tensors])
-    ms, vs = [m for _, m, _ in tensors if m is not None], [v for _, _, v in tensors if v is not None]
-    (pm, n1), (pv, n2) = _list(who, ms, want), _list(who, vs, want)
-    if n1 != _array("Q", [k for k, x in zip(n, tensors) if x[1] is not None]) or n2 != _array("Q", [k for k, x in zip(n, tensors) if x[2] is not None]):
-        raise ValueError("%s: tensors of different sizes in one entry" % who)
-    ps, rm, rv = _states(who, [s for s, _, _ in tensors], n), iter(pm), iter(pv)
-    a = _array("Q", [x for i, (_, m, v) in enumerate(tensors) for x in (ps[i], 0 if m is None else next(rm), 0 if v is None else next(rv), n[i])])
+    state, ms, vs = zip(*tensors) if tensors else ((),) * 3
+    n = _array("Q", [(v if m is None else m).numel() for m, v in zip(ms, vs)])
+    a = _table(_states(who, state, n), _optional(who, ms, want, n), _optional(who, vs, want, n), n)  # bf_adam8_moments_tensor
     check(load().bf_op_adam8_moments(dtype, len(n), _at(a), _stream()))

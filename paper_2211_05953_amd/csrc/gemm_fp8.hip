@@ -377,19 +377,36 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
 #endif
 }
 
-// C = the sum of the slices' planes in ascending order, and the epilogue
-template <typename TO>
-__global__ __launch_bounds__(256) void fp8_finish_kernel(size_t n, int N, int slices, const float* __restrict__ planes, TO* __restrict__ C,
-                                                         const float* __restrict__ bias, const TO* __restrict__ R, int accumulate) {
-  const size_t stride = (size_t)gridDim.x * 256;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
-    float x = 0.f;
+// C = the sum of the slices' planes in ascending order, and the epilogue; V neighbouring columns to a thread
+template <typename TO, int V>
+__global__ __launch_bounds__(256) void fp8_finish_kernel(uint32_t groups, uint32_t across, size_t plane, int slices, const float* __restrict__ planes,
+                                                         TO* C, const float* __restrict__ bias, const TO* R, int accumulate) {
+  typedef float F __attribute__((ext_vector_type(V)));
+  typedef TO O __attribute__((ext_vector_type(V)));
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < groups; i += gridDim.x * 256) {
+    const size_t at = (size_t)i * V;
+    F x = *reinterpret_cast<const F*>(planes + at);
 #pragma unroll 4
-    for (int s = 0; s < slices; ++s) x += planes[(size_t)s * n + i];
-    if (bias) x += bias[i % N];
-    if (R) x += (float)R[i];
-    if (accumulate) x += (float)C[i];
-    C[i] = (TO)x;
+    for (int s = 1; s < slices; ++s) x += *reinterpret_cast<const F*>(planes + s * plane + at);
+    if (bias) {
+      const uint32_t col = i % across * V;
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[e] += bias[col + e];
+    }
+    O o;
+    if (R) {
+      o = *reinterpret_cast<const O*>(R + at);
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[e] += (float)o[e];
+    }
+    if (accumulate) {
+      o = *reinterpret_cast<const O*>(C + at);
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[e] += (float)o[e];
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] = (TO)x[e];
+    *reinterpret_cast<O*>(C + at) = o;
   }
 }
 
@@ -400,18 +417,33 @@ typedef Tile8<64, 64, 2, 2, 4> Small8;
 
 struct Plan { int tile, slices, slice; };  // tile 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
 
-Plan plan_of(int M, int N, int blocks) {
-  auto tiles = [&](int e) { return (long)((M + e - 1) / e) * ((N + e - 1) / e); };
-  Plan q{tiles(256) >= 192 ? 0 : tiles(128) >= 256 ? 1 : 2, 1, blocks};
-  if (q.tile == 2 && tiles(64) < 512 && blocks >= 8) {
-    const long want = 1024 / tiles(64), most = blocks / 4;
-    const int s = (int)(want < most ? want : most);
-    if (s > 1) {
-      q.slice = (blocks + s - 1) / s;
-      q.slices = (blocks + q.slice - 1) / q.slice;
+// The tile, and the slices that the contraction is cut into, of the least estimated time.  A round of workgroups over the chip takes START + blocks x BLOCK us, BLOCK_HALF
+// where at most half of its places are taken; a split costs a second kernel and the planes' way to memory and back.  Fitted to 28 shapes from 1 x 256 x 250 to 256 x 8192 x
+// 32768 on all tiles and splits; the choice is within 12 % of the best of them for all of them in both types.  us, 64 x 64 / 128 x 128 / 256 x 256, bf16 results:
+// 200 x 3000 x 1000 5.3 / 7.9 / 15.6; 1000 x 4004 x 1000 12.3 / 9.3 / 16.8; 2048 x 2048 x 8192 49 / 33 / 75; 2048 x 6144 x 2048 46 / 35 / 28.  Splits: 1 x 8192 x 8192 into fp32
+// 33 in one, 16 in 8 slices; 256 x 8192 x 32768 into fp32 185 on 64 x 64 tiles, 126 in 8 slices on 256 x 256; most shapes lose by them (1000 x 1000 x 4096 9.6 in one, 16 in two).
+constexpr double BASE_US = 2.5, SPLIT_US = 6.0, PLANE_BYTES_US = 9e6;
+struct TileCost { int edge, slots; double start, block, block_half; };
+constexpr TileCost COST[2][3] = {{{256, 256, 4.0, 1.7, 1.16}, {128, 256, 2.0, 0.5, 0.36}, {64, 512, 0.8, 0.4, 0.19}},   // 8-bit instructions
+                                 {{256, 256, 4.0, 3.35, 2.5}, {128, 256, 2.0, 1.1, 1.1}, {64, 512, 0.8, 0.6, 0.5}}};   // widened operands
+constexpr size_t MAX_PLANES = (size_t)1 << 28;
+
+Plan plan_of(int M, int N, int blocks, bool wide) {
+  Plan best{};
+  double best_t = 0;
+  for (int t = 0; t < 3; ++t) {
+    const TileCost& c = COST[wide][t];
+    const double tiles = (double)((M + c.edge - 1) / c.edge) * ((N + c.edge - 1) / c.edge);
+    for (int s = 1; s <= 16 && s <= blocks; s *= 2) {
+      const int slice = (blocks + s - 1) / s, slices = (blocks + slice - 1) / slice;
+      const double planes = 4.0 * M * N * slices, wgs = tiles * slices;
+      if (slices != s || (s > 1 && (wgs > 4 * c.slots || planes > (double)MAX_PLANES))) break;
+      const double rounds = (double)(long)((wgs + c.slots - 1) / c.slots), fill = wgs >= c.slots ? 1 : wgs <= c.slots / 2 ? 0 : 2 * wgs / c.slots - 1;
+      const double us = BASE_US + rounds * (c.start + slice * (c.block_half + (c.block - c.block_half) * fill)) + (s > 1 ? SPLIT_US + 2 * planes / PLANE_BYTES_US : 0);
+      if (!best.slices || us < best_t) { best = {t, slices, slice}; best_t = us; }
     }
   }
-  return q;
+  return best;
 }
 
 template <typename TL, int FA, int FB, bool WIDE, typename TO>
@@ -432,12 +464,37 @@ bf_status by_tile(const Fp8Args& a, int tile, int slices, bool wide, bool f32, h
     case 1: return launch8<Mid8, FA, FB, true, float>(a, slices, st);
     default: return launch8<Small8, FA, FB, true, float>(a, slices, st);
   }
-  if (f32) return launch8<Small8, FA, FB, false, float>(a, slices, st);  // planes
+  if (f32) switch (tile) {  // planes
+    case 0: return launch8<Big8, FA, FB, false, float>(a, slices, st);
+    case 1: return launch8<Mid8, FA, FB, false, float>(a, slices, st);
+    default: return launch8<Small8, FA, FB, false, float>(a, slices, st);
+  }
   switch (tile) {
     case 0: return launch8<Big8, FA, FB, false, bf16_t>(a, slices, st);
     case 1: return launch8<Mid8, FA, FB, false, bf16_t>(a, slices, st);
     default: return launch8<Small8, FA, FB, false, bf16_t>(a, slices, st);
   }
+}
+
+template <typename TO, int V>
+void launch_finish(int M, int N, int slices, const float* planes, void* C, const float* bias, const void* R, int accumulate, hipStream_t st) {
+  const size_t n = (size_t)M * N, groups = n / V;  // (splits are of few tiles: under 2^32)
+  const unsigned grid = (unsigned)((groups + 255) / 256 < 2048 ? (groups + 255) / 256 : 2048);
+  fp8_finish_kernel<TO, V><<<grid, 256, 0, st>>>((uint32_t)groups, (uint32_t)(N / V), n, slices, planes, (TO*)C, bias, (const TO*)R, accumulate);
+}
+
+bf_status finish(int dtype, int M, int N, int slices, const float* planes, void* C, const float* bias, const void* R, int accumulate, hipStream_t st) {
+  const bool four = N % 4 == 0 && (((uintptr_t)C | (uintptr_t)R) & (dtype == BF_BF16 ? 7 : 15)) == 0;
+  if (dtype == BF_BF16) {
+    if (four) launch_finish<bf16_t, 4>(M, N, slices, planes, C, bias, R, accumulate, st);
+    else launch_finish<bf16_t, 1>(M, N, slices, planes, C, bias, R, accumulate, st);
+  } else {
+    if (four) launch_finish<float, 4>(M, N, slices, planes, C, bias, R, accumulate, st);
+    else launch_finish<float, 1>(M, N, slices, planes, C, bias, R, accumulate, st);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) { set_error("bf_op_fp8_gemm: launch failed: %s", hipGetErrorString(e)); return BF_EDEVICE; }
+  return BF_OK;
 }
 
 bool sizes_ok(int M, int N, int K) { return M >= 1 && N >= 1 && K >= 1 && M <= (1 << 21) && N <= (1 << 21) && K <= (1 << 21); }
@@ -446,8 +503,13 @@ bool sizes_ok(int M, int N, int K) { return M >= 1 && N >= 1 && K >= 1 && M <= (
 
 size_t fp8_gemm_work_bytes(int M, int N, int K) {
   if (!sizes_ok(M, N, K)) return 0;
-  const Plan q = plan_of(M, N, (K + 127) / 128);
-  return q.slices > 1 ? (size_t)q.slices * M * N * sizeof(float) : 0;
+  size_t most = 0;
+  for (const bool wide : {false, true}) {
+    const Plan q = plan_of(M, N, (K + 127) / 128, wide);
+    const size_t n = q.slices > 1 ? (size_t)q.slices * M * N * sizeof(float) : 0;
+    most = n > most ? n : most;
+  }
+  return most;
 }
 
 bf_status fp8_gemm(int fa, int fb, int dtype, int M, int N, int K, const void* A, const void* sa, const void* B, const void* sb, void* C, const float* bias,
@@ -462,10 +524,12 @@ bf_status fp8_gemm(int fa, int fb, int dtype, int M, int N, int K, const void* A
   }
   if (accumulate && dtype != BF_FP32) { set_error("bf_op_fp8_gemm: accumulates into fp32 only"); return BF_EINVAL; }
   const int blocks = (K + 127) / 128;
-  const Plan q = plan_of(M, N, blocks);
-  const bool wide = dtype == BF_FP32, split = q.slices > 1;
-  if (split && (!work || ((uintptr_t)work & 255) || work_bytes < (size_t)q.slices * M * N * sizeof(float))) {
-    set_error("bf_op_fp8_gemm: needs %zu bytes of 256-byte aligned scratch", (size_t)q.slices * M * N * sizeof(float));
+  const bool wide = dtype == BF_FP32;
+  const Plan q = plan_of(M, N, blocks, wide);
+  const bool split = q.slices > 1;
+  const size_t need = fp8_gemm_work_bytes(M, N, K);
+  if (need && (!work || ((uintptr_t)work & 255) || work_bytes < need)) {
+    set_error("bf_op_fp8_gemm: needs %zu bytes of 256-byte aligned scratch", need);
     return BF_EINVAL;
   }
   Fp8Args a{M, N, blocks, (const uint8_t*)A, (const uint8_t*)B, (const uint8_t*)sa, (const uint8_t*)sb, (M + 15) / 16 * 16, (N + 15) / 16 * 16, C, bias, R,
@@ -480,14 +544,7 @@ bf_status fp8_gemm(int fa, int fb, int dtype, int M, int N, int K, const void* A
   if (fa == BF_E4M3) s = fb == BF_E4M3 ? by_tile<0, 0>(a, q.tile, q.slices, wide, split, st) : by_tile<0, 1>(a, q.tile, q.slices, wide, split, st);
   else s = fb == BF_E4M3 ? by_tile<1, 0>(a, q.tile, q.slices, wide, split, st) : by_tile<1, 1>(a, q.tile, q.slices, wide, split, st);
   if (s != BF_OK || !split) return s;
-  const size_t n = (size_t)M * N;
-  const unsigned grid = (unsigned)((n + 255) / 256 < 4096 ? (n + 255) / 256 : 4096);
-  if (dtype == BF_BF16)
-    fp8_finish_kernel<bf16_t><<<grid, 256, 0, st>>>(n, N, q.slices, (const float*)work, (bf16_t*)C, bias, (const bf16_t*)R, accumulate);
-  else fp8_finish_kernel<float><<<grid, 256, 0, st>>>(n, N, q.slices, (const float*)work, (float*)C, bias, (const float*)R, accumulate);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) { set_error("bf_op_fp8_gemm: launch failed: %s", hipGetErrorString(e)); return BF_EDEVICE; }
-  return BF_OK;
+  return finish(dtype, M, N, q.slices, (const float*)work, C, bias, R, accumulate, st);
 }
 
 }  // namespace bf
