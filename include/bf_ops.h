@@ -296,7 +296,7 @@ bf_status bf_op_fp8_gemm(int format_a, int format_b, int dtype, int M, int N, in
  * (in 65536ths): a mean that moves by less than half a code each step still moves.  The random numbers are a hash of (seed, t, the tensor's place
  * in the list, element): the same call gives the same bits.  A v above zero is kept at the smallest code or more, 2^-18.95 of the block's
  * largest, so that no step is divided by a v that was rounded away.  t and seed are values of the call: a captured graph repeats them.
- * A coefficient that is not finite leaves the step out.  No two tensors may overlap. */
+ * The rates are double, as 1 - beta2 of an fp32 0.999 is 5e-5 off.  A coefficient that is not finite leaves the step out.  No two tensors may overlap. */
 typedef struct {
   float* w;
   void* state;
@@ -305,8 +305,8 @@ typedef struct {
   size_t n;
 } bf_adam8_tensor;
 size_t bf_op_adam8_state_bytes(size_t n);
-bf_status bf_op_adam8(int dtype, int n_tensors, const bf_adam8_tensor* tensors, const float* coef, uint64_t seed, int t, float lr, float beta1, float beta2,
-                      float adam_eps, float weight_decay, void* stream);
+bf_status bf_op_adam8(int dtype, int n_tensors, const bf_adam8_tensor* tensors, const float* coef, uint64_t seed, int t, double lr, double beta1, double beta2,
+                      double adam_eps, double weight_decay, void* stream);
 /* What states stand for: m and v of n elements each in `dtype` (bf16 holds every code times its scale exactly, but under 2^-126), either may be NULL. */
 typedef struct {
   const void* state;

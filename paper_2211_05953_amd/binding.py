@@ -149,7 +149,7 @@ _SIGNATURES = {
     "bf_op_fp8_gemm_work_bytes": (C.c_size_t, [C.c_int] * 3),
     "bf_op_fp8_gemm": (C.c_int, [C.c_int] * 6 + [_P] * 7 + [C.c_int, _P, C.c_size_t, _P]),
     "bf_op_adam8_state_bytes": (C.c_size_t, [C.c_size_t]),
-    "bf_op_adam8": (C.c_int, [C.c_int, C.c_int, _P, _P, C.c_uint64, C.c_int] + [C.c_float] * 5 + [_P]),
+    "bf_op_adam8": (C.c_int, [C.c_int, C.c_int, _P, _P, C.c_uint64, C.c_int] + [C.c_double] * 5 + [_P]),
     "bf_op_adam8_moments": (C.c_int, [C.c_int, C.c_int, _P, _P]),
     "bf_op_adam": (C.c_int, [C.c_size_t, _P, _P, _P, _P, _P, C.c_int] + [C.c_float] * 5 + [_P]),
 }

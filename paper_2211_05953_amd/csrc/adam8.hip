@@ -32,7 +32,8 @@ struct Table8 {
 };
 static_assert(sizeof(Table8) <= 3600, "kernel arguments");
 
-struct AdamArgs8 { float lr, beta1, beta2, eps, wd, c1, c2, omb1, omb2; };
+// b: beta, a: 1 - beta, each as the sum of two fp32 numbers: their own rounding would move as many codes as the moments' does
+struct AdamArgs8 { float lr, eps, wd, c1, c2, b1, b1_low, a1, a1_low, b2, b2_low, a2, a2_low; };
 
 // xor shifts and odd multipliers (the first 32 bits of the fractions of sqrt 2 and sqrt 3): over random inputs a flipped input bit flips
 // every output bit with a chance of 0.495 to 0.505
@@ -86,17 +87,26 @@ __device__ __forceinline__ float decode_v(uint32_t codes, int k) {
   return c < 16 ? (float)c * 0.0625f : __uint_as_float((c << 19) + ((uint32_t)(127 - 1) << 23));
 }
 
-// code of y >= 0 (LOW: exponent of the smallest normal code, BITS of mantissa), r: 16 random bits
+// code of y >= 0 (LOW: exponent of the smallest normal code, BITS of mantissa), r: 16 random bits.  near: the sum lies so near to a carry that y's own rounding
+// decides
 template <int LOW, int BITS>
-__device__ __forceinline__ uint32_t encode(float y, uint32_t r) {
+__device__ __forceinline__ uint32_t encode(float y, uint32_t r, bool& near) {
   const int e = max((int)(__float_as_uint(y) >> 23) - 127, LOW);
   const uint32_t k = (uint32_t)(y * __uint_as_float((uint32_t)(127 + 16 + BITS - e) << 23));  // y / step, in 65536ths
+  near = (k & 0xffffu) + r - 0xfffdu <= 5u;
+  return (uint32_t)((e - LOW) << BITS) + ((k + r) >> 16);
+}
+// the same of the moment in fp64: y = |moment| 2^-unit
+template <int LOW, int BITS>
+__device__ __forceinline__ uint32_t encode_exact(double y, uint32_t r) {
+  const int e = max((int)(__double_as_longlong(y) >> 52) - 1023, LOW);
+  const uint32_t k = (uint32_t)ldexp(y, 16 + BITS - e);
   return (uint32_t)((e - LOW) << BITS) + ((k + r) >> 16);
 }
 
-// All loads of four runs of 4 elements are in flight at once, accesses do not stay in the caches.  230 M parameters, step / reading the moments out in bf16, us: with caching
-// 871 / 271, without 830 / 267 (5.0 and 5.2 TB/s; a copy reaches 5.2 to 5.6); two runs 865 / 271; runs of 8 elements, half as many 866 / 272; 512 workgroups 926 / 457 (the
-// step's arithmetic then shows: 822 with approximate roots and quotients, which gain 0.5 % on 2048).
+// All loads of four runs of 4 elements are in flight at once, accesses do not stay in the caches.  230 M parameters, step / reading the moments out in bf16: 812 / 267 us, 5.1 and
+// 5.2 TB/s (a copy reaches 5.2 to 5.6).  Of the step: with caching 40 us more; with root and quotient to the last bit 50 more; without the second look at near carries 15 less; two
+// runs of 4, or of 8 elements 35 more; 512 workgroups 110 more.
 constexpr int VECS = 4;
 constexpr int CHUNK = NT * 4 * VECS;
 
@@ -151,10 +161,13 @@ __global__ __launch_bounds__(NT) void adam8_kernel(Table8 t, const float* __rest
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float gk = gg[i][k] * ck;
-        m[k] = fmaf(a.omb1, gk, a.beta1 * ldexpf(decode_m(cm[i], k), em0));
-        v[k] = fmaf(a.omb2 * gk, gk, a.beta2 * ldexpf(decode_v(cv[i], k), ev0));
+        const float m0 = ldexpf(decode_m(cm[i], k), em0), v0 = ldexpf(decode_v(cv[i], k), ev0), g2 = gk * gk;
+        m[k] = fmaf(a.a1, gk, fmaf(a.b1, m0, fmaf(a.a1_low, gk, a.b1_low * m0)));
+        v[k] = fmaf(a.a2, g2, fmaf(a.b2, v0, fmaf(a.a2_low, g2, a.b2_low * v0)));
         const float wk = ww[i][k];
-        ww[i][k] = fmaf(-a.lr, fmaf(a.wd, wk, m[k] * a.c1 / (sqrtf(v[k] * a.c2) + a.eps)), wk);
+        // (root and reciprocal to an ulp each; they do not take numbers below 2^-126: a root counts as 2^-63 at least)
+        const float root = __builtin_amdgcn_sqrtf(fmaxf(v[k] * a.c2, FLT_MIN));
+        ww[i][k] = fmaf(-a.lr, fmaf(a.wd, wk, m[k] * a.c1 * __builtin_amdgcn_rcpf(root + a.eps)), wk);
         o[k] = (bf16_t)(float)ww[i][k];
         tm = max(tm, finite_bits8(m[k]));
         tv = max(tv, finite_bits8(v[k]));
@@ -162,17 +175,37 @@ __global__ __launch_bounds__(NT) void adam8_kernel(Table8 t, const float* __rest
       const int em = exponent8<EXP_M, TOP_M>(max32(tm)), ev = exponent8<EXP_V, TOP_V>(max32(tv));
       const float um = __uint_as_float((uint32_t)(127 - em) << 23), uv = __uint_as_float((uint32_t)(127 - ev) << 23);
       uint32_t nm = 0, nv = 0;
+      bool any = false;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t h = mix32(q + k + key);
         const uint32_t bm = __float_as_uint(m[k]), bv = __float_as_uint(v[k]);
-        uint32_t x = min(encode<-6, 3>(fminf(fabsf(m[k]) * um, 448.f), h & 0xffffu), 0x7eu);
+        bool near_m, near_v;
+        uint32_t x = min(encode<-6, 3>(fminf(fabsf(m[k]) * um, 448.f), h & 0xffffu, near_m), 0x7eu);
         x = (bm & 0x7f800000u) == 0x7f800000u ? 0x7fu : x;
         nm |= (x | ((bm >> 24) & 0x80u)) << (8 * k);
-        uint32_t y = min(encode<0, 4>(fminf(v[k] * uv, 31744.f), h >> 16), 255u);
+        uint32_t y = min(encode<0, 4>(fminf(v[k] * uv, 31744.f), h >> 16, near_v), 255u);
         y = bv != 0 ? max(y, 1u) : 0u;
         y = (bv & 0x7f800000u) == 0x7f800000u ? 255u : y;
         nv |= y << (8 * k);
+        any |= near_m | near_v;
+      }
+      if (any) {  // (a lane in 1400: the moments again in fp64, so that the codes are the definition's and not their fp32 rounding's)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t h = mix32(q + k + key);
+          const double gk = (double)gg[i][k] * ck;
+          const double md = ((double)a.b1 + a.b1_low) * (double)ldexpf(decode_m(cm[i], k), em0) + ((double)a.a1 + a.a1_low) * gk;
+          const double vd = ((double)a.b2 + a.b2_low) * (double)ldexpf(decode_v(cv[i], k), ev0) + ((double)a.a2 + a.a2_low) * gk * gk;
+          if (fabs(md) <= FLT_MAX) {
+            const uint32_t x = min(encode_exact<-6, 3>(fmin(fabs(md) * um, 448.0), h & 0xffffu), 0x7eu);
+            nm = (nm & ~(0xffu << (8 * k))) | (x | (md < 0 ? 0x80u : 0u)) << (8 * k);
+          }
+          if (vd <= FLT_MAX && vd > 0) {
+            const uint32_t y = max(min(encode_exact<0, 4>(fmin(vd * uv, 31744.0), h >> 16), 255u), 1u);
+            nv = (nv & ~(0xffu << (8 * k))) | y << (8 * k);
+          }
+        }
       }
       if (whole) {
         __builtin_nontemporal_store(ww[i], reinterpret_cast<V4*>(w + q));
@@ -263,8 +296,8 @@ constexpr unsigned MAX_WG = 2048;
 
 size_t adam8_state_bytes(size_t n) { return blocks_of(n) * (2 * BLK + 2); }
 
-bf_status adam8_step(int dtype, int n_tensors, const bf_adam8_tensor* x, const float* coef, uint64_t seed, int step, float lr, float beta1, float beta2, float eps,
-                     float wd, hipStream_t st) {
+bf_status adam8_step(int dtype, int n_tensors, const bf_adam8_tensor* x, const float* coef, uint64_t seed, int step, double lr, double beta1, double beta2, double eps,
+                     double wd, hipStream_t st) {
   if (n_tensors < 0 || (n_tensors > 0 && !x)) { set_error("bf_op_adam8: bad list of tensors"); return BF_EINVAL; }
   if (!coef || ((uintptr_t)coef & 3) || step < 1) { set_error("bf_op_adam8: coef is null or not aligned to its elements, or step below 1"); return BF_EINVAL; }
   const size_t es = dtype == BF_BF16 ? 2 : 4;
@@ -275,8 +308,12 @@ bf_status adam8_step(int dtype, int n_tensors, const bf_adam8_tensor* x, const f
       return BF_EINVAL;
     }
   }
-  AdamArgs8 a{lr, beta1, beta2, eps, wd, (float)(1.0 / (1.0 - pow((double)beta1, (double)step))), (float)(1.0 / (1.0 - pow((double)beta2, (double)step))),
-              (float)(1.0 - (double)beta1), (float)(1.0 - (double)beta2)};
+  AdamArgs8 a{(float)lr, (float)eps, (float)wd, (float)(1.0 / (1.0 - pow(beta1, (double)step))), (float)(1.0 / (1.0 - pow(beta2, (double)step)))};
+  auto pair = [](double x, float& high, float& low) { high = (float)x; low = (float)(x - (double)high); };
+  pair(beta1, a.b1, a.b1_low);
+  pair(1.0 - beta1, a.a1, a.a1_low);
+  pair(beta2, a.b2, a.b2_low);
+  pair(1.0 - beta2, a.a2, a.a2_low);
   const uint32_t key = mix32(mix32(mix32((uint32_t)seed) ^ (uint32_t)(seed >> 32)) ^ (uint32_t)step);
   int at = 0;
   size_t off = 0;

@@ -20,8 +20,8 @@ size_t fp8_gemm_work_bytes(int M, int N, int K);
 bf_status fp8_gemm(int fa, int fb, int dtype, int M, int N, int K, const void* A, const void* sa, const void* B, const void* sb, void* C, const float* bias,
                    const void* R, int accumulate, void* work, size_t work_bytes, hipStream_t st);
 size_t adam8_state_bytes(size_t n);
-bf_status adam8_step(int dtype, int n_tensors, const bf_adam8_tensor* x, const float* coef, uint64_t seed, int step, float lr, float beta1, float beta2, float eps,
-                     float wd, hipStream_t st);
+bf_status adam8_step(int dtype, int n_tensors, const bf_adam8_tensor* x, const float* coef, uint64_t seed, int step, double lr, double beta1, double beta2,
+                     double eps, double wd, hipStream_t st);
 bf_status adam8_moments(int dtype, int n_tensors, const bf_adam8_moments_tensor* x, hipStream_t st);
 }  // namespace bf
 
@@ -292,8 +292,8 @@ bf_status bf_op_fp8_gemm(int format_a, int format_b, int dtype, int M, int N, in
 
 size_t bf_op_adam8_state_bytes(size_t n) { return adam8_state_bytes(n); }
 
-bf_status bf_op_adam8(int dtype, int n_tensors, const bf_adam8_tensor* tensors, const float* coef, uint64_t seed, int t, float lr, float beta1, float beta2,
-                      float adam_eps, float weight_decay, void* stream) {
+bf_status bf_op_adam8(int dtype, int n_tensors, const bf_adam8_tensor* tensors, const float* coef, uint64_t seed, int t, double lr, double beta1, double beta2,
+                      double adam_eps, double weight_decay, void* stream) {
   if (!dtype_ok(dtype, 0)) return BF_EINVAL;
   return adam8_step(dtype, n_tensors, tensors, coef, seed, t, lr, beta1, beta2, adam_eps, weight_decay, (hipStream_t)stream);
 }
