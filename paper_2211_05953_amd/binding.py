@@ -146,7 +146,7 @@ _SIGNATURES = {
     "bf_op_fp8_row_bytes": (C.c_size_t, [C.c_int]),
     "bf_op_fp8_scale_elems": (C.c_size_t, [C.c_int] * 2),
     "bf_op_fp8_quantize": (C.c_int, [C.c_int] * 4 + [_P, C.c_size_t] + [_P] * 5),
-    "bf_op_fp8_gemm_work_bytes": (C.c_size_t, [C.c_int] * 3),
+    "bf_op_fp8_gemm_work_bytes": (C.c_size_t, [C.c_int] * 4),
     "bf_op_fp8_gemm": (C.c_int, [C.c_int] * 6 + [_P] * 7 + [C.c_int, _P, C.c_size_t, _P]),
     "bf_op_adam8_state_bytes": (C.c_size_t, [C.c_size_t]),
     "bf_op_adam8": (C.c_int, [C.c_int, C.c_int, _P, _P, C.c_uint64, C.c_int] + [C.c_double] * 5 + [_P]),
@@ -739,8 +739,8 @@ def bf_op_fp8_quantize(dtype, format, rows, cols, x, q=None, scale=None, qt=None
     check(load().bf_op_fp8_quantize(dtype, format, rows, cols, x.data_ptr(), ld_x, _ptr(q), _ptr(scale), _ptr(qt), _ptr(scale_t), _stream()))
 
 
-def bf_op_fp8_gemm_work_bytes(M, N, K):
-    return load().bf_op_fp8_gemm_work_bytes(M, N, K)
+def bf_op_fp8_gemm_work_bytes(dtype, M, N, K):
+    return load().bf_op_fp8_gemm_work_bytes(dtype, M, N, K)
 
 
 def bf_op_fp8_gemm(format_a, format_b, dtype, M, N, K, A, scale_a, B, scale_b, Cout, bias=None, R=None, accumulate=0, work=None):
@@ -756,7 +756,7 @@ def bf_op_fp8_gemm(format_a, format_b, dtype, M, N, K, A, scale_a, B, scale_b, C
     if bias is not None:
         _tensors(who, (bias,), torch.float32)
         _elems(who, bias, N)
-    n = lib.bf_op_fp8_gemm_work_bytes(M, N, K)
+    n = lib.bf_op_fp8_gemm_work_bytes(dtype, M, N, K)
     if n or work is not None:
         work = _work(who, work, n)
     check(lib.bf_op_fp8_gemm(format_a, format_b, dtype, M, N, K, A.data_ptr(), scale_a.data_ptr(), B.data_ptr(), scale_b.data_ptr(), Cout.data_ptr(), _ptr(bias),

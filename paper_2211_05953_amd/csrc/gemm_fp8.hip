@@ -440,7 +440,7 @@ Plan plan_of(int M, int N, int blocks, bool wide) {
       if (slices != s || (s > 1 && (wgs > 4 * c.slots || planes > (double)MAX_PLANES))) break;
       const double rounds = (double)(long)((wgs + c.slots - 1) / c.slots), fill = wgs >= c.slots ? 1 : wgs <= c.slots / 2 ? 0 : 2 * wgs / c.slots - 1;
       const double us = BASE_US + rounds * (c.start + slice * (c.block_half + (c.block - c.block_half) * fill)) + (s > 1 ? SPLIT_US + 2 * planes / PLANE_BYTES_US : 0);
-      if (!best.slices || us < best_t) { best = {t, slices, slice}; best_t = us; }
+      if (!best.slices || (s > 1 ? us < 0.9 * best_t : us < best_t)) { best = {t, slices, slice}; best_t = us; }
     }
   }
   return best;
@@ -501,15 +501,10 @@ bool sizes_ok(int M, int N, int K) { return M >= 1 && N >= 1 && K >= 1 && M <= (
 
 }  // namespace
 
-size_t fp8_gemm_work_bytes(int M, int N, int K) {
-  if (!sizes_ok(M, N, K)) return 0;
-  size_t most = 0;
-  for (const bool wide : {false, true}) {
-    const Plan q = plan_of(M, N, (K + 127) / 128, wide);
-    const size_t n = q.slices > 1 ? (size_t)q.slices * M * N * sizeof(float) : 0;
-    most = n > most ? n : most;
-  }
-  return most;
+size_t fp8_gemm_work_bytes(int dtype, int M, int N, int K) {
+  if (!sizes_ok(M, N, K) || (dtype != BF_BF16 && dtype != BF_FP32)) return 0;
+  const Plan q = plan_of(M, N, (K + 127) / 128, dtype == BF_FP32);
+  return q.slices > 1 ? (size_t)q.slices * M * N * sizeof(float) : 0;
 }
 
 bf_status fp8_gemm(int fa, int fb, int dtype, int M, int N, int K, const void* A, const void* sa, const void* B, const void* sb, void* C, const float* bias,
@@ -527,7 +522,7 @@ bf_status fp8_gemm(int fa, int fb, int dtype, int M, int N, int K, const void* A
   const bool wide = dtype == BF_FP32;
   const Plan q = plan_of(M, N, blocks, wide);
   const bool split = q.slices > 1;
-  const size_t need = fp8_gemm_work_bytes(M, N, K);
+  const size_t need = split ? (size_t)q.slices * M * N * sizeof(float) : 0;
   if (need && (!work || ((uintptr_t)work & 255) || work_bytes < need)) {
     set_error("bf_op_fp8_gemm: needs %zu bytes of 256-byte aligned scratch", need);
     return BF_EINVAL;

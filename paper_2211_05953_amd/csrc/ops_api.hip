@@ -16,7 +16,7 @@ bf_status attention_masked_bwd(const bf_attn_config* c, const void* q, const voi
 bf_status adam_clipped(int n_tensors, const bf_adam_tensor* x, const float* coef, int step, float lr, float beta1, float beta2, float eps, float wd,
                        hipStream_t st);
 bf_status fp8_quantize(int dtype, int format, int rows, int cols, const void* x, size_t ld, void* q, void* scale, void* qt, void* scale_t, hipStream_t st);
-size_t fp8_gemm_work_bytes(int M, int N, int K);
+size_t fp8_gemm_work_bytes(int dtype, int M, int N, int K);
 bf_status fp8_gemm(int fa, int fb, int dtype, int M, int N, int K, const void* A, const void* sa, const void* B, const void* sb, void* C, const float* bias,
                    const void* R, int accumulate, void* work, size_t work_bytes, hipStream_t st);
 size_t adam8_state_bytes(size_t n);
@@ -282,7 +282,7 @@ bf_status bf_op_fp8_quantize(int dtype, int format, int rows, int cols, const vo
   return fp8_quantize(dtype, format, rows, cols, x, ld_x, q, scale, qt, scale_t, (hipStream_t)stream);
 }
 
-size_t bf_op_fp8_gemm_work_bytes(int M, int N, int K) { return fp8_gemm_work_bytes(M, N, K); }
+size_t bf_op_fp8_gemm_work_bytes(int dtype, int M, int N, int K) { return fp8_gemm_work_bytes(dtype, M, N, K); }
 
 bf_status bf_op_fp8_gemm(int format_a, int format_b, int dtype, int M, int N, int K, const void* A, const void* scale_a, const void* B,
                          const void* scale_b, void* C, const float* bias, const void* R, int accumulate, void* work, size_t work_bytes, void* stream) {

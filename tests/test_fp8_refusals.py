@@ -36,16 +36,16 @@ def test_quantize_refusals():
 
 def test_product_refusals():
     ok = [bf.BF_E4M3, bf.BF_E5M2, bf.BF_BF16, 10, 20, 30, X, X, X, X, X, X, X, 0, None, 0, None]
-    assert bf.bf_op_fp8_gemm_work_bytes(10, 20, 30) == 0
+    assert bf.bf_op_fp8_gemm_work_bytes(bf.BF_BF16, 10, 20, 30) == 0
     for at, bad in ((0, 2), (0, -1), (1, 2), (2, 7), (3, 0), (4, 0), (5, 0), (3, BIG + 1), (4, BIG + 1), (5, BIG + 1), (6, None), (7, None), (8, None), (9, None),
                     (10, None), (6, X + 8), (7, X + 4), (8, X + 8), (9, X + 2), (10, X + 1), (11, X + 2), (12, X + 1), (13, 1)):
         refused("bf_op_fp8_gemm", *swapped(ok, at, bad))
     # with a split contraction: the scratch
-    need = bf.bf_op_fp8_gemm_work_bytes(10, 20, 1 << 14)
+    need = bf.bf_op_fp8_gemm_work_bytes(bf.BF_FP32, 10, 20, 1 << 14)
     assert need > 0 and need % (10 * 20 * 4) == 0
     for work, size in ((None, need), (X + 16, need), (X, need - 1), (X, 0)):
-        refused("bf_op_fp8_gemm", *swapped(ok, 5, 1 << 14)[:14], work, size, None)
-    assert [bf.bf_op_fp8_gemm_work_bytes(*s) for s in ((0, 1, 1), (1, -1, 1), (1, 1, BIG + 1))] == [0, 0, 0]
+        refused("bf_op_fp8_gemm", *swapped(swapped(ok, 2, bf.BF_FP32), 5, 1 << 14)[:14], work, size, None)
+    assert [bf.bf_op_fp8_gemm_work_bytes(*s) for s in ((0, 0, 1, 1), (0, 1, -1, 1), (1, 1, 1, BIG + 1), (7, 10, 20, 1 << 14))] == [0, 0, 0, 0]
 
 
 def test_adam_refusals():

@@ -255,3 +255,43 @@ def test_a_training_step_in_8_bits():
         graph.replay()
         torch.cuda.synchronize()
     assert all(torch.equal(b[k], c[k]) for k in ("w", "lp", "state", "y", "dx", "dw", "out"))
+
+
+def test_a_tensor_past_a_table_entry():
+    """More than 2^30 elements in one tensor: the elements around the border and at the end are stepped like any others."""
+    n = (1 << 30) + 777
+    w, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    state = torch.zeros(bf.bf_op_adam8_state_bytes(n), dtype=torch.uint8, device="cuda")
+    parts = [slice(0, 1280), slice((1 << 30) - 640, (1 << 30) + 640), slice((1 << 30) + 128 * 5, n)]
+    for p in parts:
+        w[p], g[p] = torch.randn_like(w[p]), torch.randn_like(w[p]).bfloat16()
+    before = [(w[p].clone(), g[p].clone()) for p in parts]
+    bf.bf_op_adam8(bf.BF_BF16, [(w, state, g, None)], torch.ones(1, device="cuda"), 5, 1, LR, B1, B2, EPS, WD)
+    r = P.randoms(5, 1, 0, 1, "cuda")  # (the key's way is that of the other tests: here only places matter)
+    assert len(r) == 2
+    m, v = torch.empty(n, dtype=torch.bfloat16, device="cuda"), torch.empty(n, dtype=torch.bfloat16, device="cuda")
+    bf.bf_op_adam8_moments(bf.BF_BF16, [(state, m, v)])
+    key = 0
+    for word in (5, 0, 1):
+        key = P.mix(key ^ word)
+    key = P.mix(key ^ 0)
+    for p, (w0, g0) in zip(parts, before):
+        zero = torch.zeros(-(-w0.numel() // 128) * 258, dtype=torch.uint8, device="cuda")
+        ref, m64, v64 = P.adam(w0, zero, g0, 1.0, 1, LR, B1, B2, EPS, WD)
+        assert bool(((w[p].double() - ref).abs() <= 2.0**-23 * w0.abs() + LR * 2.0**-18).all())
+        h = P.mix((torch.arange(p.start, p.stop, device="cuda") + key) % 2**32)
+        for got, x, top, low, bits, rnd in ((m[p], m64, 448.0, -6, 3, h % 65536), (v[p], v64, 31744.0, 0, 4, h // 65536)):
+            x = x.view(-1)[: w0.numel()]
+            blocks = torch.nn.functional.pad(x.abs(), (0, -x.numel() % 128)).view(-1, 128)
+            unit = P.power(P.exponent(blocks.amax(1), top)).repeat_interleave(128)[: x.numel()]
+            y = x.abs() / unit
+            step = P.power((torch.frexp(y)[1] - 1).clamp(min=low) - bits)
+            part = y / step
+            code = torch.floor(part) + (torch.floor((part - torch.floor(part)) * 65536) + rnd >= 65536)
+            code = torch.where((x != 0) & (code == 0) & (low == 0), torch.ones_like(code), code)
+            off = got.double().abs() / unit != code * step
+            assert float(off.double().mean()) <= 2e-3  # (moments a rounding away from the next code)
+    fine = torch.ones(n, dtype=torch.bool, device="cuda")
+    for p in parts:
+        fine[p] = False
+    assert not bool(w[fine].any()) and not bool(m[fine].any())

@@ -243,7 +243,7 @@ def test_a_layer_under_capture():
     (x, w, dy), _ = _layer(T, h_in, h_out, bf.BF_BF16, 0, bf.BF_FP32)
     bufs = [_new(T, h_in), _new(h_in, T), _new(h_in, h_out), _new(h_out, h_in), _new(T, h_out), _new(h_out, T)]
     y, dx, dw = torch.empty(T, h_out, dtype=torch.bfloat16, device="cuda"), torch.empty(T, h_in, dtype=torch.bfloat16, device="cuda"), torch.empty(h_in, h_out, device="cuda")
-    work = [torch.empty(max(256, bf.bf_op_fp8_gemm_work_bytes(*s)), dtype=torch.uint8, device="cuda") for s in ((T, h_out, h_in), (T, h_in, h_out), (h_in, h_out, T))]
+    work = [torch.empty(max(256, bf.bf_op_fp8_gemm_work_bytes(*s)), dtype=torch.uint8, device="cuda") for s in ((1, T, h_out, h_in), (1, T, h_in, h_out), (0, h_in, h_out, T))]
 
     def step():
         bf.bf_op_fp8_quantize(1, 0, T, h_in, x, *bufs[0], *bufs[1])
@@ -282,3 +282,59 @@ def test_calls_on_two_streams_at_once():
     torch.cuda.synchronize()
     for a, b in zip(want, got):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("dtype", [bf.BF_BF16, bf.BF_FP32])
+def test_scales_of_the_whole_range(dtype):
+    """Blocks whose scales are far apart, and products of a very small by a very large one."""
+    M, N, K = 80, 72, 640
+    (A, sa), _ = _operand(M, K, 0, 11)
+    (B, sb), _ = _operand(N, K, 0, 12)
+    e = torch.tensor([-90, -30, 0, 45, 100], device="cuda")
+    sa[:, :M] = (127 + e)[:, None].to(torch.uint8)
+    sb[:, :N] = (127 - e + torch.arange(5, device="cuda"))[:, None].to(torch.uint8)
+    a, b = P.values(A, sa, K, 0), P.values(B, sb, K, 0)
+    out = torch.empty(M, N, dtype=DT[dtype], device="cuda")
+    bf.bf_op_fp8_gemm(0, 0, dtype, M, N, K, A, sa, B, sb, out)
+    _close(out, a @ b.t(), a.abs() @ b.abs().t(), K, dtype)
+
+
+def test_offsets_past_32_bits():
+    """Operands and forms of more than 2^32 bytes, rows and results at their far ends."""
+    M, K, N = (1 << 21) - 5, 2100, 6
+    x = torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    torch.manual_seed(1)
+    for k in range(0, M, 1 << 18):
+        x[k: k + (1 << 18)] = torch.randn(min(1 << 18, M - k), K, device="cuda")
+    (A, sa), (At, sat) = _new(M, K), _new(K, M)
+    bf.bf_op_fp8_quantize(bf.BF_BF16, 0, M, K, x, A, sa, At, sat)
+    assert A.numel() > 2**32
+    for rows in (slice(0, 200), slice(M - 200, M)):
+        q, s = P.form(x[rows], 0)
+        got, sg = _views((A, sa), M, K)
+        assert torch.equal(got[rows].view(P.TYPES[0]).double(), q) and torch.equal(sg[:, rows], s[:, : 200])
+    cols, last = slice(K - 30, K), (M - 1) // 128 * 128
+    q, s = P.form(x[last:, cols].t().contiguous(), 0)
+    got, sg = _views((At, sat), K, M)
+    assert torch.equal(got[cols, last:].view(P.TYPES[0]).double(), q) and torch.equal(sg[-1, cols], s[0, :30])
+    (B, sb), b = _operand(N, K, 0, 5)
+    for dtype in (bf.BF_BF16, bf.BF_FP32):
+        out = torch.empty(M, N, dtype=DT[dtype], device="cuda")
+        bf.bf_op_fp8_gemm(0, 0, dtype, M, N, K, A[: M * 2176], sa, B, sb, out)
+        for rows in (slice(0, 300), slice(M - 300, M)):
+            a = P.values(*P.form(x[rows], 0), K)
+            _close(out[rows], a @ b.t(), a.abs() @ b.abs().t(), K, dtype)
+    # a long contraction: x down its columns against itself, few rows and columns of it
+    out = torch.empty(20, 20, device="cuda")
+    T = At[: 20 * bf.bf_op_fp8_row_bytes(M)]
+    st = _views((At, sat), K, M)[1]
+    few = torch.full((st.shape[0], 32), 127, dtype=torch.uint8, device="cuda")
+    few[:, :20] = st[:, :20]
+    bf.bf_op_fp8_gemm(0, 0, bf.BF_FP32, 20, 20, M, T, few, T, few, out)
+    ref = torch.zeros(20, 20, dtype=torch.float64, device="cuda")
+    mag = torch.zeros_like(ref)
+    for k in range(0, M, 1 << 18):
+        t = P.values(*P.form(x[k: k + (1 << 18), :20].t().contiguous(), 0), min(1 << 18, M - k))
+        ref += t @ t.t()
+        mag += t.abs() @ t.abs().t()
+    _close(out, ref, mag, M, bf.BF_FP32)
