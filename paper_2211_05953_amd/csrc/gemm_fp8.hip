@@ -91,25 +91,18 @@ __device__ __forceinline__ void unrolled(F&& f) {
   }
 }
 
-// 16 codes -> 16 bf16 times 2^e (exact)
+// Codes 2 n, 2 n + 1 of eight (two registers) as bf16 times 2^e (exact), into place n of o
 template <int FMT>
-__device__ __forceinline__ void widen(v4i v, float unit, bf16x8 (&o)[2]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    bf16x2 p[4];
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      if constexpr (FMT == BF_E4M3) {
-        p[2 * w] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * h + w], unit, false);
-        p[2 * w + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * h + w], unit, true);
-      } else {
-        p[2 * w] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(v[2 * h + w], unit, false);
-        p[2 * w + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(v[2 * h + w], unit, true);
-      }
-    }
-#pragma unroll
-    for (int w = 0; w < 4; ++w) { o[h][2 * w] = p[w][0]; o[h][2 * w + 1] = p[w][1]; }
-  }
+__device__ __forceinline__ void widen2(int lo, int hi, float unit, int n, bf16x8& o) {
+  bf16x2 p;
+  if constexpr (FMT == BF_E4M3) p = n & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(n < 2 ? lo : hi, unit, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(n < 2 ? lo : hi, unit, false);
+  else p = n & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(n < 2 ? lo : hi, unit, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(n < 2 ? lo : hi, unit, false);
+  o[2 * n] = p[0];
+  o[2 * n + 1] = p[1];
+}
+
+__device__ __forceinline__ void mma_bf16(const bf16x8& a, const bf16x8& b, f32x4& c) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
 
 // Adds the epilogue's terms to G neighbouring results and stores them.
@@ -256,34 +249,71 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
   typedef std::integral_constant<int, 1> H1;
 
   if constexpr (WIDE) {
-    // One barrier per block: behind it the tile is there and the other stage is free.
-    auto body = [&](uint8_t* cur, uint8_t* nxt, int kt) {
+    // Two phases to a block, one for each 16-byte chunk of a lane, and two halves to a phase: 8 k of every fragment.  A half widens its B fragments, then its A
+    // fragments one by one, each a fragment ahead of the products that it enters; the second reads the next phase's codes into what it leaves free.
+    // After the first phase everything of the stage is in registers: the barrier stands there, and the loads of the block after next go into the stage behind it.
+    v4i ar[MI], br[NI];
+    bf16x8 aw[2], bw[NI];
+    auto unit = [](int e, int i) { return __int_as_float(((e >> (8 * i)) & 255) << 23); };
+    auto phase = [&](const uint8_t* st, int kk) __attribute__((always_inline)) {
+      unrolled<0, 2>([&](auto h) __attribute__((always_inline)) {
+        constexpr int H = decltype(h)::value;
+        unrolled<0, NI>([&](auto j) __attribute__((always_inline)) {
+#pragma unroll
+          for (int n = 0; n < 4; ++n) widen2<FB>(br[j][2 * H], br[j][2 * H + 1], unit(scb[j / GB], j % GB), n, bw[j]);
+          if (H) br[j] = chunk(st, fb, j, kk);
+        });
+#pragma unroll
+        for (int n = 0; n < 4; ++n) widen2<FA>(ar[0][2 * H], ar[0][2 * H + 1], unit(sca[0], 0), n, aw[0]);
+        if (H) ar[0] = chunk(st, fa, 0, kk);
+        unrolled<0, MI>([&](auto i) __attribute__((always_inline)) {
+          constexpr int I = decltype(i)::value, X = I & 1;
+          __builtin_amdgcn_sched_barrier(0);
+          asm volatile("s_nop 1");  // between a conversion and a matrix instruction that reads it
+          float u = 0.f;
+          if constexpr (I + 1 < MI) u = unit(sca[(I + 1) / GA], (I + 1) % GA);
+          unrolled<0, NI>([&](auto j) __attribute__((always_inline)) {
+            constexpr int J = decltype(j)::value;
+            mma_bf16(aw[X], bw[J], acc[I][J]);
+            if constexpr (I + 1 < MI) {
+#pragma unroll
+              for (int n = 0; n < 4; ++n)
+                if (n * NI / 4 == J) widen2<FA>(ar[I + 1][2 * H], ar[I + 1][2 * H + 1], u, n, aw[1 - X]);
+              if (H && J == NI - 1) ar[I + 1] = chunk(st, fa, I + 1, kk);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          });
+        });
+      });
+    };
+    auto body = [&](uint8_t* cur, uint8_t* nxt, int kt) __attribute__((always_inline)) {
+      phase(cur, 1);
       arrived(H0{});
-      if (kt + 1 < nk) issue(nxt, kt + 1);
-      scales(cur, sca, scb);
+      int na[SA], nb[SB];
+      scales(nxt, na, nb);
+      issue(cur, min(kt + 2, nk - 1));  // (behind the last block: that one again, which nothing reads)
+      phase(nxt, 0);
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        bf16x8 b[NI][2];
-        unrolled<0, NI>([&](auto j) {
-          const int e = (scb[j / GB] >> (8 * (j % GB))) & 255;
-          widen<FB>(chunk(cur, fb, j, kk), __int_as_float(e << 23), b[j]);
-        });
-        unrolled<0, MI>([&](auto i) {
-          const int e = (sca[i / GA] >> (8 * (i % GA))) & 255;
-          bf16x8 a[2];
-          widen<FA>(chunk(cur, fa, i, kk), __int_as_float(e << 23), a);
+      for (int s = 0; s < SA; ++s) sca[s] = na[s];
 #pragma unroll
-          for (int j = 0; j < NI; ++j)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[h], b[j][h], acc[i][j], 0, 0, 0);
-        });
-      }
+      for (int s = 0; s < SB; ++s) scb[s] = nb[s];
     };
     issue(stage0, 0);
-    for (int kt = 0; kt < nk; kt += 2) {
+    issue(stage1, min(1, nk - 1));
+    arrived(H1{});
+    scales(stage0, sca, scb);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) br[j] = chunk(stage0, fb, j, 0);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) ar[i] = chunk(stage0, fa, i, 0);
+    int kt = 0;
+    for (; kt + 2 <= nk; kt += 2) {
       body(stage0, stage1, kt);
-      if (kt + 1 < nk) body(stage1, stage0, kt + 1);
+      body(stage1, stage0, kt + 1);
     }
+    if (kt < nk) body(stage0, stage1, kt);
+    // nothing is on its way into LDS when the workgroup ends, and the last results are there
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15" ::: "memory");
   } else {
     // Four phases to a block, each a half of the wave's A fragments times a half of its B fragments; what the next phase needs
     // is fetched meanwhile.  By the end of the second phase everything of the stage is in registers: the barrier stands
@@ -413,19 +443,21 @@ __global__ __launch_bounds__(256) void fp8_finish_kernel(uint32_t groups, uint32
 typedef Tile8<256, 256, 4, 2> Big8;
 typedef Tile8<256, 256, 2, 4> Wide8;  // widened operands: smaller sub-tiles, two waves to a SIMD
 typedef Tile8<128, 128, 2, 2, 4> Mid8;
+typedef Tile8<128, 128, 2, 2> WideMid8;
+typedef Tile8<64, 64, 2, 2> WideSmall8;
 typedef Tile8<64, 64, 2, 2, 4> Small8;
 
 struct Plan { int tile, slices, slice; };  // tile 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
 
-// The tile, and the slices that the contraction is cut into, of the least estimated time.  A round of workgroups over the chip takes START + blocks x BLOCK us, BLOCK_HALF
-// where at most half of its places are taken; a split costs a second kernel and the planes' way to memory and back.  Fitted to 28 shapes from 1 x 256 x 250 to 256 x 8192 x
-// 32768 on all tiles and splits; the choice is within 12 % of the best of them for all of them in both types.  us, 64 x 64 / 128 x 128 / 256 x 256, bf16 results:
+// The tile, and the slices that the contraction is cut into, of the least estimated time.  A round of workgroups over the chip takes START + blocks x BLOCK us; one that takes
+// only some of its SLOTS that share of BLOCK, but LEAST at least.  A split costs a second kernel and the planes' way to memory and back.  Fitted to 28 shapes from 1 x 256 x 250 to
+// 256 x 8192 x 32768 on all tiles and splits, of which the choice is within a fifth of the best (for 50 of the 56 within a tenth), in both types.  us, 64 x 64 / 128 x 128 / 256 x 256, bf16 results:
 // 200 x 3000 x 1000 5.3 / 7.9 / 15.6; 1000 x 4004 x 1000 12.3 / 9.3 / 16.8; 2048 x 2048 x 8192 49 / 33 / 75; 2048 x 6144 x 2048 46 / 35 / 28.  Splits: 1 x 8192 x 8192 into fp32
-// 33 in one, 16 in 8 slices; 256 x 8192 x 32768 into fp32 185 on 64 x 64 tiles, 126 in 8 slices on 256 x 256; most shapes lose by them (1000 x 1000 x 4096 9.6 in one, 16 in two).
+// 30 in one, 16 in 8 slices; 256 x 8192 x 32768 into fp32 185 on 64 x 64 tiles, 126 in 8 slices on 256 x 256; most shapes lose by them (1000 x 1000 x 4096 9.6 in one, 16 in two).
 constexpr double BASE_US = 2.5, SPLIT_US = 6.0, PLANE_BYTES_US = 9e6;
-struct TileCost { int edge, slots; double start, block, block_half; };
-constexpr TileCost COST[2][3] = {{{256, 256, 4.0, 1.7, 1.16}, {128, 256, 2.0, 0.5, 0.36}, {64, 512, 0.8, 0.4, 0.19}},   // 8-bit instructions
-                                 {{256, 256, 4.0, 3.35, 2.5}, {128, 256, 2.0, 1.1, 1.1}, {64, 512, 0.8, 0.6, 0.5}}};   // widened operands
+struct TileCost { int edge, slots; double start, block, least; };
+constexpr TileCost COST[2][3] = {{{256, 256, 4.0, 1.7, 1.16}, {128, 256, 2.0, 0.5, 0.36}, {64, 512, 0.8, 0.4, 0.19}},    // 8-bit instructions
+                                 {{256, 256, 4.0, 3.3, 2.4}, {128, 512, 2.0, 1.75, 0.95}, {64, 1024, 0.8, 1.15, 0.41}}};  // widened operands
 constexpr size_t MAX_PLANES = (size_t)1 << 28;
 
 Plan plan_of(int M, int N, int blocks, bool wide) {
@@ -438,9 +470,11 @@ Plan plan_of(int M, int N, int blocks, bool wide) {
       const int slice = (blocks + s - 1) / s, slices = (blocks + slice - 1) / slice;
       const double planes = 4.0 * M * N * slices, wgs = tiles * slices;
       if (slices != s || (s > 1 && (wgs > 4 * c.slots || planes > (double)MAX_PLANES))) break;
-      const double rounds = (double)(long)((wgs + c.slots - 1) / c.slots), fill = wgs >= c.slots ? 1 : wgs <= c.slots / 2 ? 0 : 2 * wgs / c.slots - 1;
-      const double us = BASE_US + rounds * (c.start + slice * (c.block_half + (c.block - c.block_half) * fill)) + (s > 1 ? SPLIT_US + 2 * planes / PLANE_BYTES_US : 0);
-      if (!best.slices || (s > 1 ? us < 0.9 * best_t : us < best_t)) { best = {t, slices, slice}; best_t = us; }
+      const double full = (double)(long)(wgs / c.slots), part = wgs / c.slots - full;
+      double us = BASE_US + full * (c.start + slice * c.block) + (s > 1 ? SPLIT_US + 2 * planes / PLANE_BYTES_US : 0);
+      if (part > 0) us += c.start + slice * (c.block * part > c.least ? c.block * part : c.least);
+      if (s > 1) us *= 1.1;  // a split has to win by more than the estimate may be off
+      if (!best.slices || us < best_t) { best = {t, slices, slice}; best_t = us; }
     }
   }
   return best;
@@ -461,8 +495,8 @@ template <int FA, int FB>
 bf_status by_tile(const Fp8Args& a, int tile, int slices, bool wide, bool f32, hipStream_t st) {
   if (wide) switch (tile) {
     case 0: return launch8<Wide8, FA, FB, true, float>(a, slices, st);
-    case 1: return launch8<Mid8, FA, FB, true, float>(a, slices, st);
-    default: return launch8<Small8, FA, FB, true, float>(a, slices, st);
+    case 1: return launch8<WideMid8, FA, FB, true, float>(a, slices, st);
+    default: return launch8<WideSmall8, FA, FB, true, float>(a, slices, st);
   }
   if (f32) switch (tile) {  // planes
     case 0: return launch8<Big8, FA, FB, false, float>(a, slices, st);
