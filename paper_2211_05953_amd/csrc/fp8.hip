@@ -5,7 +5,7 @@
 //
 // HBM traffic: an element is read once (2 or 4 bytes) and written once or twice (1 byte each).  A workgroup has a tile of 128 x 128, whole blocks either
 // way: a thread 8 rows x 8 columns of it, a row of the tile is 16 lanes.  Rows' maxima meet by lane rotations, columns' in LDS; the codes down the
-// columns turn round in LDS, so that both forms leave in whole 128-byte lines.  8192 x 32768 in bf16: both ways 226 us, 4.75 TB/s, along the rows alone 151 us, 5.3 (a copy reaches 5.2
+// columns turn round in LDS, so that both forms leave in whole 128-byte lines.  8192 x 32768 in bf16: both ways 211 us, 5.1 TB/s, along the rows alone 151 us, 5.3 (a copy reaches 5.2
 // to 5.6); 2048 x 8192 12.4 and 8.5 us; 1 x 8192 2.9 us.  (In fp32 arithmetic, element by element, 250, 191, 17, 12 and 5.4: three to four instructions an element in place of twenty.)
 #include "../../include/bf_ops.h"
 #include "common.h"
@@ -175,11 +175,17 @@ __device__ __forceinline__ float unit_of(int e) { return __uint_as_float((uint32
 
 template <typename T, int FMT>
 __global__ __launch_bounds__(NT) void fp8_quantize_kernel(int rows, int cols, const T* __restrict__ x, size_t ld, uint8_t* __restrict__ q,
-                                                          uint8_t* __restrict__ scale, uint8_t* __restrict__ qt, uint8_t* __restrict__ scale_t) {
+                                                          uint8_t* __restrict__ scale, uint8_t* __restrict__ qt, uint8_t* __restrict__ scale_t, int by_xcd) {
   __shared__ __attribute__((aligned(16))) uint8_t turn[BLK * BLK];
   __shared__ uint32_t cmax[4][BLK];
   const int tid = threadIdx.x, tc = tid & 15, tr = tid >> 4;
-  const int r0 = blockIdx.y * BLK, c0 = blockIdx.x * BLK, row = r0 + tr * 8, col = c0 + tc * 8;
+  int bx = blockIdx.x, by = blockIdx.y;
+  if (by_xcd) {  // each XCD a contiguous range of pairs of tiles, one below the other (the host sees to even numbers)
+    const uint32_t per = gridDim.x * gridDim.y >> 3, id = by * gridDim.x + bx, lin = (id & 7) * per + (id >> 3), pair = 2 * gridDim.x;
+    by = lin / pair * 2 + (lin & 1);
+    bx = lin % pair >> 1;
+  }
+  const int r0 = by * BLK, c0 = bx * BLK, row = r0 + tr * 8, col = c0 + tc * 8;
   const size_t ldq = ((size_t)cols + BLK - 1) / BLK * BLK, ldt = ((size_t)rows + BLK - 1) / BLK * BLK;
   const int rows16 = (rows + 15) / 16 * 16, cols16 = (cols + 15) / 16 * 16;
 
@@ -211,7 +217,7 @@ __global__ __launch_bounds__(NT) void fp8_quantize_kernel(int rows, int cols, co
       o.y = v.template along<FMT>(p, 4, u);
       if (row + p < rows) *reinterpret_cast<uint2*>(q + (size_t)(row + p) * ldq + col) = o;
     }
-    if (tc == 0 && row < rows16) *reinterpret_cast<uint64_t*>(scale + (size_t)blockIdx.x * rows16 + row) = sb;
+    if (tc == 0 && row < rows16) *reinterpret_cast<uint64_t*>(scale + (size_t)bx * rows16 + row) = sb;
   }
   if (!qt) return;
 #pragma unroll
@@ -238,7 +244,7 @@ __global__ __launch_bounds__(NT) void fp8_quantize_kernel(int rows, int cols, co
     // the column group, neighbouring columns swapped in the upper half
     *reinterpret_cast<uint2*>(turn + (c ^ ((c >> 6) & 1)) * BLK + (((tr >> 1) ^ (tc & 7)) << 4) + (tr & 1) * 8) = o;
   }
-  if (tr == 0 && col < cols16) *reinterpret_cast<uint64_t*>(scale_t + (size_t)blockIdx.y * cols16 + col) = sb;
+  if (tr == 0 && col < cols16) *reinterpret_cast<uint64_t*>(scale_t + (size_t)by * cols16 + col) = sb;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -261,7 +267,10 @@ bf_status fp8_quantize(int dtype, int format, int rows, int cols, const void* x,
   if (!q != !scale || !qt != !scale_t || (!q && !qt)) { set_error("bf_op_fp8_quantize: q goes with scale and qt with scale_t, and one pair at least is needed"); return BF_EINVAL; }
   if (((uintptr_t)q | (uintptr_t)scale | (uintptr_t)qt | (uintptr_t)scale_t) & 15) { set_error("bf_op_fp8_quantize: codes and scales have to be 16-byte aligned"); return BF_EINVAL; }
   const dim3 grid((cols + BLK - 1) / BLK, (rows + BLK - 1) / BLK);
-  auto go = [&](auto kern, auto* xs) { kern<<<grid, NT, 0, st>>>(rows, cols, xs, ld, (uint8_t*)q, (uint8_t*)scale, (uint8_t*)qt, (uint8_t*)scale_t); };
+  // More bytes than the 256 MiB memory-side cache by half, and lines down the columns among them: neighbouring tiles on one XCD (8192 x 32768 bf16 both ways 226 -> 211 us, down the
+  // columns alone 175 -> 156; 2048 x 32768, which fits, 43.5 -> 45.4, along the rows alone 151 -> 150)
+  const int by_xcd = qt && (double)rows * cols * (es + 1 + (q ? 1 : 0)) > (double)((size_t)384 << 20) && grid.y % 2 == 0 && (uint64_t)grid.x * grid.y % 8 == 0;
+  auto go = [&](auto kern, auto* xs) { kern<<<grid, NT, 0, st>>>(rows, cols, xs, ld, (uint8_t*)q, (uint8_t*)scale, (uint8_t*)qt, (uint8_t*)scale_t, by_xcd); };
   if (dtype == BF_BF16) {
     if (format == BF_E4M3) go(fp8_quantize_kernel<bf16_t, BF_E4M3>, (const bf16_t*)x);
     else go(fp8_quantize_kernel<bf16_t, BF_E5M2>, (const bf16_t*)x);

@@ -338,3 +338,30 @@ def test_offsets_past_32_bits():
         ref += t @ t.t()
         mag += t.abs() @ t.abs().t()
     _close(out, ref, mag, M, bf.BF_FP32)
+
+
+@pytest.mark.parametrize("rows,cols", [(8192, 16640), (8190, 16517), (8064, 17000)])
+def test_forms_larger_than_the_caches(rows, cols):
+    """Tiles in another order: whole, ragged, and where the number of tiles keeps to the first one."""
+    x = _matrix(rows, cols, bf.BF_BF16, 1, 1.0)
+    a, d = _new(rows, cols), _new(cols, rows)
+    bf.bf_op_fp8_quantize(bf.BF_BF16, 0, rows, cols, x, *a, *d)
+    _same_form(a, x, 0)
+    _same_form(d, x.t(), 0)
+    d2 = _new(cols, rows)
+    bf.bf_op_fp8_quantize(bf.BF_BF16, 0, rows, cols, x, None, None, *d2)
+    assert torch.equal(d[0], d2[0]) and torch.equal(d[1], d2[1])
+
+
+@pytest.mark.parametrize("dtype", [bf.BF_BF16, bf.BF_FP32])
+@pytest.mark.parametrize("M,N,K", [(4100, 50004, 260), (60000, 3502, 130)])
+def test_results_that_go_past_the_caches(M, N, K, dtype):
+    (A, sa), a = _operand(M, K, 0, 1)
+    (B, sb), b = _operand(N, K, 0, 2)
+    out = torch.empty(M, N, dtype=DT[dtype], device="cuda")
+    bf.bf_op_fp8_gemm(0, 0, dtype, M, N, K, A, sa, B, sb, out)
+    for k in range(0, M, 4100):
+        rows = slice(k, min(M, k + 4100))
+        for c in range(0, N, 12501):
+            cols = slice(c, min(N, c + 12501))
+            _close(out[rows, cols], a[rows] @ b[cols].t(), a[rows].abs() @ b[cols].abs().t(), K, dtype)
