@@ -292,7 +292,8 @@ bf_status bf_op_fp8_gemm(int format_a, int format_b, int dtype, int M, int N, in
  *           behind all blocks two scale bytes for each (m's and v's; 2^(b - 127) as above).  v's codes have no sign: 4 bits of exponent, 4 of mantissa,
  *           code c below 16 is c / 16, above (1 + c % 16 / 16) 2^(c / 16 - 1).  All zero bytes: moments of zero.
  *   g       fp32 or bf16 (`dtype`), used times coef[0]
- * The step is taken from the moments before they are rounded.  They are then rounded at random, up with the chance of their distance from the code below
+ * The new moments are beta1 m + (1 - beta1) g and beta2 v + (1 - beta2) g g in fp32, each operation rounded by itself (so that their codes are the same bits wherever that is done),
+ * and the step is taken from them as they are.  They are then rounded at random, up with the chance of their distance from the code below
  * (in 65536ths): a mean that moves by less than half a code each step still moves.  The random numbers are a hash of (seed, t, the tensor's place
  * in the list, element): the same call gives the same bits.  A v above zero is kept at the smallest code or more, 2^-18.95 of the block's
  * largest, so that no step is divided by a v that was rounded away.  t and seed are values of the call: a captured graph repeats them.

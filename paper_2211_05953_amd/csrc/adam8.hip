@@ -32,8 +32,7 @@ struct Table8 {
 };
 static_assert(sizeof(Table8) <= 3600, "kernel arguments");
 
-// b: beta, a: 1 - beta, each as the sum of two fp32 numbers: their own rounding would move as many codes as the moments' does
-struct AdamArgs8 { float lr, eps, wd, c1, c2, b1, b1_low, a1, a1_low, b2, b2_low, a2, a2_low; };
+struct AdamArgs8 { float lr, eps, wd, c1, c2, beta1, beta2, omb1, omb2; };
 
 // xor shifts and odd multipliers (the first 32 bits of the fractions of sqrt 2 and sqrt 3): over random inputs a flipped input bit flips
 // every output bit with a chance of 0.495 to 0.505
@@ -87,25 +86,24 @@ __device__ __forceinline__ float decode_v(uint32_t codes, int k) {
   return c < 16 ? (float)c * 0.0625f : __uint_as_float((c << 19) + ((uint32_t)(127 - 1) << 23));
 }
 
-// code of y >= 0 (LOW: exponent of the smallest normal code, BITS of mantissa), r: 16 random bits.  near: the sum lies so near to a carry that y's own rounding
-// decides
+// New moments.  Each operation is rounded by itself, so that the codes are the same bits wherever the definition is computed like this: a moment that is
+// off by one rounding lands in another code once in a million, and a small v's next code changes its step by a third.
+__device__ __forceinline__ void moments8(float& m, float& v, float g, const AdamArgs8& a) {
+#pragma clang fp contract(off)
+  m = a.beta1 * m + a.omb1 * g;
+  v = a.beta2 * v + a.omb2 * g * g;
+}
+
+// code of y >= 0 (LOW: exponent of the smallest normal code, BITS of mantissa), r: 16 random bits
 template <int LOW, int BITS>
-__device__ __forceinline__ uint32_t encode(float y, uint32_t r, bool& near) {
+__device__ __forceinline__ uint32_t encode(float y, uint32_t r) {
   const int e = max((int)(__float_as_uint(y) >> 23) - 127, LOW);
   const uint32_t k = (uint32_t)(y * __uint_as_float((uint32_t)(127 + 16 + BITS - e) << 23));  // y / step, in 65536ths
-  near = (k & 0xffffu) + r - 0xfffdu <= 5u;
-  return (uint32_t)((e - LOW) << BITS) + ((k + r) >> 16);
-}
-// the same of the moment in fp64: y = |moment| 2^-unit
-template <int LOW, int BITS>
-__device__ __forceinline__ uint32_t encode_exact(double y, uint32_t r) {
-  const int e = max((int)(__double_as_longlong(y) >> 52) - 1023, LOW);
-  const uint32_t k = (uint32_t)ldexp(y, 16 + BITS - e);
   return (uint32_t)((e - LOW) << BITS) + ((k + r) >> 16);
 }
 
 // All loads of four runs of 4 elements are in flight at once, accesses do not stay in the caches.  230 M parameters, step / reading the moments out in bf16: 812 / 267 us, 5.1 and
-// 5.2 TB/s (a copy reaches 5.2 to 5.6).  Of the step: with caching 40 us more; with root and quotient to the last bit 50 more; without the second look at near carries 15 less; two
+// 5.2 TB/s (a copy reaches 5.2 to 5.6).  Of the step: with caching 40 us more; with root and quotient to the last bit 50 more; two
 // runs of 4, or of 8 elements 35 more; 512 workgroups 110 more.
 constexpr int VECS = 4;
 constexpr int CHUNK = NT * 4 * VECS;
@@ -161,9 +159,9 @@ __global__ __launch_bounds__(NT) void adam8_kernel(Table8 t, const float* __rest
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float gk = gg[i][k] * ck;
-        const float m0 = ldexpf(decode_m(cm[i], k), em0), v0 = ldexpf(decode_v(cv[i], k), ev0), g2 = gk * gk;
-        m[k] = fmaf(a.a1, gk, fmaf(a.b1, m0, fmaf(a.a1_low, gk, a.b1_low * m0)));
-        v[k] = fmaf(a.a2, g2, fmaf(a.b2, v0, fmaf(a.a2_low, g2, a.b2_low * v0)));
+        m[k] = ldexpf(decode_m(cm[i], k), em0);
+        v[k] = ldexpf(decode_v(cv[i], k), ev0);
+        moments8(m[k], v[k], gk, a);
         const float wk = ww[i][k];
         // (root and reciprocal to an ulp each; they do not take numbers below 2^-126: a root counts as 2^-63 at least)
         const float root = __builtin_amdgcn_sqrtf(fmaxf(v[k] * a.c2, FLT_MIN));
@@ -175,37 +173,17 @@ __global__ __launch_bounds__(NT) void adam8_kernel(Table8 t, const float* __rest
       const int em = exponent8<EXP_M, TOP_M>(max32(tm)), ev = exponent8<EXP_V, TOP_V>(max32(tv));
       const float um = __uint_as_float((uint32_t)(127 - em) << 23), uv = __uint_as_float((uint32_t)(127 - ev) << 23);
       uint32_t nm = 0, nv = 0;
-      bool any = false;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t h = mix32(q + k + key);
         const uint32_t bm = __float_as_uint(m[k]), bv = __float_as_uint(v[k]);
-        bool near_m, near_v;
-        uint32_t x = min(encode<-6, 3>(fminf(fabsf(m[k]) * um, 448.f), h & 0xffffu, near_m), 0x7eu);
+        uint32_t x = min(encode<-6, 3>(fminf(fabsf(m[k]) * um, 448.f), h & 0xffffu), 0x7eu);
         x = (bm & 0x7f800000u) == 0x7f800000u ? 0x7fu : x;
         nm |= (x | ((bm >> 24) & 0x80u)) << (8 * k);
-        uint32_t y = min(encode<0, 4>(fminf(v[k] * uv, 31744.f), h >> 16, near_v), 255u);
+        uint32_t y = min(encode<0, 4>(fminf(v[k] * uv, 31744.f), h >> 16), 255u);
         y = bv != 0 ? max(y, 1u) : 0u;
         y = (bv & 0x7f800000u) == 0x7f800000u ? 255u : y;
         nv |= y << (8 * k);
-        any |= near_m | near_v;
-      }
-      if (any) {  // (a lane in 1400: the moments again in fp64, so that the codes are the definition's and not their fp32 rounding's)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t h = mix32(q + k + key);
-          const double gk = (double)gg[i][k] * ck;
-          const double md = ((double)a.b1 + a.b1_low) * (double)ldexpf(decode_m(cm[i], k), em0) + ((double)a.a1 + a.a1_low) * gk;
-          const double vd = ((double)a.b2 + a.b2_low) * (double)ldexpf(decode_v(cv[i], k), ev0) + ((double)a.a2 + a.a2_low) * gk * gk;
-          if (fabs(md) <= FLT_MAX) {
-            const uint32_t x = min(encode_exact<-6, 3>(fmin(fabs(md) * um, 448.0), h & 0xffffu), 0x7eu);
-            nm = (nm & ~(0xffu << (8 * k))) | (x | (md < 0 ? 0x80u : 0u)) << (8 * k);
-          }
-          if (vd <= FLT_MAX && vd > 0) {
-            const uint32_t y = max(min(encode_exact<0, 4>(fmin(vd * uv, 31744.0), h >> 16), 255u), 1u);
-            nv = (nv & ~(0xffu << (8 * k))) | y << (8 * k);
-          }
-        }
       }
       if (whole) {
         __builtin_nontemporal_store(ww[i], reinterpret_cast<V4*>(w + q));
@@ -308,12 +286,8 @@ bf_status adam8_step(int dtype, int n_tensors, const bf_adam8_tensor* x, const f
       return BF_EINVAL;
     }
   }
-  AdamArgs8 a{(float)lr, (float)eps, (float)wd, (float)(1.0 / (1.0 - pow(beta1, (double)step))), (float)(1.0 / (1.0 - pow(beta2, (double)step)))};
-  auto pair = [](double x, float& high, float& low) { high = (float)x; low = (float)(x - (double)high); };
-  pair(beta1, a.b1, a.b1_low);
-  pair(1.0 - beta1, a.a1, a.a1_low);
-  pair(beta2, a.b2, a.b2_low);
-  pair(1.0 - beta2, a.a2, a.a2_low);
+  AdamArgs8 a{(float)lr, (float)eps, (float)wd, (float)(1.0 / (1.0 - pow(beta1, (double)step))), (float)(1.0 / (1.0 - pow(beta2, (double)step))),
+              (float)beta1, (float)beta2, (float)(1.0 - beta1), (float)(1.0 - beta2)};
   const uint32_t key = mix32(mix32(mix32((uint32_t)seed) ^ (uint32_t)(seed >> 32)) ^ (uint32_t)step);
   int at = 0;
   size_t off = 0;

@@ -78,6 +78,34 @@ def test_step(dtype, sizes, zero):
         _check(tensors, before, float(coef), seed, t)
 
 
+@pytest.mark.parametrize("dtype", [bf.BF_FP32, bf.BF_BF16])
+@pytest.mark.parametrize("c", [1.0, 0.37])
+def test_codes_are_those_of_fp32_operations_one_by_one(dtype, c):
+    """Every code and scale, over three steps: the definition in fp32, each operation rounded by itself."""
+    tensors = _make([(1 << 22) + 77, 3000], dtype, 12)
+    coef = torch.tensor([c], device="cuda")
+    for t in (1, 2, 3):
+        before = [x[1].clone() for x in tensors]
+        bf.bf_op_adam8(dtype, [x[:4] for x in tensors], coef, 21, t, LR, B1, B2, EPS, WD)
+        for i, ((w, state, g, *_), s0) in enumerate(zip(tensors, before)):
+            n = w.numel()
+            m, v, _, _ = (x.float() for x in P.decode(s0, n))
+            gg = torch.nn.functional.pad(g.float() * coef, (0, m.numel() - n)).view_as(m)
+            m, v = B1 * m + (1 - B1) * gg, B2 * v + (1 - B2) * gg * gg
+            want = []
+            for x, top, low, bits, r in zip((m, v), (448.0, 31744.0), (-6, 0), (3, 4), P.randoms(21, t, i, m.numel(), "cuda")):
+                x = x.double()
+                unit = P.power(P.exponent(x.abs().amax(1), top))[:, None]
+                y = x.abs() / unit
+                step = P.power((torch.frexp(y)[1] - 1).clamp(min=low) - bits)
+                part = y / step
+                code = (torch.floor(part) + (torch.floor((part - torch.floor(part)) * 65536) + r.view_as(x) >= 65536)) * step
+                code = torch.where((x != 0) & (code == 0) & (low == 0), torch.full_like(code, 1 / 16), code.clamp(max=top))
+                want.append(code.copysign(x) * unit)
+            got = P.decode(state, n)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_bits_are_a_function_of_the_call():
     first = None
     for _ in range(2):
