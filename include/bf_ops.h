@@ -261,7 +261,7 @@ bf_status bf_op_adam_clipped(int n_tensors, const bf_adam_tensor* tensors, const
  * The 8-bit form of a matrix of `rows` rows of n elements, blocks along its rows:
  *   codes   [rows][bf_op_fp8_row_bytes(n)] bytes (n rounded up to 128; zeros behind element n): BF_E4M3 (largest value 448) or
  *           BF_E5M2 (57344; its infinities are not used)
- *   scales  [ceil(n / 128)][rows rounded up to 16] bytes, bf_op_fp8_scale_elems(rows, n) in all: byte b stands for 2^(b - 127); element k of row r
+ *   scales  [ceil(n / 128)][rows rounded up to 16] bytes, bf_op_fp8_scale_elems(rows, n) in all: byte b, 254 at most, stands for 2^(b - 127); element k of row r
  *           is code[r][k] * 2^(scale[k / 128][r] - 127).  Bytes behind the last row are 127.
  * Both 16-byte aligned.  A linear layer y = x W (x [T, h_in], W [h_in, h_out]) takes, as A and B of bf_op_fp8_gemm:
  *   forward          y  [T, h_out]      x along its rows      W down its columns
@@ -275,9 +275,9 @@ bf_status bf_op_adam_clipped(int n_tensors, const bf_adam_tensor* tensors, const
  * _gemm      C[M,N] = A B^T + bias + R from the forms A [M, K] and B [N, K], dense C and R [M, N] in `dtype`, bias fp32 [N]; bias, R may be NULL,
  *            R may be C.  accumulate = 1 (fp32 only): C += that.  A bf16 C comes from the 8-bit matrix instructions, whose sums inside a block keep about 16
  *            bits (1.5e-5 of the result for normal operands, 8e-5 with large outliers in every block: under bf16's rounding of 1.7e-3); an fp32 C
- *            from operands widened to bf16, exactly, with fp32 sums.  Sums have a fixed order: no atomics.  work: device scratch, 256-byte
- *            aligned, of _work_bytes(...) bytes (0: none needed, or bad sizes), owned by the caller; calls that overlap need their own.
- *            Sizes are 1 to 2^21. */
+ *            from operands widened to bf16, with fp32 sums: exactly, but for bits under 2^-133 (of e4m3 under scales of 2^-124, of e5m2 of 2^-117) and codes that
+ *            stand for 2^128 or more, which become infinite.  Sums have a fixed order: no atomics.  work: device scratch, 256-byte aligned, of
+ *            _work_bytes(...) bytes (0: none needed, or bad sizes), owned by the caller; calls that overlap need their own.  Sizes are 1 to 2^21. */
 typedef enum { BF_E4M3 = 0, BF_E5M2 = 1 } bf_fp8_format;
 size_t bf_op_fp8_row_bytes(int n);
 size_t bf_op_fp8_scale_elems(int rows, int n);

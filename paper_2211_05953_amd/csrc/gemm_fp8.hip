@@ -10,7 +10,7 @@
 // a few neighbouring k up before it adds them and drops what falls under them: 1.5e-5 (2-norm, over the result's) on normal
 // operands, 8e-5 with outliers of 20 sigma in every block, whatever the length, and the same from the 16x16x32 form: 50 times under
 // bf16's own rounding.  fp32 results (main-grads) are held to more than that: their operands are widened in registers to bf16, which holds
-// code times scale exactly, and multiplied by v_mfma_f32_16x16x32_bf16 at half the rate.
+// code times scale exactly (down to 2^-133, its smallest step), and multiplied by v_mfma_f32_16x16x32_bf16 at half the rate.
 //
 // A workgroup computes BM x BN of C in steps of one block (128 bytes of a row).  Tiles go from memory straight into LDS (16 bytes a lane,
 // two stages).  Within an LDS row the 16-byte chunks are XOR-swizzled (conflict-free fragment reads); as the instruction
@@ -92,7 +92,7 @@ __device__ __forceinline__ void unrolled(F&& f) {
   }
 }
 
-// Codes 2 n, 2 n + 1 of eight (two registers) as bf16 times 2^e (exact), into place n of o
+// Codes 2 n, 2 n + 1 of eight (two registers) as bf16 times 2^e (exact down to 2^-133), into place n of o
 template <int FMT>
 __device__ __forceinline__ void widen2(int lo, int hi, float unit, int n, bf16x8& o) {
   bf16x2 p;

@@ -270,6 +270,32 @@ def test_a_layer_under_capture():
         assert all(torch.equal(a, b) for a, b in zip(got, (y, dx, dw))), k
 
 
+@pytest.mark.parametrize("dtype", [bf.BF_BF16, bf.BF_FP32])
+def test_two_graphs_that_share_their_scratch(dtype):
+    """Products that are cut along the contraction: graphs of two of them on the same planes, replayed in turn, with an eager call on the planes between."""
+    M, N, K = 64, 512, 16384
+    ops = [(_operand(M, K, 0, 20 + i)[0], _operand(N, K, 0, 30 + i)[0], torch.empty(M, N, dtype=DT[dtype], device="cuda")) for i in range(2)]
+    need = bf.bf_op_fp8_gemm_work_bytes(dtype, M, N, K)
+    assert need > 0
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    call = lambda i, out=None: bf.bf_op_fp8_gemm(0, 0, dtype, M, N, K, *ops[i][0], *ops[i][1], ops[i][2] if out is None else out, work=work)  # noqa: E731
+    call(0), call(1)
+    torch.cuda.synchronize()
+    want, graphs, other = [o[2].clone() for o in ops], [], torch.empty(M, N, dtype=DT[dtype], device="cuda")
+    assert not torch.equal(*want)
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(i)
+    for k in range(4):
+        ops[0][2].zero_(), ops[1][2].zero_(), work.fill_(0xFF)
+        graphs[k % 2].replay()
+        call(k % 2, other)
+        graphs[1 - k % 2].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(ops[0][2], want[0]) and torch.equal(ops[1][2], want[1]) and torch.equal(other, want[k % 2]), k
+
+
 def test_calls_on_two_streams_at_once():
     T, h_in, h_out = 200, 4096, 300
     want, streams, got = [], [torch.cuda.Stream() for _ in range(2)], []
@@ -297,6 +323,24 @@ def test_scales_of_the_whole_range(dtype):
     out = torch.empty(M, N, dtype=DT[dtype], device="cuda")
     bf.bf_op_fp8_gemm(0, 0, dtype, M, N, K, A, sa, B, sb, out)
     _close(out, a @ b.t(), a.abs() @ b.abs().t(), K, dtype)
+
+
+@pytest.mark.parametrize("fmt,scale", [(0, 0), (0, 1), (0, 3), (1, 0), (1, 5), (1, 10)])
+@pytest.mark.parametrize("dtype", [bf.BF_BF16, bf.BF_FP32])
+def test_the_smallest_scales(dtype, fmt, scale):
+    """Codes under the smallest normal numbers.  An fp32 result's operands are widened to bf16, whose step there is 2^-133: each is off by less than
+    that, and exact from a scale of 2^-124 (e4m3, whose step is 2^-9) or 2^-117 (e5m2, 2^-16) on."""
+    M, N, K = 80, 72, 250
+    (A, sa), _ = _operand(M, K, fmt, 15)
+    (B, sb), _ = _operand(N, K, 0, 16)
+    sa[:, :M], sb[:, :N] = scale, 244 - scale
+    a, b = P.values(A, sa, K, fmt), P.values(B, sb, K, 0)
+    out = torch.empty(M, N, dtype=DT[dtype], device="cuda")
+    bf.bf_op_fp8_gemm(fmt, 0, dtype, M, N, K, A, sa, B, sb, out)
+    inexact = dtype == bf.BF_FP32 and scale < (3 if fmt == 0 else 10)
+    assert out.isfinite().all()
+    _close(out, a @ b.t(), a.abs() @ b.abs().t() + (2.0**-133 * b.abs().sum(1) * 2.0**24 / (K / 32 + 32) if inexact else 0.0), K, dtype)
+
 
 
 def test_offsets_past_32_bits():
