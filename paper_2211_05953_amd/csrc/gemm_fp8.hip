@@ -106,44 +106,20 @@ __device__ __forceinline__ void mma_bf16(const bf16x8& a, const bf16x8& b, f32x4
   asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
 
-// Adds the epilogue's terms to G neighbouring results and stores them.
-template <int G, typename TO>
-__device__ __forceinline__ void put(float (&v)[G], int row, int col, const Fp8Args& p, TO* C, bool vec) {
-  if (row >= p.M || col >= p.N) return;
-  const size_t at = (size_t)row * p.N + col;
-  const TO* R = reinterpret_cast<const TO*>(p.R);
-  if (vec) {  // N is a multiple of G and the tensors are aligned to G elements: whole groups
-    typedef TO V __attribute__((ext_vector_type(G)));
-    if (p.bias) {
-#pragma unroll
-      for (int e = 0; e < G; ++e) v[e] += p.bias[col + e];
-    }
-    if (R) {
-      const V r = *reinterpret_cast<const V*>(R + at);
-#pragma unroll
-      for (int e = 0; e < G; ++e) v[e] += (float)r[e];
-    }
-    if (p.accumulate) {
-      const V r = *reinterpret_cast<const V*>(C + at);
-#pragma unroll
-      for (int e = 0; e < G; ++e) v[e] += (float)r[e];
-    }
-    V o;
-#pragma unroll
-    for (int e = 0; e < G; ++e) o[e] = (TO)v[e];
-    if (p.passing) __builtin_nontemporal_store(o, reinterpret_cast<V*>(C + at));
-    else *reinterpret_cast<V*>(C + at) = o;
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < G; ++e) {
-    if (col + e >= p.N) continue;
-    float x = v[e];
-    if (p.bias) x += p.bias[col + e];
-    if (R) x += (float)R[at + e];
-    if (p.accumulate) x += (float)C[at + e];
-    C[at + e] = (TO)x;
-  }
+// n neighbouring elements by one load or store; lanes behind the descriptor's end read zero and write nothing.  AUX 2: past the caches
+template <int BYTES>
+__device__ __forceinline__ auto load_some(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+  if constexpr (BYTES == 2) return __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0);
+  else if constexpr (BYTES == 4) return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
+  else if constexpr (BYTES == 8) return __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+  else return __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+}
+template <int AUX, typename V>
+__device__ __forceinline__ void store_some(__amdgpu_buffer_rsrc_t r, uint32_t off, V v) {
+  if constexpr (sizeof(V) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), r, off, 0, AUX);
+  else if constexpr (sizeof(V) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), r, off, 0, AUX);
+  else if constexpr (sizeof(V) == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(decltype(load_some<8>(r, off)), v), r, off, 0, AUX);
+  else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(decltype(load_some<16>(r, off)), v), r, off, 0, AUX);
 }
 
 // WIDE: bf16 instructions on widened operands.
@@ -168,18 +144,14 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
   };
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w % TL::WM, wn = w / TL::WM;
 
-  // each XCD (its own L2) a contiguous range of the tile order, which walks groups of 8 row-tiles
+  // Each XCD (its own L2) a contiguous range of the tile order, which walks groups of 8 tiles of the longer side along the shorter one: the larger operand is fetched once.  (2048 x 32768 x 8192
+  // 376 us, groups of the rows 391; 8192 x 32768 x 1024 285 and 319; groups of 4 the same on average, of 2 slower.)
   const int tiles_n = gridDim.x / p.tiles_m;
-  int lin = blockIdx.x, bm, bn;
-  if (gridDim.x % 8 == 0) lin = (lin & 7) * (gridDim.x >> 3) + (lin >> 3);
-  if (p.tiles_m % 8 == 0) {
-    const int in_group = 8 * tiles_n, gi = lin / in_group, rem = lin % in_group;
-    bm = gi * 8 + (rem & 7);
-    bn = rem >> 3;
-  } else {
-    bm = lin % p.tiles_m;
-    bn = lin / p.tiles_m;
-  }
+  const bool across = tiles_n > p.tiles_m;
+  const int len = across ? tiles_n : p.tiles_m, width = across ? p.tiles_m : tiles_n;
+  const int xcd = blockIdx.x & 7, lin = (int)(blockIdx.x >> 3) + xcd * (int)(gridDim.x >> 3) + min(xcd, (int)(gridDim.x & 7));
+  const int group = lin / (8 * width), rem = lin - group * 8 * width, size = min(8, len - group * 8), along = group * 8 + rem % size, other = rem / size;
+  const int bm = across ? other : along, bn = across ? along : other;
   const int m0 = bm * BM, n0 = bn * BN;
   const int kb0 = blockIdx.y * p.slice, nk = min(p.slice, p.blocks - kb0);
   const size_t ld = (size_t)p.blocks * BKB;
@@ -238,15 +210,16 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
   for (int kk = 0; kk < 2; ++kk) fo[kk] = (lane & 15) * BKB + (((kk * 4 + (lane >> 4)) ^ kswz8(lane & 15)) << 4);
   const int fa = wm * TL::TM * BKB, fb = BM * BKB + wn * TL::TN * BKB;
   auto chunk = [&](const uint8_t* st, int base, int t, int kk) { return *reinterpret_cast<const v4i*>(st + base + t * 16 * BKB + fo[kk]); };
-  // Everything but the last `left` blocks' loads is there, for all waves, and their reads of LDS are over.
-  auto arrived = [](auto left) {
-    constexpr int VM = decltype(left)::value * (CA + CB + 1);
+  // All but the wave's last `left` loads are there, for all waves, and their reads of LDS are over.
+  auto meet = [](auto left) {
+    constexpr int VM = decltype(left)::value;
     static_assert(VM < 64, "the counter's range");
     __builtin_amdgcn_s_waitcnt((VM & 15) | (VM >> 4) << 14 | 7 << 4);  // vmcnt(VM) lgkmcnt(0)
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
+  auto arrived = [&](auto blocks) { meet(std::integral_constant<int, decltype(blocks)::value * (CA + CB + 1)>{}); };  // but the last blocks'
   typedef std::integral_constant<int, 0> H0;
   typedef std::integral_constant<int, 1> H1;
 
@@ -318,9 +291,11 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
     asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15" ::: "memory");
   } else {
     // Four phases to a block, each a half of the wave's A fragments times a half of its B fragments; what the next phase needs
-    // is fetched meanwhile.  By the end of the second phase everything of the stage is in registers: the barrier stands
-    // there, the loads of the block after next go into the stage behind it, and the last two phases fetch the next block's first halves.
-    // (The halves of B swap roles from block to block, so that the one that is fetched first is free.)
+    // is fetched meanwhile.  The last two phases fetch the next block's first halves.  (The halves of B swap roles from block to block, so that the one that is fetched first is free.)
+    // Two stages: the first phase fetches all that is left of the stage, and behind it a barrier gives the stage up to the loads of the block after next; the next stage has to be
+    // there half a block later, at a second barrier.  (With one barrier, at half a block, the loads have a quarter of a block less to arrive: 2048 x 32768 x 8192 439 us and not 394, of
+    // 2048 x 8192 x 32768 441 and not 407; a third stage for B alone does not give more.)
+    // Four: the first two phases fetch it, and one barrier stands behind them.
     constexpr int MH = MI / 2, NH = NI / 2;
     static_assert(MI % 2 == 0 && NI % 2 == 0, "halves");
     v8i a0[MH], a1[MH], bx[2][NH];
@@ -340,9 +315,11 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
         __builtin_amdgcn_sched_barrier(0);
       });
     };
-    // loads of a tile: one after every EACH matrix instructions of the last two phases, or PER after each
-    constexpr int NMMA = MH * NH, FIT = 2 * NMMA / (CA + CB), EACH = FIT > 3 ? 3 : FIT < 1 ? 1 : FIT, PER = (CA + CB + 2 * NMMA - 1) / (2 * NMMA);
-    auto share = [&](uint8_t* st, int kt, int n) {
+    // loads of a tile: one after every EACH matrix instructions from the second (third) phase on, or PER after each
+    constexpr int NMMA = MH * NH, PHASES = NS == 2 ? 3 : 2, FIT = PHASES * NMMA / (CA + CB), MOST = NS == 2 ? 2 : 3, EACH = FIT > MOST ? MOST : FIT < 1 ? 1 : FIT,
+                  PER = (CA + CB + PHASES * NMMA - 1) / (PHASES * NMMA);
+    static_assert((PHASES * NMMA + EACH - 1) / EACH * PER >= CA + CB, "all of them");
+    auto share = [&](uint8_t* st, int kt, int n) __attribute__((always_inline)) {
       if (n % EACH) return;
 #pragma unroll
       for (int i = 0; i < PER; ++i)
@@ -356,18 +333,36 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
       uint8_t *const cur = stage(u), *const nxt = stage(std::integral_constant<int, U + 1>{});
       const int lk = min(kt + NS, nk - 1);
       int na[SA], nb[SB];
-      phase(H0{}, first_half, a0, [&](int n) { if (n < NH) read_b(cur, S, n); });
-      phase(H0{}, second_half, a0, [&](int n) { if (n < MH) read_a(cur, 1, a1, n); });
-      arrived(std::integral_constant<int, NS - 2>{});
-      scales(nxt, na, nb);
-      issue_scales(cur, lk);
-      phase(H1{}, second_half, a1, [&](int n) {
-        if (n < MH) read_a(nxt, 0, a0, n);
-        share(cur, lk, n);
+      constexpr int START = NS == 2 ? 0 : -NMMA;  // of the loads, in instructions from the second phase on
+      phase(H0{}, first_half, a0, [&](int n) __attribute__((always_inline)) {
+        if (n < NH) read_b(cur, S, n);
+        if (NS == 2 && n >= NH && n - NH < MH) read_a(cur, 1, a1, n - NH);
       });
-      phase(H1{}, first_half, a1, [&](int n) {
+      if constexpr (NS == 2) {
+        static_assert(NMMA >= NH + MH, "the first phase has a place for each read");
+        meet(std::integral_constant<int, 63>{});
+        issue_scales(cur, lk);
+      }
+      phase(H0{}, second_half, a0, [&](int n) __attribute__((always_inline)) {
+        if constexpr (NS == 2) share(cur, lk, n);
+        else if (n < MH) read_a(cur, 1, a1, n);
+      });
+      if constexpr (NS == 2) {
+        constexpr int GONE = (NMMA + EACH - 1) / EACH * PER;  // loads of the second phase
+        meet(std::integral_constant<int, (GONE < CA + CB ? GONE : CA + CB) + 1>{});
+        scales(nxt, na, nb);
+      } else {
+        arrived(std::integral_constant<int, NS - 2>{});
+        scales(nxt, na, nb);
+        issue_scales(cur, lk);
+      }
+      phase(H1{}, second_half, a1, [&](int n) __attribute__((always_inline)) {
+        if (n < MH) read_a(nxt, 0, a0, n);
+        share(cur, lk, START + NMMA + n);
+      });
+      phase(H1{}, first_half, a1, [&](int n) __attribute__((always_inline)) {
         if (n < NH) read_b(nxt, S, n);
-        share(cur, lk, NMMA + n);
+        share(cur, lk, START + 2 * NMMA + n);
       });
 #pragma unroll
       for (int s = 0; s < SA; ++s) sca[s] = na[s];
@@ -391,21 +386,80 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
     asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
   }
 
+  // The epilogue, without a branch for an element: stores by 32-bit offsets from the wave's first result, columns behind the last at offsets behind the descriptor's end, where rows behind the
+  // last are by themselves.  (With a branch for each group of results, and the bias fetched for each: 2048 x 6144 x 2048 with a bias 35.6 us and not 27, 8192 x 32768 x 2048 634 and not 536.)
+  const int mw = m0 + wm * TL::TM, nw = n0 + wn * TL::TN;
+  if (mw >= p.M || nw >= p.N) return;
+  const size_t from = (size_t)mw * p.N + nw, left = ((size_t)p.M * p.N - from) * sizeof(TO);
+  const int bytes = (int)(left < 0x7fffff00u ? left : 0x7fffff00u);
+  const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)(C + from), 0, bytes, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rr = __builtin_amdgcn_make_buffer_rsrc((void*)(p.R ? reinterpret_cast<const TO*>(p.R) + from : C + from), 0, bytes, 0x00020000);
   // lane l, register r of a fragment: row 4 (l / 16) + r, column l % 16 of it
-  const bool vec = p.N % GB == 0 && (((uintptr_t)p.C | (uintptr_t)p.R) & (GB * sizeof(TO) - 1)) == 0;
+  const int lc = (lane & 15) * GB;
+  float bias[SB][GB];
 #pragma unroll
-  for (int i = 0; i < MI; ++i)
+  for (int s = 0; s < SB; ++s)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int row = m0 + wm * TL::TM + i / GA * 16 * GA + (4 * (lane >> 4) + r) * GA + i % GA;
+    for (int e = 0; e < GB; ++e) bias[s][e] = -0.f;  // a sum with it is the other term
+  if (p.bias) {
 #pragma unroll
-      for (int s = 0; s < SB; ++s) {
-        float v[GB];
+    for (int s = 0; s < SB; ++s)
 #pragma unroll
-        for (int e = 0; e < GB; ++e) v[e] = acc[i][s * GB + e][r];
-        put<GB, TO>(v, row, n0 + wn * TL::TN + s * 16 * GB + (lane & 15) * GB, p, C, vec);
+      for (int e = 0; e < GB; ++e) bias[s][e] = p.bias[min(nw + s * 16 * GB + lc + e, p.N - 1)];
+  }
+  // E: neighbouring elements of an access, MORE: R or C's own values are added, AUX: of the stores
+  auto write = [&](auto elems, auto more, auto aux) __attribute__((always_inline)) {
+    constexpr int E = decltype(elems)::value;
+    typedef TO V __attribute__((ext_vector_type(E)));
+    uint32_t n = p.N, col[SB][GB / E];
+    asm("" : "+s"(n));  // nothing of a form of the epilogue is kept for the others
+#pragma unroll
+    for (int s = 0; s < SB; ++s)
+#pragma unroll
+      for (int e = 0; e < GB; e += E) col[s][e / E] = nw + s * 16 * GB + lc + e < p.N ? (4 * (lane >> 4) * GA * n + s * 16 * GB + lc + e) * (uint32_t)sizeof(TO) : 0x80000000u;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const uint32_t line = (uint32_t)(i / GA * 16 * GA + r * GA + i % GA) * n * sizeof(TO);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < SB; ++s)
+#pragma unroll
+          for (int e = 0; e < GB; e += E) {
+            const uint32_t at = col[s][e / E] + line;
+            float v[E];
+#pragma unroll
+            for (int k = 0; k < E; ++k) v[k] = acc[i][s * GB + e + k][r] + bias[s][e + k];
+            if constexpr (decltype(more)::value) {
+              if (p.R) {
+                const V x = __builtin_bit_cast(V, load_some<sizeof(V)>(rr, at));
+#pragma unroll
+                for (int k = 0; k < E; ++k) v[k] += (float)x[k];
+              }
+              if (p.accumulate) {
+                const V x = __builtin_bit_cast(V, load_some<sizeof(V)>(rc, at));
+#pragma unroll
+                for (int k = 0; k < E; ++k) v[k] += (float)x[k];
+              }
+            }
+            V o;
+#pragma unroll
+            for (int k = 0; k < E; ++k) o[k] = (TO)v[k];
+            store_some<decltype(aux)::value>(rc, at, o);
+          }
       }
-    }
+  };
+  typedef std::integral_constant<int, 2> Past;
+  const bool vec = p.N % GB == 0 && (((uintptr_t)p.C | (uintptr_t)p.R) & (GB * sizeof(TO) - 1)) == 0, more = p.R || p.accumulate;
+  const std::integral_constant<int, GB> elems{};
+  if constexpr (!WIDE && std::is_same<TO, float>::value) {  // planes: only the product
+    if (vec) write(elems, H0{}, H0{});
+    else write(H1{}, H0{}, H0{});
+  } else if (!vec) write(H1{}, H1{}, H0{});
+  else if (more) write(elems, H1{}, H0{});
+  else if (p.passing) write(elems, H0{}, Past{});
+  else write(elems, H0{}, H0{});
 #endif
 }
 
@@ -458,7 +512,7 @@ struct Plan { int tile, slices, slice; };  // tile 0: 256 x 256, 1: 128 x 128, 2
 // 30 in one, 16 in 8 slices; 256 x 8192 x 32768 into fp32 185 on 64 x 64 tiles, 126 in 8 slices on 256 x 256; most shapes lose by them (1000 x 1000 x 4096 9.6 in one, 16 in two).
 constexpr double BASE_US = 2.5, SPLIT_US = 6.0, PLANE_BYTES_US = 9e6;
 struct TileCost { int edge, slots; double start, block, least; };
-constexpr TileCost COST[2][3] = {{{256, 256, 4.0, 1.7, 1.16}, {128, 256, 2.0, 0.5, 0.36}, {64, 512, 0.8, 0.4, 0.19}},    // 8-bit instructions
+constexpr TileCost COST[2][3] = {{{256, 256, 4.0, 1.42, 0.92}, {128, 256, 1.8, 0.41, 0.3}, {64, 512, 0.8, 0.36, 0.17}},    // 8-bit instructions
                                  {{256, 256, 4.0, 3.3, 2.4}, {128, 512, 2.0, 1.75, 0.95}, {64, 1024, 0.8, 1.15, 0.41}}};  // widened operands
 // Operands and result larger together than the 256 MiB memory-side cache, by half: the result goes past the caches, whose lines the operands then keep.  8192 x 32768 x 2048 in bf16
 // 568 -> 511 us, 8192 x 16384 x 8192 855 -> 757, 8192 x 32768 x 2048 in fp32 921 -> 890; not 8192 x 16384 x 2048, 253 -> 257.
