@@ -102,8 +102,8 @@ __device__ __forceinline__ uint32_t encode(float y, uint32_t r) {
   return (uint32_t)((e - LOW) << BITS) + ((k + r) >> 16);
 }
 
-// All loads of four runs of 4 elements are in flight at once, accesses do not stay in the caches.  230 M parameters, step / reading the moments out in bf16: 812 / 267 us, 5.1 and
-// 5.2 TB/s (a copy reaches 5.2 to 5.6).  Of the step: with caching 40 us more; with root and quotient to the last bit 50 more; two
+// All loads of four runs of 4 elements are in flight at once, accesses do not stay in the caches.  230 M parameters, step / reading the moments out in bf16: 780 to 830 / 267 us, 5.0 to 5.3 and
+// 5.2 TB/s (a copy reaches 4.8 to 5.6).  Of the step: with caching 40 us more; with root and quotient to the last bit 50 more; two
 // runs of 4, or of 8 elements 35 more; 512 workgroups 110 more.
 constexpr int VECS = 4;
 constexpr int CHUNK = NT * 4 * VECS;

@@ -13,11 +13,14 @@
 // code times scale exactly (down to 2^-133, its smallest step), and multiplied by v_mfma_f32_16x16x32_bf16 at half the rate.
 //
 // A workgroup computes BM x BN of C in steps of one block (128 bytes of a row).  Tiles go from memory straight into LDS (16 bytes a lane,
-// two stages).  Within an LDS row the 16-byte chunks are XOR-swizzled (conflict-free fragment reads); as the instruction
+// two or four stages).  Within an LDS row the 16-byte chunks are XOR-swizzled (conflict-free fragment reads); as the instruction
 // that loads into LDS writes lane after lane, the swizzle is in the addresses that the lanes read from.  Any order of k is right as long as
 // A and B share it and a block's scale covers it: lane group q takes chunks q and q + 4.
 // LDS row 16 i + j of a group of 16 G rows (G = 4: 64 rows) holds row G j + i of it: a lane's scale bytes of G fragments are then
 // neighbours in memory (one load, picked apart by the instruction's byte selector), and so are its results of G fragments across (one store).
+//
+// Large bf16 results: 8192^3 348 to 355 us, 3.1 PFLOP/s; 2048 x 32768 x 8192 360 to 366, 3.0; 8192 x 32768 x 2048 415 to 459, 2.4 to 2.6 (half a gigabyte of results).  Instructions on registers alone reach 4.05 on
+// random operands (4.9 on zeros: the clock falls with the power), this loop without its loads 3.4; LDS has no bank conflicts.  fp32: 8192 x 8192 x 2048 213 us, 1.29.
 #include <atomic>
 #include <type_traits>
 
@@ -506,16 +509,17 @@ typedef Tile8<64, 64, 2, 2, 4> Small8;
 struct Plan { int tile, slices, slice; };  // tile 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
 
 // The tile, and the slices that the contraction is cut into, of the least estimated time.  A round of workgroups over the chip takes START + blocks x BLOCK us; one that takes
-// only some of its SLOTS that share of BLOCK, but LEAST at least.  A split costs a second kernel and the planes' way to memory and back.  Fitted to 28 shapes from 1 x 256 x 250 to
-// 256 x 8192 x 32768 on all tiles and splits, of which the choice is within a fifth of the best (for 50 of the 56 within a tenth), in both types.  us, 64 x 64 / 128 x 128 / 256 x 256, bf16 results:
-// 200 x 3000 x 1000 5.3 / 7.9 / 15.6; 1000 x 4004 x 1000 12.3 / 9.3 / 16.8; 2048 x 2048 x 8192 49 / 33 / 75; 2048 x 6144 x 2048 46 / 35 / 28.  Splits: 1 x 8192 x 8192 into fp32
-// 30 in one, 16 in 8 slices; 256 x 8192 x 32768 into fp32 185 on 64 x 64 tiles, 126 in 8 slices on 256 x 256; most shapes lose by them (1000 x 1000 x 4096 9.6 in one, 16 in two).
+// only some of its SLOTS that share of BLOCK, but LEAST at least.  A split costs a second kernel and the planes' way to memory and back.  Fitted to 30 shapes from 1 x 256 x 250 to
+// 256 x 8192 x 32768 on all tiles and splits, in both types: the choice is the best or within 10 % of it for 59 of the 60 (a fifth off: 1 x 2048 x 2048 into fp32, 8.0 us, 6.6 in four slices).  us,
+// 64 x 64 / 128 x 128 / 256 x 256, bf16 results: 200 x 3000 x 1000 4.6 / 6.5 / 12.7; 1000 x 4004 x 1000 11.4 / 8.1 / 13.6; 2048 x 2048 x 8192 49 / 31 / 69; 2048 x 6144 x 2048 44 / 32 / 25.
+// Splits: 1 x 8192 x 8192 into fp32 30 in one, 15 in 4 slices; 256 x 8192 x 32768 into fp32 179 on 64 x 64 tiles, 128 in 4 slices on 128 x 128; most shapes lose by them
+// (1000 x 1000 x 4096 9.1 in one, 16 in two).
 constexpr double BASE_US = 2.5, SPLIT_US = 6.0, PLANE_BYTES_US = 9e6;
 struct TileCost { int edge, slots; double start, block, least; };
 constexpr TileCost COST[2][3] = {{{256, 256, 4.0, 1.42, 0.92}, {128, 256, 1.8, 0.41, 0.3}, {64, 512, 0.8, 0.36, 0.17}},    // 8-bit instructions
                                  {{256, 256, 4.0, 3.3, 2.4}, {128, 512, 2.0, 1.75, 0.95}, {64, 1024, 0.8, 1.15, 0.41}}};  // widened operands
-// Operands and result larger together than the 256 MiB memory-side cache, by half: the result goes past the caches, whose lines the operands then keep.  8192 x 32768 x 2048 in bf16
-// 568 -> 511 us, 8192 x 16384 x 8192 855 -> 757, 8192 x 32768 x 2048 in fp32 921 -> 890; not 8192 x 16384 x 2048, 253 -> 257.
+// Operands and result larger together than the 256 MiB memory-side cache, by half: the result goes past the caches, whose lines the operands then keep.  us, in the caches and past them:
+// 32768 x 8192 x 2048 465 and 430, 8192 x 32768 x 1024 283 and 252, 2048 x 32768 x 8192 370 and 360, 8192 x 16384 x 4096 390 and 391.  Not results that something is added to, which were just read.
 constexpr size_t PASSING_BYTES = (size_t)384 << 20;
 constexpr size_t MAX_PLANES = (size_t)1 << 28;
 
