@@ -73,7 +73,7 @@ def on_cpu(monkeypatch):
 
     bf.load()
     monkeypatch.setattr(bf.binding, "load", lambda: Library())
-    monkeypatch.setattr(bf.binding, "_stream", lambda: 0)
+    monkeypatch.setattr(bf.binding, "_stream", lambda *a: 0)
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1, raising=False)
     return calls
 

@@ -154,7 +154,7 @@ def test_products_of_formats(M, N, K, fa, fb, dtype):
 
 
 @pytest.mark.parametrize("dtype", [bf.BF_BF16, bf.BF_FP32])
-@pytest.mark.parametrize("M,N,K,at", [(33, 70, 200, 0), (40, 64, 4200, 1), (40, 67, 4200, 0), (520, 800, 300, 0), (520, 801, 300, 0), (2100, 2200, 200, 1)])
+@pytest.mark.parametrize("M,N,K,at", [(33, 70, 200, 0), (40, 64, 4200, 1), (40, 67, 4200, 0), (520, 800, 300, 0), (520, 801, 300, 0), (2100, 2200, 200, 1), (8190, 2044, 300, 0), (8190, 2043, 130, 0)])
 def test_epilogues(M, N, K, at, dtype):
     """Bias, residual, both, the residual in place, accumulation; results that start at any element."""
     (A, sa), a = _operand(M, K, 0, 7)
@@ -409,3 +409,15 @@ def test_results_that_go_past_the_caches(M, N, K, dtype):
         for c in range(0, N, 12501):
             cols = slice(c, min(N, c + 12501))
             _close(out[rows, cols], a[rows] @ b[cols].t(), a[rows].abs() @ b[cols].abs().t(), K, dtype)
+
+
+@pytest.mark.parametrize("dtype", [bf.BF_BF16, bf.BF_FP32])
+def test_results_past_32_bits(dtype):
+    M, N, K = 40003, 60004, 130
+    (A, sa), a = _operand(M, K, 0, 17)
+    (B, sb), b = _operand(N, K, 0, 18)
+    out = torch.full((M, N), float("nan"), dtype=DT[dtype], device="cuda")
+    bf.bf_op_fp8_gemm(0, 0, dtype, M, N, K, A, sa, B, sb, out)
+    for rows in (slice(0, 100), slice(M // 2, M // 2 + 100), slice(M - 100, M)):
+        _close(out[rows], a[rows] @ b.t(), a[rows].abs() @ b.abs().t(), K, dtype)
+    assert not any(torch.isnan(out[i: i + 2000]).any() for i in range(0, M, 2000))
