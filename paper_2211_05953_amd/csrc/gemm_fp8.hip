@@ -19,8 +19,8 @@
 // LDS row 16 i + j of a group of 16 G rows (G = 4: 64 rows) holds row G j + i of it: a lane's scale bytes of G fragments are then
 // neighbours in memory (one load, picked apart by the instruction's byte selector), and so are its results of G fragments across (one store).
 //
-// Large bf16 results: 8192^3 348 to 355 us, 3.1 PFLOP/s; 2048 x 32768 x 8192 360 to 366, 3.0; 8192 x 32768 x 2048 415 to 459, 2.4 to 2.6 (half a gigabyte of results).  Instructions on registers alone reach 4.05 on
-// random operands (4.9 on zeros: the clock falls with the power); matrix cores are busy 77 to 84 % at 1.8 to 1.64 GHz, and LDS has no bank conflicts.  fp32: 8192 x 8192 x 2048 213 us, 1.29.
+// Large bf16 results: 8192^3 348 us, 3.2 PFLOP/s; 2048 x 32768 x 8192 361, 3.0; 8192 x 32768 x 2048 427, 2.6 (half a gigabyte of results).  Instructions on registers alone reach 4.05 on
+// random operands (4.9 on zeros: the clock falls with the power); matrix cores are busy 77 to 82 % at 1.82 to 1.75 GHz, and LDS has no bank conflicts.  fp32: 8192 x 8192 x 2048 213 us, 1.29.
 #include <atomic>
 #include <type_traits>
 
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
   __shared__ __attribute__((aligned(128))) uint8_t stage1[STAGE];
   __shared__ __attribute__((aligned(128))) uint8_t stage2[NS == 4 ? STAGE : 16];
   __shared__ __attribute__((aligned(128))) uint8_t stage3[NS == 4 ? STAGE : 16];
-  auto stage = [&](auto i) -> uint8_t* {
+  auto stage = [&](auto i) __attribute__((always_inline)) -> uint8_t* {
     constexpr int S = decltype(i)::value % NS;
     if constexpr (S == 0) return stage0;
     else if constexpr (S == 1) return stage1;
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
   // What is loaded: a tile's operands by 32-bit lane offsets from its first byte.  The descriptors end where the matrices end, and lanes whose row lies
   // behind it get nothing: what they compute is not stored.
   typedef __attribute__((address_space(3))) void* lds_ptr;
-  auto rest = [&](int rows) {
+  auto rest = [&](int rows) __attribute__((always_inline)) {
     const size_t n = (size_t)rows * ld - (size_t)kb0 * BKB;
     return (int)(n < 0x7fffff00u ? n : 0x7fffff00u);
   };
@@ -176,17 +176,17 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
   // chunk i of a thread is NT / 8 LDS rows, a power of two, further on: the bits of row_of are those of the two parts
   const int ch = (tid & 7) ^ kswz8(tid >> 3);
   const int off_a = row_of<GA>(tid >> 3) * (int)ld + ch * 16, off_b = GA == GB ? off_a : row_of<GB>(tid >> 3) * (int)ld + ch * 16;
-  auto issue_chunk = [&](uint8_t* st, int kt, int i) {
+  auto issue_chunk = [&](uint8_t* st, int kt, int i) __attribute__((always_inline)) {
     if (i < CA) __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(st + (i * NT + w * 64) * 16), 16, off_a + (kt * BKB + row_of<GA>(i * (NT / 8)) * (int)ld), 0, 0, 0);
     else __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(st + BM * BKB + ((i - CA) * NT + w * 64) * 16), 16, off_b + (kt * BKB + row_of<GB>((i - CA) * (NT / 8)) * (int)ld), 0, 0, 0);
   };
   // The block's scale bytes behind the tiles, 256 of A's rows (even waves, all the same) and 256 of B's (odd ones): every wave has the same number of loads
   // on its way.  Lanes behind the last row repeat its neighbours'.
   constexpr int SCALES = (BM + BN) * BKB;
-  auto issue_scales = [&](uint8_t* st, int kt) {
+  auto issue_scales = [&](uint8_t* st, int kt) __attribute__((always_inline)) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)(sp + (int64_t)kt * sld), 0, 0x7fffffff, 0x00020000), (lds_ptr)(st + SCALES + (w & 1) * 256), 4, off_s, 0, 0, 0);
   };
-  auto issue = [&](uint8_t* st, int kt) {
+  auto issue = [&](uint8_t* st, int kt) __attribute__((always_inline)) {
     issue_scales(st, kt);
 #pragma unroll
     for (int i = 0; i < CA + CB; ++i) issue_chunk(st, kt, i);
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
   // the lane's: G rows / columns to a load
   constexpr int SA = MI / GA, SB = NI / GB;
   int sca[SA], scb[SB];
-  auto scales = [&](const uint8_t* st, int (&a)[SA], int (&b)[SB]) {
+  auto scales = [&](const uint8_t* st, int (&a)[SA], int (&b)[SB]) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < SA; ++s) a[s] = load_scales<GA>(st + SCALES + wm * TL::TM + s * 16 * GA + (lane & 15) * GA);
 #pragma unroll
@@ -212,9 +212,9 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
 #pragma unroll
   for (int kk = 0; kk < 2; ++kk) fo[kk] = (lane & 15) * BKB + (((kk * 4 + (lane >> 4)) ^ kswz8(lane & 15)) << 4);
   const int fa = wm * TL::TM * BKB, fb = BM * BKB + wn * TL::TN * BKB;
-  auto chunk = [&](const uint8_t* st, int base, int t, int kk) { return *reinterpret_cast<const v4i*>(st + base + t * 16 * BKB + fo[kk]); };
+  auto chunk = [&](const uint8_t* st, int base, int t, int kk) __attribute__((always_inline)) { return *reinterpret_cast<const v4i*>(st + base + t * 16 * BKB + fo[kk]); };
   // All but the wave's last `left` loads are there, for all waves, and their reads of LDS are over.
-  auto meet = [](auto left) {
+  auto meet = [](auto left) __attribute__((always_inline)) {
     constexpr int VM = decltype(left)::value;
     static_assert(VM < 64, "the counter's range");
     __builtin_amdgcn_s_waitcnt((VM & 15) | (VM >> 4) << 14 | 7 << 4);  // vmcnt(VM) lgkmcnt(0)
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  auto arrived = [&](auto blocks) { meet(std::integral_constant<int, decltype(blocks)::value * (CA + CB + 1)>{}); };  // but the last blocks'
+  auto arrived = [&](auto blocks) __attribute__((always_inline)) { meet(std::integral_constant<int, decltype(blocks)::value * (CA + CB + 1)>{}); };  // but the last blocks'
   typedef std::integral_constant<int, 0> H0;
   typedef std::integral_constant<int, 1> H1;
 
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
     // After the first phase everything of the stage is in registers: the barrier stands there, and the loads of the block after next go into the stage behind it.
     v4i ar[MI], br[NI];
     bf16x8 aw[2], bw[NI];
-    auto unit = [](int e, int i) { return __int_as_float(((e >> (8 * i)) & 255) << 23); };
+    auto unit = [](int e, int i) __attribute__((always_inline)) { return __int_as_float(((e >> (8 * i)) & 255) << 23); };
     auto phase = [&](const uint8_t* st, int kk) __attribute__((always_inline)) {
       unrolled<0, 2>([&](auto h) __attribute__((always_inline)) {
         constexpr int H = decltype(h)::value;
@@ -302,15 +302,15 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
     constexpr int MH = MI / 2, NH = NI / 2;
     static_assert(MI % 2 == 0 && NI % 2 == 0, "halves");
     v8i a0[MH], a1[MH], bx[2][NH];
-    auto whole = [&](const uint8_t* st, int base, int t) {
+    auto whole = [&](const uint8_t* st, int base, int t) __attribute__((always_inline)) {
       const v4i x = chunk(st, base, t, 0), y = chunk(st, base, t, 1);
       return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    auto read_a = [&](const uint8_t* st, int half, v8i (&f)[MH], int i) { f[i] = whole(st, fa, half * MH + i); };
-    auto read_b = [&](const uint8_t* st, int half, int j) { bx[half][j] = whole(st, fb, half * NH + j); };
+    auto read_a = [&](const uint8_t* st, int half, v8i (&f)[MH], int i) __attribute__((always_inline)) { f[i] = whole(st, fa, half * MH + i); };
+    auto read_b = [&](const uint8_t* st, int half, int j) __attribute__((always_inline)) { bx[half][j] = whole(st, fb, half * NH + j); };
     // The instructions of a phase in the order that they are issued in: an MFMA, then what `side` has for its place.
-    auto phase = [&](auto ha, auto hb, v8i (&f)[MH], auto&& side) {
-      unrolled<0, MH * NH>([&](auto n) {
+    auto phase = [&](auto ha, auto hb, v8i (&f)[MH], auto&& side) __attribute__((always_inline)) {
+      unrolled<0, MH * NH>([&](auto n) __attribute__((always_inline)) {
         constexpr int I = decltype(n)::value / NH, JJ = decltype(n)::value % NH, J = I & 1 ? NH - 1 - JJ : JJ;  // serpentine: one operand changes
         constexpr int TI = decltype(ha)::value * MH + I, TJ = decltype(hb)::value * NH + J;
         mma_scaled<TI % GA, TJ % GB, FA, FB>(f[I], bx[decltype(hb)::value][J], acc[TI][TJ], sca[TI / GA], scb[TJ / GB]);
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
       });
     };
     // loads of a tile: one after every EACH matrix instructions from the second (third) phase on, or PER after each
-    constexpr int NMMA = MH * NH, PHASES = NS == 2 ? 3 : 2, FIT = PHASES * NMMA / (CA + CB), MOST = NS == 2 ? 2 : 3, EACH = FIT > MOST ? MOST : FIT < 1 ? 1 : FIT,
+    constexpr int NMMA = MH * NH, PHASES = NS == 2 ? 3 : 2, FIT = PHASES * NMMA / (CA + CB), MOST = NS == 2 ? NMMA / 4 : 3, EACH = FIT > MOST ? MOST : FIT < 1 ? 1 : FIT,
                   PER = (CA + CB + PHASES * NMMA - 1) / (PHASES * NMMA);
     static_assert((PHASES * NMMA + EACH - 1) / EACH * PER >= CA + CB, "all of them");
     auto share = [&](uint8_t* st, int kt, int n) __attribute__((always_inline)) {
@@ -329,7 +329,7 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
         if (n / EACH * PER + i < CA + CB) issue_chunk(st, kt, n / EACH * PER + i);
     };
     // works on block kt in stage U and loads block kt + NS into it (behind the last one: the last again, which nothing reads)
-    auto body = [&](auto u, int kt) {
+    auto body = [&](auto u, int kt) __attribute__((always_inline)) {
       constexpr int U = decltype(u)::value, S = U & 1 ? 0 : 1;
       const std::integral_constant<int, U & 1> first_half{};
       const std::integral_constant<int, S> second_half{};
@@ -373,7 +373,7 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
       for (int s = 0; s < SB; ++s) scb[s] = nb[s];
       asm volatile("s_nop 1");  // between a move and a matrix instruction that reads it
     };
-    unrolled<0, NS>([&](auto u) { issue(stage(u), min((int)decltype(u)::value, nk - 1)); });
+    unrolled<0, NS>([&](auto u) __attribute__((always_inline)) { issue(stage(u), min((int)decltype(u)::value, nk - 1)); });
     arrived(std::integral_constant<int, NS - 1>{});
     scales(stage0, sca, scb);
 #pragma unroll
@@ -381,8 +381,8 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
 #pragma unroll
     for (int j = 0; j < NH; ++j) read_b(stage0, 0, j);
     int kt = 0;
-    for (; kt + NS <= nk; kt += NS) unrolled<0, NS>([&](auto u) { body(u, kt + decltype(u)::value); });
-    unrolled<0, NS - 1>([&](auto u) {
+    for (; kt + NS <= nk; kt += NS) unrolled<0, NS>([&](auto u) __attribute__((always_inline)) { body(u, kt + decltype(u)::value); });
+    unrolled<0, NS - 1>([&](auto u) __attribute__((always_inline)) {
       if (kt + decltype(u)::value < nk) body(u, kt + decltype(u)::value);
     });
     // nothing is on its way into LDS when the workgroup ends, and the last results are there (16 passes and some)
@@ -500,6 +500,11 @@ __global__ __launch_bounds__(256) void fp8_finish_kernel(uint32_t groups, uint32
 }
 
 typedef Tile8<256, 256, 4, 2> Big8;
+// Long contractions: half the waves, each with all of a SIMD's registers, read a third less from LDS, whose power goes to the clock; with few blocks one wave waits alone for the first loads and at the epilogue.  us, four
+// waves and eight: 8192^3 348 and 356, 2048 x 32768 x 8192 361 and 367, 4096 x 8192 x 32768 691 and 704, 4095 x 8190 x 5000 133 and 138; 8192 x 32768 x 2048 427 and 435, but 16384 x 2048 x 2048 68 and 64;
+// 4096 x 16384 x 1024 71 and 70, 8192 x 2048 x 300 15.9 and 14.1.
+typedef Tile8<256, 256, 2, 2> Long8;
+constexpr int LONG_BLOCKS = 16;
 typedef Tile8<256, 256, 2, 4> Wide8;  // widened operands: smaller sub-tiles, two waves to a SIMD
 typedef Tile8<128, 128, 2, 2, 4> Mid8;
 typedef Tile8<128, 128, 2, 2> WideMid8;
@@ -567,7 +572,7 @@ bf_status by_tile(const Fp8Args& a, int tile, int slices, bool wide, bool f32, h
     default: return launch8<Small8, FA, FB, false, float>(a, slices, st);
   }
   switch (tile) {
-    case 0: return launch8<Big8, FA, FB, false, bf16_t>(a, slices, st);
+    case 0: return a.slice >= LONG_BLOCKS ? launch8<Long8, FA, FB, false, bf16_t>(a, slices, st) : launch8<Big8, FA, FB, false, bf16_t>(a, slices, st);
     case 1: return launch8<Mid8, FA, FB, false, bf16_t>(a, slices, st);
     default: return launch8<Small8, FA, FB, false, bf16_t>(a, slices, st);
   }

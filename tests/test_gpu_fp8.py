@@ -124,7 +124,8 @@ def _close(got, ref, mag, K, dtype, extra=0.0):
 
 
 SHAPES = [(1, 1, 1), (1, 5, 128), (3, 64, 129), (17, 33, 64), (64, 64, 300), (65, 130, 257), (128, 128, 1000), (100, 1003, 250), (1, 1000, 4096), (5, 300, 8200),
-          (300, 500, 640), (2000, 1030, 384), (257, 4000, 512), (2304, 2308, 256), (3000, 6148, 260)]
+          (300, 500, 640), (2000, 1030, 384), (257, 4000, 512), (2304, 2308, 256), (3000, 6148, 260),
+          (2300, 4100, 2100), (2305, 4099, 2176), (4096, 4096, 4000)]
 
 
 @pytest.mark.parametrize("dtype", [bf.BF_BF16, bf.BF_FP32])
@@ -144,7 +145,7 @@ def test_products(M, N, K, dtype):
 
 @pytest.mark.parametrize("dtype", [bf.BF_BF16, bf.BF_FP32])
 @pytest.mark.parametrize("fa,fb", [(0, 1), (1, 0), (1, 1)])
-@pytest.mark.parametrize("M,N,K", [(33, 70, 200), (100, 500, 4200), (520, 800, 300), (2100, 2200, 200)])
+@pytest.mark.parametrize("M,N,K", [(33, 70, 200), (100, 500, 4200), (520, 800, 300), (2100, 2200, 200), (2300, 4100, 2100)])
 def test_products_of_formats(M, N, K, fa, fb, dtype):
     (A, sa), a = _operand(M, K, fa, 5, True)
     (B, sb), b = _operand(N, K, fb, 6, True)
@@ -154,7 +155,7 @@ def test_products_of_formats(M, N, K, fa, fb, dtype):
 
 
 @pytest.mark.parametrize("dtype", [bf.BF_BF16, bf.BF_FP32])
-@pytest.mark.parametrize("M,N,K,at", [(33, 70, 200, 0), (40, 64, 4200, 1), (40, 67, 4200, 0), (520, 800, 300, 0), (520, 801, 300, 0), (2100, 2200, 200, 1), (8190, 2044, 300, 0), (8190, 2043, 130, 0)])
+@pytest.mark.parametrize("M,N,K,at", [(33, 70, 200, 0), (40, 64, 4200, 1), (40, 67, 4200, 0), (520, 800, 300, 0), (520, 801, 300, 0), (2100, 2200, 200, 1), (8190, 2044, 300, 0), (8190, 2043, 130, 0), (2300, 4100, 2050, 0), (2300, 4100, 2050, 1)])
 def test_epilogues(M, N, K, at, dtype):
     """Bias, residual, both, the residual in place, accumulation; results that start at any element."""
     (A, sa), a = _operand(M, K, 0, 7)
