@@ -296,7 +296,9 @@ bf_status bf_op_fp8_gemm(int format_a, int format_b, int dtype, int M, int N, in
  * and the step is taken from them as they are.  They are then rounded at random, up with the chance of their distance from the code below
  * (in 65536ths): a mean that moves by less than half a code each step still moves.  The random numbers are a hash of (seed, t, the tensor's place
  * in the list, element): the same call gives the same bits.  A v above zero is kept at the smallest code or more, 2^-18.95 of the block's
- * largest, so that no step is divided by a v that was rounded away.  t and seed are values of the call: a captured graph repeats them.
+ * largest, so that no step is divided by a v that was rounded away.  Values that are not finite stay with their element, out of its block's scales: a m that is infinite or NaN
+ * becomes NaN; a v that overflows to infinity beside a finite m is kept as that, by the code 0xff of m, which stands for m = 0 and v = infinity: but for the weight decay its
+ * weight rests from then on, as in bf_op_adam_clipped.  t and seed are values of the call: a captured graph repeats them.
  * The rates are double, as 1 - beta2 of an fp32 0.999 is 5e-5 off.  A coefficient that is not finite leaves the step out.  No two tensors may overlap. */
 typedef struct {
   float* w;

@@ -6,6 +6,8 @@
 // on the way down, half a code of v is 1.6 to 3.1 %, of m 3.1 to 6.3 %).
 // m: e4m3.  v has no sign, and the bit goes to the mantissa: codes of 4 bits of exponent and 4 of mantissa.  v is kept and not its root, so that its
 // mean is the one that is unbiased; over a block it spans 5e5, its root 700.
+// A v that is infinite has m's code 0xff, which stands for m = 0 and v = infinity: its element rests for good, but for the weight decay, as it does on fp32 moments, where a
+// finite m is divided by it.  (v's codes have no room for it, and as the largest finite code of its neighbours' scale the next step would read it as small.)  NaN is 0x7f.
 //
 // HBM traffic: 18 bytes an element (w 4 + 4, g 4, codes 2 + 2, bf16 copy 2).  A block is 32 lanes of 4 elements, so that maxima meet by lane rotations.
 #include <float.h>
@@ -86,6 +88,19 @@ __device__ __forceinline__ float decode_v(uint32_t codes, int k) {
   return c < 16 ? (float)c * 0.0625f : __uint_as_float((c << 19) + ((uint32_t)(127 - 1) << 23));
 }
 
+// whether one of the four codes of m is 0xff (a byte of the complement is zero)
+__device__ __forceinline__ bool any_rests(uint32_t codes) { return ((~codes - 0x01010101u) & codes & 0x80808080u) != 0; }
+
+// the moments that a code 0xff of m stands for
+__device__ __forceinline__ void resting(uint32_t codes, float (&m)[4], float (&v)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const bool r = ((codes >> (8 * k)) & 255u) == 0xffu;
+    m[k] = r ? 0.f : m[k];
+    v[k] = r ? __uint_as_float(0x7f800000u) : v[k];
+  }
+}
+
 // New moments.  Each operation is rounded by itself, so that the codes are the same bits wherever the definition is computed like this: a moment that is
 // off by one rounding lands in another code once in a million, and a small v's next code changes its step by a third.
 __device__ __forceinline__ void moments8(float& m, float& v, float g, const AdamArgs8& a) {
@@ -158,17 +173,22 @@ __global__ __launch_bounds__(NT) void adam8_kernel(Table8 t, const float* __rest
       B4 o;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float gk = gg[i][k] * ck;
         m[k] = ldexpf(decode_m(cm[i], k), em0);
         v[k] = ldexpf(decode_v(cv[i], k), ev0);
+      }
+      if (any_rests(cm[i])) resting(cm[i], m, v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float gk = gg[i][k] * ck;
         moments8(m[k], v[k], gk, a);
         const float wk = ww[i][k];
-        // (root and reciprocal to an ulp each; they do not take numbers below 2^-126: a root counts as 2^-63 at least)
-        const float root = __builtin_amdgcn_sqrtf(fmaxf(v[k] * a.c2, FLT_MIN));
+        // (root and reciprocal to an ulp each; they do not take numbers below 2^-126: a root counts as 2^-63 at least, of a NaN it is NaN)
+        const float vc = v[k] * a.c2, root = __builtin_amdgcn_sqrtf(vc < FLT_MIN ? FLT_MIN : vc);
         ww[i][k] = fmaf(-a.lr, fmaf(a.wd, wk, m[k] * a.c1 * __builtin_amdgcn_rcpf(root + a.eps)), wk);
         o[k] = (bf16_t)(float)ww[i][k];
-        tm = max(tm, finite_bits8(m[k]));
-        tv = max(tv, finite_bits8(v[k]));
+        const bool finite = (__float_as_uint(v[k]) & 0x7f800000u) != 0x7f800000u;
+        tm = max(tm, finite ? finite_bits8(m[k]) : 0u);
+        tv = max(tv, finite ? __float_as_uint(v[k]) : 0u);
       }
       const int em = exponent8<EXP_M, TOP_M>(max32(tm)), ev = exponent8<EXP_V, TOP_V>(max32(tv));
       const float um = __uint_as_float((uint32_t)(127 - em) << 23), uv = __uint_as_float((uint32_t)(127 - ev) << 23);
@@ -177,9 +197,10 @@ __global__ __launch_bounds__(NT) void adam8_kernel(Table8 t, const float* __rest
       for (int k = 0; k < 4; ++k) {
         const uint32_t h = mix32(q + k + key);
         const uint32_t bm = __float_as_uint(m[k]), bv = __float_as_uint(v[k]);
-        uint32_t x = min(encode<-6, 3>(fminf(fabsf(m[k]) * um, 448.f), h & 0xffffu), 0x7eu);
+        uint32_t x = min(encode<-6, 3>(fminf(fabsf(m[k]) * um, 448.f), h & 0xffffu), 0x7eu) | ((bm >> 24) & 0x80u);
+        x = (bv & 0x7f800000u) == 0x7f800000u ? 0xffu : x;
         x = (bm & 0x7f800000u) == 0x7f800000u ? 0x7fu : x;
-        nm |= (x | ((bm >> 24) & 0x80u)) << (8 * k);
+        nm |= x << (8 * k);
         uint32_t y = min(encode<0, 4>(fminf(v[k] * uv, 31744.f), h >> 16), 255u);
         y = bv != 0 ? max(y, 1u) : 0u;
         y = (bv & 0x7f800000u) == 0x7f800000u ? 255u : y;
@@ -221,11 +242,18 @@ __global__ __launch_bounds__(NT) void adam8_moments_kernel(Table8 t) {
       if (q >= n) continue;
       const uint32_t cm = codes[(size_t)b * 64 + (q % BLK) / 4], cv = codes[(size_t)b * 64 + 32 + (q % BLK) / 4];
       const uint32_t sc = *reinterpret_cast<const uint16_t*>(scales + 2 * (size_t)b);
+      float dm[4], dv[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        dm[k] = ldexpf(decode_m(cm, k), (int)(sc & 255u) - 127);
+        dv[k] = ldexpf(decode_v(cv, k), (int)(sc >> 8) - 127);
+      }
+      if (any_rests(cm)) resting(cm, dm, dv);
       V4 om, ov;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        om[k] = (T)ldexpf(decode_m(cm, k), (int)(sc & 255u) - 127);
-        ov[k] = (T)ldexpf(decode_v(cv, k), (int)(sc >> 8) - 127);
+        om[k] = (T)dm[k];
+        ov[k] = (T)dv[k];
       }
       if (q + 4 <= n) {
         if (m) __builtin_nontemporal_store(om, reinterpret_cast<V4*>(m + q));

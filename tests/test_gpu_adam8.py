@@ -215,6 +215,58 @@ def test_values_that_are_not_finite_stay_with_their_element():
     assert bool(((v - v64.view(-1)).abs()[fine] <= 2.0**-4 * v64.view(-1).abs()[fine] + 2.0**-18 * v64.max()).all())
 
 
+@pytest.mark.parametrize("dtype", [bf.BF_FP32, bf.BF_BF16])
+@pytest.mark.parametrize("c", [1.0, 4.0])
+@pytest.mark.parametrize("zero", [True, False])
+def test_a_second_moment_that_overflows_stays_infinite(dtype, c, zero):
+    """Gradients whose square is infinite in fp32, in the first step only: from then on their weights move by the weight decay alone, as on fp32 moments, and their
+    neighbours step to the same bits as beside elements whose moments are zero.  (A resting weight is one product and one sum a step: 2^-23 of it and a little.)"""
+    n, t0 = 1001, 1 if zero else 4
+    places = torch.tensor([40, 43, 127, 200] + list(range(384, 512)) + [n - 1], device="cuda")  # alone, two of four neighbours, a whole block, the last
+    sign = torch.where(places % 3 == 0, -1.0, 1.0)
+    out = []
+    for big in (1e25, 0.0):
+        (w, state, g, low, full, guarded), = _make([n], dtype, 13, odd=False, zero=zero)
+        m0, v0, um, uv = P.decode(state, n)
+        gone = torch.zeros_like(m0).view(-1)
+        gone[places] = 1
+        state.copy_(P.encode(torch.where(gone > 0, 0.0, m0.view(-1))[:n], torch.where(gone > 0, 0.0, v0.view(-1))[:n]))
+        g = (g * 1e-3).contiguous()
+        coef, steps = torch.full((1,), c, device="cuda"), []
+        kept = [w.clone(), *(x.view(-1)[:n].float().contiguous() for x in P.decode(state, n)[:2])]
+        for t in range(t0, t0 + 5):
+            first = g.clone()
+            first[places] = (big * sign if t == t0 else 1e-3 * sign * (big > 0)).to(DT[dtype])
+            bf.bf_op_adam8(dtype, [(w, state, first, low)], coef, 5, t, LR, B1, B2, EPS, WD)
+            bf.bf_op_adam_clipped([(*kept, first.float(), None)], coef, t, LR, B1, B2, EPS, WD)
+            m, v = (torch.empty(n, dtype=DT[dtype], device="cuda") for _ in range(2))
+            bf.bf_op_adam8_moments(dtype, [(state, m, v)])
+            steps.append([x.clone() for x in (w, low, state, m, v, kept[0])])
+        assert bool((guarded[state.numel():] == 0xA5).all())
+        out.append(steps)
+    rests = torch.zeros(n, dtype=torch.bool, device="cuda")
+    rests[places] = True
+    codes = torch.zeros((n + 127) // 128 * 128, dtype=torch.bool, device="cuda")
+    codes[:n] = rests
+    codes = torch.stack([codes.view(-1, 128)] * 2, 1).view(-1)
+    before = _make([n], dtype, 13, odd=False, zero=zero)[0][0].double()
+    for k, (a, b) in enumerate(zip(*out)):
+        w, low, state, m, v, fp32 = a
+        assert all(torch.equal(x[~rests], y[~rests]) for x, y in zip((w, low, m, v), (b[0], b[1], b[3], b[4]))), k
+        assert torch.equal(state[: codes.numel()][~codes], b[2][: codes.numel()][~codes]) and torch.equal(state[codes.numel():], b[2][codes.numel():]), k
+        assert bool((m[rests] == 0).all()) and bool((v[rests] == float("inf")).all()), k
+        ref = before[rests] * (1 - LR * WD) ** (k + 1)
+        for got in (w, fp32):
+            assert bool(((got[rests].double() - ref).abs() <= (k + 1) * 2.0**-22 * ref.abs()).all()), k
+        assert torch.equal(low, w.bfloat16())
+    # and a NaN ends it
+    m, v = (torch.empty(n, device="cuda") for _ in range(2))
+    w, state = out[0][-1][0], out[0][-1][2]
+    bf.bf_op_adam8(dtype, [(w, state, torch.full((n,), float("nan"), dtype=DT[dtype], device="cuda"), None)], torch.ones(1, device="cuda"), 5, 9, LR, B1, B2, EPS, WD)
+    bf.bf_op_adam8_moments(bf.BF_FP32, [(state, m, None)])
+    assert bool(torch.isnan(m).all()) and bool(torch.isnan(w).all())
+
+
 def test_captured():
     """A captured step repeats its seed and step; replays are what eager calls with them give."""
     tensors = _make(SIZES, bf.BF_FP32, 10)
