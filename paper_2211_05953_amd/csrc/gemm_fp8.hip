@@ -246,7 +246,7 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
         unrolled<0, MI>([&](auto i) __attribute__((always_inline)) {
           constexpr int I = decltype(i)::value, X = I & 1;
           __builtin_amdgcn_sched_barrier(0);
-          asm volatile("s_nop 1");  // between a conversion and a matrix instruction that reads it
+          asm volatile("s_nop 1");  // between a conversion (for the first one also the sums' zeros) and a matrix instruction that reads it
           float u = 0.f;
           if constexpr (I + 1 < MI) u = unit(sca[(I + 1) / GA], (I + 1) % GA);
           unrolled<0, NI>([&](auto j) __attribute__((always_inline)) {
@@ -336,6 +336,10 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
       const int lk = min(kt + NS, nk - 1);
       int na[SA], nb[SB];
       constexpr int START = NS == 2 ? 0 : -NMMA;  // of the loads, in instructions from the second phase on
+      // between what is moved in front of a block (scales, in front of the first one the sums' zeros) and a matrix instruction that reads it, which the compiler does not see
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_nop 1");
+      __builtin_amdgcn_sched_barrier(0);
       phase(H0{}, first_half, a0, [&](int n) __attribute__((always_inline)) {
         if (n < NH) read_b(cur, S, n);
         if (NS == 2 && n >= NH && n - NH < MH) read_a(cur, 1, a1, n - NH);
@@ -370,7 +374,6 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
       for (int s = 0; s < SA; ++s) sca[s] = na[s];
 #pragma unroll
       for (int s = 0; s < SB; ++s) scb[s] = nb[s];
-      asm volatile("s_nop 1");  // between a move and a matrix instruction that reads it
     };
     unrolled<0, NS>([&](auto u) __attribute__((always_inline)) { issue(stage(u), min((int)decltype(u)::value, nk - 1)); });
     arrived(std::integral_constant<int, NS - 1>{});
