@@ -794,9 +794,9 @@ def bf_op_adam8(dtype, tensors, coef, seed, t, lr, beta1, beta2, adam_eps, weigh
 
 
 def bf_op_adam8_moments(dtype, tensors):
-    """m and v (`dtype`) that states stand for.  tensors: (state, m, v) each, m or v or both."""
+    """m and v (`dtype`) that states stand for.  tensors: (state, m, v) each, m or v or both; an entry with neither is passed over."""
     who, want = "bf_op_adam8_moments", _torch_dtype(dtype)
     state, ms, vs = zip(*tensors) if tensors else ((),) * 3
-    n = _array("Q", [(v if m is None else m).numel() for m, v in zip(ms, vs)])
+    n = _array("Q", [0 if m is None and v is None else (v if m is None else m).numel() for m, v in zip(ms, vs)])
     a = _table(_states(who, state, n), _optional(who, ms, want, n), _optional(who, vs, want, n), n)  # bf_adam8_moments_tensor
     check(load().bf_op_adam8_moments(dtype, len(n), _at(a), _stream()))

@@ -129,3 +129,14 @@ def test_binding_of_adam(on_cpu):
         with pytest.raises(ValueError):
             bf.bf_op_adam8_moments(bf.BF_FP32, [bad])
     assert len(on_cpu) == 4
+
+
+def test_binding_of_moments_of_which_neither_is_wanted(on_cpu):
+    """Such an entry is passed over, as the library does with two null pointers; its state is looked at like the others'."""
+    s, m, v = torch.zeros(2 * 258, dtype=torch.uint8), torch.zeros(200), torch.zeros(200)
+    bf.bf_op_adam8_moments(bf.BF_FP32, [(s, None, None), (s, m, None), (s, None, None), (s, m, v)])
+    bf.bf_op_adam8_moments(bf.BF_FP32, [(s, None, None)])
+    assert [c[1][1] for c in on_cpu] == [4, 1]
+    with pytest.raises(ValueError):
+        bf.bf_op_adam8_moments(bf.BF_FP32, [(s.float(), None, None)])
+    assert len(on_cpu) == 2
