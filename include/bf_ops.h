@@ -277,13 +277,16 @@ bf_status bf_op_adam_clipped(int n_tensors, const bf_adam_tensor* tensors, const
  *            bits (1.5e-5 of the result for normal operands, 8e-5 with large outliers in every block: under bf16's rounding of 1.7e-3); an fp32 C
  *            from operands widened to bf16, with fp32 sums: exactly, but for bits under 2^-133 (of e4m3 under scales of 2^-124, of e5m2 of 2^-117) and codes that
  *            stand for 2^128 or more, which become infinite.  Sums have a fixed order: no atomics.  work: device scratch, 256-byte aligned, of
- *            _work_bytes(...) bytes (0: none needed, or bad sizes), owned by the caller; calls that overlap need their own.  Sizes are 1 to 2^21. */
+ *            _work_bytes(...) bytes (0: none needed, or bad sizes), owned by the caller; calls that overlap need their own.  Sizes are 1 to 2^21.
+ * _gemm_tile what a product of this shape runs on: tiles of edge x edge (256, 128, 64), `waves` to a workgroup, the contraction in `slices` (1: not cut).  Host arithmetic only.
+ *            Returns 1, or 0 (and zeros) for sizes or a type that _gemm refuses. */
 typedef enum { BF_E4M3 = 0, BF_E5M2 = 1 } bf_fp8_format;
 size_t bf_op_fp8_row_bytes(int n);
 size_t bf_op_fp8_scale_elems(int rows, int n);
 bf_status bf_op_fp8_quantize(int dtype, int format, int rows, int cols, const void* x, size_t ld_x, void* q, void* scale, void* qt, void* scale_t,
                              void* stream);
 size_t bf_op_fp8_gemm_work_bytes(int dtype, int M, int N, int K);
+int bf_op_fp8_gemm_tile(int dtype, int M, int N, int K, int* edge, int* waves, int* slices);
 bf_status bf_op_fp8_gemm(int format_a, int format_b, int dtype, int M, int N, int K, const void* A, const void* scale_a, const void* B,
                          const void* scale_b, void* C, const float* bias, const void* R, int accumulate, void* work, size_t work_bytes, void* stream);
 

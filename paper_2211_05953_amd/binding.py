@@ -147,6 +147,7 @@ _SIGNATURES = {
     "bf_op_fp8_scale_elems": (C.c_size_t, [C.c_int] * 2),
     "bf_op_fp8_quantize": (C.c_int, [C.c_int] * 4 + [_P, C.c_size_t] + [_P] * 5),
     "bf_op_fp8_gemm_work_bytes": (C.c_size_t, [C.c_int] * 4),
+    "bf_op_fp8_gemm_tile": (C.c_int, [C.c_int] * 4 + [C.POINTER(C.c_int)] * 3),
     "bf_op_fp8_gemm": (C.c_int, [C.c_int] * 6 + [_P] * 7 + [C.c_int, _P, C.c_size_t, _P]),
     "bf_op_adam8_state_bytes": (C.c_size_t, [C.c_size_t]),
     "bf_op_adam8": (C.c_int, [C.c_int, C.c_int, _P, _P, C.c_uint64, C.c_int] + [C.c_double] * 5 + [_P]),
@@ -743,6 +744,13 @@ def bf_op_fp8_quantize(dtype, format, rows, cols, x, q=None, scale=None, qt=None
 
 def bf_op_fp8_gemm_work_bytes(dtype, M, N, K):
     return load().bf_op_fp8_gemm_work_bytes(dtype, M, N, K)
+
+
+def bf_op_fp8_gemm_tile(dtype, M, N, K):
+    """(edge of a tile, waves to a workgroup, slices of the contraction) that this product runs on, or None for sizes or a type that it refuses."""
+    e, w, s = C.c_int(0), C.c_int(0), C.c_int(0)
+    ok = load().bf_op_fp8_gemm_tile(dtype, M, N, K, C.byref(e), C.byref(w), C.byref(s))
+    return (e.value, w.value, s.value) if ok else None
 
 
 def bf_op_fp8_gemm(format_a, format_b, dtype, M, N, K, A, scale_a, B, scale_b, Cout, bias=None, R=None, accumulate=0, work=None):

@@ -550,6 +550,9 @@ Plan plan_of(int M, int N, int blocks, bool wide) {
   return best;
 }
 
+// whether a 256 x 256 tile of 8-bit instructions that writes its result itself is the one of four waves
+bool is_long(int slice, int slices) { return slices == 1 && slice >= LONG_BLOCKS; }
+
 template <typename TL, int FA, int FB, bool WIDE, typename TO>
 bf_status launch8(Fp8Args a, int slices, hipStream_t st) {
   a.tiles_m = (a.M + TL::BM - 1) / TL::BM;
@@ -574,7 +577,7 @@ bf_status by_tile(const Fp8Args& a, int tile, int slices, bool wide, bool f32, h
     default: return launch8<Small8, FA, FB, false, float>(a, slices, st);
   }
   switch (tile) {
-    case 0: return a.slice >= LONG_BLOCKS ? launch8<Long8, FA, FB, false, bf16_t>(a, slices, st) : launch8<Big8, FA, FB, false, bf16_t>(a, slices, st);
+    case 0: return is_long(a.slice, slices) ? launch8<Long8, FA, FB, false, bf16_t>(a, slices, st) : launch8<Big8, FA, FB, false, bf16_t>(a, slices, st);
     case 1: return launch8<Mid8, FA, FB, false, bf16_t>(a, slices, st);
     default: return launch8<Small8, FA, FB, false, bf16_t>(a, slices, st);
   }
@@ -609,6 +612,18 @@ size_t fp8_gemm_work_bytes(int dtype, int M, int N, int K) {
   if (!sizes_ok(M, N, K) || (dtype != BF_BF16 && dtype != BF_FP32)) return 0;
   const Plan q = plan_of(M, N, (K + 127) / 128, dtype == BF_FP32);
   return q.slices > 1 ? (size_t)q.slices * M * N * sizeof(float) : 0;
+}
+
+bool fp8_gemm_tile(int dtype, int M, int N, int K, int* edge, int* waves, int* slices) {
+  *edge = *waves = *slices = 0;
+  if (!sizes_ok(M, N, K) || (dtype != BF_BF16 && dtype != BF_FP32)) return false;
+  const bool wide = dtype == BF_FP32;
+  const Plan q = plan_of(M, N, (K + 127) / 128, wide);
+  const int nt[3] = {wide ? Wide8::NT : is_long(q.slice, q.slices) ? Long8::NT : Big8::NT, wide ? WideMid8::NT : Mid8::NT, wide ? WideSmall8::NT : Small8::NT};
+  *edge = COST[wide][q.tile].edge;
+  *waves = nt[q.tile] / 64;
+  *slices = q.slices;
+  return true;
 }
 
 bf_status fp8_gemm(int fa, int fb, int dtype, int M, int N, int K, const void* A, const void* sa, const void* B, const void* sb, void* C, const float* bias,

@@ -17,6 +17,7 @@ bf_status adam_clipped(int n_tensors, const bf_adam_tensor* x, const float* coef
                        hipStream_t st);
 bf_status fp8_quantize(int dtype, int format, int rows, int cols, const void* x, size_t ld, void* q, void* scale, void* qt, void* scale_t, hipStream_t st);
 size_t fp8_gemm_work_bytes(int dtype, int M, int N, int K);
+bool fp8_gemm_tile(int dtype, int M, int N, int K, int* edge, int* waves, int* slices);
 bf_status fp8_gemm(int fa, int fb, int dtype, int M, int N, int K, const void* A, const void* sa, const void* B, const void* sb, void* C, const float* bias,
                    const void* R, int accumulate, void* work, size_t work_bytes, hipStream_t st);
 size_t adam8_state_bytes(size_t n);
@@ -283,6 +284,10 @@ bf_status bf_op_fp8_quantize(int dtype, int format, int rows, int cols, const vo
 }
 
 size_t bf_op_fp8_gemm_work_bytes(int dtype, int M, int N, int K) { return fp8_gemm_work_bytes(dtype, M, N, K); }
+
+int bf_op_fp8_gemm_tile(int dtype, int M, int N, int K, int* edge, int* waves, int* slices) {
+  return edge && waves && slices && fp8_gemm_tile(dtype, M, N, K, edge, waves, slices) ? 1 : 0;
+}
 
 bf_status bf_op_fp8_gemm(int format_a, int format_b, int dtype, int M, int N, int K, const void* A, const void* scale_a, const void* B,
                          const void* scale_b, void* C, const float* bias, const void* R, int accumulate, void* work, size_t work_bytes, void* stream) {
