@@ -502,11 +502,13 @@ __global__ __launch_bounds__(256) void fp8_finish_kernel(uint32_t groups, uint32
 }
 
 typedef Tile8<256, 256, 4, 2> Big8;
-// Long contractions: half the waves, each with all of a SIMD's registers, read a third less from LDS, whose power goes to the clock; with few blocks one wave waits alone for the first loads and at the epilogue.  us, four
-// waves and eight: 8192^3 348 and 356, 2048 x 32768 x 8192 361 and 367, 4096 x 8192 x 32768 691 and 704, 4095 x 8190 x 5000 133 and 138; 8192 x 32768 x 2048 427 and 435, but 16384 x 2048 x 2048 68 and 64;
-// 4096 x 16384 x 1024 71 and 70, 8192 x 2048 x 300 15.9 and 14.1.
+// Long contractions: half the waves, each with all of a SIMD's registers, read a third less from LDS, whose power goes to the clock; with few blocks one wave waits alone for the first loads and at the epilogue.  What
+// four waves take more (+) or less than eight, in %, at 8 / 12 / 16 / 20 / 24 / 32 / 40 / 64 / 128 blocks: 2304 x 4096 results +3.1 +1.8 +1.6 +1.5 +1.3 -1.1 +1.3 +0.1 -0.4; 2048 x 6144 +2.4 +0.9 +0.2 +1.7 -0.1 -0.7
+// -0.8 -1.1 -2.8; 4096 x 4096 +2.0 +1.0 +0.3 -0.4 -1.5 -1.3 -1.6 -1.5 -3.0; 5000 x 4000 +1.5 +0.8 +0.5 -0.5 -0.7 -0.7 -0.9 -1.7 -2.1; 4096 x 8192 -2.6 -2.0 -1.8 -1.4 -1.2 -2.3 -1.2 -2.1 -2.2; 16384 x 2048 +7.6
+// +6.7 +5.3 +3.7 +2.9 +1.6 +1.4 -1.1 -1.4; 8192 x 8192 -6.5 -1.9 -1.5 -0.5 -2.0 -1.2 -1.8 -1.8 -2.3; 2048 x 32768 -2.6 +0.1 +0.2 -0.2 -1.6 -1.2 -1.6 -1.7 -2.2; 8192 x 32768 +0.1 +0.5 -0.7 -1.2 -0.7 -1.5
+// -1.7 -2.7 -2.0.  Their mean is +0.5 at 16, +0.3 at 20, -0.4 at 24 and -0.9 at 32.
 typedef Tile8<256, 256, 2, 2> Long8;
-constexpr int LONG_BLOCKS = 16;
+constexpr int LONG_BLOCKS = 24;
 typedef Tile8<256, 256, 2, 4> Wide8;  // widened operands: smaller sub-tiles, two waves to a SIMD
 typedef Tile8<128, 128, 2, 2, 4> Mid8;
 typedef Tile8<128, 128, 2, 2> WideMid8;

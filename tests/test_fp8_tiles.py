@@ -18,7 +18,7 @@ SHAPES = {
     (1, 2000, 1029, 1150): (128, 4, 1), (1, 2048, 2048, 8192): (128, 4, 1),
     (1, 640, 2301, 16380): (128, 4, 2), (1, 200, 2304, 16384): (128, 4, 4), (1, 100, 2999, 12200): (128, 4, 8), (1, 200, 768, 20480): (128, 4, 16),
     (1, 2301, 4099, 128): (256, 8, 1), (1, 2304, 4096, 256): (256, 8, 1), (1, 2301, 4100, 300): (256, 8, 1), (1, 2304, 4096, 1920): (256, 8, 1),
-    (1, 2304, 4096, 2048): (256, 4, 1), (1, 2301, 4099, 2100): (256, 4, 1),
+    (1, 2304, 4096, 2048): (256, 8, 1), (1, 2301, 4099, 2100): (256, 8, 1), (1, 2304, 4096, 3200): (256, 4, 1), (1, 2301, 4099, 3300): (256, 4, 1),
     (1, 2000, 2301, 12200): (256, 8, 2), (1, 1000, 2304, 51200): (256, 8, 4), (1, 200, 5000, 32768): (256, 8, 8),
     # widened operands
     (0, 33, 70, 200): (64, 4, 1), (0, 5, 300, 8200): (64, 4, 8),
