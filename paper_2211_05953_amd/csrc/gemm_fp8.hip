@@ -20,7 +20,7 @@
 // neighbours in memory (one load, picked apart by the instruction's byte selector), and so are its results of G fragments across (one store).
 //
 // Large bf16 results: 8192^3 348 us, 3.2 PFLOP/s; 2048 x 32768 x 8192 361, 3.0; 8192 x 32768 x 2048 427, 2.6 (half a gigabyte of results).  Instructions on registers alone reach 4.05 on
-// random operands (4.9 on zeros: the clock falls with the power); matrix cores are busy 77 to 82 % at 1.82 to 1.75 GHz, and LDS has no bank conflicts.  fp32: 8192 x 8192 x 2048 213 us, 1.29.
+// random operands (4.9 on zeros: the clock falls with the power); matrix cores are busy 76 to 80 % at 1.89 to 1.79 GHz, and LDS has no bank conflicts.  fp32: 8192 x 8192 x 2048 213 us, 1.29.
 #include <type_traits>
 
 #include "../../include/bf_ops.h"
